@@ -450,6 +450,114 @@ lsgd_status lsgd_sgd_update(float* d_W, float* d_U, const float* d_G,
                             float weight_decay, int32_t nesterov,
                             void* stream);
 
+/*
+ * Matrices in 8 bits with a scale for each block of 128 values of a row: the
+ * operands of lsgd_grouped_gemm_blocks. Format LSGD_E4M3 (four exponent bits,
+ * largest value 448, no infinity) or LSGD_E5M2 (five, 57344). A row of n
+ * values takes up(n, 128) bytes, zeros past the n-th, and
+ * up(ceil(n / 128), 4) scale bytes, 127 past the last block's; up(v, m) is v
+ * rounded up to a multiple of m. A block's scale 2^e has the smallest
+ * -127 <= e <= 127 with max |x| <= 2^e F (F the format's largest value, the
+ * maximum over the block's finite values; e = 0 where that is 0) and is held
+ * as the byte e + 127. A value x is held as x 2^-e rounded to nearest, ties to
+ * even, so nothing finite overflows; a NaN as a NaN, an infinity as the format's
+ * (LSGD_E4M3: as a NaN).
+ */
+enum { LSGD_E4M3 = 0, LSGD_E5M2 = 1 };
+
+/*
+ * Writes G matrices X_g [M][N] (dtype LSGD_FP32 or LSGD_BF16, row pitch
+ * ldx >= N, group stride sX >= 0 in elements) in blocks: d_Q [G][M][up(N, 128)]
+ * with d_S [G][M][up(ceil(N / 128), 4)], blocks along N; and with d_Qt, the
+ * transposes, d_Qt [G][N][up(M, 128)] with d_St [G][N][up(ceil(M / 128), 4)],
+ * blocks along M. Either pair may be NULL (both pointers), not both pairs; one
+ * call reads X once for the two. All padding is written. d_Q and d_Qt are
+ * 16-byte aligned, X aligned to its elements, else LSGD_E_INVALID.
+ */
+lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G,
+                                 int32_t M, int32_t N, const void* d_X,
+                                 int64_t ldx, int64_t sX, uint8_t* d_Q,
+                                 uint8_t* d_S, uint8_t* d_Qt, uint8_t* d_St,
+                                 void* stream);
+
+/*
+ * Grouped product of matrices in blocks along the contracted dimension:
+ *   C_g[M][N] = A_g[M][Kd] * B_g[N][Kd]^T   (fp32 accumulation)
+ * A_g is M rows, B_g N rows of Kd values in the layout above (format_a,
+ * format_b may differ): the forward product y = x w takes x and the transpose of
+ * w, the input gradient dy w^T takes dy and w, the weight gradient x^T dy the
+ * transposes of both. sA, sB (bytes, multiples of 16) and sSA, sSB (scale bytes,
+ * multiples of 4) are the group strides; 0 shares one matrix among the groups.
+ * d_A, d_B 16-byte, d_SA, d_SB 4-byte aligned. The bytes past Kd of a row
+ * must be zeros, as lsgd_quantise_blocks leaves them, and its scale bytes
+ * below 255. C is out_dtype LSGD_FP32 or LSGD_BF16 (rounded once), row pitch
+ * ldc >= N, group stride sC >= M * ldc (any value for G == 1); nothing between
+ * its rows is written. d_ws: workspace of
+ * lsgd_grouped_gemm_blocks_workspace_bytes (which may be 0; then NULL is
+ * allowed), 16-byte aligned, LSGD_E_WORKSPACE if smaller. A result does not
+ * depend on what the workspace held.
+ */
+lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t G, int32_t M,
+                                                     int32_t N, int32_t Kd,
+                                                     size_t* bytes);
+lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b,
+                                     int32_t out_dtype, int32_t G, int32_t M,
+                                     int32_t N, int32_t Kd, const uint8_t* d_A,
+                                     int64_t sA, const uint8_t* d_SA,
+                                     int64_t sSA, const uint8_t* d_B,
+                                     int64_t sB, const uint8_t* d_SB,
+                                     int64_t sSB, void* d_C, int64_t ldc,
+                                     int64_t sC, void* d_ws, size_t ws_bytes,
+                                     void* stream);
+
+/*
+ * Orthogonalised momentum. O(X) takes X = U S V^T towards U V^T: from
+ * X / (||X||_F + eps), `steps` Newton-Schulz steps
+ *   A = X X^T,  B = b A + c A A,  X := a X + B X
+ * (on X^T where M > N), h_coefficients = {a, b, c} (host). The products
+ * take fp32 precision for dtype LSGD_FP32 (two fp16 pieces of each operand on
+ * the matrix cores) and, for LSGD_BF16, operands of 11 significant bits but
+ * an X held in two pieces all the same. A zero matrix stays zero; an
+ * infinity or a NaN makes the whole result NaN.
+ *
+ * Arguments, else LSGD_E_INVALID: 1 <= G <= 65535, M, N >= 1 with
+ * up(M, 64) up(N, 64) <= 2^30, 1 <= steps <= 64, finite coefficients under
+ * which no singular value in [0, 1] grows past 32 on the way, eps finite and
+ * > 0. Row pitches are at least N; the groups of a matrix that is written
+ * must not overlap (group stride >= the group's extent, or rows of at least G
+ * groups side by side). Workspace: caller-owned device memory of
+ * lsgd_orthogonalise_workspace_bytes for the dtype, 256-byte aligned
+ * (LSGD_E_WORKSPACE if smaller); one workspace serves one call at a time.
+ */
+lsgd_status lsgd_orthogonalise_workspace_bytes(int32_t dtype, int32_t G,
+                                               int32_t M, int32_t N,
+                                               size_t* bytes);
+
+/* Y_g = O(X_g) for G matrices, X and Y of `dtype` (pitches and strides in
+ * elements). Y may be X itself (same pitch and stride). */
+lsgd_status lsgd_orthogonalise(int32_t dtype, int32_t G, int32_t M, int32_t N,
+                               const void* d_X, int64_t ldx, int64_t sX,
+                               void* d_Y, int64_t ldy, int64_t sY,
+                               int32_t steps, const float* h_coefficients,
+                               float eps, void* d_ws, size_t ws_bytes,
+                               void* stream);
+
+/* The update by the orthogonalised momentum, in place on fp32 W and U:
+ *   u = m u + g;  d = nesterov ? g + m u : u;
+ *   w = (1 - lr wd) w - lr scale O(d).
+ * gemm_dtype: the precision of O's products (as dtype above). Pointers may point into
+ * the replicas' flat rows (a layer's W of every replica: sW the row length). lr,
+ * weight_decay and scale finite, 0 <= momentum < 1, nesterov 0 or 1. */
+lsgd_status lsgd_orthogonal_update(int32_t gemm_dtype, int32_t G, int32_t M,
+                                   int32_t N, float* d_W, int64_t ldw,
+                                   int64_t sW, float* d_U, int64_t ldu,
+                                   int64_t sU, const float* d_G, int64_t ldg,
+                                   int64_t sG, float lr, float momentum,
+                                   float weight_decay, int32_t nesterov,
+                                   float scale, int32_t steps,
+                                   const float* h_coefficients, float eps,
+                                   void* d_ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -277,6 +277,88 @@ Layout make_layout(const lsgd_config* c) {
   return l;
 }
 
+lsgd_status block_status(hipError_t e) {
+  return e == hipSuccess ? LSGD_OK : (e == hipErrorInvalidValue ? LSGD_E_INVALID : LSGD_E_HIP);
+}
+
+bool ortho_sizes(int32_t G, int32_t M, int32_t N) {
+  if (G < 1 || G > 65535 || M < 1 || N < 1) return false;
+  const int64_t m = (M + 63LL) / 64 * 64, n = (N + 63LL) / 64 * 64;
+  return m <= (1LL << 30) / n;
+}
+
+// A matrix that a call writes: G groups [M][N] that do not overlap, either one
+// after the other or side by side in rows that hold them all.
+bool written_groups(int32_t G, int32_t M, int32_t N, const void* p, int64_t ld, int64_t s,
+                    size_t esz) {
+  if (!p || ld < N || (uintptr_t)p % esz) return false;
+  if (G == 1) return true;
+  if (s < N) return false;
+  return (s - N) / ld >= M - 1 || (ld - N) / s >= G - 1;
+}
+
+// The steps' coefficients and the powers of two that X, A and B are held at (see
+// ortho.hip): the largest singular value on the way, from 1 on, bounds every entry of X,
+// its square those of A and the largest |b t + c t^2| those of B; a power of two
+// puts the bound below fp16's largest value (0.9 of it, for rounding). X's is no
+// larger than sqrt(M N), which brings its entries to about 1 at the start: a
+// larger one would move nothing out of fp16's subnormal range that matters.
+bool ortho_numbers(lsgd::OrthoArgs& a, int32_t steps, const float* h, float eps) {
+  if (steps < 1 || steps > 64 || !h || !std::isfinite(eps) || !(eps > 0.f)) return false;
+  const double ca = h[0], cb = h[1], cc = h[2];
+  if (!std::isfinite(ca) || !std::isfinite(cb) || !std::isfinite(cc)) return false;
+  double top = 1.0, s = 1.0, poly = 0.0;
+  for (int t = 0; t < steps; ++t) {
+    // |s (a + b s^2 + c s^4)| is largest at an end or where its derivative vanishes
+    auto p = [&](double x) { return std::fabs(x * (ca + x * x * (cb + x * x * cc))); };
+    double most = p(s);
+    const double disc = 9.0 * cb * cb - 20.0 * ca * cc;
+    for (int sign = -1; sign <= 1; sign += 2) {
+      double r = -1.0;
+      if (cc != 0.0 && disc >= 0.0) r = (-3.0 * cb + sign * std::sqrt(disc)) / (10.0 * cc);
+      if (cc == 0.0 && cb != 0.0) r = -ca / (3.0 * cb);
+      if (r > 0.0 && r < s * s) most = std::max(most, p(std::sqrt(r)));
+    }
+    s = most;
+    top = std::max(top, s);
+    if (!(top <= 32.0)) return false;
+  }
+  const double t = top * top;
+  poly = std::fabs(cb * t + cc * t * t);
+  if (cc != 0.0) {
+    const double r = -cb / (2.0 * cc);
+    if (r > 0.0 && r < t) poly = std::max(poly, std::fabs(cb * r + cc * r * r));
+  }
+  // |p(s) / s| = |a + b t + c t^2| for t = s^2 up to top^2
+  double ratio = std::max(std::fabs(ca), std::fabs(ca + cb * t + cc * t * t));
+  if (cc != 0.0 && -cb / (2.0 * cc) > 0.0 && -cb / (2.0 * cc) < t)
+    ratio = std::max(ratio, std::fabs(ca - cb * cb / (4.0 * cc)));
+  a.grow = std::max(0, (int)std::ceil(std::log2(std::max(ratio, 1e-30))));
+  const double room = 0.9 * 65504.0;
+  auto pow2_below = [](double v) { return std::exp2(std::floor(std::log2(v))); };
+  const double sx = pow2_below(std::min(std::sqrt((double)a.M * a.N), room / top));
+  const double sa = pow2_below(room / t);
+  const double sb = pow2_below(room / std::max(poly, 1.0));
+  a.steps = steps;
+  a.eps = eps;
+  a.scale_x = (float)sx;
+  a.f_xx = (float)(sa / (sx * sx));
+  a.f_aa = (float)(cc * sb / (sa * sa));
+  a.f_a = (float)(cb * sb / sa);
+  a.f_bx = (float)(1.0 / sb);
+  a.f_out = (float)(1.0 / (sb * sx));
+  a.f_x = h[0];
+  return true;
+}
+
+lsgd_status ortho_launch(int32_t dtype, const lsgd::OrthoArgs& a, void* d_ws, size_t ws_bytes,
+                         void* stream) {
+  const int pieces = dtype == LSGD_BF16 ? 1 : 2;
+  if (!d_ws || (uintptr_t)d_ws % kAlign) return LSGD_E_INVALID;
+  if (ws_bytes < lsgd::ortho_workspace_bytes(pieces, a.G, a.M, a.N)) return LSGD_E_WORKSPACE;
+  return block_status(lsgd::launch_ortho(pieces, a, d_ws, (hipStream_t)stream));
+}
+
 }  // namespace
 
 // Opt-in per-launch timing: a pair of HIP events on the context's stream
@@ -1714,6 +1796,137 @@ lsgd_status lsgd_sgd_update(float* d_W, float* d_U, const float* d_G, int64_t n,
                                          weight_decay, nesterov,
                                          (hipStream_t)stream);
   return e == hipSuccess ? LSGD_OK : LSGD_E_HIP;
+}
+
+// ------------------------------------------------- tensors in 8-bit blocks
+lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G, int32_t M, int32_t N,
+                                 const void* d_X, int64_t ldx, int64_t sX, uint8_t* d_Q,
+                                 uint8_t* d_S, uint8_t* d_Qt, uint8_t* d_St, void* stream) {
+  if ((dtype != LSGD_FP32 && dtype != LSGD_BF16) || (format != LSGD_E4M3 && format != LSGD_E5M2))
+    return LSGD_E_INVALID;
+  if (G < 1 || M < 1 || N < 1 || G > 65535 || !d_X || ldx < N || sX < 0) return LSGD_E_INVALID;
+  if ((uintptr_t)d_X % (dtype == LSGD_BF16 ? 2 : 4)) return LSGD_E_INVALID;
+  if (!d_Q != !d_S || !d_Qt != !d_St || (!d_Q && !d_Qt)) return LSGD_E_INVALID;
+  if ((uintptr_t)d_Q % 16 || (uintptr_t)d_Qt % 16) return LSGD_E_INVALID;
+  lsgd::QuantArgs a{G, M, N, d_X, ldx, sX, d_Q, d_S, d_Qt, d_St};
+  return block_status(
+      lsgd::launch_quantise(dtype == LSGD_BF16, format, a, (hipStream_t)stream));
+}
+
+lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t G, int32_t M, int32_t N, int32_t Kd,
+                                                     size_t* bytes) {
+  if (!bytes || G < 1 || M < 1 || N < 1 || Kd < 1 || G > 65535) return LSGD_E_INVALID;
+  *bytes = lsgd::gemm_blocks_workspace_bytes(G, M, N, Kd);
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b, int32_t out_dtype,
+                                     int32_t G, int32_t M, int32_t N, int32_t Kd,
+                                     const uint8_t* d_A, int64_t sA, const uint8_t* d_SA,
+                                     int64_t sSA, const uint8_t* d_B, int64_t sB,
+                                     const uint8_t* d_SB, int64_t sSB, void* d_C, int64_t ldc,
+                                     int64_t sC, void* d_ws, size_t ws_bytes, void* stream) {
+  if ((format_a != LSGD_E4M3 && format_a != LSGD_E5M2) ||
+      (format_b != LSGD_E4M3 && format_b != LSGD_E5M2) ||
+      (out_dtype != LSGD_FP32 && out_dtype != LSGD_BF16))
+    return LSGD_E_INVALID;
+  if (G < 1 || M < 1 || N < 1 || Kd < 1 || G > 65535) return LSGD_E_INVALID;
+  if (!d_A || !d_SA || !d_B || !d_SB || !d_C || ldc < N) return LSGD_E_INVALID;
+  if (sA < 0 || sB < 0 || sSA < 0 || sSB < 0 || sA % 16 || sB % 16 || sSA % 4 || sSB % 4)
+    return LSGD_E_INVALID;
+  if (G > 1 && sC / M < ldc) return LSGD_E_INVALID;
+  if ((uintptr_t)d_A % 16 || (uintptr_t)d_B % 16 || (uintptr_t)d_SA % 4 || (uintptr_t)d_SB % 4 ||
+      (uintptr_t)d_C % (out_dtype == LSGD_BF16 ? 2 : 4))
+    return LSGD_E_INVALID;
+  const size_t need = lsgd::gemm_blocks_workspace_bytes(G, M, N, Kd);
+  if (need && ((uintptr_t)d_ws % 16 || !d_ws)) return LSGD_E_INVALID;
+  if (ws_bytes < need) return LSGD_E_WORKSPACE;
+  lsgd::BlockGemmArgs a{};
+  a.G = G;
+  a.M = M;
+  a.N = N;
+  a.Kd = Kd;
+  a.A = d_A;
+  a.SA = d_SA;
+  a.sA = sA;
+  a.sSA = sSA;
+  a.B = d_B;
+  a.SB = d_SB;
+  a.sB = sB;
+  a.sSB = sSB;
+  a.C = d_C;
+  a.ldc = ldc;
+  a.sC = sC;
+  a.out_bf16 = out_dtype == LSGD_BF16;
+  a.part = (float*)d_ws;
+  return block_status(lsgd::launch_gemm_blocks(format_a, format_b, a, (hipStream_t)stream));
+}
+
+// ------------------------------------------------- orthogonalised momentum
+lsgd_status lsgd_orthogonalise_workspace_bytes(int32_t dtype, int32_t G, int32_t M, int32_t N,
+                                               size_t* bytes) {
+  if (!bytes || (dtype != LSGD_FP32 && dtype != LSGD_BF16) || !ortho_sizes(G, M, N))
+    return LSGD_E_INVALID;
+  *bytes = lsgd::ortho_workspace_bytes(dtype == LSGD_BF16 ? 1 : 2, G, M, N);
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_orthogonalise(int32_t dtype, int32_t G, int32_t M, int32_t N, const void* d_X,
+                               int64_t ldx, int64_t sX, void* d_Y, int64_t ldy, int64_t sY,
+                               int32_t steps, const float* h_coefficients, float eps, void* d_ws,
+                               size_t ws_bytes, void* stream) {
+  if (dtype != LSGD_FP32 && dtype != LSGD_BF16) return LSGD_E_INVALID;
+  const size_t esz = dtype == LSGD_BF16 ? 2 : 4;
+  lsgd::OrthoArgs a{};
+  if (!ortho_sizes(G, M, N) || !d_X || ldx < N || sX < 0 || (uintptr_t)d_X % esz ||
+      !written_groups(G, M, N, d_Y, ldy, sY, esz))
+    return LSGD_E_INVALID;
+  a.G = G;
+  a.M = M;
+  a.N = N;
+  if (!ortho_numbers(a, steps, h_coefficients, eps)) return LSGD_E_INVALID;
+  a.X = d_X;
+  a.ldx = ldx;
+  a.sX = sX;
+  a.x_bf16 = dtype == LSGD_BF16;
+  a.Y = d_Y;
+  a.ldy = ldy;
+  a.sY = sY;
+  return ortho_launch(dtype, a, d_ws, ws_bytes, stream);
+}
+
+lsgd_status lsgd_orthogonal_update(int32_t gemm_dtype, int32_t G, int32_t M, int32_t N, float* d_W,
+                                   int64_t ldw, int64_t sW, float* d_U, int64_t ldu, int64_t sU,
+                                   const float* d_G, int64_t ldg, int64_t sG, float lr,
+                                   float momentum, float weight_decay, int32_t nesterov,
+                                   float scale, int32_t steps, const float* h_coefficients,
+                                   float eps, void* d_ws, size_t ws_bytes, void* stream) {
+  if (gemm_dtype != LSGD_FP32 && gemm_dtype != LSGD_BF16) return LSGD_E_INVALID;
+  lsgd::OrthoArgs a{};
+  if (!ortho_sizes(G, M, N) || !d_G || ldg < N || sG < 0 || (uintptr_t)d_G % 4 ||
+      !written_groups(G, M, N, d_W, ldw, sW, 4) || !written_groups(G, M, N, d_U, ldu, sU, 4))
+    return LSGD_E_INVALID;
+  if (!std::isfinite(lr) || !std::isfinite(weight_decay) || !std::isfinite(scale) ||
+      !std::isfinite(momentum) || momentum < 0.f || momentum >= 1.f || (nesterov & ~1))
+    return LSGD_E_INVALID;
+  a.G = G;
+  a.M = M;
+  a.N = N;
+  if (!ortho_numbers(a, steps, h_coefficients, eps)) return LSGD_E_INVALID;
+  a.X = d_G;
+  a.ldx = ldg;
+  a.sX = sG;
+  a.U = d_U;
+  a.ldu = ldu;
+  a.sU = sU;
+  a.W = d_W;
+  a.ldw = ldw;
+  a.sW = sW;
+  a.mom = momentum;
+  a.nesterov = nesterov;
+  a.keep = (float)(1.0 - (double)lr * weight_decay);
+  a.step = (float)(-(double)lr * scale);
+  return ortho_launch(gemm_dtype, a, d_ws, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -1,10 +1,23 @@
-// Device functions shared by the sampling kernels and the single-launch
-// round: the Philox4x32-10 generator, the per-epoch Feistel permutation, and
-// the replica summation tree.
+// Functions shared between the kernels' files: long grids, the Philox4x32-10
+// generator, the per-epoch Feistel permutation, and the replica summation tree.
 #pragma once
 #include "kernels.h"
 
 namespace lsgd {
+
+// ------------------------------------------------------------------- grids
+constexpr int kXcds = 8;
+// A launch of n workgroups in order: on the grid's x axis, and past 2^23 of them
+// in rows of that (an axis holds fewer than 2^32 threads; a longer one is cut
+// short without an error).
+constexpr int kGridShift = 23;
+inline dim3 grid_of(long long n) {
+  if (n <= 1LL << kGridShift) return dim3((unsigned)n);
+  return dim3(1u << kGridShift, (unsigned)((n + (1LL << kGridShift) - 1) >> kGridShift));
+}
+inline __device__ unsigned workgroup_id() {
+  return (blockIdx.y << kGridShift) + blockIdx.x;
+}
 
 // ------------------------------------------------------------------ Philox
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw, SC'11): ten rounds of two

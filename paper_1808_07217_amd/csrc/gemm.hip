@@ -63,23 +63,10 @@ typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
 constexpr int kThreads = 256;
-constexpr int kXcds = 8;
 
 struct Tile {
   int g, s, m0, n0;
 };
-
-// A launch of n workgroups in order: on the grid's x axis, and past 2^23 of them
-// in rows of that (an axis holds fewer than 2^32 threads; a longer one is cut
-// short without an error).
-constexpr int kGridShift = 23;
-dim3 grid_of(long long n) {
-  if (n <= 1LL << kGridShift) return dim3((unsigned)n);
-  return dim3(1u << kGridShift, (unsigned)((n + (1LL << kGridShift) - 1) >> kGridShift));
-}
-__device__ __forceinline__ unsigned workgroup_id() {
-  return (blockIdx.y << kGridShift) + blockIdx.x;
-}
 
 // (g < 0: past the last tile)
 __device__ __forceinline__ Tile decode_tile(const GemmArgs& a, int BM, int BN) {

@@ -129,6 +129,66 @@ hipError_t launch_gemm_update(int dtype, const GemmArgs* list, int n, const Step
 void step_tail_sample(StepTail& t, int epoch, uint64_t seed, int64_t step, int64_t N,
                       int32_t* idx);
 
+// ------------------------------------------------- tensors in 8-bit blocks
+// (blocks.hip) An 8-bit matrix of R rows and n columns: rows of
+// up(n, 128) bytes, zeros past column n; scale bytes e + 127 of the row's blocks
+// of 128, up(blocks, 4) of them, 127 past the last block.
+enum { kFmtE4M3 = 0, kFmtE5M2 = 1 };  // the matrix instructions' codes
+struct QuantArgs {
+  int G, M, N;
+  const void* X;      // [G][M][N], row pitch ldx, group stride sX (elements)
+  long long ldx, sX;
+  uint8_t *Q, *S;     // blocks along N, M rows a group; nullptr: not wanted
+  uint8_t *Qt, *St;   // the transpose's, N rows a group; nullptr: not wanted
+};
+hipError_t launch_quantise(int bf16, int fmt, const QuantArgs& a, hipStream_t s);
+// C[g] = A[g] B[g]^T over Kd (M, N rows; group strides in bytes, 0 shares one
+// matrix), C fp32 or bf16 at row pitch ldc, group stride sC (elements).
+struct BlockGemmArgs {
+  int G, M, N, Kd;
+  const uint8_t *A, *SA;
+  long long sA, sSA;
+  const uint8_t *B, *SB;
+  long long sB, sSB;
+  void* C;
+  long long ldc, sC;
+  int out_bf16;
+  float* part;  // workspace
+};
+size_t gemm_blocks_workspace_bytes(int G, int M, int N, int Kd);
+hipError_t launch_gemm_blocks(int fmt_a, int fmt_b, const BlockGemmArgs& a, hipStream_t s);
+
+// ------------------------------------------------- orthogonalised momentum
+// (ortho.hip) G matrices [M][N] taken to their orthogonal factors; U set: the
+// update of W by the momentum U and the gradient X, else Y = O(X).
+struct OrthoArgs {
+  int G, M, N, steps;
+  const void* X;      // fp32 or bf16 (x_bf16): the matrices, or the gradients (fp32)
+  long long ldx, sX;
+  int x_bf16;
+  void* Y;            // of X's type
+  long long ldy, sY;
+  float *U, *W;
+  long long ldu, sU, ldw, sW;
+  float mom, keep, step;  // w = keep w + step O
+  int nesterov;
+  float eps;
+  // the scales of X, A and B (powers of two, X's here) and the coefficients with
+  // them: A = f_xx (X X), B = f_aa (A A) + f_a A, X = f_bx (B X) + f_x X, the
+  // last step's result f_out (B X) + f_x / scale_x X (all times the powers of two
+  // by which a small matrix is held higher)
+  float scale_x, f_xx, f_aa, f_a, f_bx, f_out, f_x;
+  int grow;  // X grows by at most 2^grow a step
+  // set by launch_ortho
+  int flip, mp, np;
+  double* part;
+  int* kexp;
+  _Float16 *Xr, *Xt[2], *A, *B;
+};
+// `pieces`: 2 for fp32 products, 1 for the bf16 form. Workspace 256-byte aligned.
+size_t ortho_workspace_bytes(int pieces, int G, int M, int N);
+hipError_t launch_ortho(int pieces, OrthoArgs a, void* ws, hipStream_t s);
+
 // ---------------------------------------------------------------- head
 // Output layer with few classes, fused around the loss (head.hip).
 constexpr int kHeadMaxClasses = 32;

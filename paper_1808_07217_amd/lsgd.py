@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -50,6 +50,7 @@ class Config(_c.Structure):
 
 _lib = _c.CDLL(LIB_PATH)
 _P = _c.c_void_p
+_I, _L = _c.c_int32, _c.c_int64
 _SIGS = {
     "lsgd_param_count": [_c.POINTER(Config), _c.POINTER(_c.c_int64)],
     "lsgd_workspace_bytes": [_c.POINTER(Config), _c.POINTER(_c.c_size_t)],
@@ -98,6 +99,16 @@ _SIGS = {
     "lsgd_replica_average_blocks": [_P, _c.c_int32, _c.c_int32, _c.c_int64, _P],
     "lsgd_sgd_update": [_P, _P, _P, _c.c_int64, _c.c_float, _c.c_float,
                         _c.c_float, _c.c_int32, _P],
+    "lsgd_quantise_blocks": [_I, _I, _I, _I, _I, _P, _L, _L, _P, _P, _P, _P, _P],
+    "lsgd_grouped_gemm_blocks_workspace_bytes": [_I, _I, _I, _I, _c.POINTER(_c.c_size_t)],
+    "lsgd_grouped_gemm_blocks": [_I, _I, _I, _I, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _L,
+                                 _P, _L, _L, _P, _c.c_size_t, _P],
+    "lsgd_orthogonalise_workspace_bytes": [_I, _I, _I, _I, _c.POINTER(_c.c_size_t)],
+    "lsgd_orthogonalise": [_I, _I, _I, _I, _P, _L, _L, _P, _L, _L, _I, _c.POINTER(_c.c_float),
+                           _c.c_float, _P, _c.c_size_t, _P],
+    "lsgd_orthogonal_update": [_I, _I, _I, _I, _P, _L, _L, _P, _L, _L, _P, _L, _L, _c.c_float,
+                               _c.c_float, _c.c_float, _I, _c.c_float, _I,
+                               _c.POINTER(_c.c_float), _c.c_float, _P, _c.c_size_t, _P],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -528,3 +539,216 @@ def sgd_update(W, U, G, lr, momentum, weight_decay, nesterov=False,
         _ptr(W), _ptr(U), _ptr(G), W.numel(), float(lr), float(momentum),
         float(weight_decay), int(bool(nesterov)) | (2 if sign_step else 0),
         _stream_handle(torch.cuda.current_stream(W.device))))
+
+
+# -- large layers: products in 8 bits, orthogonalised updates --------------
+FORMATS = {"e4m3": (0, torch.float8_e4m3fn), "e5m2": (1, torch.float8_e5m2)}
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)  # of five Newton-Schulz steps
+
+
+class Blocks(NamedTuple):
+    """G matrices of M rows and n columns in 8 bits with a scale for each row
+    and 128 columns (the layout of lsgd_quantise_blocks): q [G][M][up(n, 128)],
+    float8_e4m3fn or float8_e5m2, zeros past column n, and scale
+    [G][M][up(ceil(n / 128), 4)], float8_e8m0fnu, 1 past the last block."""
+    q: torch.Tensor
+    scale: torch.Tensor
+    n: int
+
+
+def _up(n: int, m: int) -> int:
+    return (n + m - 1) // m * m
+
+
+class _on:
+    """The calling thread's device set to ``device`` while a call enqueues."""
+
+    def __init__(self, device: torch.device):
+        self.device = device
+        self.prev = None
+
+    def __enter__(self):
+        current = torch.cuda.current_device()
+        if self.device.index != current:
+            self.prev = current
+            torch.cuda.set_device(self.device)
+        return _stream_handle(torch.cuda.current_stream(self.device))
+
+    def __exit__(self, *exc):
+        if self.prev is not None:
+            torch.cuda.set_device(self.prev)
+
+
+def _matrices(name: str, X: torch.Tensor, dtypes) -> Tuple[int, int]:
+    """Row pitch and group stride of a [G][M][N] device tensor whose columns are
+    contiguous."""
+    if X.dim() != 3 or X.dtype not in dtypes:
+        raise ValueError(f"{name} must be [G][M][N] of "
+                         + " or ".join(str(t).replace("torch.", "") for t in dtypes))
+    if X.device.type != "cuda":
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    G, M, N = X.shape
+    if X.numel() == 0:
+        raise ValueError(f"{name} is empty")
+    if N > 1 and X.stride(2) != 1:
+        raise ValueError(f"{name}'s columns must be contiguous")
+    return (X.stride(1) if M > 1 else N), (X.stride(0) if G > 1 else 0)
+
+
+def _same_device(*ts):
+    if any(t.device != ts[0].device for t in ts[1:]):
+        raise ValueError("all tensors must be on one device")
+
+
+def _new_blocks(G: int, M: int, n: int, dtype, device) -> Blocks:
+    return Blocks(torch.empty((G, M, _up(n, 128)), dtype=dtype, device=device),
+                  torch.empty((G, M, _up((n + 127) // 128, 4)), dtype=torch.float8_e8m0fnu,
+                              device=device), n)
+
+
+def quantise_blocks(X: torch.Tensor, fmt: str = "e4m3", both: bool = False
+                    ) -> Union[Blocks, Tuple[Blocks, Blocks]]:
+    """X [G][M][N] (float32 or bfloat16, columns contiguous) in 8 bits with a
+    power-of-two scale for each row and 128 columns (lsgd_quantise_blocks);
+    ``both``: (X's blocks, its transpose's) from one read of X."""
+    ldx, sX = _matrices("X", X, (torch.float32, torch.bfloat16))
+    if fmt not in FORMATS:
+        raise ValueError("fmt must be 'e4m3' or 'e5m2'")
+    code, dtype = FORMATS[fmt]
+    G, M, N = X.shape
+    q = _new_blocks(G, M, N, dtype, X.device)
+    t = _new_blocks(G, N, M, dtype, X.device) if both else None
+    with _on(X.device) as stream:
+        _check(_lib.lsgd_quantise_blocks(
+            BF16 if X.dtype == torch.bfloat16 else FP32, code, G, M, N, X.data_ptr(), ldx, sX,
+            q.q.data_ptr(), q.scale.data_ptr(), t.q.data_ptr() if both else None,
+            t.scale.data_ptr() if both else None, stream))
+    return (q, t) if both else q
+
+
+def _block_operand(name: str, X: Blocks) -> Tuple[int, int, int, int, int]:
+    """Format code, groups, rows and the two group strides of an operand."""
+    q, s = X.q, X.scale
+    codes = {d: c for c, d in FORMATS.values()}
+    if q.dim() != 3 or s.dim() != 3 or q.dtype not in codes or s.dtype != torch.float8_e8m0fnu:
+        raise ValueError(f"{name} must hold 3-D float8 values and float8_e8m0fnu scales")
+    if X.n < 1 or q.shape[2] != _up(X.n, 128) or s.shape[2] != _up((X.n + 127) // 128, 4) or (
+            q.shape[:2] != s.shape[:2]) or q.numel() == 0:
+        raise ValueError(f"{name}: shapes do not match the block layout of {X.n} columns")
+    for t in (q, s):
+        if t.device.type != "cuda":
+            raise ValueError(f"{name} must be on a CUDA (HIP) device")
+        if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+            raise ValueError(f"{name}: rows must be contiguous and unpadded")
+    G = q.shape[0]
+    return (codes[q.dtype], G, q.shape[1], q.stride(0) if G > 1 else 0,
+            s.stride(0) if G > 1 else 0)
+
+
+def grouped_gemm_blocks(A: Blocks, B: Blocks, out: Optional[torch.Tensor] = None,
+                        out_dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """C[g] = A[g] @ B[g]^T of two tensors in blocks along the contracted
+    dimension (lsgd_grouped_gemm_blocks), fp32 accumulation, C float32 or
+    bfloat16. y = x w takes x and w's transpose, dy w^T takes dy and w, and
+    x^T dy the transposes of x and dy. A group stride of 0 (``expand``) shares a
+    matrix among the groups."""
+    fa, G, M, sA, sSA = _block_operand("A", A)
+    fb, Gb, N, sB, sSB = _block_operand("B", B)
+    if A.n != B.n or G != Gb:
+        raise ValueError("A and B must have the same groups and inner dimension")
+    if out is None:
+        if out_dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("out_dtype must be float32 or bfloat16")
+        out = torch.empty((G, M, N), dtype=out_dtype, device=A.q.device)
+    ldc, sC = _matrices("out", out, (torch.float32, torch.bfloat16))
+    if out.shape != (G, M, N):
+        raise ValueError("out must be [G][M][N]")
+    _same_device(A.q, A.scale, B.q, B.scale, out)
+    nb = _c.c_size_t()
+    _check(_lib.lsgd_grouped_gemm_blocks_workspace_bytes(G, M, N, A.n, _c.byref(nb)))
+    with _on(out.device) as stream:
+        ws = torch.empty(nb.value, dtype=torch.uint8, device=out.device) if nb.value else None
+        _check(_lib.lsgd_grouped_gemm_blocks(
+            fa, fb, BF16 if out.dtype == torch.bfloat16 else FP32, G, M, N, A.n,
+            A.q.data_ptr(), sA, A.scale.data_ptr(), sSA, B.q.data_ptr(), sB,
+            B.scale.data_ptr(), sSB, out.data_ptr(), ldc, sC, _ptr(ws), nb.value, stream))
+    return out
+
+
+def orthogonalise_workspace(G: int, M: int, N: int, dtype: torch.dtype = torch.float32,
+                            device="cuda") -> torch.Tensor:
+    """A workspace for ``orthogonalise`` / ``orthogonal_update`` on [G][M][N]
+    (``dtype``: the products' precision), for callers that keep one. One
+    workspace serves one call at a time: calls on several streams take one each."""
+    nb = _c.c_size_t()
+    _check(_lib.lsgd_orthogonalise_workspace_bytes(_precision(dtype), G, M, N, _c.byref(nb)))
+    return _aligned_bytes(nb.value, device)
+
+
+def _precision(dtype: torch.dtype) -> int:
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("the precision must be float32 or bfloat16")
+    return BF16 if dtype == torch.bfloat16 else FP32
+
+
+def _coefficients(c: Sequence[float]):
+    if len(c) != 3:
+        raise ValueError("coefficients must be (a, b, c)")
+    return (_c.c_float * 3)(*[float(v) for v in c])
+
+
+def _workspace_for(ws, G, M, N, dtype, device) -> torch.Tensor:
+    if ws is None:
+        return orthogonalise_workspace(G, M, N, dtype, device)
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != device:
+        raise ValueError("workspace must be a contiguous uint8 tensor on the same device")
+    return ws
+
+
+def orthogonalise(X: torch.Tensor, steps: int = 5, coefficients: Sequence[float] = COEFFICIENTS,
+                  eps: float = 1e-7, out: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The matrices X [G][M][N] (float32 or bfloat16) taken towards their
+    orthogonal factors by Newton-Schulz steps (lsgd_orthogonalise); ``out`` may be
+    X itself."""
+    ldx, sX = _matrices("X", X, (torch.float32, torch.bfloat16))
+    G, M, N = X.shape
+    out = torch.empty((G, M, N), dtype=X.dtype, device=X.device) if out is None else out
+    ldy, sY = _matrices("out", out, (X.dtype,))
+    if out.shape != X.shape:
+        raise ValueError("out must have X's shape")
+    _same_device(X, out)
+    co = _coefficients(coefficients)
+    with _on(X.device) as stream:
+        ws = _workspace_for(workspace, G, M, N, X.dtype, X.device)
+        _check(_lib.lsgd_orthogonalise(
+            _precision(X.dtype), G, M, N, X.data_ptr(), ldx, sX, out.data_ptr(), ldy, sY,
+            int(steps), co, float(eps), ws.data_ptr(), ws.numel(), stream))
+    return out
+
+
+def orthogonal_update(W: torch.Tensor, U: torch.Tensor, G: torch.Tensor, lr: float,
+                      momentum: float, weight_decay: float = 0.0, nesterov: bool = False,
+                      scale: float = 1.0, steps: int = 5,
+                      coefficients: Sequence[float] = COEFFICIENTS, eps: float = 1e-7,
+                      gemm_dtype: torch.dtype = torch.float32,
+                      workspace: Optional[torch.Tensor] = None) -> None:
+    """In-place update of W [K][M][N] and its momentum U with gradient G (all
+    float32, columns contiguous; views into the replicas' flat rows are fine):
+    u = m u + g, d = g + m u (``nesterov``) or u, w = (1 - lr wd) w - lr scale O(d)
+    with O of ``orthogonalise`` (lsgd_orthogonal_update)."""
+    f = (torch.float32,)
+    (ldw, sW), (ldu, sU), (ldg, sG) = (_matrices("W", W, f), _matrices("U", U, f),
+                                       _matrices("G", G, f))
+    if U.shape != W.shape or G.shape != W.shape:
+        raise ValueError("W, U, G must have one shape")
+    _same_device(W, U, G)
+    K, M, N = W.shape
+    co = _coefficients(coefficients)
+    with _on(W.device) as stream:
+        ws = _workspace_for(workspace, K, M, N, gemm_dtype, W.device)
+        _check(_lib.lsgd_orthogonal_update(
+            _precision(gemm_dtype), K, M, N, W.data_ptr(), ldw, sW, U.data_ptr(), ldu, sU,
+            G.data_ptr(), ldg, sG, float(lr), float(momentum), float(weight_decay),
+            int(bool(nesterov)), float(scale), int(steps), co, float(eps), ws.data_ptr(),
+            ws.numel(), stream))

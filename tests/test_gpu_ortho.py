@@ -1,0 +1,253 @@
+"""GPU tests of the orthogonalised momentum against the float64 oracle.
+
+Tolerance: the oracle run with the roundings of the kernels' precision (fp16
+pieces, fp32 sums) lands at some distance from the exact result; a kernel of
+that precision, whose sums run in another order, may be four times as far, in
+norm and at the worst entry, plus its output's own rounding (half a step). With
+few values that distance is one sample of a random sum and may come out near zero,
+so a floor stands beside it: the last step's three terms a s, b s^3, c s^5 add to
+(3.44 + 4.78 1.45 + 2.03 2.1) 1.2 = 17.6 at the largest s = 1.2, and each is rounded to 24
+bits twice at least (as pieces and as a sum), 35 2^-24 in all of a result near 1."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import blocks_oracle as B
+from gpu_util import device, to_dev
+
+pytestmark = pytest.mark.gpu
+
+
+def _lsgd():
+    from paper_1808_07217_amd import lsgd as L
+    return L
+
+
+def _np(t):
+    return t.to(torch.float32).cpu().numpy().astype(np.float64)
+
+
+def _matrices(rng, G, M, N, low=False):
+    x = rng.standard_normal((G, M, N))
+    r = max(1, min(M, N) // 16)
+    part = rng.standard_normal((G, M, r)) @ rng.standard_normal((G, r, N))
+    return (x * 0.02 + part) if low else x + part / np.sqrt(r)
+
+
+def _check(got, X, bf16, **kw):
+    want = B.newton_schulz(X, **kw)
+    near = B.newton_schulz_rounded(X, 1 if bf16 else 2, **kw)
+    half = 2.0 ** -8 if bf16 else 2.0 ** -24
+    for g in range(X.shape[0]):
+        e, d, w = np.abs(got[g] - want[g]), np.abs(near[g] - want[g]), np.abs(want[g])
+        floor = half + 35 * 2.0 ** -24
+        tol = 4 * np.linalg.norm(d) + floor * np.linalg.norm(w)
+        assert np.linalg.norm(e) <= tol, (g, np.linalg.norm(e), tol)
+        tol = 4 * d.max() + floor * w.max()
+        assert e.max() <= tol, (g, e.max(), tol)
+
+
+SHAPES = [(1, 1, 1), (2, 1, 7), (3, 5, 1), (2, 16, 16), (4, 64, 64), (2, 65, 63), (2, 128, 100),
+          (2, 129, 130), (1, 130, 257), (3, 257, 100), (1, 200, 1000), (1, 700, 64), (2, 512, 512),
+          (1, 33, 3000), (1, 640, 900)]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("low", [False, True])
+def test_orthogonalise_matches_oracle(shape, dtype, low):
+    L = _lsgd()
+    print(f"orthogonalise {shape} {dtype} low={low}", flush=True)
+    X = _matrices(np.random.default_rng(sum(shape)), *shape, low=low)
+    Xd = to_dev(X.astype(np.float32)).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    Y = L.orthogonalise(Xd)
+    assert Y.dtype == Xd.dtype and Y.shape == Xd.shape
+    _check(_np(Y), _np(Xd), dtype == "bf16")
+
+
+@pytest.mark.parametrize("steps,co", [(1, (3.4445, -4.7750, 2.0315)), (2, (1.5, -0.5, 0.0)),
+                                      (12, (1.875, -1.25, 0.375)), (3, (0.5, 0.0, 0.0)),
+                                      (64, (1.5, -0.5, 0.0)), (4, (2.0, -1.5, 0.5))])
+def test_orthogonalise_steps_and_coefficients(steps, co):
+    L = _lsgd()
+    print(f"orthogonalise {steps} {co}", flush=True)
+    X = _matrices(np.random.default_rng(steps), 2, 70, 150)
+    for dt in (torch.float32, torch.bfloat16):
+        Xd = to_dev(X.astype(np.float32)).to(dt)
+        Y = L.orthogonalise(Xd, steps=steps, coefficients=co)
+        _check(_np(Y), _np(Xd), dt == torch.bfloat16, steps=steps, coefficients=co)
+
+
+@pytest.mark.parametrize("shape", [(2, 40, 60), (1, 150, 200)])
+@pytest.mark.parametrize("size", [1e30, 1e-9, 1e-13, 1e-25])
+def test_orthogonalise_sizes(size, shape):
+    """Norms whose square leaves fp32's range, and norms far below eps, where the
+    result is a small multiple of X (with its precision all the same)."""
+    L = _lsgd()
+    print(f"orthogonalise {shape} times {size}", flush=True)
+    X = (_matrices(np.random.default_rng(4), *shape) * size).astype(np.float32)
+    got = _np(L.orthogonalise(to_dev(X)))
+    want = B.newton_schulz(X.astype(np.float64))
+    # as the fp32 cases of ordinary size, whose distance is below 2e-6
+    e = np.linalg.norm(got - want) / np.linalg.norm(want)
+    assert e <= 1e-5, e
+
+
+def test_orthogonalise_zeros_and_specials():
+    """A zero matrix stays zero; one NaN or infinity makes its own matrix NaN and
+    leaves the other groups' bits alone."""
+    L = _lsgd()
+    for shape in ((4, 20, 30), (4, 200, 150)):
+        print(f"orthogonalise specials {shape}", flush=True)
+        X = _matrices(np.random.default_rng(6), *shape).astype(np.float32)
+        clean = L.orthogonalise(to_dev(X))
+        X[1] = 0
+        X[2, 3, 5] = np.nan
+        X[3, 0, 0] = np.inf
+        Y = L.orthogonalise(to_dev(X))
+        assert torch.equal(Y[0], clean[0])
+        assert (Y[1] == 0).all()
+        assert torch.isnan(Y[2]).all() and torch.isnan(Y[3]).all()
+
+
+def test_orthogonalise_views_in_place_and_shared():
+    """Views at odd offsets with padded rows, groups side by side in a row, out = X,
+    one matrix for all groups: the same bits as contiguous tensors, and nothing
+    written outside."""
+    L = _lsgd()
+    rng = np.random.default_rng(7)
+    for dt in (torch.float32, torch.bfloat16):
+        for M, N in ((30, 41), (150, 141), (141, 300)):
+            print(f"orthogonalise views {dt} {M} {N}", flush=True)
+            room = to_dev(rng.standard_normal((3, M + 3, N + 5)).astype(np.float32)).to(dt)
+            X = room[:, 1:M + 1, 3:N + 3]
+            want = L.orthogonalise(X.contiguous())
+            keep = room.clone()
+            out = torch.full((M, 3, N + 2), 9.0, device=device(), dtype=dt)
+            L.orthogonalise(X, out=out[:, :, :N].transpose(0, 1))
+            assert torch.equal(out[:, :, :N].transpose(0, 1), want) and (out[:, :, N:] == 9.0).all()
+            L.orthogonalise(X, out=X)
+            assert torch.equal(X, want)
+            keep[:, 1:M + 1, 3:N + 3] = want
+            assert torch.equal(room, keep)
+            E = keep[:1, 1:M + 1, 3:N + 3].expand(3, M, N)
+            Y = L.orthogonalise(E)
+            assert torch.equal(Y[0], Y[2])
+
+
+@pytest.mark.parametrize("nesterov", [False, True])
+@pytest.mark.parametrize("shape", [(3, 24, 40), (2, 100, 100), (4, 130, 70), (2, 150, 260)])
+def test_orthogonal_update_matches_oracle(shape, nesterov):
+    """The update of a layer inside flat rows (as the replicas hold it), at an
+    offset that is no multiple of four; the rest of the rows stays."""
+    L = _lsgd()
+    print(f"update {shape} nesterov={nesterov}", flush=True)
+    K, M, N = shape
+    rng = np.random.default_rng(sum(shape))
+    Pn = M * N + 77
+    flat = rng.standard_normal((2, K, Pn)).astype(np.float32)
+    W, U = to_dev(flat[0]), to_dev(flat[1])
+    G = to_dev(_matrices(rng, K, M, N).astype(np.float32))
+    view = lambda t: t[:, 13:13 + M * N].view(K, M, N)  # noqa: E731
+    w0, u0 = _np(view(W)), _np(view(U))
+    lr, m, wd, scale = 0.05, 0.9, 0.1, 1.7
+    L.orthogonal_update(view(W), view(U), G, lr, m, wd, nesterov=nesterov, scale=scale)
+    w, u, o = B.orthogonal_update(w0, u0, _np(G), lr, m, wd, nesterov, scale)
+    got_u, got_w = _np(view(U)), _np(view(W))
+    # u = m u + g and w = keep w + step o: two roundings each
+    assert np.all(np.abs(got_u - u) <= 2 * 2.0 ** -24 * (np.abs(u0) + np.abs(_np(G))))
+    f = np.float32
+    d = (_np(G) + float(f(m)) * u) if nesterov else u
+    near = np.abs(B.newton_schulz_rounded(d, 2) - o).max()
+    tol = 3 * 2.0 ** -24 * (np.abs(w0) + lr * scale * np.abs(o)) + lr * scale * (
+        4 * near + 2 * 2.0 ** -24 * np.abs(o).max())
+    assert np.all(np.abs(got_w - w) <= tol), np.max(np.abs(got_w - w) / tol)
+    for t, want in ((W, flat[0]), (U, flat[1])):
+        t = t.cpu().numpy()
+        assert np.array_equal(t[:, :13], want[:, :13])
+        assert np.array_equal(t[:, 13 + M * N:], want[:, 13 + M * N:])
+
+
+def test_orthogonal_update_in_bf16_precision():
+    L = _lsgd()
+    print("update bf16 precision", flush=True)
+    rng = np.random.default_rng(21)
+    for K, M, N in ((2, 48, 64), (2, 200, 160)):
+        W0 = rng.standard_normal((K, M, N)).astype(np.float32)
+        U0 = rng.standard_normal((K, M, N)).astype(np.float32)
+        G0 = _matrices(rng, K, M, N).astype(np.float32)
+        W, U = to_dev(W0), to_dev(U0)
+        L.orthogonal_update(W, U, to_dev(G0), 0.1, 0.9, gemm_dtype=torch.bfloat16)
+        w, u, o = B.orthogonal_update(W0.astype(np.float64), U0.astype(np.float64),
+                                      G0.astype(np.float64), 0.1, 0.9, 0.0, False, 1.0)
+        near = np.abs(B.newton_schulz_rounded(u, 1) - o).max()
+        assert np.abs(_np(W) - w).max() <= 0.1 * 4 * near + 2.0 ** -22 * np.abs(w).max()
+
+
+def test_updates_on_streams_and_in_graphs():
+    """Two captured graphs with a workspace each, replayed in turn with eager calls
+    between them, and a call on a side stream: the eager bits every time."""
+    L = _lsgd()
+    print("update streams and graphs", flush=True)
+    rng = np.random.default_rng(31)
+    for K, M, N in ((2, 60, 90), (2, 140, 190)):
+        W = [to_dev(rng.standard_normal((K, M, N)).astype(np.float32)) for _ in range(2)]
+        U = [torch.zeros_like(W[0]) for _ in range(2)]
+        G = to_dev(rng.standard_normal((K, M, N)).astype(np.float32))
+        eager = [(w.clone(), u.clone()) for w, u in zip(W, U)]
+        ws = [L.orthogonalise_workspace(K, M, N) for _ in range(2)]
+        args = (0.1, 0.9, 0.01)
+        graphs = []
+        for i in range(2):
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[i]):
+                L.orthogonal_update(W[i], U[i], G, *args, workspace=ws[i])
+        for k in range(3):
+            for i in range(2):
+                graphs[i].replay()
+                L.orthogonal_update(*eager[i], G, *args)
+            torch.cuda.synchronize()
+            for i in range(2):
+                assert torch.equal(W[i], eager[i][0]) and torch.equal(U[i], eager[i][1])
+            G.copy_(to_dev(rng.standard_normal((K, M, N)).astype(np.float32)))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        want = L.orthogonalise(G)
+        with torch.cuda.stream(side):
+            got = L.orthogonalise(G)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
+def test_local_step_of_a_large_layer():
+    """The operators together, as a round uses them: K replicas of one linear
+    layer fit a target by products in 8 bits, orthogonalised updates and the
+    replica average; every quantity against the formulas in float64 on the same
+    8-bit values, step by step."""
+    L = _lsgd()
+    print("local step of a large layer", flush=True)
+    rng = np.random.default_rng(41)
+    K, T, I, O = 3, 64, 96, 80
+    flat = to_dev(np.repeat(0.1 * rng.standard_normal((1, I * O)), K, axis=0).astype(np.float32))
+    W = flat.view(K, I, O)
+    U = torch.zeros_like(W)
+    for step in range(3):
+        x = to_dev(rng.standard_normal((K, T, I)).astype(np.float32))
+        target = to_dev(rng.standard_normal((K, T, O)).astype(np.float32))
+        xq, xt = L.quantise_blocks(x, both=True)
+        _, wt = L.quantise_blocks(W, both=True)
+        y = L.grouped_gemm_blocks(xq, wt)
+        _, dt = L.quantise_blocks((y - target) / T, "e5m2", both=True)
+        dw = L.grouped_gemm_blocks(xt, dt)
+        val = lambda t: B.values(_np(t.q), _np(t.scale))  # noqa: E731
+        exact_dw = (val(xt) @ val(dt).transpose(0, 2, 1))
+        assert np.abs(_np(dw) - exact_dw).max() <= 1e-5 * np.abs(exact_dw).max()
+        w0, u0 = _np(W), _np(U)
+        L.orthogonal_update(W, U, dw, 0.02, 0.95, 0.01, nesterov=True)
+        w, u, o = B.orthogonal_update(w0, u0, _np(dw), 0.02, 0.95, 0.01, True, 1.0)
+        assert np.abs(_np(U) - u).max() <= 1e-6 * np.abs(u).max()
+        assert np.abs(_np(W) - w).max() <= 0.02 * 1e-4 * np.abs(o).max() + 1e-6 * np.abs(w).max()
+    mean = _np(flat).mean(axis=0)
+    L.replica_average(flat)
+    assert np.abs(_np(flat) - mean).max() <= 1e-6 * np.abs(mean).max()
