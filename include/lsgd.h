@@ -490,7 +490,7 @@ lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G,
  * multiples of 4) are the group strides; 0 shares one matrix among the groups.
  * d_A, d_B 16-byte, d_SA, d_SB 4-byte aligned. The bytes past Kd of a row
  * must be zeros, as lsgd_quantise_blocks leaves them, and its scale bytes
- * below 255. C is out_dtype LSGD_FP32 or LSGD_BF16 (rounded once), row pitch
+ * below 255. Kd <= 2^22. C is out_dtype LSGD_FP32 or LSGD_BF16 (rounded once), row pitch
  * ldc >= N, group stride sC >= M * ldc (any value for G == 1); nothing between
  * its rows is written. d_ws: workspace of
  * lsgd_grouped_gemm_blocks_workspace_bytes (which may be 0; then NULL is

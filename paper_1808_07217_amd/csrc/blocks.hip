@@ -9,17 +9,16 @@
 // non-zero value, so each element is rounded once. Infinities and NaN stay
 // out of the maximum and are stored as the format has them (e4m3 holds no
 // infinity: NaN), so that every product that reads one shows it.
-#include "device_common.h"
+#include <type_traits>
+
 #include "kernels.h"
+#include "tile_loop.h"
 
 namespace lsgd {
 namespace {
 
-typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v8i __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // vectors at any element's alignment
@@ -225,86 +224,170 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
   return bf16x8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
 }
 
-// 4 wavefronts, each 32 x 32 of a 64 x 64 tile.
-template <int FA, int FB, bool OUTBF>
-__global__ __launch_bounds__(kThreads) void k_gemm_blocks(BlockGemmArgs a, int tm, int tn,
-                                                          int total) {
+// The scales of a tile's rows, at the end of a stage: for each row the dword with the bytes
+// of four steps, this step's among them (a load to LDS moves dwords; three of four are
+// read again from L2).
+template <int BP, int BQ, int FP, int FQ>
+struct Scales {
+  static constexpr int kLoads = (BP + BQ) / 64, kAt = (BP + BQ) * 128;
+  const uint8_t *P, *Q;
+  int leftp, leftq, ld, wave, row, rp, rq;
+  uint32_t sp[FP], sq[FQ];
+  // (arguments as TileLoop::init's; wp, wq: the wavefront's place in the tile)
+  __device__ __forceinline__ void init(const uint8_t* p, const uint8_t* q, int pitch, int np,
+                                       int nq, int wp, int wq) {
+    const int lane = threadIdx.x & 63;
+    // (a tile of fewer rows than threads loads them more than once)
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kLoads;
+    P = p;
+    Q = q;
+    ld = pitch;
+    leftp = min(np, BP) * ld;
+    leftq = min(nq, BQ) * ld;
+    row = ((wave < BP / 64 ? wave : wave - BP / 64) * 64 + lane) * ld;
+    rp = kAt + 4 * (wp + (lane & 15));
+    rq = kAt + 4 * (BP + wq + (lane & 15));
+  }
+  __device__ __forceinline__ void load(uint8_t* stage, int k, bool want) {
+    const bool isp = wave < BP / 64;
+    const int at = k & ~3, left = (isp ? leftp : leftq) - at;
+    const __amdgpu_buffer_rsrc_t b = __builtin_amdgcn_make_buffer_rsrc(
+        (void*)((isp ? P : Q) + at), 0, want ? left : 0, kRsrcRaw);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        b, (__attribute__((address_space(3))) void*)(stage + kAt + wave * 256), 4, row, 0, 0, 0);
+  }
+  __device__ __forceinline__ void begin(const uint8_t* stage, int k) {
+#pragma unroll
+    for (int i = 0; i < FP; ++i) sp[i] = stage[rp + (k & 3) + i * 64];
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) sq[j] = stage[rq + (k & 3) + j * 64];
+  }
+};
+
+// The 8-bit matrix instruction.
+template <int FA, int FB, int BP, int BQ, int FP, int FQ>
+struct MacBlocks : Scales<BP, BQ, FP, FQ> {
+  typedef Frag P;
+  typedef Frag Q;
+  __device__ __forceinline__ P p(const Frag& f, int) const { return f; }
+  __device__ __forceinline__ Q q(const Frag& f, int) const { return f; }
+  __device__ __forceinline__ void mac(v4f& c, const P& p, int i, const Q& q, int j) const {
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, FB, FA, 0, this->sp[i], 0,
+                                                         this->sq[j]);
+  }
+};
+
+// The values widened to bf16.
+struct Wide {
+  bf16x8 v[4];
+};
+template <int FA, int FB, int BP, int BQ, int FP, int FQ>
+struct MacWide : Scales<BP, BQ, FP, FQ> {
+  typedef Wide P;
+  typedef Wide Q;
+  template <int FMT>
+  static __device__ __forceinline__ Wide wide(const Frag& f, uint32_t byte) {
+    const float scale = __uint_as_float(byte << 23);
+    Wide w;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) w.v[h] = widen<FMT>(f[2 * h], f[2 * h + 1], scale);
+    return w;
+  }
+  __device__ __forceinline__ P p(const Frag& f, int i) const { return wide<FB>(f, this->sp[i]); }
+  __device__ __forceinline__ Q q(const Frag& f, int j) const { return wide<FA>(f, this->sq[j]); }
+  __device__ __forceinline__ void mac(v4f& c, const P& p, int, const Q& q, int) const {
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(p.v[h], q.v[h], c, 0, 0, 0);
+  }
+};
+
+// Four neighbours of a row of C.
+template <bool OUTBF>
+__device__ __forceinline__ void store4(void* C, long long at, const v4f& v, int n) {
+  if constexpr (OUTBF) {
+    bf16_t* c = (bf16_t*)C + at;
+    uint32_t h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = f32_to_bf16(v[e]);
+    if (n >= 4) {
+      *(u32x2_any*)c = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < n) c[e] = (bf16_t)h[e];
+    }
+  } else {
+    float* c = (float*)C + at;
+    if (n >= 4) {
+      *(v4f_any*)c = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < n) c[e] = v[e];
+    }
+  }
+}
+
+template <int FA, int FB, bool OUTBF, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ), 2) void k_gemm_tile(BlockGemmArgs a,
+                                                                             int tp, int tq,
+                                                                             int total) {
+  using T = TileLoop<BP, BQ, WP, WQ, (BP + BQ) * 4>;
+  __shared__ __align__(16) uint8_t s0[T::kStage];
+  __shared__ __align__(16) uint8_t s1[T::kStage];
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
-  const int g = id / (tm * tn), mt = id % (tm * tn) / tn, nt = id % tn;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lq = lane >> 4;
-  const int m0 = mt * 64 + (wave >> 1) * 32, n0 = nt * 64 + (wave & 1) * 32;
-  const int nb = (a.Kd + 127) / 128;
-  const long long ld = nb * 128LL, lds = (nb + 3) / 4 * 4;
-  const uint8_t *pa[2], *pb[2], *qa[2], *qb[2];
+  const int l = xcd_order(id, total), g = l / (tp * tq);
+  int pt, qt;
+  band_order(l % (tp * tq), tp, tq, pt, qt);
+  const int p0 = pt * BP, q0 = qt * BQ;
+  const int nb = (a.Kd + 127) / 128, ld = nb * 128, lds = (nb + 3) / 4 * 4;
+  T t;
+  t.init(a.B + (long long)g * a.sB + (long long)p0 * ld,
+         a.A + (long long)g * a.sA + (long long)q0 * ld, ld, a.N - p0, a.M - q0);
+  std::conditional_t<OUTBF, MacBlocks<FA, FB, BP, BQ, T::FP, T::FQ>,
+                     MacWide<FA, FB, BP, BQ, T::FP, T::FQ>> mac;
+  mac.init(a.SB + (long long)g * a.sSB + (long long)p0 * lds,
+           a.SA + (long long)g * a.sSA + (long long)q0 * lds, lds, a.N - p0, a.M - q0, t.wp,
+           t.wq);
+  v4f acc[T::FP][T::FQ] = {};
+  t.run(s0, s1, nb, mac, acc);
+  const int lr = t.lane & 15, lq = t.lane >> 4;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int m = min(m0 + i * 16 + lr, a.M - 1), n = min(n0 + i * 16 + lr, a.N - 1);
-    pa[i] = a.A + (long long)g * a.sA + m * ld + lq * 16;
-    pb[i] = a.B + (long long)g * a.sB + n * ld + lq * 16;
-    qa[i] = a.SA + (long long)g * a.sSA + m * lds;
-    qb[i] = a.SB + (long long)g * a.sSB + n * lds;
-  }
-  v4f acc[2][2] = {};
-  for (int kb = 0; kb < nb; ++kb) {
-    v8i va[2], vb[2];
-    int fa[2], fb[2];
+  for (int j = 0; j < T::FQ; ++j) {
+    const int m = q0 + t.wq + j * 16 + lr;
+    if (m >= a.M) continue;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const v4i a0 = *(const v4i*)(pa[i] + kb * 128LL), a1 = *(const v4i*)(pa[i] + kb * 128LL + 64);
-      const v4i b0 = *(const v4i*)(pb[i] + kb * 128LL), b1 = *(const v4i*)(pb[i] + kb * 128LL + 64);
-      va[i] = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
-      vb[i] = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7);
-      fa[i] = qa[i][kb];
-      fb[i] = qb[i][kb];
+    for (int i = 0; i < T::FP; ++i) {
+      const int n = p0 + t.wp + i * 16 + lq * 4;
+      store4<OUTBF>(a.C, (long long)g * a.sC + (long long)m * a.ldc + n, acc[i][j], a.N - n);
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if constexpr (OUTBF) {
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-              vb[j], va[i], acc[i][j], FB, FA, 0, fb[j], 0, fa[i]);
-        } else {
-#pragma unroll
-          for (int h = 0; h < 8; h += 2)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                widen<FB>(vb[j][h], vb[j][h + 1], __uint_as_float((unsigned)fb[j] << 23)),
-                widen<FA>(va[i][h], va[i][h + 1], __uint_as_float((unsigned)fa[i] << 23)),
-                acc[i][j], 0, 0, 0);
-        }
-      }
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int m = m0 + i * 16 + lr, n = n0 + j * 16 + lq * 4;
-      if (m >= a.M) continue;
-      const long long at = (long long)g * a.sC + (long long)m * a.ldc + n;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (n + e < a.N) {
-          if constexpr (OUTBF)
-            ((bf16_t*)a.C)[at + e] = f32_to_bf16(acc[i][j][e]);
-          else
-            ((float*)a.C)[at + e] = acc[i][j][e];
-        }
-    }
+}
+
+template <int FA, int FB, bool OUTBF, int BP, int BQ, int WP, int WQ>
+hipError_t launch_tile(const BlockGemmArgs& a, hipStream_t s) {
+  const long long tp = (a.N + BP - 1LL) / BP, tq = (a.M + BQ - 1LL) / BQ;
+  if (tp * tq > 0x7fffffffLL / a.G) return hipErrorInvalidValue;
+  const long long total = tp * tq * a.G;
+  hipLaunchKernelGGL((k_gemm_tile<FA, FB, OUTBF, BP, BQ, WP, WQ>), grid_of(total),
+                     dim3(64 * (BP / WP) * (BQ / WQ)), 0, s, a, (int)tp, (int)tq, (int)total);
+  return hipGetLastError();
 }
 
 template <int FA, int FB>
 hipError_t gemm_blocks(const BlockGemmArgs& a, hipStream_t s) {
-  const long long tm = (a.M + 63LL) / 64, tn = (a.N + 63LL) / 64;
-  if (tm * tn > 0x7fffffffLL / a.G) return hipErrorInvalidValue;
-  const long long total = tm * tn * a.G;
-  if (a.out_bf16)
-    hipLaunchKernelGGL((k_gemm_blocks<FA, FB, true>), grid_of(total), dim3(kThreads), 0, s, a,
-                       (int)tm, (int)tn, (int)total);
-  else
-    hipLaunchKernelGGL((k_gemm_blocks<FA, FB, false>), grid_of(total), dim3(kThreads), 0, s, a,
-                       (int)tm, (int)tn, (int)total);
-  return hipGetLastError();
+  auto tiles = [&](int b) {
+    return ((a.N + b - 1LL) / b) * ((a.M + b - 1LL) / b) * a.G;
+  };
+  if (a.out_bf16) {
+    if (tiles(256) >= 256) return launch_tile<FA, FB, true, 256, 256, 128, 64>(a, s);
+    if (tiles(128) >= 256) return launch_tile<FA, FB, true, 128, 128, 64, 64>(a, s);
+    return launch_tile<FA, FB, true, 64, 64, 32, 32>(a, s);
+  }
+  if (tiles(128) >= 256) return launch_tile<FA, FB, false, 128, 128, 64, 64>(a, s);
+  return launch_tile<FA, FB, false, 64, 64, 32, 32>(a, s);
 }
 
 }  // namespace

@@ -277,6 +277,9 @@ Layout make_layout(const lsgd_config* c) {
   return l;
 }
 
+// Inner range of a product of blocks: a tile's rows are addressed by 32-bit offsets.
+constexpr int32_t kMaxInner = 1 << 22;
+
 lsgd_status block_status(hipError_t e) {
   return e == hipSuccess ? LSGD_OK : (e == hipErrorInvalidValue ? LSGD_E_INVALID : LSGD_E_HIP);
 }
@@ -1815,7 +1818,8 @@ lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G, int32
 
 lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t G, int32_t M, int32_t N, int32_t Kd,
                                                      size_t* bytes) {
-  if (!bytes || G < 1 || M < 1 || N < 1 || Kd < 1 || G > 65535) return LSGD_E_INVALID;
+  if (!bytes || G < 1 || M < 1 || N < 1 || Kd < 1 || G > 65535 || Kd > kMaxInner)
+    return LSGD_E_INVALID;
   *bytes = lsgd::gemm_blocks_workspace_bytes(G, M, N, Kd);
   return LSGD_OK;
 }
@@ -1830,7 +1834,7 @@ lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b, int32_t
       (format_b != LSGD_E4M3 && format_b != LSGD_E5M2) ||
       (out_dtype != LSGD_FP32 && out_dtype != LSGD_BF16))
     return LSGD_E_INVALID;
-  if (G < 1 || M < 1 || N < 1 || Kd < 1 || G > 65535) return LSGD_E_INVALID;
+  if (G < 1 || M < 1 || N < 1 || Kd < 1 || G > 65535 || Kd > kMaxInner) return LSGD_E_INVALID;
   if (!d_A || !d_SA || !d_B || !d_SB || !d_C || ldc < N) return LSGD_E_INVALID;
   if (sA < 0 || sB < 0 || sSA < 0 || sSB < 0 || sA % 16 || sB % 16 || sSA % 4 || sSB % 4)
     return LSGD_E_INVALID;

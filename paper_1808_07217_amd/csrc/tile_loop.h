@@ -1,0 +1,175 @@
+// The inner loop shared by the products whose two operands both have the contracted
+// index contiguous: tiles of rows of 128 bytes a step, whatever the element type.
+//
+// A workgroup computes BP x BQ results of P Q^T, its wavefronts WP x WQ each, as
+// 16 x 16 blocks: lane l holds two vectors of 16 bytes of row l % 16 of a fragment, the
+// 16-byte pieces l / 16 and l / 16 + 4 of the row's 128 bytes, and result e of lane l is at
+// row 4 (l / 16) + e of P and row l % 16 of Q.
+//
+// Operands go from memory straight to LDS (16 bytes a lane), into two stages. LDS
+// holds rows of 128 bytes without padding; piece c of row r lies in slot c ^ (r % 8),
+// so that eight rows' pieces c fall into different banks. The lanes fetch the
+// pieces in that order, each row still one whole 128-byte line.
+// One barrier a step, before its last row of fragments: every wavefront has then
+// read the stage (it may be overwritten) and its own loads of the next one have
+// landed. What remains of the step's matrix instructions runs while the next step's
+// first fragments are read.
+#pragma once
+#include "device_common.h"
+
+namespace lsgd {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+
+using Frag = v8i;  // pieces l / 16 and l / 16 + 4
+
+// The tile a workgroup of a launch of `total` works on. The hardware deals
+// consecutive ids round-robin to the XCDs, each with an L2 of its own: every XCD
+// takes a contiguous range, and walks it in bands of kBand tile rows, so that the
+// tiles at work at one time share few rows and columns.
+constexpr int kBand = 8;
+__device__ __forceinline__ int xcd_order(int p, int total) {
+  const int x = p % kXcds, each = total / kXcds, rest = total % kXcds;
+  return x * each + min(x, rest) + p / kXcds;
+}
+__device__ __forceinline__ void band_order(int l, int tp, int tq, int& p, int& q) {
+  const int band = l / (kBand * tq), in = l - band * kBand * tq;
+  const int rows = min(kBand, tp - band * kBand);
+  p = band * kBand + in % rows;
+  q = in / rows;
+}
+
+// The last word of a buffer descriptor: plain bytes, bounds checked against its size.
+constexpr int kRsrcRaw = 0x00027000;
+
+// Policy M: types M::P and M::Q (what a fragment becomes once read, by m.p(frag, i) and
+// m.q(frag, j)), m.mac(acc, p, i, q, j), and for what else a step needs m.load(stage, k,
+// want), which starts it on its way to the kExtra bytes at the end of a stage, and
+// m.begin(stage, k), which reads it from there.
+template <int BP, int BQ, int WP, int WQ, int kExtra = 0>
+struct TileLoop {
+  static constexpr int kWaves = (BP / WP) * (BQ / WQ), kThreads = 64 * kWaves;
+  static constexpr int FP = WP / 16, FQ = WQ / 16;
+  static constexpr int kStage = (BP + BQ) * 128 + kExtra;  // bytes
+  static constexpr int kLoads = (BP + BQ) / 8 / kWaves;   // a wavefront's, of 8 rows
+  static_assert(BP / 8 % kWaves == 0 && BQ / 8 % kWaves == 0 && FP % 2 == 0, "tile shape");
+
+  using Rsrc = __amdgpu_buffer_rsrc_t;
+  const uint8_t *P, *Q;  // the tiles' first rows, at the step to be loaded next
+  int leftp, leftq;      // bytes from there to the end of the last row
+  int off, every;        // the lane's place in a load's 8 rows; 8 kWaves rows
+  int lane, wave, wp, wq;
+  uint32_t rp, rq;       // LDS offset of the lane's first piece
+
+  // ld: the row pitch in bytes, 256 ld < 2^31; np, nq: the rows from the tile's first
+  // on that exist. The buffer descriptors end behind the last of them, so that nothing
+  // past it is read; what LDS then holds in its place reaches only results that are
+  // not stored.
+  __device__ __forceinline__ void init(const uint8_t* p, const uint8_t* q, int ld, int np, int nq) {
+    lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    P = p;
+    Q = q;
+    leftp = min(np, BP) * ld;
+    leftq = min(nq, BQ) * ld;
+    off = (lane >> 3) * ld + ((lane & 7) ^ (lane >> 3)) * 16;
+    every = 8 * ld;
+    wp = wave / (BQ / WQ) * WP;
+    wq = wave % (BQ / WQ) * WQ;
+    const int lr = lane & 15, slot = (lane >> 4) ^ (lr & 7);
+    rp = (uint32_t)((wp + lr) * 128 + slot * 16);
+    rq = (uint32_t)((BP + wq + lr) * 128 + slot * 16);
+  }
+  // one step into a stage; !want: nothing is read (no branch: the matrix instructions
+  // before one would be moved past it)
+  __device__ __forceinline__ void load(uint8_t* stage, bool want = true) {
+    const Rsrc bp = __builtin_amdgcn_make_buffer_rsrc((void*)P, 0, want ? leftp : 0, kRsrcRaw);
+    const Rsrc bq = __builtin_amdgcn_make_buffer_rsrc((void*)Q, 0, want ? leftq : 0, kRsrcRaw);
+#pragma unroll
+    for (int t = 0; t < kLoads; ++t) {
+      const int at = wave + t * kWaves;  // the load's eighth of the tile's rows
+      // (a load's wavefronts all fetch P or all Q)
+      if (t < BP / 8 / kWaves)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            bp, (__attribute__((address_space(3))) void*)(stage + at * 1024), 16,
+            off + at * every, 0, 0, 0);
+      else
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            bq, (__attribute__((address_space(3))) void*)(stage + at * 1024), 16,
+            off + (at - BP / 8) * every, 0, 0, 0);
+    }
+    P += 128;
+    Q += 128;
+    leftp -= 128;
+    leftq -= 128;
+  }
+  __device__ __forceinline__ Frag read(const uint8_t* stage, uint32_t at, int i) const {
+    const v4i lo = *(const v4i*)(stage + at + i * 2048);
+    const v4i hi = *(const v4i*)(stage + (at ^ 64) + i * 2048);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+
+  // Step k, from stage `cur`; the loads of step k + 1 are on their way to `nxt`.
+  template <class M>
+  __device__ __forceinline__ void step(uint8_t* cur, uint8_t* nxt, int k, int n, M& m,
+                                       typename M::P (&p)[2], typename M::Q (&q)[FQ],
+                                       v4f (&acc)[FP][FQ]) {
+#pragma unroll
+    for (int i = 0; i + 1 < FP; ++i) {
+      p[(i + 1) & 1] = m.p(read(cur, rp, i + 1), i + 1);
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) m.mac(acc[i][j], p[i & 1], i, q[j], j);
+      __builtin_amdgcn_sched_barrier(0);  // no fragment is read earlier than that
+    }
+    // the next stage is whole, and this one read by everyone
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    load(cur, k + 2 < n);
+    m.load(cur, k + 2, k + 2 < n);
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) m.mac(acc[FP - 1][j], p[1], FP - 1, q[j], j);
+    m.begin(nxt, k + 1);
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) q[j] = m.q(read(nxt, rq, j), j);
+    p[0] = m.p(read(nxt, rp, 0), 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  // The steps 0 .. n - 1 (n >= 1) are multiplied into acc; s0, s1: the two stages.
+  template <class M>
+  __device__ __forceinline__ void run(uint8_t* s0, uint8_t* s1, int n, M& m,
+                                      v4f (&acc)[FP][FQ]) {
+    load(s0);
+    m.load(s0, 0, true);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    load(s1, n > 1);
+    m.load(s1, 1, n > 1);
+    m.begin(s0, 0);
+    typename M::Q q[FQ];
+    typename M::P p[2];
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) q[j] = m.q(read(s0, rq, j), j);
+    p[0] = m.p(read(s0, rp, 0), 0);
+    int k = 0;
+    for (; k + 2 < n; k += 2) {
+      step(s0, s1, k, n, m, p, q, acc);
+      step(s1, s0, k + 1, n, m, p, q, acc);
+    }
+    // one or two steps are left, the last without a next one
+    if (k + 1 < n) step(s0, s1, k, n, m, p, q, acc);
+    const uint8_t* cur = k + 1 < n ? s1 : s0;
+#pragma unroll
+    for (int i = 0; i < FP; ++i) {
+      if (i + 1 < FP) p[(i + 1) & 1] = m.p(read(cur, rp, i + 1), i + 1);
+#pragma unroll
+      for (int j = 0; j < FQ; ++j) m.mac(acc[i][j], p[i & 1], i, q[j], j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
+}  // namespace lsgd

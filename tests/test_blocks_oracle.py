@@ -85,7 +85,7 @@ def test_grouped_gemm_blocks_refusals():
     f, nb = P(4096), ctypes.c_size_t()
     lib = _lib()
     assert lib.lsgd_grouped_gemm_blocks_workspace_bytes(2, 3, 4, 5, None) == 1
-    for bad in ((0, 3, 4, 5), (2, 0, 4, 5), (2, 3, 0, 5), (2, 3, 4, 0), (65536, 3, 4, 5)):
+    for bad in ((0, 3, 4, 5), (2, 3, 4, 2**22 + 1), (2, 0, 4, 5), (2, 3, 0, 5), (2, 3, 4, 0), (65536, 3, 4, 5)):
         assert lib.lsgd_grouped_gemm_blocks_workspace_bytes(*bad, ctypes.byref(nb)) == 1
     ok = [0, 0, 0, 2, 3, 4, 5, f, 384, f, 12, f, 512, f, 16, f, 4, 12, f, 1 << 40, None]
 
@@ -96,7 +96,7 @@ def test_grouped_gemm_blocks_refusals():
         return lib.lsgd_grouped_gemm_blocks(*a)
 
     for bad in (dict(_0=2), dict(_1=-1), dict(_2=2), dict(_3=0), dict(_3=65536), dict(_4=0),
-                dict(_5=0), dict(_6=0), dict(_7=None), dict(_7=P(4104)), dict(_8=-16),
+                dict(_5=0), dict(_6=0), dict(_6=2**22 + 1), dict(_7=None), dict(_7=P(4104)), dict(_8=-16),
                 dict(_8=8), dict(_9=None), dict(_9=P(4098)), dict(_10=-4), dict(_10=3),
                 dict(_11=None), dict(_11=P(4097)), dict(_12=24), dict(_13=None), dict(_13=P(4097)),
                 dict(_14=6), dict(_15=None), dict(_15=P(4098)), dict(_16=3), dict(_17=11)):
