@@ -520,7 +520,7 @@ lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b,
  * an X held in two pieces all the same. A zero matrix stays zero; an
  * infinity or a NaN makes the whole result NaN.
  *
- * Arguments, else LSGD_E_INVALID: 1 <= G <= 65535, M, N >= 1 with
+ * Arguments, else LSGD_E_INVALID: 1 <= G <= 65535, 1 <= M, N <= 2^20 with
  * up(M, 64) up(N, 64) <= 2^30, 1 <= steps <= 64, finite coefficients under
  * which no singular value in [0, 1] grows past 32 on the way, eps finite and
  * > 0. Row pitches are at least N; the groups of a matrix that is written

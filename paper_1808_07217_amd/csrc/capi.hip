@@ -285,7 +285,8 @@ lsgd_status block_status(hipError_t e) {
 }
 
 bool ortho_sizes(int32_t G, int32_t M, int32_t N) {
-  if (G < 1 || G > 65535 || M < 1 || N < 1) return false;
+  // (rows of a tile are addressed by 32-bit offsets: 256 rows of 2^20 values in 4 bytes)
+  if (G < 1 || G > 65535 || M < 1 || N < 1 || M > (1 << 20) || N > (1 << 20)) return false;
   const int64_t m = (M + 63LL) / 64 * 64, n = (N + 63LL) / 64 * 64;
   return m <= (1LL << 30) / n;
 }

@@ -119,7 +119,7 @@ def test_orthogonalise_refusals():
     size = lib.lsgd_orthogonalise_workspace_bytes
     assert size(0, 2, 3, 5, None) == 1
     for bad in ((2, 2, 3, 5), (0, 0, 3, 5), (0, 65536, 3, 5), (0, 2, 0, 5), (0, 2, 3, 0),
-                (0, 1, 1 << 16, 1 << 16), (0, 1, 2**31 - 1, 1), (1, 1, 2**31 - 1, 2**31 - 1)):
+                (0, 1, 1 << 16, 1 << 16), (0, 1, 2**20 + 1, 1), (0, 1, 2**31 - 1, 1), (1, 1, 2**31 - 1, 2**31 - 1)):
         assert size(*bad, ctypes.byref(nb)) == 1, bad
     assert size(0, 2, 3, 5, ctypes.byref(nb)) == 0 and nb.value > 0
     inf, nan = float("inf"), float("nan")
