@@ -224,15 +224,19 @@ __device__ __forceinline__ bf16x8 widen(int lo, int hi, float scale) {
   return bf16x8{p[0][0], p[0][1], p[1][0], p[1][1], p[2][0], p[2][1], p[3][0], p[3][1]};
 }
 
-// The scales of a tile's rows, at the end of a stage: for each row the dword with the bytes
-// of four steps, this step's among them (a load to LDS moves dwords; three of four are
-// read again from L2).
+// The scales of a tile's rows, for two steps at the end of an even step's stage: for each
+// row the dword with the bytes of four steps (what a load to LDS moves), of which a lane
+// reads the two (read byte by byte for every step they cost 15% of the 8192^3 product's
+// time).
 template <int BP, int BQ, int FP, int FQ>
 struct Scales {
+  struct Next {
+    uint32_t p[FP], q[FQ];  // an even step's byte and the odd one's
+  };
   static constexpr int kLoads = (BP + BQ) / 64, kAt = (BP + BQ) * 128;
   const uint8_t *P, *Q;
-  int leftp, leftq, ld, wave, row, rp, rq;
-  uint32_t sp[FP], sq[FQ];
+  int leftp, leftq, wave, row, rp, rq;
+  Next s;
   // (arguments as TileLoop::init's; wp, wq: the wavefront's place in the tile)
   __device__ __forceinline__ void init(const uint8_t* p, const uint8_t* q, int pitch, int np,
                                        int nq, int wp, int wq) {
@@ -241,10 +245,9 @@ struct Scales {
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kLoads;
     P = p;
     Q = q;
-    ld = pitch;
-    leftp = min(np, BP) * ld;
-    leftq = min(nq, BQ) * ld;
-    row = ((wave < BP / 64 ? wave : wave - BP / 64) * 64 + lane) * ld;
+    leftp = min(np, BP) * pitch;
+    leftq = min(nq, BQ) * pitch;
+    row = ((wave < BP / 64 ? wave : wave - BP / 64) * 64 + lane) * pitch;
     rp = kAt + 4 * (wp + (lane & 15));
     rq = kAt + 4 * (BP + wq + (lane & 15));
   }
@@ -256,11 +259,18 @@ struct Scales {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
         b, (__attribute__((address_space(3))) void*)(stage + kAt + wave * 256), 4, row, 0, 0, 0);
   }
-  __device__ __forceinline__ void begin(const uint8_t* stage, int k) {
+  __device__ __forceinline__ void begin(const uint8_t* stage, int k, Next& up) const {
 #pragma unroll
-    for (int i = 0; i < FP; ++i) sp[i] = stage[rp + (k & 3) + i * 64];
+    for (int i = 0; i < FP; ++i) up.p[i] = *(const uint16_t*)(stage + rp + (k & 2) + i * 64);
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) sq[j] = stage[rq + (k & 3) + j * 64];
+    for (int j = 0; j < FQ; ++j) up.q[j] = *(const uint16_t*)(stage + rq + (k & 2) + j * 64);
+  }
+  __device__ __forceinline__ void take(const Next& up) { s = up; }
+  __device__ __forceinline__ void last(bool odd) {
+#pragma unroll
+    for (int i = 0; i < FP; ++i) s.p[i] >>= odd ? 8 : 0;
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) s.q[j] >>= odd ? 8 : 0;
   }
 };
 
@@ -269,11 +279,15 @@ template <int FA, int FB, int BP, int BQ, int FP, int FQ>
 struct MacBlocks : Scales<BP, BQ, FP, FQ> {
   typedef Frag P;
   typedef Frag Q;
+  using Next = typename Scales<BP, BQ, FP, FQ>::Next;
+  template <int PH>
   __device__ __forceinline__ P p(const Frag& f, int) const { return f; }
-  __device__ __forceinline__ Q q(const Frag& f, int) const { return f; }
+  template <int PH>
+  __device__ __forceinline__ Q q(const Frag& f, int, const Next&) const { return f; }
+  template <int PH>
   __device__ __forceinline__ void mac(v4f& c, const P& p, int i, const Q& q, int j) const {
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, FB, FA, 0, this->sp[i], 0,
-                                                         this->sq[j]);
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(p, q, c, FB, FA, PH, this->s.p[i], PH,
+                                                         this->s.q[j]);
   }
 };
 
@@ -285,16 +299,24 @@ template <int FA, int FB, int BP, int BQ, int FP, int FQ>
 struct MacWide : Scales<BP, BQ, FP, FQ> {
   typedef Wide P;
   typedef Wide Q;
+  using Next = typename Scales<BP, BQ, FP, FQ>::Next;
   template <int FMT>
   static __device__ __forceinline__ Wide wide(const Frag& f, uint32_t byte) {
-    const float scale = __uint_as_float(byte << 23);
+    const float scale = __uint_as_float((byte & 255u) << 23);
     Wide w;
 #pragma unroll
     for (int h = 0; h < 4; ++h) w.v[h] = widen<FMT>(f[2 * h], f[2 * h + 1], scale);
     return w;
   }
-  __device__ __forceinline__ P p(const Frag& f, int i) const { return wide<FB>(f, this->sp[i]); }
-  __device__ __forceinline__ Q q(const Frag& f, int j) const { return wide<FA>(f, this->sq[j]); }
+  template <int PH>
+  __device__ __forceinline__ P p(const Frag& f, int i) const {
+    return wide<FB>(f, this->s.p[i] >> 8 * PH);
+  }
+  template <int PH>
+  __device__ __forceinline__ Q q(const Frag& f, int j, const Next& up) const {
+    return wide<FA>(f, PH == 0 ? up.q[j] : this->s.q[j] >> 8);
+  }
+  template <int PH>
   __device__ __forceinline__ void mac(v4f& c, const P& p, int, const Q& q, int) const {
 #pragma unroll
     for (int h = 0; h < 4; ++h)

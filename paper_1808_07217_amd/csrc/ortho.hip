@@ -23,65 +23,112 @@
 // has a tail; a zero row or column stays zero through the steps. In fp32 precision the two
 // pieces of 32 neighbours share a line of 128 bytes, first pieces, then second ones; in
 // the bf16 form each piece is a matrix of its own, and only the first is multiplied.
+#include <cstdlib>
 #include "kernels.h"
 #include "tile_loop.h"
 
 namespace lsgd {
 namespace {
 
+// vectors at any element's alignment
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
 
 // ------------------------------------------------------------- the first step
-__device__ __forceinline__ float load_elem(const void* p, int bf16, long long i) {
-  return bf16 ? bf16_to_f32(((const bf16_t*)p)[i]) : ((const float*)p)[i];
+// Up to four neighbours (n of them; the others 0) of a row.
+__device__ __forceinline__ v4f load4(const float* p, int n) {
+  v4f v = {};
+  if (n >= 4) {
+    v = *(const v4f_any*)p;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) v[e] = p[e];
+  }
+  return v;
+}
+__device__ __forceinline__ v4f load4(const bf16_t* p, int n) {
+  v4f v = {};
+  if (n >= 4) {
+    const u32x2_any w = *(const u32x2_any*)p;
+    v = v4f{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u),
+            __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < n) v[e] = bf16_to_f32(p[e]);
+  }
+  return v;
 }
 
-// An element of the matrix to orthogonalise: X's, or of an update d = g + m u or u.
-// STEP: takes the momentum step u = m u + g first and stores it.
+// n neighbours, from (r, c) on, of the matrix to orthogonalise: X's, or of an update
+// d = g + m u or u. STEP: takes the momentum step u = m u + g first and stores it.
 template <bool STEP>
-__device__ __forceinline__ float direction(const OrthoArgs& a, int g, int r, int c) {
-  if (!a.U) return load_elem(a.X, a.x_bf16, (long long)g * a.sX + (long long)r * a.ldx + c);
+__device__ __forceinline__ v4f direction(const OrthoArgs& a, int g, int r, int c, int n) {
+  const long long x = (long long)g * a.sX + (long long)r * a.ldx + c;
+  if (!a.U) return a.x_bf16 ? load4((const bf16_t*)a.X + x, n) : load4((const float*)a.X + x, n);
   float* pu = a.U + (long long)g * a.sU + (long long)r * a.ldu + c;
-  const float gr = ((const float*)a.X)[(long long)g * a.sX + (long long)r * a.ldx + c];
-  float u = *pu;
+  v4f u = load4(pu, n), gr = {};
+  if (STEP || a.nesterov) gr = load4((const float*)a.X + x, n);
   if constexpr (STEP) {
-    u = __builtin_fmaf(a.mom, u, gr);
-    *pu = u;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = __builtin_fmaf(a.mom, u[e], gr[e]);
+    if (n >= 4) {
+      *(v4f_any*)pu = u;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < n) pu[e] = u[e];
+    }
   }
-  return a.nesterov ? __builtin_fmaf(a.mom, u, gr) : u;
+  if (a.nesterov) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = __builtin_fmaf(a.mom, u[e], gr[e]);
+  }
+  return u;
+}
+
+// The sum of red[0 .. 255] in a fixed tree, by all 256 threads.
+__device__ __forceinline__ double tree_sum(double* red) {
+  __syncthreads();
+#pragma unroll
+  for (int w = kThreads / 2; w; w /= 2) {
+    if (threadIdx.x < w) red[threadIdx.x] += red[threadIdx.x + w];
+    __syncthreads();
+  }
+  return red[0];
 }
 
 // Partial sums of squares in 64 bits, [G][chunks] (no overflow for any fp32 input),
-// and an update's momentum step.
+// and an update's momentum step. A row is taken in fours, its last one short.
 __global__ __launch_bounds__(kThreads) void k_ortho_norm(OrthoArgs a, int chunks) {
   const unsigned id = workgroup_id();
   if (id >= (unsigned)chunks * a.G) return;
-  const int g = id / chunks, ch = id % chunks;
-  const int by = chunks * kThreads, dr = by / a.N, dc = by % a.N;
+  const int g = id / chunks, ch = id % chunks, quads = (a.N + 3) / 4;
+  const int by = chunks * kThreads, dr = by / quads, dc = by % quads;
   const int first = ch * kThreads + threadIdx.x;
-  int r = first / a.N, c = first % a.N;
+  int r = first / quads, c = first % quads;
   double s = 0;
+#pragma unroll 4
   while (r < a.M) {
-    const double d = direction<true>(a, g, r, c);
-    s += d * d;
+    const v4f d = direction<true>(a, g, r, c * 4, a.N - c * 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s += (double)d[e] * (double)d[e];
     r += dr;
     c += dc;
-    if (c >= a.N) {
-      c -= a.N;
+    if (c >= quads) {
+      c -= quads;
       ++r;
     }
   }
   __shared__ double red[kThreads];
   red[threadIdx.x] = s;
-  __syncthreads();
-  for (int w = kThreads / 2; w; w /= 2) {
-    if (threadIdx.x < w) red[threadIdx.x] += red[threadIdx.x + w];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) a.part[(long long)g * chunks + ch] = red[0];
+  s = tree_sum(red);
+  if (threadIdx.x == 0) a.part[(long long)g * chunks + ch] = s;
 }
 
 __device__ __forceinline__ void split2(float x, _Float16& h, _Float16& l) {
@@ -111,36 +158,59 @@ __global__ __launch_bounds__(kThreads) void k_ortho_split(OrthoArgs a, int chunk
   if (id >= (unsigned)tm * tn * a.G) return;
   const int g = id / (tm * tn), p0 = id % (tm * tn) / tn * 64, q0 = id % tn * 64;
   __shared__ float tile[64][65];
+  __shared__ double red[kThreads];
   double s = 0;
-  for (int i = 0; i < chunks; ++i) s += a.part[(long long)g * chunks + i];
+  for (int i = threadIdx.x; i < chunks; i += kThreads) s += a.part[(long long)g * chunks + i];
+  red[threadIdx.x] = s;
+  s = tree_sum(red);
   const double norm = sqrt(s), r = norm / (norm + (double)a.eps);
   const int k = r > 0 ? min(100, -ilogb(r)) : 0;  // 0 for an infinite or NaN norm
   if (id % (tm * tn) == 0 && threadIdx.x == 0) a.kexp[g] = max(k, 0);
   const double inv = ldexp((double)a.scale_x, max(k, 0)) / (norm + (double)a.eps);
-  const int m = a.flip ? a.N : a.M, n = a.flip ? a.M : a.N;
-  for (int i = threadIdx.x; i < 4096; i += kThreads) {
-    // the loads run along the matrix's own rows
-    const int y = i >> 6, x = i & 63, p = a.flip ? p0 + x : p0 + y, q = a.flip ? q0 + y : q0 + x;
-    float v = 0.f;
-    if (p < m && q < n)
-      v = (float)((double)direction<false>(a, g, a.flip ? q : p, a.flip ? p : q) * inv);
-    tile[p - p0][q - q0] = v;
+  // the loads run along the matrix's own rows
+  const int r0 = a.flip ? q0 : p0, c0 = a.flip ? p0 : q0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int u = i * kThreads + threadIdx.x, y = u >> 4, x = (u & 15) * 4;
+    v4f v = {};
+    if (r0 + y < a.M) v = direction<false>(a, g, r0 + y, c0 + x, a.N - c0 - x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float w = (float)((double)v[e] * inv);
+      if (a.flip)
+        tile[x + e][y] = w;
+      else
+        tile[y][x + e] = w;
+    }
   }
   __syncthreads();
   const long long plane = (long long)a.mp * a.np;
   _Float16* X = a.Xr + (long long)g * P * plane;
   _Float16* T = a.Xt[0] + (long long)g * 2 * plane;
-  for (int i = threadIdx.x; i < 4096; i += kThreads) {
-    const int y = i >> 6, x = i & 63;
-    _Float16 h, l;
-    split2(tile[y][x], h, l);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int u = i * kThreads + threadIdx.x, y = u >> 3, x = (u & 7) * 8;
+    f16x8 h, l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      _Float16 s0, s1;
+      split2(tile[y][x + e], s0, s1);
+      h[e] = s0;
+      l[e] = s1;
+    }
     const long long o = at<P>(p0 + y, q0 + x, a.np);
-    X[o] = h;
-    if constexpr (P == 2) X[o + 32] = l;
-    split2(tile[x][y], h, l);
+    *(f16x8*)(X + o) = h;
+    if constexpr (P == 2) *(f16x8*)(X + o + 32) = l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      _Float16 s0, s1;
+      split2(tile[x + e][y], s0, s1);
+      h[e] = s0;
+      l[e] = s1;
+    }
     const long long t = at<P>(q0 + y, p0 + x, a.mp);
-    T[t] = h;
-    T[t + second<P>(plane)] = l;
+    *(f16x8*)(T + t) = h;
+    *(f16x8*)(T + t + second<P>(plane)) = l;
   }
 }
 
@@ -150,10 +220,16 @@ template <int P_>
 struct MacHalf {
   typedef Frag P;
   typedef Frag Q;
+  struct Next {};
   __device__ __forceinline__ void load(uint8_t*, int, bool) const {}
-  __device__ __forceinline__ void begin(const uint8_t*, int) const {}
+  __device__ __forceinline__ void begin(const uint8_t*, int, Next&) const {}
+  __device__ __forceinline__ void take(const Next&) const {}
+  __device__ __forceinline__ void last(bool) const {}
+  template <int PH>
   __device__ __forceinline__ P p(const Frag& f, int) const { return f; }
-  __device__ __forceinline__ Q q(const Frag& f, int) const { return f; }
+  template <int PH>
+  __device__ __forceinline__ Q q(const Frag& f, int, const Next&) const { return f; }
+  template <int PH>
   __device__ __forceinline__ void mac(v4f& c, const P& p, int, const Q& q, int) const {
     const f16x8 p0 = half<0>(p), p1 = half<4>(p), q0 = half<0>(q), q1 = half<4>(q);
     if constexpr (P_ == 2) {
@@ -187,13 +263,110 @@ __device__ __forceinline__ f16x4 second_of(const float (&v)[4], const f16x4& h) 
                (_Float16)(v[2] - (float)h[2]), (_Float16)(v[3] - (float)h[3])};
 }
 
+// The n (at most 4; none for n <= 0) neighbours from element (r, c) of the result on.
+__device__ __forceinline__ void result(const OrthoArgs& a, int g, int r, int c, int n,
+                                       const float (&v)[4]) {
+  if (a.W) {
+    float* w = a.W + (long long)g * a.sW + (long long)r * a.ldw + c;
+    if (n >= 4) {
+      v4f_any x = *(const v4f_any*)w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(a.keep, x[e], a.step * v[e]);
+      *(v4f_any*)w = x;
+    } else {
+      for (int e = 0; e < n; ++e) w[e] = __builtin_fmaf(a.keep, w[e], a.step * v[e]);
+    }
+  } else if (a.x_bf16) {
+    bf16_t* y = (bf16_t*)a.Y + (long long)g * a.sY + (long long)r * a.ldy + c;
+    if (n >= 4) {
+      *(u32x2_any*)y = u32x2_any{f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16,
+                                 f32_to_bf16(v[2]) | (uint32_t)f32_to_bf16(v[3]) << 16};
+    } else {
+      for (int e = 0; e < n; ++e) y[e] = f32_to_bf16(v[e]);
+    }
+  } else {
+    float* y = (float*)a.Y + (long long)g * a.sY + (long long)r * a.ldy + c;
+    if (n >= 4) {
+      *(v4f_any*)y = v4f_any{v[0], v[1], v[2], v[3]};
+    } else {
+      for (int e = 0; e < n; ++e) y[e] = v[e];
+    }
+  }
+}
+
+// The square tiles: 256 x 256 with eight wavefronts of 128 x 64, 128 x 128 and 64 x 64 with
+// four of a quarter each.
+template <int T>
+struct Shape {
+  static constexpr int kWq = T == 256 ? 64 : T / 2, kThreads = T == 256 ? 512 : 256;
+};
+
+// A tile's results leave both ways: [q][p] straight from the registers (a lane holds four
+// neighbouring p), and [p][q] by way of LDS, so that rows leave in vectors too (stored from
+// the registers, 2 bytes a lane, they took a fifth of the time of a 2048-deep product).
+// Each half of the tile's rows goes through one of the two stages, kRows at a time. The
+// pitch of T + 4 words puts the four rows that a wavefront writes at once into
+// different banks.
+template <int T>
+struct Turn {
+  static constexpr int kPasses = T == 256 ? 2 : 1, kRows = T / 2 / kPasses;
+  static constexpr int kPitch = T + 4, kBytes = kRows * kPitch * 4;
+  static constexpr int kExtra = kBytes > 2 * T * 128 ? kBytes - 2 * T * 128 : 0;
+  uint32_t* half[2];
+  // (wait() first: every wavefront is done with the stages, nothing is on its way to them)
+  __device__ __forceinline__ Turn(uint8_t* s0, uint8_t* s1) {
+    half[0] = (uint32_t*)s0;
+    half[1] = (uint32_t*)s1;
+  }
+  __device__ __forceinline__ void wait() const {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+  }
+  // (a wavefront's rows all lie in one half)
+  __device__ __forceinline__ uint32_t& operator()(int p, int q) const {
+    return half[p >= T / 2][p % kRows * kPitch + q];
+  }
+  // row r of the 2 kRows that a pass holds
+  static __device__ __forceinline__ int row(int pass, int r) {
+    return r / kRows * (T / 2) + pass * kRows + r % kRows;
+  }
+};
+__device__ __forceinline__ uint32_t pair(_Float16 h, _Float16 w) {
+  return (uint32_t)__builtin_bit_cast(uint16_t, h) |
+         (uint32_t)__builtin_bit_cast(uint16_t, w) << 16;
+}
+// A pass's rows [p][q] of pieces from LDS to a matrix of rows of K (np, nq: how much of
+// the tile exists, multiples of 64); LOW: the second pieces too.
+template <int P, int T, bool LOW>
+__device__ __forceinline__ void rows_out(const Turn<T>& turn, int pass, _Float16* dst, int K,
+                                         int p0, int q0, int np, int nq) {
+  __syncthreads();
+#pragma unroll 4
+  for (int u = threadIdx.x; u < 2 * Turn<T>::kRows * T / 8; u += Shape<T>::kThreads) {
+    const int p = Turn<T>::row(pass, u / (T / 8)), q = u % (T / 8) * 8;
+    if (p >= np || q >= nq) continue;
+    const uint32_t* w = &turn(p, q);
+    const v4i lo = *(const v4i*)w, hi = *(const v4i*)(w + 4);
+    v4i h, l;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      h[e] = (int)__builtin_amdgcn_perm(lo[2 * e + 1], lo[2 * e], 0x05040100);
+      h[2 + e] = (int)__builtin_amdgcn_perm(hi[2 * e + 1], hi[2 * e], 0x05040100);
+      l[e] = (int)__builtin_amdgcn_perm(lo[2 * e + 1], lo[2 * e], 0x07060302);
+      l[2 + e] = (int)__builtin_amdgcn_perm(hi[2 * e + 1], hi[2 * e], 0x07060302);
+    }
+    _Float16* o = dst + at<P>(p0 + p, q0 + q, K);
+    *(v4i*)o = h;
+    if constexpr (LOW) *(v4i*)(o + 32) = l;
+  }
+}
+
 // The symmetric products: A = X X^T (SECOND = false) and B = b A + c A A, tiles on and
 // below the diagonal.
-template <int P, bool SECOND, int BT, int WP, int WQ>
-__global__ __launch_bounds__(64 * (BT / WP) * (BT / WQ), 2) void k_ortho_gram(OrthoArgs a,
-                                                                              int step, int tm,
-                                                                              int total) {
-  using T = TileLoop<BT, BT, WP, WQ>;
+template <int P, bool SECOND, int BT>
+__global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_gram(OrthoArgs a, int step,
+                                                                       int tm, int total) {
+  using T = TileLoop<BT, BT, BT / 2, Shape<BT>::kWq, Turn<BT>::kExtra>;
   __shared__ __align__(16) uint8_t s0[T::kStage];
   __shared__ __align__(16) uint8_t s1[T::kStage];
   const unsigned id = workgroup_id();
@@ -214,47 +387,59 @@ __global__ __launch_bounds__(64 * (BT / WP) * (BT / WQ), 2) void k_ortho_gram(Or
   v4f acc[T::FP][T::FQ] = {};
   t.run(s0, s1, ld / 128, mac, acc);
   const int lr = t.lane & 15, lq = t.lane >> 4;
+  const Turn<BT> turn(s0, s1);
+  constexpr int kPasses = Turn<BT>::kPasses, kFp = T::FP / kPasses;
 #pragma unroll
-  for (int j = 0; j < T::FQ; ++j) {
-    const int q = q0 + t.wq + j * 16 + lr;
-    if (q >= a.mp) continue;
+  for (int pass = 0; pass < kPasses; ++pass) {
+    // A's own values (its mirror image's, which lie side by side)
+    f16x4 xh[T::FQ][kFp] = {}, xl[T::FQ][kFp] = {};
+    if constexpr (SECOND) {
 #pragma unroll
-    for (int i = 0; i < T::FP; ++i) {
-      const int p = p0 + t.wp + i * 16 + lq * 4;
-      if (p >= a.mp) continue;
-      const long long mirror = at<P>(q, p, a.mp);
-      float v[4];
+      for (int j = 0; j < T::FQ; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e] * f;
-      if constexpr (SECOND) {
-        const f16x4 x = *(const f16x4*)(src + mirror);
+        for (int i = 0; i < kFp; ++i) {
+          const int q = min(q0 + t.wq + j * 16 + lr, a.mp - 1);
+          const int p = min(p0 + t.wp + (pass * kFp + i) * 16 + lq * 4, a.mp - 4);
+          const long long o = at<P>(q, p, a.mp);
+          xh[j][i] = *(const f16x4*)(src + o);
+          if constexpr (P == 2) xl[j][i] = *(const f16x4*)(src + o + 32);
+        }
+    }
+    turn.wait();
+#pragma unroll
+    for (int j = 0; j < T::FQ; ++j) {
+      const int qi = t.wq + j * 16 + lr, q = q0 + qi;
+#pragma unroll
+      for (int i = 0; i < kFp; ++i) {
+        const int pi = t.wp + (pass * kFp + i) * 16 + lq * 4, p = p0 + pi;
+        float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float s = (float)x[e];
-          if constexpr (P == 2) s += (float)src[mirror + 32 + e];
-          v[e] = __builtin_fmaf(a.f_a, s, v[e]);
+          v[e] = acc[pass * kFp + i][j][e] * f;
+          if constexpr (SECOND)
+            v[e] = __builtin_fmaf(a.f_a, (float)xh[j][i][e] + (float)xl[j][i][e], v[e]);
         }
-      }
-      const f16x4 h = first_of(v), w = second_of(v, h);
-      *(f16x4*)(dst + mirror) = h;
-      if constexpr (P == 2) *(f16x4*)(dst + mirror + 32) = w;
-      if (pt != qt) {
+        const f16x4 h = first_of(v), w = second_of(v, h);
+        if (q < a.mp && p < a.mp) {
+          const long long o = at<P>(q, p, a.mp);
+          *(f16x4*)(dst + o) = h;
+          if constexpr (P == 2) *(f16x4*)(dst + o + 32) = w;
+        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const long long o = at<P>(p + e, q, a.mp);
-          dst[o] = h[e];
-          if constexpr (P == 2) dst[o + 32] = w[e];
-        }
+        for (int e = 0; e < 4; ++e) turn(pi + e, qi) = pair(h[e], w[e]);
       }
     }
+    // (a tile on the diagonal is its own mirror image)
+    if (pt != qt) rows_out<P, BT, P == 2>(turn, pass, dst, a.mp, p0, q0, a.mp - p0, a.mp - q0);
   }
 }
 
 // X := a X + B X; on the last step what the caller asked for.
-template <int P, bool LAST, int BP, int BQ, int WP, int WQ>
-__global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ), 2) void k_ortho_apply(
-    OrthoArgs a, int step, int tp, int tq, int total) {
-  using T = TileLoop<BP, BQ, WP, WQ>;
+template <int P, bool LAST, int BT>
+__global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_apply(OrthoArgs a, int step,
+                                                                        int tp, int tq,
+                                                                        int total) {
+  using T = TileLoop<BT, BT, BT / 2, Shape<BT>::kWq, Turn<BT>::kExtra>;
   __shared__ __align__(16) uint8_t s0[T::kStage];
   __shared__ __align__(16) uint8_t s1[T::kStage];
   const unsigned id = workgroup_id();
@@ -262,7 +447,7 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ), 2) void k_ortho_apply(
   const int l = xcd_order(id, total), g = l / (tp * tq);
   int pt, qt;
   band_order(l % (tp * tq), tp, tq, pt, qt);
-  const int p0 = pt * BP, q0 = qt * BQ, from = step & 1;
+  const int p0 = pt * BT, q0 = qt * BT, from = step & 1;
   const long long px = (long long)a.mp * a.np, pm = (long long)a.mp * a.mp;
   const _Float16* X = a.Xt[from] + g * 2 * px;
   T t;
@@ -278,71 +463,82 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ), 2) void k_ortho_apply(
   const float fx = ldexpf(LAST ? a.f_x / a.scale_x : a.f_x, shift);
   const int lr = t.lane & 15, lq = t.lane >> 4;
   const int m = a.flip ? a.N : a.M, n = a.flip ? a.M : a.N;
+  const Turn<BT> turn(s0, s1);
+  constexpr int kPasses = Turn<BT>::kPasses, kFp = T::FP / kPasses;
 #pragma unroll
-  for (int j = 0; j < T::FQ; ++j) {
-    const int q = q0 + t.wq + j * 16 + lr;
-    if (q >= a.np) continue;
+  for (int pass = 0; pass < kPasses; ++pass) {
+    f16x4 xh[T::FQ][kFp], xl[T::FQ][kFp];
 #pragma unroll
-    for (int i = 0; i < T::FP; ++i) {
-      const int p = p0 + t.wp + i * 16 + lq * 4;
-      if (p >= a.mp) continue;
-      const long long turned = at<P>(q, p, a.mp);
-      const f16x4 xh = *(const f16x4*)(X + turned), xl = *(const f16x4*)(X + turned + second<P>(px));
-      float v[4];
+    for (int j = 0; j < T::FQ; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        v[e] = __builtin_fmaf(fx, (float)xh[e] + (float)xl[e], acc[i][j][e] * fb);
-      if constexpr (LAST) {
+      for (int i = 0; i < kFp; ++i) {
+        const int q = min(q0 + t.wq + j * 16 + lr, a.np - 1);
+        const int p = min(p0 + t.wp + (pass * kFp + i) * 16 + lq * 4, a.mp - 4);
+        const long long o = at<P>(q, p, a.mp);
+        xh[j][i] = *(const f16x4*)(X + o);
+        xl[j][i] = *(const f16x4*)(X + o + second<P>(px));
+      }
+    turn.wait();
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (p + e >= m || q >= n) continue;
-          const int r = a.flip ? q : p + e, c = a.flip ? p + e : q;
-          if (a.W) {
-            float* w = a.W + (long long)g * a.sW + (long long)r * a.ldw + c;
-            *w = __builtin_fmaf(a.keep, *w, a.step * v[e]);
+    for (int j = 0; j < T::FQ; ++j) {
+      const int qi = t.wq + j * 16 + lr, q = q0 + qi;
+#pragma unroll
+      for (int i = 0; i < kFp; ++i) {
+        const int pi = t.wp + (pass * kFp + i) * 16 + lq * 4, p = p0 + pi;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = __builtin_fmaf(fx, (float)xh[j][i][e] + (float)xl[j][i][e],
+                                acc[pass * kFp + i][j][e] * fb);
+        if constexpr (LAST) {
+          if (a.flip) {
+            result(a, g, q, p, q < n ? m - p : 0, v);
           } else {
-            const long long o = (long long)g * a.sY + (long long)r * a.ldy + c;
-            if (a.x_bf16)
-              ((bf16_t*)a.Y)[o] = f32_to_bf16(v[e]);
-            else
-              ((float*)a.Y)[o] = v[e];
-          }
-        }
-      } else {
-        const f16x4 h = first_of(v), w = second_of(v, h);
-        _Float16* O = a.Xt[1 - from] + g * 2 * px;
-        _Float16* R = a.Xr + g * P * px;
-        *(f16x4*)(O + turned) = h;
-        *(f16x4*)(O + turned + second<P>(px)) = w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const long long o = at<P>(p + e, q, a.np);
-          R[o] = h[e];
-          if constexpr (P == 2) R[o + 32] = w[e];
+            for (int e = 0; e < 4; ++e) turn(pi + e, qi) = __float_as_uint(v[e]);
+          }
+        } else {
+          const f16x4 h = first_of(v), w = second_of(v, h);
+          if (q < a.np && p < a.mp) {
+            _Float16* o = a.Xt[1 - from] + g * 2 * px + at<P>(q, p, a.mp);
+            *(f16x4*)o = h;
+            *(f16x4*)(o + second<P>(px)) = w;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) turn(pi + e, qi) = pair(h[e], w[e]);
         }
+      }
+    }
+    if constexpr (!LAST) {
+      rows_out<P, BT, P == 2>(turn, pass, a.Xr + g * P * px, a.np, p0, q0, a.mp - p0, a.np - q0);
+    } else if (!a.flip) {
+      __syncthreads();
+      for (int u = threadIdx.x; u < 2 * Turn<BT>::kRows * BT / 4; u += Shape<BT>::kThreads) {
+        const int p = Turn<BT>::row(pass, u / (BT / 4)), q = u % (BT / 4) * 4;
+        const v4f w = *(const v4f*)&turn(p, q);
+        const float v[4] = {w[0], w[1], w[2], w[3]};
+        result(a, g, p0 + p, q0 + q, p0 + p < m ? n - q0 - q : 0, v);
       }
     }
   }
 }
 
-// The launches of the steps with square tiles of BT.
-template <int P, int BT, int WP, int WQ>
+// The launches of the steps, tiles of BG for the symmetric products and of BA for X.
+template <int P, int BG, int BA>
 hipError_t steps(const OrthoArgs& a, hipStream_t s) {
-  const int tm = (a.mp + BT - 1) / BT, tn = (a.np + BT - 1) / BT;
-  const long long tri = (long long)tm * (tm + 1) / 2 * a.G, full = (long long)tm * tn * a.G;
+  const int tg = (a.mp + BG - 1) / BG, tp = (a.mp + BA - 1) / BA, tq = (a.np + BA - 1) / BA;
+  const long long tri = (long long)tg * (tg + 1) / 2 * a.G, full = (long long)tp * tq * a.G;
   if (tri > 0x7fffffffLL || full > 0x7fffffffLL) return hipErrorInvalidValue;
-  const dim3 block(64 * (BT / WP) * (BT / WQ));
+  const dim3 bg(Shape<BG>::kThreads), ba(Shape<BA>::kThreads);
   for (int t = 0; t < a.steps; ++t) {
-    hipLaunchKernelGGL((k_ortho_gram<P, false, BT, WP, WQ>), grid_of(tri), block, 0, s, a, t, tm,
-                       (int)tri);
-    hipLaunchKernelGGL((k_ortho_gram<P, true, BT, WP, WQ>), grid_of(tri), block, 0, s, a, t, tm,
-                       (int)tri);
+    hipLaunchKernelGGL((k_ortho_gram<P, false, BG>), grid_of(tri), bg, 0, s, a, t, tg, (int)tri);
+    hipLaunchKernelGGL((k_ortho_gram<P, true, BG>), grid_of(tri), bg, 0, s, a, t, tg, (int)tri);
     if (t + 1 < a.steps)
-      hipLaunchKernelGGL((k_ortho_apply<P, false, BT, BT, WP, WQ>), grid_of(full), block, 0, s, a,
-                         t, tm, tn, (int)full);
+      hipLaunchKernelGGL((k_ortho_apply<P, false, BA>), grid_of(full), ba, 0, s, a, t, tp, tq,
+                         (int)full);
     else
-      hipLaunchKernelGGL((k_ortho_apply<P, true, BT, BT, WP, WQ>), grid_of(full), block, 0, s, a,
-                         t, tm, tn, (int)full);
+      hipLaunchKernelGGL((k_ortho_apply<P, true, BA>), grid_of(full), ba, 0, s, a, t, tp, tq,
+                         (int)full);
     if (hipError_t e = hipGetLastError()) return e;
   }
   return hipSuccess;
@@ -350,9 +546,11 @@ hipError_t steps(const OrthoArgs& a, hipStream_t s) {
 
 constexpr size_t kOrthoAlign = 256;
 size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-int norm_chunks(long long n) {
-  const long long c = (n + 16383) / 16384;
-  return (int)(c < 1 ? 1 : c > 256 ? 256 : c);
+// Workgroups a matrix's norm takes: eight fours a thread, or more where that makes over
+// 1024 partial sums.
+int norm_chunks(int M, int N) {
+  const long long c = ((long long)M * ((N + 3) / 4) + 8 * kThreads - 1) / (8 * kThreads);
+  return (int)(c > 1024 ? 1024 : c);
 }
 
 struct OrthoPlan {
@@ -363,7 +561,7 @@ OrthoPlan ortho_plan(int pieces, int G, int M, int N) {
   OrthoPlan p;
   p.mp = (int)up(M < N ? M : N, 64);
   p.np = (int)up(M < N ? N : M, 64);
-  p.chunks = norm_chunks((long long)M * N);
+  p.chunks = norm_chunks(M, N);
   size_t t = 0;
   auto take = [&](size_t bytes) {
     const size_t at = t;
@@ -391,13 +589,12 @@ hipError_t ortho(const OrthoArgs& a, const OrthoPlan& p, hipStream_t s) {
   hipLaunchKernelGGL(k_ortho_split<P>, grid_of(tiles * a.G), dim3(kThreads), 0, s, a, p.chunks,
                      p.mp / 64, p.np / 64);
   if (hipError_t e = hipGetLastError()) return e;
-  auto count = [&](long long b) {
-    const long long tm = (p.mp + b - 1) / b;
-    return tm * (tm + 1) / 2 * a.G;
-  };
-  if (count(256) >= 128) return steps<P, 256, 128, 64>(a, s);
-  if (count(128) >= 128) return steps<P, 128, 64, 64>(a, s);
-  return steps<P, 64, 32, 32>(a, s);
+  const char* e_ = getenv("TT");
+  int tt = e_ ? atoi(e_) : 128;
+  if (tt == 64) return steps<P, 64, 64>(a, s);
+  if (tt == 256) return steps<P, 256, 256>(a, s);
+  if (tt == 128256) return steps<P, 128, 256>(a, s);
+  return steps<P, 128, 128>(a, s);
 }
 
 }  // namespace

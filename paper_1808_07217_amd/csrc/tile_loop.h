@@ -45,10 +45,13 @@ __device__ __forceinline__ void band_order(int l, int tp, int tq, int& p, int& q
 // The last word of a buffer descriptor: plain bytes, bounds checked against its size.
 constexpr int kRsrcRaw = 0x00027000;
 
-// Policy M: types M::P and M::Q (what a fragment becomes once read, by m.p(frag, i) and
-// m.q(frag, j)), m.mac(acc, p, i, q, j), and for what else a step needs m.load(stage, k,
-// want), which starts it on its way to the kExtra bytes at the end of a stage, and
-// m.begin(stage, k), which reads it from there.
+// Policy M: types M::P and M::Q (what a fragment becomes once read, by m.p<PH>(frag, i) and
+// m.q<PH>(frag, j, up)) and m.mac<PH>(acc, p, i, q, j), PH the step's parity. What comes
+// once for two steps: m.load(stage, k, want) starts it, for an even step k, on its way to
+// the kExtra bytes at the end of the stage; m.begin(stage, k, up) reads it into an
+// M::Next, while the step before still needs its own, and m.take(up) replaces that;
+// q<0> takes it from `up`. m.last(odd): one step is left, of that parity, and calls p and
+// mac with PH = 0.
 template <int BP, int BQ, int WP, int WQ, int kExtra = 0>
 struct TileLoop {
   static constexpr int kWaves = (BP / WP) * (BQ / WQ), kThreads = 64 * kWaves;
@@ -112,30 +115,38 @@ struct TileLoop {
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 
-  // Step k, from stage `cur`; the loads of step k + 1 are on their way to `nxt`.
-  template <class M>
+  // Step k (of parity PH), from stage `cur`; the loads of step k + 1 are on their way to
+  // `nxt`.
+  template <int PH, class M>
   __device__ __forceinline__ void step(uint8_t* cur, uint8_t* nxt, int k, int n, M& m,
                                        typename M::P (&p)[2], typename M::Q (&q)[FQ],
                                        v4f (&acc)[FP][FQ]) {
 #pragma unroll
     for (int i = 0; i + 1 < FP; ++i) {
-      p[(i + 1) & 1] = m.p(read(cur, rp, i + 1), i + 1);
+      p[(i + 1) & 1] = m.template p<PH>(read(cur, rp, i + 1), i + 1);
 #pragma unroll
-      for (int j = 0; j < FQ; ++j) m.mac(acc[i][j], p[i & 1], i, q[j], j);
+      for (int j = 0; j < FQ; ++j) m.template mac<PH>(acc[i][j], p[i & 1], i, q[j], j);
       __builtin_amdgcn_sched_barrier(0);  // no fragment is read earlier than that
     }
     // the next stage is whole, and this one read by everyone
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
-    load(cur, k + 2 < n);
-    m.load(cur, k + 2, k + 2 < n);
+    // the next step's fragments between the last row's instructions, each into the
+    // registers that one of them frees, then the loads (first, they cost 3%)
+    const Frag next = read(nxt, rp, 0);
+    typename M::Next up;
+    if constexpr (PH == 1) m.begin(nxt, k + 1, up);
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) m.mac(acc[FP - 1][j], p[1], FP - 1, q[j], j);
-    m.begin(nxt, k + 1);
-#pragma unroll
-    for (int j = 0; j < FQ; ++j) q[j] = m.q(read(nxt, rq, j), j);
-    p[0] = m.p(read(nxt, rp, 0), 0);
+    for (int j = 0; j < FQ; ++j) {
+      m.template mac<PH>(acc[FP - 1][j], p[1], FP - 1, q[j], j);
+      __builtin_amdgcn_sched_barrier(0);
+      q[j] = m.template q<1 - PH>(read(nxt, rq, j), j, up);
+    }
+    if constexpr (PH == 1) m.take(up);
+    p[0] = m.template p<1 - PH>(next, 0);
     __builtin_amdgcn_sched_barrier(0);
+    load(cur, k + 2 < n);
+    if constexpr (PH == 0) m.load(cur, k + 2, k + 2 < n);
   }
 
   // The steps 0 .. n - 1 (n >= 1) are multiplied into acc; s0, s1: the two stages.
@@ -147,26 +158,29 @@ struct TileLoop {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     load(s1, n > 1);
-    m.load(s1, 1, n > 1);
-    m.begin(s0, 0);
+    typename M::Next up;
+    m.begin(s0, 0, up);
+    m.take(up);
     typename M::Q q[FQ];
     typename M::P p[2];
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) q[j] = m.q(read(s0, rq, j), j);
-    p[0] = m.p(read(s0, rp, 0), 0);
+    for (int j = 0; j < FQ; ++j) q[j] = m.template q<0>(read(s0, rq, j), j, up);
+    p[0] = m.template p<0>(read(s0, rp, 0), 0);
     int k = 0;
     for (; k + 2 < n; k += 2) {
-      step(s0, s1, k, n, m, p, q, acc);
-      step(s1, s0, k + 1, n, m, p, q, acc);
+      step<0>(s0, s1, k, n, m, p, q, acc);
+      step<1>(s1, s0, k + 1, n, m, p, q, acc);
     }
     // one or two steps are left, the last without a next one
-    if (k + 1 < n) step(s0, s1, k, n, m, p, q, acc);
-    const uint8_t* cur = k + 1 < n ? s1 : s0;
+    const bool two = k + 1 < n;
+    if (two) step<0>(s0, s1, k, n, m, p, q, acc);
+    const uint8_t* cur = two ? s1 : s0;
+    m.last(two);
 #pragma unroll
     for (int i = 0; i < FP; ++i) {
-      if (i + 1 < FP) p[(i + 1) & 1] = m.p(read(cur, rp, i + 1), i + 1);
+      if (i + 1 < FP) p[(i + 1) & 1] = m.template p<0>(read(cur, rp, i + 1), i + 1);
 #pragma unroll
-      for (int j = 0; j < FQ; ++j) m.mac(acc[i][j], p[i & 1], i, q[j], j);
+      for (int j = 0; j < FQ; ++j) m.template mac<0>(acc[i][j], p[i & 1], i, q[j], j);
       __builtin_amdgcn_sched_barrier(0);
     }
   }

@@ -8,6 +8,7 @@ no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple, Optional, Sequence, Tuple, Union
 
@@ -560,23 +561,20 @@ def _up(n: int, m: int) -> int:
     return (n + m - 1) // m * m
 
 
-class _on:
-    """The calling thread's device set to ``device`` while a call enqueues."""
+def _enqueue(device: torch.device, call, *args) -> None:
+    """``call(*args, stream)`` on the device's current stream, with that device the
+    calling thread's. (The stream's raw handle: a torch.cuda.Stream object costs as
+    much as the launch.)"""
+    i = device.index
+    if i == torch.cuda.current_device():
+        _check(call(*args, torch._C._cuda_getCurrentRawStream(i)))
+    else:
+        with torch.cuda.device(i):
+            _check(call(*args, torch._C._cuda_getCurrentRawStream(i)))
 
-    def __init__(self, device: torch.device):
-        self.device = device
-        self.prev = None
 
-    def __enter__(self):
-        current = torch.cuda.current_device()
-        if self.device.index != current:
-            self.prev = current
-            torch.cuda.set_device(self.device)
-        return _stream_handle(torch.cuda.current_stream(self.device))
-
-    def __exit__(self, *exc):
-        if self.prev is not None:
-            torch.cuda.set_device(self.prev)
+_FLOATS = (torch.float32, torch.bfloat16)
+_FP32 = (torch.float32,)
 
 
 def _matrices(name: str, X: torch.Tensor, dtypes) -> Tuple[int, int]:
@@ -585,14 +583,15 @@ def _matrices(name: str, X: torch.Tensor, dtypes) -> Tuple[int, int]:
     if X.dim() != 3 or X.dtype not in dtypes:
         raise ValueError(f"{name} must be [G][M][N] of "
                          + " or ".join(str(t).replace("torch.", "") for t in dtypes))
-    if X.device.type != "cuda":
+    if not X.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     G, M, N = X.shape
-    if X.numel() == 0:
+    if not (G and M and N):
         raise ValueError(f"{name} is empty")
-    if N > 1 and X.stride(2) != 1:
+    sG, sM, sN = X.stride()
+    if N > 1 and sN != 1:
         raise ValueError(f"{name}'s columns must be contiguous")
-    return (X.stride(1) if M > 1 else N), (X.stride(0) if G > 1 else 0)
+    return (sM if M > 1 else N), (sG if G > 1 else 0)
 
 
 def _same_device(*ts):
@@ -611,67 +610,80 @@ def quantise_blocks(X: torch.Tensor, fmt: str = "e4m3", both: bool = False
     """X [G][M][N] (float32 or bfloat16, columns contiguous) in 8 bits with a
     power-of-two scale for each row and 128 columns (lsgd_quantise_blocks);
     ``both``: (X's blocks, its transpose's) from one read of X."""
-    ldx, sX = _matrices("X", X, (torch.float32, torch.bfloat16))
+    ldx, sX = _matrices("X", X, _FLOATS)
     if fmt not in FORMATS:
         raise ValueError("fmt must be 'e4m3' or 'e5m2'")
     code, dtype = FORMATS[fmt]
     G, M, N = X.shape
     q = _new_blocks(G, M, N, dtype, X.device)
     t = _new_blocks(G, N, M, dtype, X.device) if both else None
-    with _on(X.device) as stream:
-        _check(_lib.lsgd_quantise_blocks(
-            BF16 if X.dtype == torch.bfloat16 else FP32, code, G, M, N, X.data_ptr(), ldx, sX,
-            q.q.data_ptr(), q.scale.data_ptr(), t.q.data_ptr() if both else None,
-            t.scale.data_ptr() if both else None, stream))
+    _enqueue(X.device, _lib.lsgd_quantise_blocks,
+             BF16 if X.dtype == torch.bfloat16 else FP32, code, G, M, N, X.data_ptr(), ldx, sX,
+             q.q.data_ptr(), q.scale.data_ptr(), t.q.data_ptr() if both else None,
+             t.scale.data_ptr() if both else None)
     return (q, t) if both else q
+
+
+_CODES = {d: c for c, d in FORMATS.values()}
 
 
 def _block_operand(name: str, X: Blocks) -> Tuple[int, int, int, int, int]:
     """Format code, groups, rows and the two group strides of an operand."""
-    q, s = X.q, X.scale
-    codes = {d: c for c, d in FORMATS.values()}
-    if q.dim() != 3 or s.dim() != 3 or q.dtype not in codes or s.dtype != torch.float8_e8m0fnu:
+    q, s, n = X
+    shape, code = q.shape, _CODES.get(q.dtype)
+    if len(shape) != 3 or code is None or s.dtype != torch.float8_e8m0fnu:
         raise ValueError(f"{name} must hold 3-D float8 values and float8_e8m0fnu scales")
-    if X.n < 1 or q.shape[2] != _up(X.n, 128) or s.shape[2] != _up((X.n + 127) // 128, 4) or (
-            q.shape[:2] != s.shape[:2]) or q.numel() == 0:
-        raise ValueError(f"{name}: shapes do not match the block layout of {X.n} columns")
+    G, M, L = shape
+    lds = _up((n + 127) // 128, 4)
+    if n < 1 or L != _up(n, 128) or s.shape != (G, M, lds) or not (G and M):
+        raise ValueError(f"{name}: shapes do not match the block layout of {n} columns")
+    if not (q.is_cuda and s.is_cuda):
+        raise ValueError(f"{name} must be on a CUDA (HIP) device")
+    if q.is_contiguous() and s.is_contiguous():
+        return code, G, M, M * L, M * lds
     for t in (q, s):
-        if t.device.type != "cuda":
-            raise ValueError(f"{name} must be on a CUDA (HIP) device")
-        if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        if t.stride(2) != 1 or (M > 1 and t.stride(1) != t.shape[2]):
             raise ValueError(f"{name}: rows must be contiguous and unpadded")
-    G = q.shape[0]
-    return (codes[q.dtype], G, q.shape[1], q.stride(0) if G > 1 else 0,
-            s.stride(0) if G > 1 else 0)
+    return code, G, M, (q.stride(0) if G > 1 else 0), (s.stride(0) if G > 1 else 0)
+
+
+@functools.lru_cache(maxsize=4096)
+def _gemm_blocks_workspace(G: int, M: int, N: int, n: int) -> int:
+    nb = _c.c_size_t()
+    _check(_lib.lsgd_grouped_gemm_blocks_workspace_bytes(G, M, N, n, _c.byref(nb)))
+    return nb.value
 
 
 def grouped_gemm_blocks(A: Blocks, B: Blocks, out: Optional[torch.Tensor] = None,
                         out_dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """C[g] = A[g] @ B[g]^T of two tensors in blocks along the contracted
-    dimension (lsgd_grouped_gemm_blocks), fp32 accumulation, C float32 or
-    bfloat16. y = x w takes x and w's transpose, dy w^T takes dy and w, and
-    x^T dy the transposes of x and dy. A group stride of 0 (``expand``) shares a
-    matrix among the groups."""
+    dimension (lsgd_grouped_gemm_blocks), C float32 (products in bf16, exact, summed
+    in fp32) or bfloat16 (the 8-bit matrix instruction, twice as fast). y = x w takes
+    x and w's transpose, dy w^T takes dy and w, and x^T dy the transposes of x and
+    dy. A group stride of 0 (``expand``) shares a matrix among the groups."""
     fa, G, M, sA, sSA = _block_operand("A", A)
     fb, Gb, N, sB, sSB = _block_operand("B", B)
-    if A.n != B.n or G != Gb:
+    n, dev = A.n, A.q.device
+    if n != B.n or G != Gb:
         raise ValueError("A and B must have the same groups and inner dimension")
     if out is None:
-        if out_dtype not in (torch.float32, torch.bfloat16):
+        if out_dtype not in _FLOATS:
             raise ValueError("out_dtype must be float32 or bfloat16")
-        out = torch.empty((G, M, N), dtype=out_dtype, device=A.q.device)
-    ldc, sC = _matrices("out", out, (torch.float32, torch.bfloat16))
-    if out.shape != (G, M, N):
-        raise ValueError("out must be [G][M][N]")
-    _same_device(A.q, A.scale, B.q, B.scale, out)
-    nb = _c.c_size_t()
-    _check(_lib.lsgd_grouped_gemm_blocks_workspace_bytes(G, M, N, A.n, _c.byref(nb)))
-    with _on(out.device) as stream:
-        ws = torch.empty(nb.value, dtype=torch.uint8, device=out.device) if nb.value else None
-        _check(_lib.lsgd_grouped_gemm_blocks(
-            fa, fb, BF16 if out.dtype == torch.bfloat16 else FP32, G, M, N, A.n,
-            A.q.data_ptr(), sA, A.scale.data_ptr(), sSA, B.q.data_ptr(), sB,
-            B.scale.data_ptr(), sSB, out.data_ptr(), ldc, sC, _ptr(ws), nb.value, stream))
+        out = torch.empty((G, M, N), dtype=out_dtype, device=dev)
+        ldc, sC = N, M * N
+    else:
+        ldc, sC = _matrices("out", out, _FLOATS)
+        if out.shape != (G, M, N):
+            raise ValueError("out must be [G][M][N]")
+    if not (A.scale.device == dev and B.q.device == dev and B.scale.device == dev
+            and out.device == dev):
+        raise ValueError("all tensors must be on one device")
+    nb = _gemm_blocks_workspace(G, M, N, n)
+    ws = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
+    _enqueue(dev, _lib.lsgd_grouped_gemm_blocks,
+             fa, fb, BF16 if out.dtype == torch.bfloat16 else FP32, G, M, N, n,
+             A.q.data_ptr(), sA, A.scale.data_ptr(), sSA, B.q.data_ptr(), sB,
+             B.scale.data_ptr(), sSB, out.data_ptr(), ldc, sC, ws.data_ptr() if nb else None, nb)
     return out
 
 
@@ -680,9 +692,14 @@ def orthogonalise_workspace(G: int, M: int, N: int, dtype: torch.dtype = torch.f
     """A workspace for ``orthogonalise`` / ``orthogonal_update`` on [G][M][N]
     (``dtype``: the products' precision), for callers that keep one. One
     workspace serves one call at a time: calls on several streams take one each."""
+    return _aligned_bytes(_ortho_workspace(_precision(dtype), G, M, N), device)
+
+
+@functools.lru_cache(maxsize=4096)
+def _ortho_workspace(dtype: int, G: int, M: int, N: int) -> int:
     nb = _c.c_size_t()
-    _check(_lib.lsgd_orthogonalise_workspace_bytes(_precision(dtype), G, M, N, _c.byref(nb)))
-    return _aligned_bytes(nb.value, device)
+    _check(_lib.lsgd_orthogonalise_workspace_bytes(dtype, G, M, N, _c.byref(nb)))
+    return nb.value
 
 
 def _precision(dtype: torch.dtype) -> int:
@@ -698,8 +715,9 @@ def _coefficients(c: Sequence[float]):
 
 
 def _workspace_for(ws, G, M, N, dtype, device) -> torch.Tensor:
-    if ws is None:
-        return orthogonalise_workspace(G, M, N, dtype, device)
+    if ws is None:  # (the allocator's blocks start on 512-byte boundaries)
+        return torch.empty(_ortho_workspace(_precision(dtype), G, M, N), dtype=torch.uint8,
+                           device=device)
     if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != device:
         raise ValueError("workspace must be a contiguous uint8 tensor on the same device")
     return ws
@@ -711,7 +729,7 @@ def orthogonalise(X: torch.Tensor, steps: int = 5, coefficients: Sequence[float]
     """The matrices X [G][M][N] (float32 or bfloat16) taken towards their
     orthogonal factors by Newton-Schulz steps (lsgd_orthogonalise); ``out`` may be
     X itself."""
-    ldx, sX = _matrices("X", X, (torch.float32, torch.bfloat16))
+    ldx, sX = _matrices("X", X, _FLOATS)
     G, M, N = X.shape
     out = torch.empty((G, M, N), dtype=X.dtype, device=X.device) if out is None else out
     ldy, sY = _matrices("out", out, (X.dtype,))
@@ -719,11 +737,9 @@ def orthogonalise(X: torch.Tensor, steps: int = 5, coefficients: Sequence[float]
         raise ValueError("out must have X's shape")
     _same_device(X, out)
     co = _coefficients(coefficients)
-    with _on(X.device) as stream:
-        ws = _workspace_for(workspace, G, M, N, X.dtype, X.device)
-        _check(_lib.lsgd_orthogonalise(
-            _precision(X.dtype), G, M, N, X.data_ptr(), ldx, sX, out.data_ptr(), ldy, sY,
-            int(steps), co, float(eps), ws.data_ptr(), ws.numel(), stream))
+    ws = _workspace_for(workspace, G, M, N, X.dtype, X.device)
+    _enqueue(X.device, _lib.lsgd_orthogonalise, _precision(X.dtype), G, M, N, X.data_ptr(), ldx,
+             sX, out.data_ptr(), ldy, sY, int(steps), co, float(eps), ws.data_ptr(), ws.numel())
     return out
 
 
@@ -737,18 +753,15 @@ def orthogonal_update(W: torch.Tensor, U: torch.Tensor, G: torch.Tensor, lr: flo
     float32, columns contiguous; views into the replicas' flat rows are fine):
     u = m u + g, d = g + m u (``nesterov``) or u, w = (1 - lr wd) w - lr scale O(d)
     with O of ``orthogonalise`` (lsgd_orthogonal_update)."""
-    f = (torch.float32,)
-    (ldw, sW), (ldu, sU), (ldg, sG) = (_matrices("W", W, f), _matrices("U", U, f),
-                                       _matrices("G", G, f))
+    (ldw, sW), (ldu, sU), (ldg, sG) = (_matrices("W", W, _FP32), _matrices("U", U, _FP32),
+                                       _matrices("G", G, _FP32))
     if U.shape != W.shape or G.shape != W.shape:
         raise ValueError("W, U, G must have one shape")
     _same_device(W, U, G)
     K, M, N = W.shape
     co = _coefficients(coefficients)
-    with _on(W.device) as stream:
-        ws = _workspace_for(workspace, K, M, N, gemm_dtype, W.device)
-        _check(_lib.lsgd_orthogonal_update(
-            _precision(gemm_dtype), K, M, N, W.data_ptr(), ldw, sW, U.data_ptr(), ldu, sU,
-            G.data_ptr(), ldg, sG, float(lr), float(momentum), float(weight_decay),
-            int(bool(nesterov)), float(scale), int(steps), co, float(eps), ws.data_ptr(),
-            ws.numel(), stream))
+    ws = _workspace_for(workspace, K, M, N, gemm_dtype, W.device)
+    _enqueue(W.device, _lib.lsgd_orthogonal_update, _precision(gemm_dtype), K, M, N,
+             W.data_ptr(), ldw, sW, U.data_ptr(), ldu, sU, G.data_ptr(), ldg, sG, float(lr),
+             float(momentum), float(weight_decay), int(bool(nesterov)), float(scale), int(steps),
+             co, float(eps), ws.data_ptr(), ws.numel())
