@@ -526,8 +526,9 @@ lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b,
  * > 0. Row pitches are at least N; the groups of a matrix that is written
  * must not overlap (group stride >= the group's extent, or rows of at least G
  * groups side by side). Workspace: caller-owned device memory of
- * lsgd_orthogonalise_workspace_bytes for the dtype, 256-byte aligned
- * (LSGD_E_WORKSPACE if smaller); one workspace serves one call at a time.
+ * lsgd_orthogonalise_workspace_bytes for the dtype (0 for small matrices; then
+ * NULL is allowed), 256-byte aligned (LSGD_E_WORKSPACE if smaller); one
+ * workspace serves one call at a time.
  */
 lsgd_status lsgd_orthogonalise_workspace_bytes(int32_t dtype, int32_t G,
                                                int32_t M, int32_t N,

@@ -233,7 +233,7 @@ struct Scales {
   struct Next {
     uint32_t p[FP], q[FQ];  // an even step's byte and the odd one's
   };
-  static constexpr int kLoads = (BP + BQ) / 64, kAt = (BP + BQ) * 128;
+  static constexpr int kEvenLoads = 1, kLoads = (BP + BQ) / 64, kAt = (BP + BQ) * 128;
   const uint8_t *P, *Q;
   int leftp, leftq, wave, row, rp, rq;
   Next s;
@@ -351,13 +351,12 @@ __device__ __forceinline__ void store4(void* C, long long at, const v4f& v, int 
   }
 }
 
-template <int FA, int FB, bool OUTBF, int BP, int BQ, int WP, int WQ>
+template <int FA, int FB, bool OUTBF, int BP, int BQ, int WP, int WQ, int S>
 __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ), 2) void k_gemm_tile(BlockGemmArgs a,
                                                                              int tp, int tq,
                                                                              int total) {
-  using T = TileLoop<BP, BQ, WP, WQ, (BP + BQ) * 4>;
-  __shared__ __align__(16) uint8_t s0[T::kStage];
-  __shared__ __align__(16) uint8_t s1[T::kStage];
+  using T = TileLoop<BP, BQ, WP, WQ, S, (BP + BQ) * 4>;
+  LSGD_TILE_STAGES(st, S, T::kStage);
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
   const int l = xcd_order(id, total), g = l / (tp * tq);
@@ -374,7 +373,7 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ), 2) void k_gemm_tile(Blo
            a.SA + (long long)g * a.sSA + (long long)q0 * lds, lds, a.N - p0, a.M - q0, t.wp,
            t.wq);
   v4f acc[T::FP][T::FQ] = {};
-  t.run(s0, s1, nb, mac, acc);
+  t.run(st, nb, mac, acc);
   const int lr = t.lane & 15, lq = t.lane >> 4;
 #pragma unroll
   for (int j = 0; j < T::FQ; ++j) {
@@ -388,12 +387,12 @@ __global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ), 2) void k_gemm_tile(Blo
   }
 }
 
-template <int FA, int FB, bool OUTBF, int BP, int BQ, int WP, int WQ>
+template <int FA, int FB, bool OUTBF, int BP, int BQ, int WP, int WQ, int S = 2>
 hipError_t launch_tile(const BlockGemmArgs& a, hipStream_t s) {
   const long long tp = (a.N + BP - 1LL) / BP, tq = (a.M + BQ - 1LL) / BQ;
   if (tp * tq > 0x7fffffffLL / a.G) return hipErrorInvalidValue;
   const long long total = tp * tq * a.G;
-  hipLaunchKernelGGL((k_gemm_tile<FA, FB, OUTBF, BP, BQ, WP, WQ>), grid_of(total),
+  hipLaunchKernelGGL((k_gemm_tile<FA, FB, OUTBF, BP, BQ, WP, WQ, S>), grid_of(total),
                      dim3(64 * (BP / WP) * (BQ / WQ)), 0, s, a, (int)tp, (int)tq, (int)total);
   return hipGetLastError();
 }
@@ -406,10 +405,10 @@ hipError_t gemm_blocks(const BlockGemmArgs& a, hipStream_t s) {
   if (a.out_bf16) {
     if (tiles(256) >= 256) return launch_tile<FA, FB, true, 256, 256, 128, 64>(a, s);
     if (tiles(128) >= 256) return launch_tile<FA, FB, true, 128, 128, 64, 64>(a, s);
-    return launch_tile<FA, FB, true, 64, 64, 32, 32>(a, s);
+    return launch_tile<FA, FB, true, 64, 64, 32, 32, 4>(a, s);
   }
   if (tiles(128) >= 256) return launch_tile<FA, FB, false, 128, 128, 64, 64>(a, s);
-  return launch_tile<FA, FB, false, 64, 64, 32, 32>(a, s);
+  return launch_tile<FA, FB, false, 64, 64, 32, 32, 4>(a, s);
 }
 
 }  // namespace

@@ -358,8 +358,9 @@ bool ortho_numbers(lsgd::OrthoArgs& a, int32_t steps, const float* h, float eps)
 lsgd_status ortho_launch(int32_t dtype, const lsgd::OrthoArgs& a, void* d_ws, size_t ws_bytes,
                          void* stream) {
   const int pieces = dtype == LSGD_BF16 ? 1 : 2;
-  if (!d_ws || (uintptr_t)d_ws % kAlign) return LSGD_E_INVALID;
-  if (ws_bytes < lsgd::ortho_workspace_bytes(pieces, a.G, a.M, a.N)) return LSGD_E_WORKSPACE;
+  const size_t need = lsgd::ortho_workspace_bytes(pieces, a.G, a.M, a.N);
+  if (need && (!d_ws || (uintptr_t)d_ws % kAlign)) return LSGD_E_INVALID;
+  if (ws_bytes < need) return LSGD_E_WORKSPACE;
   return block_status(lsgd::launch_ortho(pieces, a, d_ws, (hipStream_t)stream));
 }
 

@@ -23,7 +23,11 @@
 // has a tail; a zero row or column stays zero through the steps. In fp32 precision the two
 // pieces of 32 neighbours share a line of 128 bytes, first pieces, then second ones; in
 // the bf16 form each piece is a matrix of its own, and only the first is multiplied.
+#include <atomic>
+#include <cmath>
+#include <cstdio>
 #include <cstdlib>
+
 #include "kernels.h"
 #include "tile_loop.h"
 
@@ -221,6 +225,7 @@ struct MacHalf {
   typedef Frag P;
   typedef Frag Q;
   struct Next {};
+  static constexpr int kEvenLoads = 0;
   __device__ __forceinline__ void load(uint8_t*, int, bool) const {}
   __device__ __forceinline__ void begin(const uint8_t*, int, Next&) const {}
   __device__ __forceinline__ void take(const Next&) const {}
@@ -296,9 +301,10 @@ __device__ __forceinline__ void result(const OrthoArgs& a, int g, int r, int c, 
 
 // The square tiles: 256 x 256 with eight wavefronts of 128 x 64, 128 x 128 and 64 x 64 with
 // four of a quarter each.
-template <int T>
+template <int T, int S>
 struct Shape {
-  static constexpr int kWq = T == 256 ? 64 : T / 2, kThreads = T == 256 ? 512 : 256;
+  static constexpr bool kEight = T == 256 || (T == 128 && S == 4);
+  static constexpr int kWq = T / (kEight ? 4 : 2), kThreads = kEight ? 512 : 256;
 };
 
 // A tile's results leave both ways: [q][p] straight from the registers (a lane holds four
@@ -337,12 +343,12 @@ __device__ __forceinline__ uint32_t pair(_Float16 h, _Float16 w) {
 }
 // A pass's rows [p][q] of pieces from LDS to a matrix of rows of K (np, nq: how much of
 // the tile exists, multiples of 64); LOW: the second pieces too.
-template <int P, int T, bool LOW>
+template <int P, int T, bool LOW, int THREADS>
 __device__ __forceinline__ void rows_out(const Turn<T>& turn, int pass, _Float16* dst, int K,
                                          int p0, int q0, int np, int nq) {
   __syncthreads();
 #pragma unroll 4
-  for (int u = threadIdx.x; u < 2 * Turn<T>::kRows * T / 8; u += Shape<T>::kThreads) {
+  for (int u = threadIdx.x; u < 2 * Turn<T>::kRows * T / 8; u += THREADS) {
     const int p = Turn<T>::row(pass, u / (T / 8)), q = u % (T / 8) * 8;
     if (p >= np || q >= nq) continue;
     const uint32_t* w = &turn(p, q);
@@ -363,12 +369,11 @@ __device__ __forceinline__ void rows_out(const Turn<T>& turn, int pass, _Float16
 
 // The symmetric products: A = X X^T (SECOND = false) and B = b A + c A A, tiles on and
 // below the diagonal.
-template <int P, bool SECOND, int BT>
-__global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_gram(OrthoArgs a, int step,
+template <int P, bool SECOND, int BT, int S>
+__global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_gram(OrthoArgs a, int step,
                                                                        int tm, int total) {
-  using T = TileLoop<BT, BT, BT / 2, Shape<BT>::kWq, Turn<BT>::kExtra>;
-  __shared__ __align__(16) uint8_t s0[T::kStage];
-  __shared__ __align__(16) uint8_t s1[T::kStage];
+  using T = TileLoop<BT, BT, BT / 2, Shape<BT, S>::kWq, S, Turn<BT>::kExtra>;
+  LSGD_TILE_STAGES(st, S, T::kStage);
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
   const int tri = tm * (tm + 1) / 2, l = xcd_order(id, total), g = l / tri;
@@ -383,28 +388,31 @@ __global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_gram(OrthoArgs
   const int ld = K * P * 2;
   t.init((const uint8_t*)src + (long long)p0 * ld, (const uint8_t*)src + (long long)q0 * ld, ld,
          a.mp - p0, a.mp - q0);
+  const int lr = t.lane & 15, lq = t.lane >> 4;
+  constexpr int kPasses = Turn<BT>::kPasses, kFp = T::FP / kPasses;
+  // A's own values (its mirror image's, which lie side by side). A tile of one pass takes
+  // them before the product, where their way from memory is hidden.
+  f16x4 xh[T::FQ][kFp] = {}, xl[T::FQ][kFp] = {};
+  auto own = [&](int pass) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < T::FQ; ++j)
+#pragma unroll
+      for (int i = 0; i < kFp; ++i) {
+        const int q = min(q0 + t.wq + j * 16 + lr, a.mp - 1);
+        const int p = min(p0 + t.wp + (pass * kFp + i) * 16 + lq * 4, a.mp - 4);
+        const long long o = at<P>(q, p, a.mp);
+        xh[j][i] = *(const f16x4*)(src + o);
+        if constexpr (P == 2) xl[j][i] = *(const f16x4*)(src + o + 32);
+      }
+  };
+  if constexpr (SECOND && kPasses == 1) own(0);
   MacHalf<P> mac;
   v4f acc[T::FP][T::FQ] = {};
-  t.run(s0, s1, ld / 128, mac, acc);
-  const int lr = t.lane & 15, lq = t.lane >> 4;
-  const Turn<BT> turn(s0, s1);
-  constexpr int kPasses = Turn<BT>::kPasses, kFp = T::FP / kPasses;
+  t.run(st, ld / 128, mac, acc);
+  const Turn<BT> turn(st[0], st[1]);
 #pragma unroll
   for (int pass = 0; pass < kPasses; ++pass) {
-    // A's own values (its mirror image's, which lie side by side)
-    f16x4 xh[T::FQ][kFp] = {}, xl[T::FQ][kFp] = {};
-    if constexpr (SECOND) {
-#pragma unroll
-      for (int j = 0; j < T::FQ; ++j)
-#pragma unroll
-        for (int i = 0; i < kFp; ++i) {
-          const int q = min(q0 + t.wq + j * 16 + lr, a.mp - 1);
-          const int p = min(p0 + t.wp + (pass * kFp + i) * 16 + lq * 4, a.mp - 4);
-          const long long o = at<P>(q, p, a.mp);
-          xh[j][i] = *(const f16x4*)(src + o);
-          if constexpr (P == 2) xl[j][i] = *(const f16x4*)(src + o + 32);
-        }
-    }
+    if constexpr (SECOND && kPasses > 1) own(pass);
     turn.wait();
 #pragma unroll
     for (int j = 0; j < T::FQ; ++j) {
@@ -430,18 +438,17 @@ __global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_gram(OrthoArgs
       }
     }
     // (a tile on the diagonal is its own mirror image)
-    if (pt != qt) rows_out<P, BT, P == 2>(turn, pass, dst, a.mp, p0, q0, a.mp - p0, a.mp - q0);
+    if (pt != qt) rows_out<P, BT, P == 2, Shape<BT, S>::kThreads>(turn, pass, dst, a.mp, p0, q0, a.mp - p0, a.mp - q0);
   }
 }
 
 // X := a X + B X; on the last step what the caller asked for.
-template <int P, bool LAST, int BT>
-__global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_apply(OrthoArgs a, int step,
+template <int P, bool LAST, int BT, int S>
+__global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_apply(OrthoArgs a, int step,
                                                                         int tp, int tq,
                                                                         int total) {
-  using T = TileLoop<BT, BT, BT / 2, Shape<BT>::kWq, Turn<BT>::kExtra>;
-  __shared__ __align__(16) uint8_t s0[T::kStage];
-  __shared__ __align__(16) uint8_t s1[T::kStage];
+  using T = TileLoop<BT, BT, BT / 2, Shape<BT, S>::kWq, S, Turn<BT>::kExtra>;
+  LSGD_TILE_STAGES(st, S, T::kStage);
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
   const int l = xcd_order(id, total), g = l / (tp * tq);
@@ -454,20 +461,16 @@ __global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_apply(OrthoArg
   const int ld = a.mp * P * 2;
   t.init((const uint8_t*)(a.B + g * P * pm) + (long long)p0 * ld,
          (const uint8_t*)X + (long long)q0 * ld, ld, a.mp - p0, a.np - q0);
-  MacHalf<P> mac;
-  v4f acc[T::FP][T::FQ] = {};
-  t.run(s0, s1, ld / 128, mac, acc);
   const int k = raise(a, g, step);
   const int shift = LAST ? -k : raise(a, g, step + 1) - k;
   const float fb = ldexpf(LAST ? a.f_out : a.f_bx, shift);
   const float fx = ldexpf(LAST ? a.f_x / a.scale_x : a.f_x, shift);
   const int lr = t.lane & 15, lq = t.lane >> 4;
   const int m = a.flip ? a.N : a.M, n = a.flip ? a.M : a.N;
-  const Turn<BT> turn(s0, s1);
   constexpr int kPasses = Turn<BT>::kPasses, kFp = T::FP / kPasses;
-#pragma unroll
-  for (int pass = 0; pass < kPasses; ++pass) {
-    f16x4 xh[T::FQ][kFp], xl[T::FQ][kFp];
+  // X's own values, as in k_ortho_gram
+  f16x4 xh[T::FQ][kFp], xl[T::FQ][kFp];
+  auto own = [&](int pass) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < T::FQ; ++j)
 #pragma unroll
@@ -478,6 +481,15 @@ __global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_apply(OrthoArg
         xh[j][i] = *(const f16x4*)(X + o);
         xl[j][i] = *(const f16x4*)(X + o + second<P>(px));
       }
+  };
+  if constexpr (kPasses == 1) own(0);
+  MacHalf<P> mac;
+  v4f acc[T::FP][T::FQ] = {};
+  t.run(st, ld / 128, mac, acc);
+  const Turn<BT> turn(st[0], st[1]);
+#pragma unroll
+  for (int pass = 0; pass < kPasses; ++pass) {
+    if constexpr (kPasses > 1) own(pass);
     turn.wait();
 #pragma unroll
     for (int j = 0; j < T::FQ; ++j) {
@@ -510,10 +522,10 @@ __global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_apply(OrthoArg
       }
     }
     if constexpr (!LAST) {
-      rows_out<P, BT, P == 2>(turn, pass, a.Xr + g * P * px, a.np, p0, q0, a.mp - p0, a.np - q0);
+      rows_out<P, BT, P == 2, Shape<BT, S>::kThreads>(turn, pass, a.Xr + g * P * px, a.np, p0, q0, a.mp - p0, a.np - q0);
     } else if (!a.flip) {
       __syncthreads();
-      for (int u = threadIdx.x; u < 2 * Turn<BT>::kRows * BT / 4; u += Shape<BT>::kThreads) {
+      for (int u = threadIdx.x; u < 2 * Turn<BT>::kRows * BT / 4; u += Shape<BT, S>::kThreads) {
         const int p = Turn<BT>::row(pass, u / (BT / 4)), q = u % (BT / 4) * 4;
         const v4f w = *(const v4f*)&turn(p, q);
         const float v[4] = {w[0], w[1], w[2], w[3]};
@@ -523,25 +535,311 @@ __global__ __launch_bounds__(Shape<BT>::kThreads, 2) void k_ortho_apply(OrthoArg
   }
 }
 
-// The launches of the steps, tiles of BG for the symmetric products and of BA for X.
-template <int P, int BG, int BA>
-hipError_t steps(const OrthoArgs& a, hipStream_t s) {
-  const int tg = (a.mp + BG - 1) / BG, tp = (a.mp + BA - 1) / BA, tq = (a.np + BA - 1) / BA;
-  const long long tri = (long long)tg * (tg + 1) / 2 * a.G, full = (long long)tp * tq * a.G;
-  if (tri > 0x7fffffffLL || full > 0x7fffffffLL) return hipErrorInvalidValue;
-  const dim3 bg(Shape<BG>::kThreads), ba(Shape<BA>::kThreads);
-  for (int t = 0; t < a.steps; ++t) {
-    hipLaunchKernelGGL((k_ortho_gram<P, false, BG>), grid_of(tri), bg, 0, s, a, t, tg, (int)tri);
-    hipLaunchKernelGGL((k_ortho_gram<P, true, BG>), grid_of(tri), bg, 0, s, a, t, tg, (int)tri);
-    if (t + 1 < a.steps)
-      hipLaunchKernelGGL((k_ortho_apply<P, false, BA>), grid_of(full), ba, 0, s, a, t, tp, tq,
-                         (int)full);
-    else
-      hipLaunchKernelGGL((k_ortho_apply<P, true, BA>), grid_of(full), ba, 0, s, a, t, tp, tq,
-                         (int)full);
-    if (hipError_t e = hipGetLastError()) return e;
+// -------------------------------------------------------------- small matrices
+// A whole matrix in one workgroup's LDS, all steps in one launch (as launches of their own
+// the steps of 64 x 64 matrices took 72 us, nearly all of it between kernels). X lies
+// there once, its two pieces as rows of np + 8 (fragment reads of eight rows fall into
+// different banks); B X takes its columns with ds_read_b64_tr_b16, which gives each lane of
+// 16 its column's four k from a 4 x 16 block. A and B share a place: B replaces A when
+// all of A A is in registers, as X' replaces X. Both precisions take two pieces
+// here: the products are not what such a matrix waits for. Rows and columns are padded
+// with zeros to multiples of 32, a wavefront works on 32 x 32 blocks.
+constexpr int kSmallThreads = 512, kSmallWaves = kSmallThreads / 64, kSmallMost = 128;
+constexpr int kSmallBlocks = 5;  // of X a wavefront
+constexpr size_t kSmallLds = 160 * 1024;
+__host__ __device__ constexpr int pitch(int n) { return n + 8; }
+constexpr size_t small_lds(int mp, int np) {
+  return 4 * (size_t)mp * (pitch(np) + pitch(mp));
+}
+
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+struct Plane2 {  // a matrix's two pieces in LDS
+  _Float16* p[2];
+  int ld;
+};
+// acc += F S^T over K: F's rows from r0 (COLS: its columns, K the slow index) and S's
+// rows from c0 on.
+template <bool COLS>
+__device__ __forceinline__ void block_product(const Plane2& F, int r0, const Plane2& S, int c0,
+                                              int K, int lr, int lq, v4f (&acc)[2][2]) {
+#pragma unroll 1
+  for (int k = 0; k < K; k += 32) {
+    f16x8 f[2][2], g[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        if constexpr (COLS) {
+          typedef short s16x4 __attribute__((ext_vector_type(4)));
+          typedef short s16x8 __attribute__((ext_vector_type(8)));
+          using L = __attribute__((address_space(3))) s16x4;
+          const _Float16* b =
+              F.p[w] + (k + 8 * lq + (lr >> 2)) * F.ld + r0 + i * 16 + 4 * (lr & 3);
+          const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)b);
+          const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(b + 4 * F.ld));
+          f[i][w] = __builtin_bit_cast(
+              f16x8, s16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
+        } else {
+          f[i][w] = *(const f16x8*)(F.p[w] + (r0 + i * 16 + lr) * F.ld + k + 8 * lq);
+        }
+        g[i][w] = *(const f16x8*)(S.p[w] + (c0 + i * 16 + lr) * S.ld + k + 8 * lq);
+      }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[i][1], g[j][0], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[i][0], g[j][1], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[i][0], g[j][0], acc[i][j], 0, 0, 0);
+      }
   }
-  return hipSuccess;
+}
+
+__global__ __launch_bounds__(kSmallThreads) void k_ortho_small(OrthoArgs a, int mp, int np) {
+  extern __shared__ __align__(16) uint8_t small[];
+  const int g = workgroup_id();
+  if (g >= a.G) return;
+  const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lq = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Plane2 X, A;
+  X.ld = pitch(np);
+  A.ld = pitch(mp);
+  X.p[0] = (_Float16*)small;
+  X.p[1] = X.p[0] + mp * X.ld;
+  A.p[0] = X.p[1] + mp * X.ld;
+  A.p[1] = A.p[0] + mp * A.ld;
+
+  // the norm, an update's momentum step with it, in the place of A
+  double* red = (double*)A.p[0];
+  const int quads = (a.N + 3) / 4;
+  double s = 0;
+  for (int u = tid; u < a.M * quads; u += kSmallThreads) {
+    const int r = u / quads, c = u % quads * 4;
+    const v4f d = direction<true>(a, g, r, c, a.N - c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s += (double)d[e] * (double)d[e];
+  }
+  red[tid] = s;
+  for (int w = kSmallThreads / 2; w; w /= 2) {
+    __syncthreads();
+    if (tid < w) red[tid] += red[tid + w];
+  }
+  __syncthreads();
+  const double norm = sqrt(red[0]), ratio = norm / (norm + (double)a.eps);
+  const int k0 = ratio > 0 ? max(0, min(100, -ilogb(ratio))) : 0;  // see k_ortho_split
+  const double inv = ldexp((double)a.scale_x, k0) / (norm + (double)a.eps);
+  // (each thread reads what it wrote itself above)
+  const int rows = a.flip ? np : mp, cols = (a.flip ? mp : np) / 4;
+  for (int u = tid; u < a.M * quads; u += kSmallThreads) {
+    const int r = u / quads, c = u % quads * 4;
+    const v4f d = direction<false>(a, g, r, c, a.N - c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int o = a.flip ? (c + e) * X.ld + r : r * X.ld + c + e;
+      split2((float)((double)d[e] * inv), X.p[0][o], X.p[1][o]);
+    }
+  }
+  // zeros behind the last row and behind each row's last four
+  for (int u = tid; u < rows * cols; u += kSmallThreads) {
+    const int r = u / cols, c = u % cols * 4;
+    if (r < a.M && c < a.N) continue;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int o = a.flip ? (c + e) * X.ld + r : r * X.ld + c + e;
+      X.p[0][o] = X.p[1][o] = (_Float16)0.f;
+    }
+  }
+  __syncthreads();
+
+  const int bm = mp / 32, blocks = bm * bm, xblocks = bm * (np / 32);
+  auto put = [&](const Plane2& to, int r, int c, const float (&v)[4]) __attribute__((always_inline)) {
+    const f16x4 h = first_of(v), l = second_of(v, h);
+    *(f16x4*)(to.p[0] + r * to.ld + c) = h;
+    *(f16x4*)(to.p[1] + r * to.ld + c) = l;
+  };
+  auto get = [&](const Plane2& from, int r, int c) __attribute__((always_inline)) {
+    const f16x4 h = *(const f16x4*)(from.p[0] + r * from.ld + c);
+    const f16x4 l = *(const f16x4*)(from.p[1] + r * from.ld + c);
+    return v4f{(float)h[0] + (float)l[0], (float)h[1] + (float)l[1], (float)h[2] + (float)l[2],
+               (float)h[3] + (float)l[3]};
+  };
+#pragma unroll 1
+  for (int t = 0; t < a.steps; ++t) {
+    const int k = max(0, k0 - t * a.grow), kn = max(0, k0 - (t + 1) * a.grow);
+    const bool last = t + 1 == a.steps;
+    // A = X X^T; symmetric, so a lane's four results go to one row (all blocks: half of
+    // them would leave wavefronts idle)
+    const float fxx = ldexpf(a.f_xx, -2 * k);
+#pragma unroll 1
+    for (int b = wave; b < blocks; b += kSmallWaves) {
+      const int p0 = b / bm * 32, q0 = b % bm * 32;
+      v4f acc[2][2] = {};
+      block_product<false>(X, p0, X, q0, np, lr, lq, acc);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float v[4] = {acc[i][j][0] * fxx, acc[i][j][1] * fxx, acc[i][j][2] * fxx,
+                              acc[i][j][3] * fxx};
+          put(A, q0 + j * 16 + lr, p0 + i * 16 + lq * 4, v);
+        }
+    }
+    __syncthreads();
+    // B = b A + c A A
+    {
+      constexpr int kEach = (kSmallMost / 32) * (kSmallMost / 32) / kSmallWaves;
+      v4f acc[kEach][2][2] = {};
+#pragma unroll
+      for (int n = 0; n < kEach; ++n) {
+        const int b = wave + n * kSmallWaves;
+        if (b < blocks)
+          block_product<false>(A, b / bm * 32, A, b % bm * 32, mp, lr, lq, acc[n]);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int n = 0; n < kEach; ++n) {
+        const int b = wave + n * kSmallWaves;
+        if (b >= blocks) continue;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = b % bm * 32 + j * 16 + lr, c = b / bm * 32 + i * 16 + lq * 4;
+            const v4f x = get(A, r, c);
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              v[e] = __builtin_fmaf(a.f_a, x[e], acc[n][i][j][e] * a.f_aa);
+            put(A, r, c, v);
+          }
+      }
+    }
+    __syncthreads();
+    // X = a X + B X: X's columns as the first operand, so that a lane's results lie in a row
+    const int shift = last ? -k : kn - k;
+    const float fb = ldexpf(last ? a.f_out : a.f_bx, shift);
+    const float fx = ldexpf(last ? a.f_x / a.scale_x : a.f_x, shift);
+    v4f acc[kSmallBlocks][2][2] = {};
+#pragma unroll
+    for (int n = 0; n < kSmallBlocks; ++n) {
+      const int b = wave + n * kSmallWaves;
+      if (b < xblocks)
+        block_product<true>(X, b / bm * 32, A, b % bm * 32, mp, lr, lq, acc[n]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < kSmallBlocks; ++n) {
+      const int b = wave + n * kSmallWaves;
+      if (b >= xblocks) continue;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = b % bm * 32 + j * 16 + lr, c = b / bm * 32 + i * 16 + lq * 4;
+          const v4f x = get(X, r, c);
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[e] = __builtin_fmaf(fx, x[e], acc[n][i][j][e] * fb);
+          if (!last) {
+            put(X, r, c, v);
+          } else {  // the fp32 result, its two halves in the pieces' places
+            u16x4 h, l;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              h[e] = (uint16_t)(__float_as_uint(v[e]) >> 16);
+              l[e] = (uint16_t)__float_as_uint(v[e]);
+            }
+            *(u16x4*)(X.p[0] + r * X.ld + c) = h;
+            *(u16x4*)(X.p[1] + r * X.ld + c) = l;
+          }
+        }
+    }
+    __syncthreads();
+  }
+  for (int u = tid; u < a.M * quads; u += kSmallThreads) {
+    const int r = u / quads, c = u % quads * 4;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int o = a.flip ? (c + e) * X.ld + r : r * X.ld + c + e;
+      v[e] = __uint_as_float((uint32_t)((const uint16_t*)X.p[0])[o] << 16 |
+                             ((const uint16_t*)X.p[1])[o]);
+    }
+    result(a, g, r, c, a.N - c, v);
+  }
+}
+
+// More than 64 KB of LDS has to be asked for once on each device.
+hipError_t allow_small_lds() {
+  static std::atomic<bool> done[64] = {};
+  int dev = 0;
+  if (hipError_t e = hipGetDevice(&dev)) return e;
+  if (dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+  if (done[dev].load(std::memory_order_acquire)) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute(
+      (const void*)k_ortho_small, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kSmallLds);
+  if (e == hipSuccess) done[dev].store(true, std::memory_order_release);
+  return e;
+}
+
+// ------------------------------------------------------------------ launches
+// How a product is cut into n tiles: their size, and how many stages of loads are in
+// flight. More stages hide a load's latency where few workgroups share a compute unit.
+struct Cut {
+  int tile, stages;
+};
+constexpr int kCus = 256;
+// The cut of least estimated time, in units of a 64 x 64 tile's share of a busy compute
+// unit; tiles(T): how many tiles of T there are. Rounds are whole: the last one takes
+// as long as a full one.
+template <class F>
+Cut best_cut(F tiles) {
+  const char* e_ = getenv("TT");
+  if (e_ && atoi(e_)) return Cut{atoi(e_) / 10, atoi(e_) % 10};
+  const Cut cuts[5] = {{64, 4}, {64, 3}, {128, 4}, {128, 2}, {256, 2}};
+  const int per_cu[5] = {2, 3, 1, 2, 1};
+  const double each[5] = {1.5, 1.4, 5.0, 4.0, 13.4};
+  int at = 0;
+  double least = 0;
+  for (int i = 0; i < 5; ++i) {
+    const double rounds = std::ceil((double)tiles(cuts[i].tile) / (kCus * per_cu[i]));
+    const double t = rounds * per_cu[i] * each[i];
+    if (i == 0 || t < least) {
+      at = i;
+      least = t;
+    }
+  }
+  return cuts[at];
+}
+
+template <int P, bool SECOND, int T, int S>
+void launch_gram(const OrthoArgs& a, int step, hipStream_t s) {
+  const int tm = (a.mp + T - 1) / T, total = tm * (tm + 1) / 2 * a.G;
+  hipLaunchKernelGGL((k_ortho_gram<P, SECOND, T, S>), grid_of(total), dim3((Shape<T, S>::kThreads)), 0,
+                     s, a, step, tm, total);
+}
+template <int P, bool SECOND>
+void gram(Cut c, const OrthoArgs& a, int step, hipStream_t s) {
+  if (c.tile == 256) return launch_gram<P, SECOND, 256, 2>(a, step, s);
+  if (c.tile == 128 && c.stages == 2) return launch_gram<P, SECOND, 128, 2>(a, step, s);
+  if (c.tile == 128) return launch_gram<P, SECOND, 128, 4>(a, step, s);
+  if (c.stages == 3) return launch_gram<P, SECOND, 64, 3>(a, step, s);
+  return launch_gram<P, SECOND, 64, 4>(a, step, s);
+}
+template <int P, bool LAST, int T, int S>
+void launch_apply(const OrthoArgs& a, int step, hipStream_t s) {
+  const int tp = (a.mp + T - 1) / T, tq = (a.np + T - 1) / T, total = tp * tq * a.G;
+  hipLaunchKernelGGL((k_ortho_apply<P, LAST, T, S>), grid_of(total), dim3((Shape<T, S>::kThreads)), 0,
+                     s, a, step, tp, tq, total);
+}
+template <int P, bool LAST>
+void apply(Cut c, const OrthoArgs& a, int step, hipStream_t s) {
+  if (c.tile == 256) return launch_apply<P, LAST, 256, 2>(a, step, s);
+  if (c.tile == 128 && c.stages == 2) return launch_apply<P, LAST, 128, 2>(a, step, s);
+  if (c.tile == 128) return launch_apply<P, LAST, 128, 4>(a, step, s);
+  if (c.stages == 3) return launch_apply<P, LAST, 64, 3>(a, step, s);
+  return launch_apply<P, LAST, 64, 4>(a, step, s);
 }
 
 constexpr size_t kOrthoAlign = 256;
@@ -554,11 +852,16 @@ int norm_chunks(int M, int N) {
 }
 
 struct OrthoPlan {
+  bool small;
   int mp, np, chunks;
   size_t part, kexp, xr, xt[2], A, B, total;
 };
 OrthoPlan ortho_plan(int pieces, int G, int M, int N) {
-  OrthoPlan p;
+  OrthoPlan p{};
+  p.mp = (int)up(M < N ? M : N, 32);
+  p.np = (int)up(M < N ? N : M, 32);
+  p.small = p.mp <= kSmallMost && small_lds(p.mp, p.np) <= kSmallLds;
+  if (p.small) return p;
   p.mp = (int)up(M < N ? M : N, 64);
   p.np = (int)up(M < N ? N : M, 64);
   p.chunks = norm_chunks(M, N);
@@ -582,19 +885,28 @@ OrthoPlan ortho_plan(int pieces, int G, int M, int N) {
 
 template <int P>
 hipError_t ortho(const OrthoArgs& a, const OrthoPlan& p, hipStream_t s) {
+  // (64 x 64 tiles are the most there are of anything)
   const long long tiles = (long long)(p.mp / 64) * (p.np / 64);
   if (tiles * a.G > 0x7fffffffLL) return hipErrorInvalidValue;
   hipLaunchKernelGGL(k_ortho_norm, grid_of((long long)p.chunks * a.G), dim3(kThreads), 0, s, a,
                      p.chunks);
   hipLaunchKernelGGL(k_ortho_split<P>, grid_of(tiles * a.G), dim3(kThreads), 0, s, a, p.chunks,
                      p.mp / 64, p.np / 64);
-  if (hipError_t e = hipGetLastError()) return e;
-  const char* e_ = getenv("TT");
-  int tt = e_ ? atoi(e_) : 128;
-  if (tt == 64) return steps<P, 64, 64>(a, s);
-  if (tt == 256) return steps<P, 256, 256>(a, s);
-  if (tt == 128256) return steps<P, 128, 256>(a, s);
-  return steps<P, 128, 128>(a, s);
+  auto across = [](long long r, int T) { return (r + T - 1) / T; };
+  const Cut cg = best_cut([&](int T) {
+    return across(p.mp, T) * (across(p.mp, T) + 1) / 2 * a.G;
+  });
+  const Cut ca = best_cut([&](int T) { return across(p.mp, T) * across(p.np, T) * a.G; });
+  for (int t = 0; t < a.steps; ++t) {
+    gram<P, false>(cg, a, t, s);
+    gram<P, true>(cg, a, t, s);
+    if (t + 1 < a.steps)
+      apply<P, false>(ca, a, t, s);
+    else
+      apply<P, true>(ca, a, t, s);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
@@ -616,6 +928,12 @@ hipError_t launch_ortho(int pieces, OrthoArgs a, void* ws, hipStream_t s) {
   a.flip = a.M > a.N;
   a.mp = p.mp;
   a.np = p.np;
+  if (p.small) {
+    const size_t lds = small_lds(p.mp, p.np);
+    if (hipError_t e = allow_small_lds()) return e;
+    hipLaunchKernelGGL(k_ortho_small, grid_of(a.G), dim3(kSmallThreads), lds, s, a, p.mp, p.np);
+    return hipGetLastError();
+  }
   return pieces == 2 ? ortho<2>(a, p, s) : ortho<1>(a, p, s);
 }
 

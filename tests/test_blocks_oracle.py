@@ -121,13 +121,16 @@ def test_orthogonalise_refusals():
     for bad in ((2, 2, 3, 5), (0, 0, 3, 5), (0, 65536, 3, 5), (0, 2, 0, 5), (0, 2, 3, 0),
                 (0, 1, 1 << 16, 1 << 16), (0, 1, 2**20 + 1, 1), (0, 1, 2**31 - 1, 1), (1, 1, 2**31 - 1, 2**31 - 1)):
         assert size(*bad, ctypes.byref(nb)) == 1, bad
-    assert size(0, 2, 3, 5, ctypes.byref(nb)) == 0 and nb.value > 0
+    assert size(0, 2, 3, 5, ctypes.byref(nb)) == 0
+    # (150 x 200: larger than one launch takes, so there is a workspace)
+    assert size(0, 2, 150, 200, ctypes.byref(nb)) == 0 and nb.value > 0
     inf, nan = float("inf"), float("nan")
 
     def co(*v):
         return (ctypes.c_float * 3)(*v)
 
-    ok = [0, 2, 3, 5, f, 5, 15, f, 5, 15, 5, CO, ctypes.c_float(1e-7), f, nb.value, None]
+    M, N, S = 150, 200, 150 * 200
+    ok = [0, 2, M, N, f, N, S, f, N, S, 5, CO, ctypes.c_float(1e-7), f, nb.value, None]
 
     def call(**kw):
         a = list(ok)
@@ -136,8 +139,9 @@ def test_orthogonalise_refusals():
         return lib.lsgd_orthogonalise(*a)
 
     for bad in (dict(_0=2), dict(_1=0), dict(_2=0), dict(_3=0), dict(_4=None), dict(_4=P(4098)),
-                dict(_5=4), dict(_6=-1), dict(_7=None), dict(_7=P(4097)), dict(_8=4), dict(_9=14),
-                dict(_9=-15), dict(_9=0), dict(_8=9, _9=5), dict(_10=0), dict(_10=65),
+                dict(_5=N - 1), dict(_6=-1), dict(_7=None), dict(_7=P(4097)), dict(_8=N - 1),
+                dict(_9=S - 1), dict(_9=-S), dict(_9=0), dict(_8=2 * N - 1, _9=N), dict(_10=0),
+                dict(_10=65),
                 dict(_11=None), dict(_11=co(inf, 0, 0)), dict(_11=co(1, nan, 0)),
                 dict(_11=co(40, 0, 0)), dict(_11=co(3, 0, 0)), dict(_12=ctypes.c_float(0.0)),
                 dict(_12=ctypes.c_float(-1e-7)), dict(_12=ctypes.c_float(nan)),
@@ -149,9 +153,10 @@ def test_orthogonalise_refusals():
 def test_orthogonal_update_refusals():
     f, nb = P(4096), ctypes.c_size_t()
     lib = _lib()
-    assert lib.lsgd_orthogonalise_workspace_bytes(0, 2, 3, 5, ctypes.byref(nb)) == 0
+    M, N, S = 150, 200, 150 * 200
+    assert lib.lsgd_orthogonalise_workspace_bytes(0, 2, M, N, ctypes.byref(nb)) == 0
     c = ctypes.c_float
-    ok = [0, 2, 3, 5, f, 5, 15, f, 5, 15, f, 5, 15, c(0.1), c(0.9), c(0.01), 0, c(1.0), 5, CO,
+    ok = [0, 2, M, N, f, N, S, f, N, S, f, N, S, c(0.1), c(0.9), c(0.01), 0, c(1.0), 5, CO,
           c(1e-7), f, nb.value, None]
 
     def call(**kw):
@@ -161,9 +166,9 @@ def test_orthogonal_update_refusals():
         return lib.lsgd_orthogonal_update(*a)
 
     nan = float("nan")
-    for bad in (dict(_0=2), dict(_1=0), dict(_2=0), dict(_3=0), dict(_4=None), dict(_5=4),
-                dict(_6=14), dict(_6=0), dict(_7=None), dict(_7=P(4098)), dict(_8=4), dict(_9=7),
-                dict(_10=None), dict(_11=4), dict(_12=-1), dict(_13=c(nan)), dict(_14=c(1.0)),
+    for bad in (dict(_0=2), dict(_1=0), dict(_2=0), dict(_3=0), dict(_4=None), dict(_5=N - 1),
+                dict(_6=S - 1), dict(_6=0), dict(_7=None), dict(_7=P(4098)), dict(_8=N - 1),
+                dict(_9=N - 1), dict(_10=None), dict(_11=N - 1), dict(_12=-1), dict(_13=c(nan)), dict(_14=c(1.0)),
                 dict(_14=c(-0.1)), dict(_14=c(nan)), dict(_15=c(nan)), dict(_16=2),
                 dict(_17=c(nan)), dict(_18=0), dict(_19=None), dict(_20=c(0.0)), dict(_21=None)):
         assert call(**bad) == 1, bad
