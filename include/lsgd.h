@@ -482,8 +482,12 @@ lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G,
 
 /*
  * Grouped product of matrices in blocks along the contracted dimension:
- *   C_g[M][N] = A_g[M][Kd] * B_g[N][Kd]^T   (fp32 accumulation)
- * A_g is M rows, B_g N rows of Kd values in the layout above (format_a,
+ *   C_g[M][N] = A_g[M][Kd] * B_g[N][Kd]^T
+ * with the precision of C: to LSGD_FP32 every product is exact and summed in
+ * fp32; to LSGD_BF16 the 8-bit matrix instruction, which sums eight
+ * neighbouring products at a time with 13 bits below the largest of them (an
+ * error of about 2^-15 of sum |a b|, 2^-10 at worst) and those sums in fp32, and
+ * one rounding at the end. A_g is M rows, B_g N rows of Kd values in the layout above (format_a,
  * format_b may differ): the forward product y = x w takes x and the transpose of
  * w, the input gradient dy w^T takes dy and w, the weight gradient x^T dy the
  * transposes of both. sA, sB (bytes, multiples of 16) and sSA, sSB (scale bytes,
@@ -493,11 +497,12 @@ lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G,
  * below 255. Kd <= 2^22. C is out_dtype LSGD_FP32 or LSGD_BF16 (rounded once), row pitch
  * ldc >= N, group stride sC >= M * ldc (any value for G == 1); nothing between
  * its rows is written. d_ws: workspace of
- * lsgd_grouped_gemm_blocks_workspace_bytes (which may be 0; then NULL is
+ * lsgd_grouped_gemm_blocks_workspace_bytes (for the same sizes; which may be 0; then NULL is
  * allowed), 16-byte aligned, LSGD_E_WORKSPACE if smaller. A result does not
  * depend on what the workspace held.
  */
-lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t G, int32_t M,
+lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t out_dtype,
+                                                     int32_t G, int32_t M,
                                                      int32_t N, int32_t Kd,
                                                      size_t* bytes);
 lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b,

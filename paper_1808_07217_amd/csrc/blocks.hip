@@ -9,6 +9,8 @@
 // non-zero value, so each element is rounded once. Infinities and NaN stay
 // out of the maximum and are stored as the format has them (e4m3 holds no
 // infinity: NaN), so that every product that reads one shows it.
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "kernels.h"
@@ -237,16 +239,17 @@ struct Scales {
   const uint8_t *P, *Q;
   int leftp, leftq, wave, row, rp, rq;
   Next s;
-  // (arguments as TileLoop::init's; wp, wq: the wavefront's place in the tile)
+  // (arguments as TileLoop::init's; wp, wq: the wavefront's place in the tile;
+  // k0: the first step, a multiple of four)
   __device__ __forceinline__ void init(const uint8_t* p, const uint8_t* q, int pitch, int np,
-                                       int nq, int wp, int wq) {
+                                       int nq, int wp, int wq, int k0) {
     const int lane = threadIdx.x & 63;
     // (a tile of fewer rows than threads loads them more than once)
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kLoads;
-    P = p;
-    Q = q;
-    leftp = min(np, BP) * pitch;
-    leftq = min(nq, BQ) * pitch;
+    P = p + k0;
+    Q = q + k0;
+    leftp = min(np, BP) * pitch - k0;
+    leftq = min(nq, BQ) * pitch - k0;
     row = ((wave < BP / 64 ? wave : wave - BP / 64) * 64 + lane) * pitch;
     rp = kAt + 4 * (wp + (lane & 15));
     rq = kAt + 4 * (BP + wq + (lane & 15));
@@ -324,91 +327,218 @@ struct MacWide : Scales<BP, BQ, FP, FQ> {
   }
 };
 
-// Four neighbours of a row of C.
-template <bool OUTBF>
-__device__ __forceinline__ void store4(void* C, long long at, const v4f& v, int n) {
-  if constexpr (OUTBF) {
+// Eight neighbours of a row of C from LDS, n of them.
+template <bool BF>
+__device__ __forceinline__ void store8(void* C, long long at, const uint8_t* from, int n) {
+  if constexpr (BF) {
     bf16_t* c = (bf16_t*)C + at;
-    uint32_t h[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = f32_to_bf16(v[e]);
-    if (n >= 4) {
-      *(u32x2_any*)c = u32x2{h[0] | h[1] << 16, h[2] | h[3] << 16};
+    if (n >= 8) {
+      *(u32x4_any*)c = *(const u32x4*)from;
     } else {
-#pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (e < n) c[e] = (bf16_t)h[e];
+      for (int e = 0; e < n; ++e) c[e] = ((const bf16_t*)from)[e];
     }
   } else {
     float* c = (float*)C + at;
-    if (n >= 4) {
-      *(v4f_any*)c = v;
+    if (n >= 8) {
+      *(v4f_any*)c = *(const v4f*)from;
+      *(v4f_any*)(c + 4) = *(const v4f*)(from + 16);
     } else {
-#pragma unroll
-      for (int e = 0; e < 3; ++e)
-        if (e < n) c[e] = v[e];
+      for (int e = 0; e < n; ++e) c[e] = ((const float*)from)[e];
     }
   }
 }
 
+// Tiles of C by way of LDS, in C's type, so that whole rows of a tile leave at once (the
+// halves of its rows in two of the stages; a pitch of 16 bytes more than a row spreads the
+// sixteen rows that a wavefront writes at once over the banks).
+template <bool BF, int THREADS, class T>
+__device__ __forceinline__ void tile_out(const T& t, const v4f (&acc)[T::FP][T::FQ], uint8_t* s0,
+                                         uint8_t* s1, void* C, long long row0, long long ldc,
+                                         int np, int nq) {
+  constexpr int kSize = BF ? 2 : 4, kPitch = T::kP * kSize + 16, kHalf = T::kQ / 2;
+  static_assert(kHalf * kPitch <= T::kStage, "half a tile fits a stage");
+  auto at = [&](int q, int p) __attribute__((always_inline)) {
+    return (q < kHalf ? s0 : s1) + q % kHalf * kPitch + p * kSize;
+  };
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int j = 0; j < T::FQ; ++j)
+#pragma unroll
+    for (int i = 0; i < T::FP; ++i) {
+      uint8_t* to = at(t.wq + j * 16 + (t.lane & 15), t.wp + i * 16 + (t.lane >> 4) * 4);
+      const v4f v = acc[i][j];
+      if constexpr (BF)
+        *(u32x2*)to = u32x2{f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16,
+                            f32_to_bf16(v[2]) | (uint32_t)f32_to_bf16(v[3]) << 16};
+      else
+        *(v4f*)to = v;
+    }
+  __syncthreads();
+#pragma unroll 2
+  for (int u = threadIdx.x; u < T::kP * T::kQ / 8; u += THREADS) {
+    const int q = u / (T::kP / 8), p = u % (T::kP / 8) * 8;
+    if (q < nq && p < np) store8<BF>(C, row0 + (long long)q * ldc + p, at(q, p), np - p);
+  }
+}
+
+// The tile of BP rows of B and BQ rows of A, over one of `splits` ranges of the inner
+// dimension (chunk steps each, a multiple of four); a split's sums go to `part`.
 template <int FA, int FB, bool OUTBF, int BP, int BQ, int WP, int WQ, int S>
-__global__ __launch_bounds__(64 * (BP / WP) * (BQ / WQ), 2) void k_gemm_tile(BlockGemmArgs a,
-                                                                             int tp, int tq,
-                                                                             int total) {
+__global__ __launch_bounds__((64 * (BP / WP) * (BQ / WQ)), 2) void k_gemm_tile(BlockGemmArgs a,
+                                                                               int tp, int tq,
+                                                                               int total) {
   using T = TileLoop<BP, BQ, WP, WQ, S, (BP + BQ) * 4>;
   LSGD_TILE_STAGES(st, S, T::kStage);
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
-  const int l = xcd_order(id, total), g = l / (tp * tq);
+  int l = xcd_order(id, total);
+  const int sg = l / (tp * tq), g = sg % a.G, split = sg / a.G;
   int pt, qt;
   band_order(l % (tp * tq), tp, tq, pt, qt);
   const int p0 = pt * BP, q0 = qt * BQ;
   const int nb = (a.Kd + 127) / 128, ld = nb * 128, lds = (nb + 3) / 4 * 4;
+  const int k0 = split * a.chunk, steps = min(a.chunk, nb - k0);
   T t;
-  t.init(a.B + (long long)g * a.sB + (long long)p0 * ld,
-         a.A + (long long)g * a.sA + (long long)q0 * ld, ld, a.N - p0, a.M - q0);
+  t.init(a.B + (long long)g * a.sB + (long long)p0 * ld, a.A + (long long)g * a.sA + (long long)q0 * ld,
+         ld, a.N - p0, a.M - q0);
+  t.skip(k0);
   std::conditional_t<OUTBF, MacBlocks<FA, FB, BP, BQ, T::FP, T::FQ>,
                      MacWide<FA, FB, BP, BQ, T::FP, T::FQ>> mac;
   mac.init(a.SB + (long long)g * a.sSB + (long long)p0 * lds,
            a.SA + (long long)g * a.sSA + (long long)q0 * lds, lds, a.N - p0, a.M - q0, t.wp,
-           t.wq);
+           t.wq, k0);
   v4f acc[T::FP][T::FQ] = {};
-  t.run(st, nb, mac, acc);
-  const int lr = t.lane & 15, lq = t.lane >> 4;
-#pragma unroll
-  for (int j = 0; j < T::FQ; ++j) {
-    const int m = q0 + t.wq + j * 16 + lr;
-    if (m >= a.M) continue;
-#pragma unroll
-    for (int i = 0; i < T::FP; ++i) {
-      const int n = p0 + t.wp + i * 16 + lq * 4;
-      store4<OUTBF>(a.C, (long long)g * a.sC + (long long)m * a.ldc + n, acc[i][j], a.N - n);
+  t.run(st, steps, mac, acc);
+  if constexpr (T::kStage >= BQ / 2 * (BP * 4 + 16)) {
+    if (a.splits > 1) {
+      tile_out<false, T::kThreads>(t, acc, st[0], st[1], a.part,
+                                   ((long long)sg * a.M + q0) * a.N + p0, a.N, a.N - p0, a.M - q0);
+      return;
     }
   }
+  tile_out<OUTBF, T::kThreads>(t, acc, st[0], st[1], a.C,
+                               (long long)g * a.sC + (long long)q0 * a.ldc + p0, a.ldc, a.N - p0,
+                               a.M - q0);
 }
 
-template <int FA, int FB, bool OUTBF, int BP, int BQ, int WP, int WQ, int S = 2>
+// C = the splits' sums in ascending order, four neighbours a thread.
+template <bool OUTBF>
+__global__ __launch_bounds__(kThreads) void k_gemm_join(BlockGemmArgs a, int quads,
+                                                        long long total) {
+  const long long i = (long long)workgroup_id() * kThreads + threadIdx.x;
+  if (i >= total) return;
+  const long long row = i / quads;  // of G M
+  const int n = (int)(i % quads) * 4, left = a.N - n;
+  const long long each = (long long)a.G * a.M * a.N;
+  const float* p = a.part + row * a.N + n;
+  v4f v = {};
+  for (int s = 0; s < a.splits; ++s, p += each) {
+    if (left >= 4) {
+      v += *(const v4f_any*)p;
+    } else {
+      for (int e = 0; e < left; ++e) v[e] += p[e];
+    }
+  }
+  const long long at = row / a.M * a.sC + row % a.M * a.ldc + n;
+  for (int e = 0; e < 4 && e < left; ++e) {
+    if constexpr (OUTBF)
+      ((bf16_t*)a.C)[at + e] = f32_to_bf16(v[e]);
+    else
+      ((float*)a.C)[at + e] = v[e];
+  }
+}
+
+// ------------------------------------------------------------------ launches
+constexpr int kCus = 256;
+long long tiles_of(int G, int M, int N, long long b) {
+  return (N + b - 1) / b * ((M + b - 1) / b) * G;
+}
+
+// Ranges the inner dimension is cut into: as many as leave the least estimated time where
+// 64 x 64 tiles leave compute units idle. A workgroup alone on its unit takes 0.18 us a
+// step (0.39 to fp32), all of them together cannot beat 5 TB/s, and a second launch
+// joins the sums (4 us, and their bytes). Measured in us, cut in 1 / 2 / 4 / 8: 512 x 512 x
+// 8192 to bf16 17 / 12 / 11 / 15, 512 x 512 x 65536 126 / 71 / 46 / 44, 128 x 4096 x 4096 to bf16
+// 8.8 / 10.5 / 15 / 20, 1 x 8192 x 8192 to fp32 28 / 20 / 19 / 23.
+int splits_of(bool bf16, int G, int M, int N, int Kd) {
+  const long long tiles = tiles_of(G, M, N, 64), nb = (Kd + 127) / 128;
+  const double step = bf16 ? 0.18 : 0.39;
+  const double bytes = (double)G * ((double)M + N) * nb * 128 / 5e6;
+  const double sums = 2.0 * G * M * N * sizeof(float) / 4e6;  // written and read, a range
+  int best = 1;
+  double least = std::max(step * nb, bytes);
+  for (int s = 2; s <= 64 && tiles * s <= 2 * kCus && nb >= 4 * s; s *= 2) {
+    const double t = std::max(step * nb / s, bytes) + 4 + sums * s;
+    if (t < least) {
+      best = s;
+      least = t;
+    }
+  }
+  // whole groups of four steps: fewer ranges may do
+  const long long chunk = (nb + 4 * best - 1) / (4 * best) * 4;
+  return (int)((nb + chunk - 1) / chunk);
+}
+
+// Tile sizes and stages, by estimated time: see ortho.hip's for what the numbers mean;
+// these are from 4096^3 and 8192^3 (us, to bf16 112 / 82 / 73 / 62 and 886 / 597 / 492 / 404;
+// to fp32 170 / 147 / 125 and 1294 / 1031 / 889).
+struct BlockCut {
+  int tile, stages;
+};
+BlockCut block_cut(bool bf16, int G, int M, int N) {
+  const BlockCut cuts[4] = {{64, 4}, {128, 4}, {128, 2}, {256, 2}};
+  const int per_cu[4] = {2, 1, 2, 1};
+  const double each[2][4] = {{1.6, 5.3, 4.5, 0.0}, {1.6, 4.5, 3.8, 12.6}};
+  int at = 0;
+  double least = 0;
+  for (int i = 0; i < (bf16 ? 4 : 3); ++i) {
+    const double rounds =
+        std::ceil((double)tiles_of(G, M, N, cuts[i].tile) / (kCus * per_cu[i]));
+    const double t = rounds * per_cu[i] * each[bf16][i];
+    if (i == 0 || t < least) {
+      at = i;
+      least = t;
+    }
+  }
+  return cuts[at];
+}
+
+template <int FA, int FB, bool OUTBF, int B, int W, int S>
 hipError_t launch_tile(const BlockGemmArgs& a, hipStream_t s) {
-  const long long tp = (a.N + BP - 1LL) / BP, tq = (a.M + BQ - 1LL) / BQ;
-  if (tp * tq > 0x7fffffffLL / a.G) return hipErrorInvalidValue;
-  const long long total = tp * tq * a.G;
-  hipLaunchKernelGGL((k_gemm_tile<FA, FB, OUTBF, BP, BQ, WP, WQ, S>), grid_of(total),
-                     dim3(64 * (BP / WP) * (BQ / WQ)), 0, s, a, (int)tp, (int)tq, (int)total);
+  constexpr int WP = B == 256 ? 128 : B / 2;
+  const long long tp = (a.N + B - 1LL) / B, tq = (a.M + B - 1LL) / B;
+  if (tp * tq > 0x7fffffffLL / a.G / a.splits) return hipErrorInvalidValue;
+  const long long total = tp * tq * a.G * a.splits;
+  hipLaunchKernelGGL((k_gemm_tile<FA, FB, OUTBF, B, B, WP, W, S>), grid_of(total),
+                     dim3(64 * (B / WP) * (B / W)), 0, s, a, (int)tp, (int)tq, (int)total);
   return hipGetLastError();
 }
-
+template <int FA, int FB, bool OUTBF>
+hipError_t gemm_blocks(BlockGemmArgs a, hipStream_t s) {
+  a.splits = splits_of(OUTBF, a.G, a.M, a.N, a.Kd);
+  const int nb = (a.Kd + 127) / 128;
+  a.chunk = (nb + 4 * a.splits - 1) / (4 * a.splits) * 4;
+  const BlockCut c = a.splits > 1 ? BlockCut{64, 4} : block_cut(OUTBF, a.G, a.M, a.N);
+  hipError_t e;
+  if (c.tile == 64)
+    e = launch_tile<FA, FB, OUTBF, 64, 32, 4>(a, s);
+  else if (c.tile == 128 && c.stages == 4)
+    e = launch_tile<FA, FB, OUTBF, 128, 32, 4>(a, s);
+  else if (c.tile == 128)
+    e = launch_tile<FA, FB, OUTBF, 128, 64, 2>(a, s);
+  else  // (to bf16 only)
+    e = launch_tile<FA, FB, true, 256, 64, 2>(a, s);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int quads = (a.N + 3) / 4;
+  const long long total = (long long)a.G * a.M * quads;
+  hipLaunchKernelGGL((k_gemm_join<OUTBF>), grid_of((total + kThreads - 1) / kThreads),
+                     dim3(kThreads), 0, s, a, quads, total);
+  return hipGetLastError();
+}
 template <int FA, int FB>
 hipError_t gemm_blocks(const BlockGemmArgs& a, hipStream_t s) {
-  auto tiles = [&](int b) {
-    return ((a.N + b - 1LL) / b) * ((a.M + b - 1LL) / b) * a.G;
-  };
-  if (a.out_bf16) {
-    if (tiles(256) >= 256) return launch_tile<FA, FB, true, 256, 256, 128, 64>(a, s);
-    if (tiles(128) >= 256) return launch_tile<FA, FB, true, 128, 128, 64, 64>(a, s);
-    return launch_tile<FA, FB, true, 64, 64, 32, 32, 4>(a, s);
-  }
-  if (tiles(128) >= 256) return launch_tile<FA, FB, false, 128, 128, 64, 64>(a, s);
-  return launch_tile<FA, FB, false, 64, 64, 32, 32, 4>(a, s);
+  return a.out_bf16 ? gemm_blocks<FA, FB, true>(a, s) : gemm_blocks<FA, FB, false>(a, s);
 }
 
 }  // namespace
@@ -419,7 +549,10 @@ hipError_t launch_quantise(int bf16, int fmt, const QuantArgs& a, hipStream_t s)
   return bf16 ? quantise<true, kFmtE5M2>(a, s) : quantise<false, kFmtE5M2>(a, s);
 }
 
-size_t gemm_blocks_workspace_bytes(int, int, int, int) { return 0; }
+size_t gemm_blocks_workspace_bytes(int bf16, int G, int M, int N, int Kd) {
+  const int s = splits_of(bf16, G, M, N, Kd);
+  return s == 1 ? 0 : (size_t)s * G * M * N * sizeof(float);
+}
 
 hipError_t launch_gemm_blocks(int fmt_a, int fmt_b, const BlockGemmArgs& a, hipStream_t s) {
   if (fmt_a == kFmtE4M3)

@@ -1818,11 +1818,12 @@ lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G, int32
       lsgd::launch_quantise(dtype == LSGD_BF16, format, a, (hipStream_t)stream));
 }
 
-lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t G, int32_t M, int32_t N, int32_t Kd,
-                                                     size_t* bytes) {
+lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t out_dtype, int32_t G, int32_t M,
+                                                     int32_t N, int32_t Kd, size_t* bytes) {
+  if (out_dtype != LSGD_FP32 && out_dtype != LSGD_BF16) return LSGD_E_INVALID;
   if (!bytes || G < 1 || M < 1 || N < 1 || Kd < 1 || G > 65535 || Kd > kMaxInner)
     return LSGD_E_INVALID;
-  *bytes = lsgd::gemm_blocks_workspace_bytes(G, M, N, Kd);
+  *bytes = lsgd::gemm_blocks_workspace_bytes(out_dtype == LSGD_BF16, G, M, N, Kd);
   return LSGD_OK;
 }
 
@@ -1844,7 +1845,7 @@ lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b, int32_t
   if ((uintptr_t)d_A % 16 || (uintptr_t)d_B % 16 || (uintptr_t)d_SA % 4 || (uintptr_t)d_SB % 4 ||
       (uintptr_t)d_C % (out_dtype == LSGD_BF16 ? 2 : 4))
     return LSGD_E_INVALID;
-  const size_t need = lsgd::gemm_blocks_workspace_bytes(G, M, N, Kd);
+  const size_t need = lsgd::gemm_blocks_workspace_bytes(out_dtype == LSGD_BF16, G, M, N, Kd);
   if (need && ((uintptr_t)d_ws % 16 || !d_ws)) return LSGD_E_INVALID;
   if (ws_bytes < need) return LSGD_E_WORKSPACE;
   lsgd::BlockGemmArgs a{};

@@ -153,9 +153,11 @@ struct BlockGemmArgs {
   void* C;
   long long ldc, sC;
   int out_bf16;
-  float* part;  // workspace
+  float* part;  // workspace: the splits' sums [splits][G][M][N]
+  // set by launch_gemm_blocks: ranges of `chunk` steps of 128
+  int splits, chunk;
 };
-size_t gemm_blocks_workspace_bytes(int G, int M, int N, int Kd);
+size_t gemm_blocks_workspace_bytes(int bf16, int G, int M, int N, int Kd);
 hipError_t launch_gemm_blocks(int fmt_a, int fmt_b, const BlockGemmArgs& a, hipStream_t s);
 
 // ------------------------------------------------- orthogonalised momentum

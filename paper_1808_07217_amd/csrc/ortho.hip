@@ -25,8 +25,6 @@
 // the bf16 form each piece is a matrix of its own, and only the first is multiplied.
 #include <atomic>
 #include <cmath>
-#include <cstdio>
-#include <cstdlib>
 
 #include "kernels.h"
 #include "tile_loop.h"
@@ -299,71 +297,79 @@ __device__ __forceinline__ void result(const OrthoArgs& a, int g, int r, int c, 
   }
 }
 
-// The square tiles: 256 x 256 with eight wavefronts of 128 x 64, 128 x 128 and 64 x 64 with
-// four of a quarter each.
+// The square tiles: 256 x 256 with eight wavefronts of 128 x 64; 128 x 128 with four of a
+// quarter each, or, with four stages and so alone on a compute unit, eight of 64 x 32; 64 x
+// 64 with four.
 template <int T, int S>
 struct Shape {
   static constexpr bool kEight = T == 256 || (T == 128 && S == 4);
   static constexpr int kWq = T / (kEight ? 4 : 2), kThreads = kEight ? 512 : 256;
 };
 
-// A tile's results leave both ways: [q][p] straight from the registers (a lane holds four
-// neighbouring p), and [p][q] by way of LDS, so that rows leave in vectors too (stored from
-// the registers, 2 bytes a lane, they took a fifth of the time of a 2048-deep product).
-// Each half of the tile's rows goes through one of the two stages, kRows at a time. The
-// pitch of T + 4 words puts the four rows that a wavefront writes at once into
-// different banks.
-template <int T>
+// A tile's results leave both ways, [q][p] and [p][q], by way of LDS: first as columns,
+// when each thread adds what belongs to its eight neighbours, then as rows, in vectors of
+// 16 bytes. Everything after the sums' way to LDS is a rolled loop: instructions that a
+// workgroup runs once are fetched from far away, and the same work written out over the
+// accumulators took 10.5 to 14.5 us for a 256 x 256 product of 128 x 128 tiles where this
+// takes 8.8 to 10.7.
+// The halves of the tile's rows go through two of the stages, kRows of them at a time. The
+// pitch of T + 4 words keeps the rows that a wavefront touches at once in different
+// banks, but for pairs of columns' pieces.
+template <int T, int THREADS>
 struct Turn {
   static constexpr int kPasses = T == 256 ? 2 : 1, kRows = T / 2 / kPasses;
   static constexpr int kPitch = T + 4, kBytes = kRows * kPitch * 4;
   static constexpr int kExtra = kBytes > 2 * T * 128 ? kBytes - 2 * T * 128 : 0;
-  uint32_t* half[2];
-  // (wait() first: every wavefront is done with the stages, nothing is on its way to them)
-  __device__ __forceinline__ Turn(uint8_t* s0, uint8_t* s1) {
-    half[0] = (uint32_t*)s0;
-    half[1] = (uint32_t*)s1;
-  }
-  __device__ __forceinline__ void wait() const {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-  }
+  static constexpr int kUnits = 2 * kRows * T / 8 / THREADS;  // eights a thread and pass
+  float* half[2];
+  __device__ __forceinline__ Turn(uint8_t* s0, uint8_t* s1) : half{(float*)s0, (float*)s1} {}
   // (a wavefront's rows all lie in one half)
-  __device__ __forceinline__ uint32_t& operator()(int p, int q) const {
-    return half[p >= T / 2][p % kRows * kPitch + q];
+  __device__ __forceinline__ float* at(int p, int q) const {
+    return half[p >= T / 2] + p % kRows * kPitch + q;
   }
   // row r of the 2 kRows that a pass holds
   static __device__ __forceinline__ int row(int pass, int r) {
     return r / kRows * (T / 2) + pass * kRows + r % kRows;
   }
-};
-__device__ __forceinline__ uint32_t pair(_Float16 h, _Float16 w) {
-  return (uint32_t)__builtin_bit_cast(uint16_t, h) |
-         (uint32_t)__builtin_bit_cast(uint16_t, w) << 16;
-}
-// A pass's rows [p][q] of pieces from LDS to a matrix of rows of K (np, nq: how much of
-// the tile exists, multiples of 64); LOW: the second pieces too.
-template <int P, int T, bool LOW, int THREADS>
-__device__ __forceinline__ void rows_out(const Turn<T>& turn, int pass, _Float16* dst, int K,
-                                         int p0, int q0, int np, int nq) {
-  __syncthreads();
-#pragma unroll 4
-  for (int u = threadIdx.x; u < 2 * Turn<T>::kRows * T / 8; u += THREADS) {
-    const int p = Turn<T>::row(pass, u / (T / 8)), q = u % (T / 8) * 8;
-    if (p >= np || q >= nq) continue;
-    const uint32_t* w = &turn(p, q);
-    const v4i lo = *(const v4i*)w, hi = *(const v4i*)(w + 4);
-    v4i h, l;
+  // A pass's sums, times f, when every wavefront is done with what LDS held and
+  // nothing is on its way there.
+  template <class L>
+  __device__ __forceinline__ void fill(int pass, const L& t, const v4f (&acc)[L::FP][L::FQ],
+                                       float f) const {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    constexpr int n = L::FP / kPasses;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      h[e] = (int)__builtin_amdgcn_perm(lo[2 * e + 1], lo[2 * e], 0x05040100);
-      h[2 + e] = (int)__builtin_amdgcn_perm(hi[2 * e + 1], hi[2 * e], 0x05040100);
-      l[e] = (int)__builtin_amdgcn_perm(lo[2 * e + 1], lo[2 * e], 0x07060302);
-      l[2 + e] = (int)__builtin_amdgcn_perm(hi[2 * e + 1], hi[2 * e], 0x07060302);
-    }
-    _Float16* o = dst + at<P>(p0 + p, q0 + q, K);
-    *(v4i*)o = h;
-    if constexpr (LOW) *(v4i*)(o + 32) = l;
+    for (int i = 0; i < n; ++i)
+#pragma unroll
+      for (int j = 0; j < L::FQ; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *at(t.wp + (pass * n + i) * 16 + (t.lane >> 4) * 4 + e,
+              t.wq + j * 16 + (t.lane & 15)) = acc[pass * n + i][j][e] * f;
+    __syncthreads();
+  }
+  // Unit u of a thread: as columns, four lanes share 32 p of a column (a line of pieces).
+  static __device__ __forceinline__ void column(int pass, int u, int& p, int& q) {
+    const int x = u * THREADS + (int)threadIdx.x;
+    q = (x >> 2) % T;
+    p = row(pass, ((x >> 2) / T * 4 + (x & 3)) * 8);
+  }
+  static __device__ __forceinline__ void across(int pass, int u, int& p, int& q) {
+    const int x = u * THREADS + (int)threadIdx.x;
+    p = row(pass, x / (T / 8));
+    q = x % (T / 8) * 8;
+  }
+};
+
+// Eight values in pieces.
+__device__ __forceinline__ void to_pieces(const float (&v)[8], f16x8& h, f16x8& l) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    _Float16 a, b;
+    split2(v[e], a, b);
+    h[e] = a;
+    l[e] = b;
   }
 }
 
@@ -372,7 +378,8 @@ __device__ __forceinline__ void rows_out(const Turn<T>& turn, int pass, _Float16
 template <int P, bool SECOND, int BT, int S>
 __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_gram(OrthoArgs a, int step,
                                                                        int tm, int total) {
-  using T = TileLoop<BT, BT, BT / 2, Shape<BT, S>::kWq, S, Turn<BT>::kExtra>;
+  using Out = Turn<BT, Shape<BT, S>::kThreads>;
+  using T = TileLoop<BT, BT, BT / 2, Shape<BT, S>::kWq, S, Out::kExtra>;
   LSGD_TILE_STAGES(st, S, T::kStage);
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
@@ -388,57 +395,58 @@ __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_gram(Orth
   const int ld = K * P * 2;
   t.init((const uint8_t*)src + (long long)p0 * ld, (const uint8_t*)src + (long long)q0 * ld, ld,
          a.mp - p0, a.mp - q0);
-  const int lr = t.lane & 15, lq = t.lane >> 4;
-  constexpr int kPasses = Turn<BT>::kPasses, kFp = T::FP / kPasses;
-  // A's own values (its mirror image's, which lie side by side). A tile of one pass takes
-  // them before the product, where their way from memory is hidden.
-  f16x4 xh[T::FQ][kFp] = {}, xl[T::FQ][kFp] = {};
-  auto own = [&](int pass) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < T::FQ; ++j)
-#pragma unroll
-      for (int i = 0; i < kFp; ++i) {
-        const int q = min(q0 + t.wq + j * 16 + lr, a.mp - 1);
-        const int p = min(p0 + t.wp + (pass * kFp + i) * 16 + lq * 4, a.mp - 4);
-        const long long o = at<P>(q, p, a.mp);
-        xh[j][i] = *(const f16x4*)(src + o);
-        if constexpr (P == 2) xl[j][i] = *(const f16x4*)(src + o + 32);
-      }
-  };
-  if constexpr (SECOND && kPasses == 1) own(0);
   MacHalf<P> mac;
   v4f acc[T::FP][T::FQ] = {};
   t.run(st, ld / 128, mac, acc);
-  const Turn<BT> turn(st[0], st[1]);
+  const Out out(st[0], st[1]);
+#pragma unroll 1
+  for (int pass = 0; pass < Out::kPasses; ++pass) {
+    if (pass == 0)
+      out.fill(0, t, acc, f);
+    else
+      out.fill(Out::kPasses - 1, t, acc, f);
 #pragma unroll
-  for (int pass = 0; pass < kPasses; ++pass) {
-    if constexpr (SECOND && kPasses > 1) own(pass);
-    turn.wait();
+    for (int u = 0; u < Out::kUnits; ++u) {
+      int p, q;
+      Out::column(pass, u, p, q);
+      if (q0 + q >= a.mp || p0 + p >= a.mp) continue;
+      const long long o = at<P>(q0 + q, p0 + p, a.mp);
+      float v[8];
 #pragma unroll
-    for (int j = 0; j < T::FQ; ++j) {
-      const int qi = t.wq + j * 16 + lr, q = q0 + qi;
+      for (int e = 0; e < 8; ++e) v[e] = *out.at(p + e, q);
+      if constexpr (SECOND) {  // A's own values: its mirror image's, which lie side by side
+        const f16x8 xh = *(const f16x8*)(src + o);
+        f16x8 xl = {};
+        if constexpr (P == 2) xl = *(const f16x8*)(src + o + 32);
 #pragma unroll
-      for (int i = 0; i < kFp; ++i) {
-        const int pi = t.wp + (pass * kFp + i) * 16 + lq * 4, p = p0 + pi;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = acc[pass * kFp + i][j][e] * f;
-          if constexpr (SECOND)
-            v[e] = __builtin_fmaf(a.f_a, (float)xh[j][i][e] + (float)xl[j][i][e], v[e]);
+        for (int e = 0; e < 8; ++e) {
+          v[e] = __builtin_fmaf(a.f_a, (float)xh[e] + (float)xl[e], v[e]);
+          *out.at(p + e, q) = v[e];
         }
-        const f16x4 h = first_of(v), w = second_of(v, h);
-        if (q < a.mp && p < a.mp) {
-          const long long o = at<P>(q, p, a.mp);
-          *(f16x4*)(dst + o) = h;
-          if constexpr (P == 2) *(f16x4*)(dst + o + 32) = w;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) turn(pi + e, qi) = pair(h[e], w[e]);
       }
+      f16x8 h, w;
+      to_pieces(v, h, w);
+      *(f16x8*)(dst + o) = h;
+      if constexpr (P == 2) *(f16x8*)(dst + o + 32) = w;
     }
     // (a tile on the diagonal is its own mirror image)
-    if (pt != qt) rows_out<P, BT, P == 2, Shape<BT, S>::kThreads>(turn, pass, dst, a.mp, p0, q0, a.mp - p0, a.mp - q0);
+    if (pt != qt) {
+      if constexpr (SECOND) __syncthreads();
+#pragma unroll 1
+      for (int u = 0; u < Out::kUnits; ++u) {
+        int p, q;
+        Out::across(pass, u, p, q);
+        if (q0 + q >= a.mp || p0 + p >= a.mp) continue;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = out.at(p, q)[e];
+        f16x8 h, w;
+        to_pieces(v, h, w);
+        _Float16* o = dst + at<P>(p0 + p, q0 + q, a.mp);
+        *(f16x8*)o = h;
+        if constexpr (P == 2) *(f16x8*)(o + 32) = w;
+      }
+    }
   }
 }
 
@@ -447,7 +455,8 @@ template <int P, bool LAST, int BT, int S>
 __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_apply(OrthoArgs a, int step,
                                                                         int tp, int tq,
                                                                         int total) {
-  using T = TileLoop<BT, BT, BT / 2, Shape<BT, S>::kWq, S, Turn<BT>::kExtra>;
+  using Out = Turn<BT, Shape<BT, S>::kThreads>;
+  using T = TileLoop<BT, BT, BT / 2, Shape<BT, S>::kWq, S, Out::kExtra>;
   LSGD_TILE_STAGES(st, S, T::kStage);
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
@@ -465,71 +474,65 @@ __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_apply(Ort
   const int shift = LAST ? -k : raise(a, g, step + 1) - k;
   const float fb = ldexpf(LAST ? a.f_out : a.f_bx, shift);
   const float fx = ldexpf(LAST ? a.f_x / a.scale_x : a.f_x, shift);
-  const int lr = t.lane & 15, lq = t.lane >> 4;
-  const int m = a.flip ? a.N : a.M, n = a.flip ? a.M : a.N;
-  constexpr int kPasses = Turn<BT>::kPasses, kFp = T::FP / kPasses;
-  // X's own values, as in k_ortho_gram
-  f16x4 xh[T::FQ][kFp], xl[T::FQ][kFp];
-  auto own = [&](int pass) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < T::FQ; ++j)
-#pragma unroll
-      for (int i = 0; i < kFp; ++i) {
-        const int q = min(q0 + t.wq + j * 16 + lr, a.np - 1);
-        const int p = min(p0 + t.wp + (pass * kFp + i) * 16 + lq * 4, a.mp - 4);
-        const long long o = at<P>(q, p, a.mp);
-        xh[j][i] = *(const f16x4*)(X + o);
-        xl[j][i] = *(const f16x4*)(X + o + second<P>(px));
-      }
-  };
-  if constexpr (kPasses == 1) own(0);
   MacHalf<P> mac;
   v4f acc[T::FP][T::FQ] = {};
   t.run(st, ld / 128, mac, acc);
-  const Turn<BT> turn(st[0], st[1]);
+  const Out out(st[0], st[1]);
+#pragma unroll 1
+  for (int pass = 0; pass < Out::kPasses; ++pass) {
+    if (pass == 0)
+      out.fill(0, t, acc, fb);
+    else
+      out.fill(Out::kPasses - 1, t, acc, fb);
+#pragma unroll 4
+    for (int u = 0; u < Out::kUnits; ++u) {
+      int p, q;
+      Out::column(pass, u, p, q);
+      if (q0 + q >= a.np || p0 + p >= a.mp) continue;
+      const long long o = at<P>(q0 + q, p0 + p, a.mp);
+      const f16x8 xh = *(const f16x8*)(X + o), xl = *(const f16x8*)(X + o + second<P>(px));
+      float v[8];
 #pragma unroll
-  for (int pass = 0; pass < kPasses; ++pass) {
-    if constexpr (kPasses > 1) own(pass);
-    turn.wait();
-#pragma unroll
-    for (int j = 0; j < T::FQ; ++j) {
-      const int qi = t.wq + j * 16 + lr, q = q0 + qi;
-#pragma unroll
-      for (int i = 0; i < kFp; ++i) {
-        const int pi = t.wp + (pass * kFp + i) * 16 + lq * 4, p = p0 + pi;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[e] = __builtin_fmaf(fx, (float)xh[j][i][e] + (float)xl[j][i][e],
-                                acc[pass * kFp + i][j][e] * fb);
-        if constexpr (LAST) {
-          if (a.flip) {
-            result(a, g, q, p, q < n ? m - p : 0, v);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) turn(pi + e, qi) = __float_as_uint(v[e]);
-          }
-        } else {
-          const f16x4 h = first_of(v), w = second_of(v, h);
-          if (q < a.np && p < a.mp) {
-            _Float16* o = a.Xt[1 - from] + g * 2 * px + at<P>(q, p, a.mp);
-            *(f16x4*)o = h;
-            *(f16x4*)(o + second<P>(px)) = w;
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) turn(pi + e, qi) = pair(h[e], w[e]);
-        }
+      for (int e = 0; e < 8; ++e) {
+        v[e] = __builtin_fmaf(fx, (float)xh[e] + (float)xl[e], *out.at(p + e, q));
+        *out.at(p + e, q) = v[e];
+      }
+      if constexpr (!LAST) {
+        f16x8 h, w;
+        to_pieces(v, h, w);
+        _Float16* to = a.Xt[1 - from] + g * 2 * px + o;
+        *(f16x8*)to = h;
+        *(f16x8*)(to + second<P>(px)) = w;
       }
     }
-    if constexpr (!LAST) {
-      rows_out<P, BT, P == 2, Shape<BT, S>::kThreads>(turn, pass, a.Xr + g * P * px, a.np, p0, q0, a.mp - p0, a.np - q0);
-    } else if (!a.flip) {
-      __syncthreads();
-      for (int u = threadIdx.x; u < 2 * Turn<BT>::kRows * BT / 4; u += Shape<BT, S>::kThreads) {
-        const int p = Turn<BT>::row(pass, u / (BT / 4)), q = u % (BT / 4) * 4;
-        const v4f w = *(const v4f*)&turn(p, q);
-        const float v[4] = {w[0], w[1], w[2], w[3]};
-        result(a, g, p0 + p, q0 + q, p0 + p < m ? n - q0 - q : 0, v);
+    __syncthreads();
+    // rows of [p][q], or in the end of the result
+#pragma unroll 1
+    for (int u = 0; u < Out::kUnits; ++u) {
+      int p, q;
+      float v[8];
+      if (LAST && a.flip) {
+        Out::column(pass, u, p, q);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = *out.at(p + e, q);
+      } else {
+        Out::across(pass, u, p, q);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = out.at(p, q)[e];
+      }
+      if constexpr (LAST) {
+        const int r = a.flip ? q0 + q : p0 + p, c = a.flip ? p0 + p : q0 + q;
+        const int left = r < a.M ? a.N - c : 0;
+        const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+        result(a, g, r, c, left, lo);
+        result(a, g, r, c + 4, left - 4, hi);
+      } else {
+        if (q0 + q >= a.np || p0 + p >= a.mp) continue;
+        f16x8 h, w;
+        to_pieces(v, h, w);
+        _Float16* o = a.Xr + g * P * px + at<P>(p0 + p, q0 + q, a.np);
+        *(f16x8*)o = h;
+        if constexpr (P == 2) *(f16x8*)(o + 32) = w;
       }
     }
   }
@@ -784,22 +787,24 @@ hipError_t allow_small_lds() {
 }
 
 // ------------------------------------------------------------------ launches
-// How a product is cut into n tiles: their size, and how many stages of loads are in
-// flight. More stages hide a load's latency where few workgroups share a compute unit.
+// How a product is cut into tiles: their size, and how many stages of loads are in flight.
 struct Cut {
   int tile, stages;
 };
+// The cut of least estimated time; tiles(T): how many tiles of T there are. A compute unit
+// takes per_cu workgroups at once (LDS), a round of them costs per_cu times `each`, and the
+// last round as much as a full one. `each` is what one tile took of a full round, in
+// units of about 10 us at an inner range of 2048 in fp32 precision, measured on 8 x
+// 2048^2 and 4096^2 with one cut forced for all products (16, 16, 44, 38, 133 us). At the
+// other end, with one workgroup to a unit, a product waits for loads and launches:
+// 512^2 takes 125 us in 64 x 64 tiles of four stages, 136 of three, 213 / 282 in 128 x 128
+// tiles of four / two, 609 in 256 x 256 ones.
 constexpr int kCus = 256;
-// The cut of least estimated time, in units of a 64 x 64 tile's share of a busy compute
-// unit; tiles(T): how many tiles of T there are. Rounds are whole: the last one takes
-// as long as a full one.
 template <class F>
 Cut best_cut(F tiles) {
-  const char* e_ = getenv("TT");
-  if (e_ && atoi(e_)) return Cut{atoi(e_) / 10, atoi(e_) % 10};
   const Cut cuts[5] = {{64, 4}, {64, 3}, {128, 4}, {128, 2}, {256, 2}};
   const int per_cu[5] = {2, 3, 1, 2, 1};
-  const double each[5] = {1.5, 1.4, 5.0, 4.0, 13.4};
+  const double each[5] = {1.6, 1.55, 4.3, 3.8, 12.6};
   int at = 0;
   double least = 0;
   for (int i = 0; i < 5; ++i) {

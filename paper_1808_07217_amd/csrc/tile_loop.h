@@ -65,7 +65,7 @@ constexpr int kMostStages = 4;
 // mac with PH = 0.
 template <int BP, int BQ, int WP, int WQ, int S = 2, int kExtra = 0>
 struct TileLoop {
-  static constexpr int kStages = S, kWaves = (BP / WP) * (BQ / WQ), kThreads = 64 * kWaves;
+  static constexpr int kP = BP, kQ = BQ, kWaves = (BP / WP) * (BQ / WQ), kThreads = 64 * kWaves;
   static constexpr int FP = WP / 16, FQ = WQ / 16;
   static constexpr int kStage = (BP + BQ) * 128 + kExtra;  // bytes
   static constexpr int kLoads = (BP + BQ) / 8 / kWaves;   // a wavefront's, of 8 rows
@@ -97,6 +97,13 @@ struct TileLoop {
     const int lr = lane & 15, slot = (lane >> 4) ^ (lr & 7);
     rp = (uint32_t)((wp + lr) * 128 + slot * 16);
     rq = (uint32_t)((BP + wq + lr) * 128 + slot * 16);
+  }
+  // (before the first load) the first n steps are left out
+  __device__ __forceinline__ void skip(int n) {
+    P += 128LL * n;
+    Q += 128LL * n;
+    leftp -= 128 * n;
+    leftq -= 128 * n;
   }
   // one step into a stage; !want: nothing is read (no branch: the matrix instructions
   // before one would be moved past it)

@@ -101,7 +101,7 @@ _SIGS = {
     "lsgd_sgd_update": [_P, _P, _P, _c.c_int64, _c.c_float, _c.c_float,
                         _c.c_float, _c.c_int32, _P],
     "lsgd_quantise_blocks": [_I, _I, _I, _I, _I, _P, _L, _L, _P, _P, _P, _P, _P],
-    "lsgd_grouped_gemm_blocks_workspace_bytes": [_I, _I, _I, _I, _c.POINTER(_c.c_size_t)],
+    "lsgd_grouped_gemm_blocks_workspace_bytes": [_I, _I, _I, _I, _I, _c.POINTER(_c.c_size_t)],
     "lsgd_grouped_gemm_blocks": [_I, _I, _I, _I, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _L,
                                  _P, _L, _L, _P, _c.c_size_t, _P],
     "lsgd_orthogonalise_workspace_bytes": [_I, _I, _I, _I, _c.POINTER(_c.c_size_t)],
@@ -648,9 +648,9 @@ def _block_operand(name: str, X: Blocks) -> Tuple[int, int, int, int, int]:
 
 
 @functools.lru_cache(maxsize=4096)
-def _gemm_blocks_workspace(G: int, M: int, N: int, n: int) -> int:
+def _gemm_blocks_workspace(out: int, G: int, M: int, N: int, n: int) -> int:
     nb = _c.c_size_t()
-    _check(_lib.lsgd_grouped_gemm_blocks_workspace_bytes(G, M, N, n, _c.byref(nb)))
+    _check(_lib.lsgd_grouped_gemm_blocks_workspace_bytes(out, G, M, N, n, _c.byref(nb)))
     return nb.value
 
 
@@ -678,10 +678,11 @@ def grouped_gemm_blocks(A: Blocks, B: Blocks, out: Optional[torch.Tensor] = None
     if not (A.scale.device == dev and B.q.device == dev and B.scale.device == dev
             and out.device == dev):
         raise ValueError("all tensors must be on one device")
-    nb = _gemm_blocks_workspace(G, M, N, n)
+    dt = BF16 if out.dtype == torch.bfloat16 else FP32
+    nb = _gemm_blocks_workspace(dt, G, M, N, n)
     ws = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
     _enqueue(dev, _lib.lsgd_grouped_gemm_blocks,
-             fa, fb, BF16 if out.dtype == torch.bfloat16 else FP32, G, M, N, n,
+             fa, fb, dt, G, M, N, n,
              A.q.data_ptr(), sA, A.scale.data_ptr(), sSA, B.q.data_ptr(), sB,
              B.scale.data_ptr(), sSB, out.data_ptr(), ldc, sC, ws.data_ptr() if nb else None, nb)
     return out

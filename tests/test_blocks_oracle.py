@@ -84,9 +84,10 @@ def test_quantise_refusals():
 def test_grouped_gemm_blocks_refusals():
     f, nb = P(4096), ctypes.c_size_t()
     lib = _lib()
-    assert lib.lsgd_grouped_gemm_blocks_workspace_bytes(2, 3, 4, 5, None) == 1
+    assert lib.lsgd_grouped_gemm_blocks_workspace_bytes(0, 2, 3, 4, 5, None) == 1
+    assert lib.lsgd_grouped_gemm_blocks_workspace_bytes(2, 2, 3, 4, 5, ctypes.byref(nb)) == 1
     for bad in ((0, 3, 4, 5), (2, 3, 4, 2**22 + 1), (2, 0, 4, 5), (2, 3, 0, 5), (2, 3, 4, 0), (65536, 3, 4, 5)):
-        assert lib.lsgd_grouped_gemm_blocks_workspace_bytes(*bad, ctypes.byref(nb)) == 1
+        assert lib.lsgd_grouped_gemm_blocks_workspace_bytes(0, *bad, ctypes.byref(nb)) == 1
     ok = [0, 0, 0, 2, 3, 4, 5, f, 384, f, 12, f, 512, f, 16, f, 4, 12, f, 1 << 40, None]
 
     def call(**kw):
@@ -102,12 +103,12 @@ def test_grouped_gemm_blocks_refusals():
                 dict(_14=6), dict(_15=None), dict(_15=P(4098)), dict(_16=3), dict(_17=11)):
         assert call(**bad) == 1, bad
     # a product that wants a workspace, without one and with one too small
-    assert lib.lsgd_grouped_gemm_blocks_workspace_bytes(1, 1, 8192, 8192, ctypes.byref(nb)) == 0
-    if nb.value:
-        big = dict(_3=1, _4=1, _5=8192, _6=8192, _16=8192)
-        assert call(**big, _18=None) == 1
-        assert call(**big, _18=P(4100)) == 1
-        assert call(**big, _19=nb.value - 1) == 2
+    assert lib.lsgd_grouped_gemm_blocks_workspace_bytes(0, 1, 64, 64, 65536, ctypes.byref(nb)) == 0
+    assert nb.value > 0
+    big = dict(_3=1, _4=64, _5=64, _6=65536, _16=64)
+    assert call(**big, _18=None) == 1
+    assert call(**big, _18=P(4100)) == 1
+    assert call(**big, _19=nb.value - 1) == 2
 
 
 CO = (ctypes.c_float * 3)(3.4445, -4.7750, 2.0315)

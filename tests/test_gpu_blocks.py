@@ -143,6 +143,46 @@ def test_product_formats(shape, fa, fb):
     _check_product(L.grouped_gemm_blocks(a, b), a, b)
 
 
+@pytest.mark.parametrize("shape", [(1, 64, 64, 8192), (2, 3, 130, 20001), (1, 70, 33, 4100)])
+def test_product_split_over_the_inner_dimension(shape):
+    """Few results and a long inner dimension: partial sums joined by a second
+    launch, whatever the workspace held, the same bits each time."""
+    L = _lsgd()
+    print(f"product split {shape}", flush=True)
+    G, M, N, K = shape
+    a, b = _operands(L, np.random.default_rng(5), *shape, "e4m3", "e5m2")
+    assert L._gemm_blocks_workspace(0, G, M, N, K) > 0
+    for dt in (torch.float32, torch.bfloat16):
+        C = L.grouped_gemm_blocks(a, b, out_dtype=dt)
+        _check_product(C, a, b)
+        torch.full((1 << 22,), float("nan"), device=device())  # where a workspace may lie next
+        assert torch.equal(C, L.grouped_gemm_blocks(a, b, out_dtype=dt))
+
+
+# the sizes at which every cut of a product is taken: 64, 128 (two and four stages) and
+# 256, their last tiles ragged
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 2000, 2040, 500), (1, 4100, 3900, 260), (3, 1537, 771, 384),
+                                   (1, 260, 8200, 1100)])
+def test_product_large_tiles(shape, out):
+    """Checked on the device in float64 (products of 8-bit values and powers of two
+    are exact there, sums of 1100 of them to 2^-42 of their size)."""
+    L = _lsgd()
+    print(f"product large {shape} {out}", flush=True)
+    a, b = _operands(L, np.random.default_rng(2), *shape, "e4m3", "e4m3")
+    val = lambda t: (t.q.to(torch.float64).view(*t.q.shape[:2], -1, 128)  # noqa: E731
+                     * t.scale.to(torch.float64)[:, :, :t.q.shape[2] // 128, None]).flatten(2)
+    va, vb = val(a), val(b)
+    ref = va @ vb.transpose(1, 2).contiguous()
+    size = va.abs() @ vb.abs().transpose(1, 2).contiguous()
+    bound = gamma(a.n + 1) * size + 1e-38
+    if out == "bf16":
+        bound = bound + 2.0 ** -10 * size
+        bound = bound + 2.0 ** -8 * (ref.abs() + bound)
+    C = L.grouped_gemm_blocks(a, b, out_dtype=torch.bfloat16 if out == "bf16" else torch.float32)
+    assert bool(((C.double() - ref).abs() <= bound).all())
+
+
 def test_product_extreme_scales_and_specials():
     """Scales at both ends of their range, and a NaN and an infinity, which show
     in their row or column alone."""
