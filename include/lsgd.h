@@ -521,8 +521,8 @@ lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b,
  *   A = X X^T,  B = b A + c A A,  X := a X + B X
  * (on X^T where M > N), h_coefficients = {a, b, c} (host). The products
  * take fp32 precision for dtype LSGD_FP32 (two fp16 pieces of each operand on
- * the matrix cores) and, for LSGD_BF16, operands of 11 significant bits but
- * an X held in two pieces all the same. A zero matrix stays zero; an
+ * the matrix cores); for LSGD_BF16 operands of 11 significant bits do where
+ * min(M, N) > 384 (X itself is held in two pieces all the same). A zero matrix stays zero; an
  * infinity or a NaN makes the whole result NaN.
  *
  * Arguments, else LSGD_E_INVALID: 1 <= G <= 65535, 1 <= M, N <= 2^20 with

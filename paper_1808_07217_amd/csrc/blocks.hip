@@ -282,6 +282,7 @@ template <int FA, int FB, int BP, int BQ, int FP, int FQ>
 struct MacBlocks : Scales<BP, BQ, FP, FQ> {
   typedef Frag P;
   typedef Frag Q;
+  typedef v4f Acc;
   using Next = typename Scales<BP, BQ, FP, FQ>::Next;
   template <int PH>
   __device__ __forceinline__ P p(const Frag& f, int) const { return f; }
@@ -302,6 +303,7 @@ template <int FA, int FB, int BP, int BQ, int FP, int FQ>
 struct MacWide : Scales<BP, BQ, FP, FQ> {
   typedef Wide P;
   typedef Wide Q;
+  typedef v4f Acc;
   using Next = typename Scales<BP, BQ, FP, FQ>::Next;
   template <int FMT>
   static __device__ __forceinline__ Wide wide(const Frag& f, uint32_t byte) {

@@ -357,11 +357,11 @@ bool ortho_numbers(lsgd::OrthoArgs& a, int32_t steps, const float* h, float eps)
 
 lsgd_status ortho_launch(int32_t dtype, const lsgd::OrthoArgs& a, void* d_ws, size_t ws_bytes,
                          void* stream) {
-  const int pieces = dtype == LSGD_BF16 ? 1 : 2;
-  const size_t need = lsgd::ortho_workspace_bytes(pieces, a.G, a.M, a.N);
+  const bool bf16 = dtype == LSGD_BF16;
+  const size_t need = lsgd::ortho_workspace_bytes(bf16, a.G, a.M, a.N);
   if (need && (!d_ws || (uintptr_t)d_ws % kAlign)) return LSGD_E_INVALID;
   if (ws_bytes < need) return LSGD_E_WORKSPACE;
-  return block_status(lsgd::launch_ortho(pieces, a, d_ws, (hipStream_t)stream));
+  return block_status(lsgd::launch_ortho(bf16, a, d_ws, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -1874,7 +1874,7 @@ lsgd_status lsgd_orthogonalise_workspace_bytes(int32_t dtype, int32_t G, int32_t
                                                size_t* bytes) {
   if (!bytes || (dtype != LSGD_FP32 && dtype != LSGD_BF16) || !ortho_sizes(G, M, N))
     return LSGD_E_INVALID;
-  *bytes = lsgd::ortho_workspace_bytes(dtype == LSGD_BF16 ? 1 : 2, G, M, N);
+  *bytes = lsgd::ortho_workspace_bytes(dtype == LSGD_BF16, G, M, N);
   return LSGD_OK;
 }
 

@@ -187,9 +187,9 @@ struct OrthoArgs {
   int* kexp;
   _Float16 *Xr, *Xt[2], *A, *B;
 };
-// `pieces`: 2 for fp32 products, 1 for the bf16 form. Workspace 256-byte aligned.
-size_t ortho_workspace_bytes(int pieces, int G, int M, int N);
-hipError_t launch_ortho(int pieces, OrthoArgs a, void* ws, hipStream_t s);
+// `bf16`: the products' precision. Workspace 256-byte aligned.
+size_t ortho_workspace_bytes(int bf16, int G, int M, int N);
+hipError_t launch_ortho(int bf16, OrthoArgs a, void* ws, hipStream_t s);
 
 // ---------------------------------------------------------------- head
 // Output layer with few classes, fused around the loss (head.hip).

@@ -8,8 +8,10 @@
 // each matrix where fp16 is exact enough: a value is held as two fp16 pieces,
 // x = x1 + x2 (22 to 24 significant bits), and fp32 products are x1 y1 + x1 y2 + x2 y1,
 // each exact in fp32; what is left out is 2^-24 |x y| at worst. In the bf16 form
-// the products take the first piece alone (2^-12), an eighth of bf16's own
-// rounding; X keeps both pieces there too, because a X passes on the small
+// the products of matrices of kOnePieceFrom rows and more take the first piece alone
+// (2^-12, an eighth of bf16's own rounding; the fewer rows, the less its errors average
+// out: the result was off by 2.0e-3 at 2048 rows and 2.5e-3 at 160, rounding to bf16
+// alone 1.7e-3). X keeps both pieces there too, because a X passes on the small
 // singular directions, which the steps amplify by a each time: rounding X itself to
 // 11 bits loses them (error 1.8e-2 instead of 1.7e-3 for matrices of low rank in noise).
 //
@@ -25,6 +27,7 @@
 // the bf16 form each piece is a matrix of its own, and only the first is multiplied.
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "kernels.h"
 #include "tile_loop.h"
@@ -217,11 +220,19 @@ __global__ __launch_bounds__(kThreads) void k_ortho_split(OrthoArgs a, int chunk
 }
 
 // ------------------------------------------------------------------ products
-// A fragment is 32 k of both pieces (P == 2) or 64 of the first.
-template <int P_>
+// A fragment is 32 k of both pieces (P == 2) or 64 of the first. TWO: x1 y1 has sums of
+// its own, so that they round once in 32 k, not three times; it keeps long products (X X^T
+// of few long rows: 40 x 3000 off by 2.0e-6 without) as exact as sums in fp32 are.
+struct TwoSums {
+  v4f a, b;
+};
+template <int P_, bool TWO>
 struct MacHalf {
   typedef Frag P;
   typedef Frag Q;
+  typedef std::conditional_t<TWO, TwoSums, v4f> Acc;
+  static __device__ __forceinline__ v4f sum(const v4f& c) { return c; }
+  static __device__ __forceinline__ v4f sum(const TwoSums& c) { return c.a + c.b; }
   struct Next {};
   static constexpr int kEvenLoads = 0;
   __device__ __forceinline__ void load(uint8_t*, int, bool) const {}
@@ -233,9 +244,17 @@ struct MacHalf {
   template <int PH>
   __device__ __forceinline__ Q q(const Frag& f, int, const Next&) const { return f; }
   template <int PH>
-  __device__ __forceinline__ void mac(v4f& c, const P& p, int, const Q& q, int) const {
-    const f16x8 p0 = half<0>(p), p1 = half<4>(p), q0 = half<0>(q), q1 = half<4>(q);
-    if constexpr (P_ == 2) {
+  __device__ __forceinline__ void mac(Acc& c, const P& p, int, const Q& q, int) const {
+    mac(c, half<0>(p), half<4>(p), half<0>(q), half<4>(q));
+  }
+  static __device__ __forceinline__ void mac(Acc& c, const f16x8& p0, const f16x8& p1,
+                                             const f16x8& q0, const f16x8& q1) {
+    if constexpr (TWO) {
+      static_assert(P_ == 2, "of two pieces");
+      c.b = __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, q0, c.b, 0, 0, 0);
+      c.b = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, q1, c.b, 0, 0, 0);
+      c.a = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, q0, c.a, 0, 0, 0);
+    } else if constexpr (P_ == 2) {
       c = __builtin_amdgcn_mfma_f32_16x16x32_f16(p1, q0, c, 0, 0, 0);
       c = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, q1, c, 0, 0, 0);
       c = __builtin_amdgcn_mfma_f32_16x16x32_f16(p0, q0, c, 0, 0, 0);
@@ -333,20 +352,22 @@ struct Turn {
   }
   // A pass's sums, times f, when every wavefront is done with what LDS held and
   // nothing is on its way there.
-  template <class L>
-  __device__ __forceinline__ void fill(int pass, const L& t, const v4f (&acc)[L::FP][L::FQ],
-                                       float f) const {
+  template <class M, class L>
+  __device__ __forceinline__ void fill(int pass, const L& t,
+                                       const typename M::Acc (&acc)[L::FP][L::FQ], float f) const {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     constexpr int n = L::FP / kPasses;
 #pragma unroll
     for (int i = 0; i < n; ++i)
 #pragma unroll
-      for (int j = 0; j < L::FQ; ++j)
+      for (int j = 0; j < L::FQ; ++j) {
+        const v4f v = M::sum(acc[pass * n + i][j]);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           *at(t.wp + (pass * n + i) * 16 + (t.lane >> 4) * 4 + e,
-              t.wq + j * 16 + (t.lane & 15)) = acc[pass * n + i][j][e] * f;
+              t.wq + j * 16 + (t.lane & 15)) = v[e] * f;
+      }
     __syncthreads();
   }
   // Unit u of a thread: as columns, four lanes share 32 p of a column (a line of pieces).
@@ -395,16 +416,18 @@ __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_gram(Orth
   const int ld = K * P * 2;
   t.init((const uint8_t*)src + (long long)p0 * ld, (const uint8_t*)src + (long long)q0 * ld, ld,
          a.mp - p0, a.mp - q0);
-  MacHalf<P> mac;
-  v4f acc[T::FP][T::FQ] = {};
+  // (256 x 256 tiles have no room for two; theirs are products of thousands both ways)
+  using Mac = MacHalf<P, P == 2 && !SECOND && BT <= 128>;
+  Mac mac;
+  typename Mac::Acc acc[T::FP][T::FQ] = {};
   t.run(st, ld / 128, mac, acc);
   const Out out(st[0], st[1]);
 #pragma unroll 1
   for (int pass = 0; pass < Out::kPasses; ++pass) {
     if (pass == 0)
-      out.fill(0, t, acc, f);
+      out.template fill<Mac>(0, t, acc, f);
     else
-      out.fill(Out::kPasses - 1, t, acc, f);
+      out.template fill<Mac>(Out::kPasses - 1, t, acc, f);
 #pragma unroll
     for (int u = 0; u < Out::kUnits; ++u) {
       int p, q;
@@ -474,16 +497,17 @@ __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_apply(Ort
   const int shift = LAST ? -k : raise(a, g, step + 1) - k;
   const float fb = ldexpf(LAST ? a.f_out : a.f_bx, shift);
   const float fx = ldexpf(LAST ? a.f_x / a.scale_x : a.f_x, shift);
-  MacHalf<P> mac;
-  v4f acc[T::FP][T::FQ] = {};
+  using Mac = MacHalf<P, false>;
+  Mac mac;
+  typename Mac::Acc acc[T::FP][T::FQ] = {};
   t.run(st, ld / 128, mac, acc);
   const Out out(st[0], st[1]);
 #pragma unroll 1
   for (int pass = 0; pass < Out::kPasses; ++pass) {
     if (pass == 0)
-      out.fill(0, t, acc, fb);
+      out.template fill<Mac>(0, t, acc, fb);
     else
-      out.fill(Out::kPasses - 1, t, acc, fb);
+      out.template fill<Mac>(Out::kPasses - 1, t, acc, fb);
 #pragma unroll 4
     for (int u = 0; u < Out::kUnits; ++u) {
       int p, q;
@@ -562,9 +586,10 @@ struct Plane2 {  // a matrix's two pieces in LDS
 };
 // acc += F S^T over K: F's rows from r0 (COLS: its columns, K the slow index) and S's
 // rows from c0 on.
-template <bool COLS>
+template <bool COLS, class Mac>
 __device__ __forceinline__ void block_product(const Plane2& F, int r0, const Plane2& S, int c0,
-                                              int K, int lr, int lq, v4f (&acc)[2][2]) {
+                                              int K, int lr, int lq,
+                                              typename Mac::Acc (&acc)[2][2]) {
 #pragma unroll 1
   for (int k = 0; k < K; k += 32) {
     f16x8 f[2][2], g[2][2];
@@ -590,11 +615,7 @@ __device__ __forceinline__ void block_product(const Plane2& F, int r0, const Pla
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[i][1], g[j][0], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[i][0], g[j][1], acc[i][j], 0, 0, 0);
-        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f[i][0], g[j][0], acc[i][j], 0, 0, 0);
-      }
+      for (int j = 0; j < 2; ++j) Mac::mac(acc[i][j], f[i][0], f[i][1], g[j][0], g[j][1]);
   }
 }
 
@@ -676,14 +697,15 @@ __global__ __launch_bounds__(kSmallThreads) void k_ortho_small(OrthoArgs a, int 
 #pragma unroll 1
     for (int b = wave; b < blocks; b += kSmallWaves) {
       const int p0 = b / bm * 32, q0 = b % bm * 32;
-      v4f acc[2][2] = {};
-      block_product<false>(X, p0, X, q0, np, lr, lq, acc);
+      using Mac = MacHalf<2, true>;
+      typename Mac::Acc sums[2][2] = {};
+      block_product<false, Mac>(X, p0, X, q0, np, lr, lq, sums);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float v[4] = {acc[i][j][0] * fxx, acc[i][j][1] * fxx, acc[i][j][2] * fxx,
-                              acc[i][j][3] * fxx};
+          const v4f x = Mac::sum(sums[i][j]) * fxx;
+          const float v[4] = {x[0], x[1], x[2], x[3]};
           put(A, q0 + j * 16 + lr, p0 + i * 16 + lq * 4, v);
         }
     }
@@ -696,7 +718,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_ortho_small(OrthoArgs a, int 
       for (int n = 0; n < kEach; ++n) {
         const int b = wave + n * kSmallWaves;
         if (b < blocks)
-          block_product<false>(A, b / bm * 32, A, b % bm * 32, mp, lr, lq, acc[n]);
+          block_product<false, MacHalf<2, false>>(A, b / bm * 32, A, b % bm * 32, mp, lr, lq, acc[n]);
       }
       __syncthreads();
 #pragma unroll
@@ -727,7 +749,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_ortho_small(OrthoArgs a, int 
     for (int n = 0; n < kSmallBlocks; ++n) {
       const int b = wave + n * kSmallWaves;
       if (b < xblocks)
-        block_product<true>(X, b / bm * 32, A, b % bm * 32, mp, lr, lq, acc[n]);
+        block_product<true, MacHalf<2, false>>(X, b / bm * 32, A, b % bm * 32, mp, lr, lq, acc[n]);
     }
     __syncthreads();
 #pragma unroll
@@ -856,13 +878,17 @@ int norm_chunks(int M, int N) {
   return (int)(c > 1024 ? 1024 : c);
 }
 
+constexpr int kOnePieceFrom = 385;
+
 struct OrthoPlan {
   bool small;
+  int pieces;
   int mp, np, chunks;
   size_t part, kexp, xr, xt[2], A, B, total;
 };
-OrthoPlan ortho_plan(int pieces, int G, int M, int N) {
+OrthoPlan ortho_plan(bool bf16, int G, int M, int N) {
   OrthoPlan p{};
+  p.pieces = bf16 && (M < N ? M : N) >= kOnePieceFrom ? 1 : 2;
   p.mp = (int)up(M < N ? M : N, 32);
   p.np = (int)up(M < N ? N : M, 32);
   p.small = p.mp <= kSmallMost && small_lds(p.mp, p.np) <= kSmallLds;
@@ -876,10 +902,10 @@ OrthoPlan ortho_plan(int pieces, int G, int M, int N) {
     t = up(t + bytes, kOrthoAlign);
     return at;
   };
-  const size_t x = (size_t)G * p.mp * p.np * 2, s = (size_t)G * pieces * p.mp * p.mp * 2;
+  const size_t x = (size_t)G * p.mp * p.np * 2, s = (size_t)G * p.pieces * p.mp * p.mp * 2;
   p.part = take((size_t)G * p.chunks * 8);
   p.kexp = take((size_t)G * 4);
-  p.xr = take(x * pieces);
+  p.xr = take(x * p.pieces);
   p.xt[0] = take(x * 2);
   p.xt[1] = take(x * 2);
   p.A = take(s);
@@ -916,12 +942,12 @@ hipError_t ortho(const OrthoArgs& a, const OrthoPlan& p, hipStream_t s) {
 
 }  // namespace
 
-size_t ortho_workspace_bytes(int pieces, int G, int M, int N) {
-  return ortho_plan(pieces, G, M, N).total;
+size_t ortho_workspace_bytes(int bf16, int G, int M, int N) {
+  return ortho_plan(bf16, G, M, N).total;
 }
 
-hipError_t launch_ortho(int pieces, OrthoArgs a, void* ws, hipStream_t s) {
-  const OrthoPlan p = ortho_plan(pieces, a.G, a.M, a.N);
+hipError_t launch_ortho(int bf16, OrthoArgs a, void* ws, hipStream_t s) {
+  const OrthoPlan p = ortho_plan(bf16, a.G, a.M, a.N);
   char* w = (char*)ws;
   a.part = (double*)(w + p.part);
   a.kexp = (int*)(w + p.kexp);
@@ -939,7 +965,7 @@ hipError_t launch_ortho(int pieces, OrthoArgs a, void* ws, hipStream_t s) {
     hipLaunchKernelGGL(k_ortho_small, grid_of(a.G), dim3(kSmallThreads), lds, s, a, p.mp, p.np);
     return hipGetLastError();
   }
-  return pieces == 2 ? ortho<2>(a, p, s) : ortho<1>(a, p, s);
+  return p.pieces == 2 ? ortho<2>(a, p, s) : ortho<1>(a, p, s);
 }
 
 }  // namespace lsgd

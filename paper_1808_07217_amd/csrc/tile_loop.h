@@ -57,7 +57,8 @@ constexpr int kMostStages = 4;
   uint8_t* const st[kMostStages] = {st##0, st##1, st##2, st##3}
 
 // Policy M: types M::P and M::Q (what a fragment becomes once read, by m.p<PH>(frag, i) and
-// m.q<PH>(frag, j, up)) and m.mac<PH>(acc, p, i, q, j), PH the step's parity. What comes
+// m.q<PH>(frag, j, up)), M::Acc (a block's sums) and m.mac<PH>(acc, p, i, q, j), PH the step's
+// parity. What comes
 // once for two steps: m.load(stage, k, want) starts it (by M::kEvenLoads loads), for an
 // even step k, on its way to the kExtra bytes at the end of the stage; m.begin(stage, k, up) reads it into an
 // M::Next, while the step before still needs its own, and m.take(up) replaces that;
@@ -147,7 +148,7 @@ struct TileLoop {
   template <int PH, class M>
   __device__ __forceinline__ void step(uint8_t* cur, uint8_t* nxt, int k, int n, M& m,
                                        typename M::P (&p)[2], typename M::Q (&q)[FQ],
-                                       v4f (&acc)[FP][FQ]) {
+                                       typename M::Acc (&acc)[FP][FQ]) {
 #pragma unroll
     for (int i = 0; i + 1 < FP; ++i) {
       p[(i + 1) & 1] = m.template p<PH>(read(cur, rp, i + 1), i + 1);
@@ -178,7 +179,8 @@ struct TileLoop {
 
   // The steps 0 .. n - 1 (n >= 1) are multiplied into acc; st: the stages.
   template <class M>
-  __device__ __forceinline__ void run(uint8_t* const (&st)[kMostStages], int n, M& m, v4f (&acc)[FP][FQ]) {
+  __device__ __forceinline__ void run(uint8_t* const (&st)[kMostStages], int n, M& m,
+                                      typename M::Acc (&acc)[FP][FQ]) {
     constexpr int U = S % 2 ? 2 * S : S;  // steps until stage and parity repeat
 #pragma unroll
     for (int i = 0; i < S; ++i) {
