@@ -31,18 +31,38 @@ typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------- quantise
-// |x| as an integer that orders like it; 0 for infinities and NaN.
-__device__ __forceinline__ uint32_t finite_bits(float x) {
-  const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-  return b < 0x7f800000u ? b : 0u;
+// The larger of two magnitudes; a NaN counts for nothing.
+__device__ __forceinline__ float larger(float m, float x) { return fmaxf(m, fabsf(x)); }
+// 0 in place of an infinity or a NaN
+__device__ __forceinline__ float finite(float x) {
+  return fabsf(x) <= 3.402823466e38f ? x : 0.f;
 }
-// The biased exponent byte e + 127 of a block with max |x| = amax (its bits).
+// The largest of a row of 16 lanes, in all of them: max with the row rotated by 8, 4, 2, 1.
+__device__ __forceinline__ float row_max(float m) {
+#define LSGD_ROTATED(n) \
+  __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(m), 0x120 + n, 0xf, 0xf, false))
+  m = fmaxf(m, LSGD_ROTATED(8));
+  m = fmaxf(m, LSGD_ROTATED(4));
+  m = fmaxf(m, LSGD_ROTATED(2));
+  return fmaxf(m, LSGD_ROTATED(1));
+#undef LSGD_ROTATED
+}
+// The largest of a wavefront's four lanes l, l + 16, l + 32, l + 48, in all of them.
+__device__ __forceinline__ float column_max(float m) {
+  const uint32_t b = __float_as_uint(m);
+  const auto p = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+  const uint32_t c = __float_as_uint(fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])));
+  const auto q = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+// The biased exponent byte e + 127 of a block whose largest finite magnitude is `max`.
 template <int FMT>
-__device__ __forceinline__ uint32_t scale_byte(uint32_t amax) {
+__device__ __forceinline__ uint32_t scale_byte(float max) {
   constexpr int kTop = FMT == kFmtE4M3 ? 8 : 15;
+  const uint32_t amax = __float_as_uint(max);
   if (amax == 0) return 127u;
   const int e = (int)(amax >> 23) - kTop + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return (uint32_t)max(e, 0);
+  return (uint32_t)(e > 0 ? e : 0);
 }
 // 2^-e of a scale byte (e <= 120, so it is a normal number)
 __device__ __forceinline__ float inv_scale(uint32_t byte) {
@@ -66,13 +86,18 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
 // 8 columns from 8 (t % 16), all in registers. BOTH (RP = 8: a square tile): the
 // transposed tensor as well, whose blocks run down the tile's columns, its bytes
 // turned in LDS so that each row leaves as a whole 128-byte line.
-constexpr int kTurnPitch = 144;  // bytes; 16-byte aligned, not a multiple of the banks' 256
-template <bool BF, int FMT, int RP, bool BOTH>
+// (rows of 128 bytes; piece k of 16 lies in slot k ^ (row / 8 % 8), which spreads the rows,
+// eight apart, that a wavefront writes at once over the banks)
+__device__ __forceinline__ int turned(int row, int byte) {
+  return row * 128 + (byte ^ (row / 8 % 8 * 16));
+}
+template <bool BF, int FMT, int RP, bool BOTH, bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_quantise(QuantArgs a, int tm, int tn, int total) {
   static_assert(!BOTH || RP == 8, "the transposed blocks need 128 rows");
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
-  const int g = id / (tm * tn), mt = id % (tm * tn) / tn, nt = id % tn;
+  const int l = xcd_order(id, total);
+  const int g = l / (tm * tn), mt = l % (tm * tn) / tn, nt = l % tn;
   const int tid = threadIdx.x, c = tid & 15, rg = tid >> 4;
   const int n0 = nt * 128, m0 = mt * 16 * RP;
   const int n = n0 + c * 8, r0 = m0 + rg * RP;
@@ -107,16 +132,42 @@ __global__ __launch_bounds__(kThreads) void k_quantise(QuantArgs a, int tm, int 
       }
     }
   }
+  // past the caches where they could not hold the tensors anyway
+  auto put = [&](auto value, auto* to) __attribute__((always_inline)) {
+    if constexpr (STREAM)
+      __builtin_nontemporal_store(value, to);
+    else
+      *to = value;
+  };
+  // Largest magnitudes of the rows and of the columns. With an infinity among them (rare, and
+  // looked for only here) once more over the finite values.
+  float rm[RP], cm[8];
+  auto maxima = [&](auto value) __attribute__((always_inline)) {
+#pragma unroll
+    for (int p = 0; p < RP; ++p) {
+      rm[p] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rm[p] = larger(rm[p], value(v[p][i]));
+    }
+    if constexpr (BOTH) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        cm[i] = 0.f;
+#pragma unroll
+        for (int p = 0; p < RP; ++p) cm[i] = larger(cm[i], value(v[p][i]));
+      }
+    }
+  };
+  maxima([](float x) { return x; });
+  float most = 0.f;
+#pragma unroll
+  for (int p = 0; p < RP; ++p) most = fmaxf(most, rm[p]);
+  if (most == __builtin_inff()) maxima([](float x) { return finite(x); });
   const int ldq = (a.N + 127) / 128 * 128, nb = ldq / 128, lds = (nb + 3) / 4 * 4;
   if (a.Q) {
 #pragma unroll
     for (int p = 0; p < RP; ++p) {
-      uint32_t amax = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) amax = max(amax, finite_bits(v[p][i]));
-#pragma unroll
-      for (int s = 1; s < 16; s *= 2) amax = max(amax, (uint32_t)__shfl_xor((int)amax, s));
-      const uint32_t byte = scale_byte<FMT>(amax);
+      const uint32_t byte = scale_byte<FMT>(row_max(rm[p]));
       const float f = inv_scale(byte);
       const int m = r0 + p;
       if (m >= a.M) continue;
@@ -126,75 +177,79 @@ __global__ __launch_bounds__(kThreads) void k_quantise(QuantArgs a, int tm, int 
       for (int h = 0; h < 2; ++h)
         q[h] = pack4<FMT>(v[p][4 * h] * f, v[p][4 * h + 1] * f, v[p][4 * h + 2] * f,
                           v[p][4 * h + 3] * f);
-      *(u32x2*)(a.Q + row * ldq + n) = q;
+      put(q, (u32x2*)(a.Q + row * ldq + n));
       // the block's scale, and behind a row's last block the padding
       if (c == 0) a.S[row * lds + nt] = (uint8_t)byte;
       else if (nt + 1 == nb && nt + c < lds) a.S[row * lds + nt + c] = 127;
     }
   }
   if constexpr (BOTH) {
-    __shared__ uint32_t cmax[4][128];
-    __shared__ __align__(16) uint8_t turn[128 * kTurnPitch];
+    __shared__ float cmax[4][128];
+    __shared__ uint8_t bytes[128];
+    __shared__ __align__(16) uint8_t turn[128 * 128];
     const int wave = tid >> 6, lane = tid & 63;
-    uint32_t am[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      am[i] = 0;
-#pragma unroll
-      for (int p = 0; p < RP; ++p) am[i] = max(am[i], finite_bits(v[p][i]));
-      am[i] = max(am[i], (uint32_t)__shfl_xor((int)am[i], 16));
-      am[i] = max(am[i], (uint32_t)__shfl_xor((int)am[i], 32));
-    }
+    for (int i = 0; i < 8; ++i) cm[i] = column_max(cm[i]);
     if (lane < 16) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) cmax[wave][c * 8 + i] = am[i];
+      for (int i = 0; i < 8; ++i) cmax[wave][c * 8 + i] = cm[i];
     }
     __syncthreads();
     const int ldt = (a.M + 127) / 128 * 128, mb = ldt / 128, ldst = (mb + 3) / 4 * 4;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int j = c * 8 + i;
-      const uint32_t amax = max(max(cmax[0][j], cmax[1][j]), max(cmax[2][j], cmax[3][j]));
-      const uint32_t byte = scale_byte<FMT>(amax);
+      const uint32_t byte = scale_byte<FMT>(
+          fmaxf(fmaxf(cmax[0][j], cmax[1][j]), fmaxf(cmax[2][j], cmax[3][j])));
       const float f = inv_scale(byte);
       u32x2 q;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         q[h] = pack4<FMT>(v[4 * h][i] * f, v[4 * h + 1][i] * f, v[4 * h + 2][i] * f,
                           v[4 * h + 3][i] * f);
-      *(u32x2*)(turn + j * kTurnPitch + rg * 8) = q;
-      if (n + i < a.N) {
-        uint8_t* st = a.St + ((long long)g * a.N + n + i) * ldst + mt;
-        if (rg == 0) *st = (uint8_t)byte;
-        else if (mt + 1 == mb && mt + rg < ldst) st[rg] = 127;
-      }
+      *(u32x2*)(turn + turned(j, rg * 8)) = q;
+      if (rg == 0) bytes[j] = (uint8_t)byte;
     }
     __syncthreads();
+    if (tid < 128 && n0 + tid < a.N) {
+      uint8_t* st = a.St + ((long long)g * a.N + n0 + tid) * ldst + mt;
+      *st = bytes[tid];
+      for (int k = 1; mt + 1 == mb && mt + k < ldst; ++k) st[k] = 127;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int at = i * kThreads + tid, j = at >> 3, k = (at & 7) * 16;
       if (n0 + j < a.N)
-        *(u32x4*)(a.Qt + ((long long)g * a.N + n0 + j) * ldt + m0 + k) =
-            *(const u32x4*)(turn + j * kTurnPitch + k);
+        put(*(const u32x4*)(turn + turned(j, k)),
+            (u32x4*)(a.Qt + ((long long)g * a.N + n0 + j) * ldt + m0 + k));
     }
   }
 }
 
+// From kNtBytesCaller of input and output on the values are streamed: 16384 x 8192 in bf16
+// both ways (537 MB) 156 -> 116 us; with 268 MB (8192^2) the call itself gains as much, but
+// the product that reads the values next loses more (506 -> 519 us together).
 template <bool BF, int FMT>
 hipError_t quantise(const QuantArgs& a, hipStream_t s) {
+  const double bytes = (double)a.M * a.N * a.G *
+                       ((BF ? 2 : 4) + (a.Q != nullptr) + (a.Qt != nullptr));
+  const bool stream = bytes >= (double)kNtBytesCaller;
   const long long tn = (a.N + 127LL) / 128;
   // a tile of 128 rows where the columns' blocks need it, 16 otherwise
   const int rows = a.Qt ? 128 : 16;
   const long long tm = ((long long)a.M + rows - 1) / rows;
   if (tm * tn > 0x7fffffffLL / a.G) return hipErrorInvalidValue;
   const long long total = tm * tn * a.G;
+  auto launch = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid_of(total), dim3(kThreads), 0, s, a, (int)tm, (int)tn,
+                       (int)total);
+    return hipGetLastError();
+  };
   if (a.Qt)
-    hipLaunchKernelGGL((k_quantise<BF, FMT, 8, true>), grid_of(total), dim3(kThreads), 0, s, a,
-                       (int)tm, (int)tn, (int)total);
-  else
-    hipLaunchKernelGGL((k_quantise<BF, FMT, 1, false>), grid_of(total), dim3(kThreads), 0, s, a,
-                       (int)tm, (int)tn, (int)total);
-  return hipGetLastError();
+    return stream ? launch(k_quantise<BF, FMT, 8, true, true>)
+                  : launch(k_quantise<BF, FMT, 8, true, false>);
+  return stream ? launch(k_quantise<BF, FMT, 1, false, true>)
+                : launch(k_quantise<BF, FMT, 1, false, false>);
 }
 
 // ------------------------------------------------------------------ product
