@@ -71,17 +71,32 @@ __device__ __forceinline__ v4f load4(const bf16_t* p, int n) {
 }
 
 // n neighbours, from (r, c) on, of the matrix to orthogonalise: X's, or of an update
-// d = g + m u or u. STEP: takes the momentum step u = m u + g first and stores it.
+// d = g + m u or u; fetch() loads them, take() makes d of them. STEP: takes the momentum
+// step u = m u + g first and stores it.
+struct Fetched {
+  v4f x, u;
+};
 template <bool STEP>
-__device__ __forceinline__ v4f direction(const OrthoArgs& a, int g, int r, int c, int n) {
+__device__ __forceinline__ Fetched fetch(const OrthoArgs& a, int g, int r, int c, int n) {
   const long long x = (long long)g * a.sX + (long long)r * a.ldx + c;
-  if (!a.U) return a.x_bf16 ? load4((const bf16_t*)a.X + x, n) : load4((const float*)a.X + x, n);
-  float* pu = a.U + (long long)g * a.sU + (long long)r * a.ldu + c;
-  v4f u = load4(pu, n), gr = {};
-  if (STEP || a.nesterov) gr = load4((const float*)a.X + x, n);
+  Fetched f{};
+  if (!a.U) {
+    f.x = a.x_bf16 ? load4((const bf16_t*)a.X + x, n) : load4((const float*)a.X + x, n);
+  } else {
+    f.u = load4(a.U + (long long)g * a.sU + (long long)r * a.ldu + c, n);
+    if (STEP || a.nesterov) f.x = load4((const float*)a.X + x, n);
+  }
+  return f;
+}
+template <bool STEP>
+__device__ __forceinline__ v4f take(const OrthoArgs& a, int g, int r, int c, int n,
+                                    const Fetched& f) {
+  if (!a.U) return f.x;
+  v4f u = f.u;
   if constexpr (STEP) {
+    float* pu = a.U + (long long)g * a.sU + (long long)r * a.ldu + c;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) u[e] = __builtin_fmaf(a.mom, u[e], gr[e]);
+    for (int e = 0; e < 4; ++e) u[e] = __builtin_fmaf(a.mom, u[e], f.x[e]);
     if (n >= 4) {
       *(v4f_any*)pu = u;
     } else {
@@ -92,7 +107,7 @@ __device__ __forceinline__ v4f direction(const OrthoArgs& a, int g, int r, int c
   }
   if (a.nesterov) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) u[e] = __builtin_fmaf(a.mom, u[e], gr[e]);
+    for (int e = 0; e < 4; ++e) u[e] = __builtin_fmaf(a.mom, u[e], f.x[e]);
   }
   return u;
 }
@@ -114,20 +129,34 @@ __global__ __launch_bounds__(kThreads) void k_ortho_norm(OrthoArgs a, int chunks
   const unsigned id = workgroup_id();
   if (id >= (unsigned)chunks * a.G) return;
   const int g = id / chunks, ch = id % chunks, quads = (a.N + 3) / 4;
+  // four fours at a time: their loads wait for none of the stores
   const int by = chunks * kThreads, dr = by / quads, dc = by % quads;
   const int first = ch * kThreads + threadIdx.x;
   int r = first / quads, c = first % quads;
   double s = 0;
-#pragma unroll 4
   while (r < a.M) {
-    const v4f d = direction<true>(a, g, r, c * 4, a.N - c * 4);
+    constexpr int kAtOnce = 4;
+    Fetched f[kAtOnce];
+    int fr[kAtOnce], fc[kAtOnce];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s += (double)d[e] * (double)d[e];
-    r += dr;
-    c += dc;
-    if (c >= quads) {
-      c -= quads;
-      ++r;
+    for (int i = 0; i < kAtOnce; ++i) {
+      fr[i] = r;
+      fc[i] = c * 4;
+      if (r < a.M) f[i] = fetch<true>(a, g, r, c * 4, a.N - c * 4);
+      r += dr;
+      c += dc;
+      if (c >= quads) {
+        c -= quads;
+        ++r;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (fr[i] < a.M) {
+        const v4f d = take<true>(a, g, fr[i], fc[i], a.N - fc[i], f[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += (double)d[e] * (double)d[e];
+      }
     }
   }
   __shared__ double red[kThreads];
@@ -164,6 +193,14 @@ __global__ __launch_bounds__(kThreads) void k_ortho_split(OrthoArgs a, int chunk
   const int g = id / (tm * tn), p0 = id % (tm * tn) / tn * 64, q0 = id % tn * 64;
   __shared__ float tile[64][65];
   __shared__ double red[kThreads];
+  // the loads run along the matrix's own rows
+  const int r0 = a.flip ? q0 : p0, c0 = a.flip ? p0 : q0;
+  Fetched f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int u = i * kThreads + threadIdx.x, y = u >> 4, x = (u & 15) * 4;
+    if (r0 + y < a.M) f[i] = fetch<false>(a, g, r0 + y, c0 + x, a.N - c0 - x);
+  }
   double s = 0;
   for (int i = threadIdx.x; i < chunks; i += kThreads) s += a.part[(long long)g * chunks + i];
   red[threadIdx.x] = s;
@@ -172,13 +209,11 @@ __global__ __launch_bounds__(kThreads) void k_ortho_split(OrthoArgs a, int chunk
   const int k = r > 0 ? min(100, -ilogb(r)) : 0;  // 0 for an infinite or NaN norm
   if (id % (tm * tn) == 0 && threadIdx.x == 0) a.kexp[g] = max(k, 0);
   const double inv = ldexp((double)a.scale_x, max(k, 0)) / (norm + (double)a.eps);
-  // the loads run along the matrix's own rows
-  const int r0 = a.flip ? q0 : p0, c0 = a.flip ? p0 : q0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int u = i * kThreads + threadIdx.x, y = u >> 4, x = (u & 15) * 4;
     v4f v = {};
-    if (r0 + y < a.M) v = direction<false>(a, g, r0 + y, c0 + x, a.N - c0 - x);
+    if (r0 + y < a.M) v = take<false>(a, g, r0 + y, c0 + x, a.N - c0 - x, f[i]);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float w = (float)((double)v[e] * inv);
@@ -192,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void k_ortho_split(OrthoArgs a, int chunk
   const long long plane = (long long)a.mp * a.np;
   _Float16* X = a.Xr + (long long)g * P * plane;
   _Float16* T = a.Xt[0] + (long long)g * 2 * plane;
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < 2; ++i) {
     const int u = i * kThreads + threadIdx.x, y = u >> 3, x = (u & 7) * 8;
     f16x8 h, l;
@@ -285,18 +320,21 @@ __device__ __forceinline__ f16x4 second_of(const float (&v)[4], const f16x4& h) 
                (_Float16)(v[2] - (float)h[2]), (_Float16)(v[3] - (float)h[3])};
 }
 
-// The n (at most 4; none for n <= 0) neighbours from element (r, c) of the result on.
+// The n (at most 4; none for n <= 0) neighbours from element (r, c) of the result on; x: the
+// weights an update finds there.
 __device__ __forceinline__ void result(const OrthoArgs& a, int g, int r, int c, int n,
-                                       const float (&v)[4]) {
+                                       const float (&v)[4], const v4f& x) {
   if (a.W) {
     float* w = a.W + (long long)g * a.sW + (long long)r * a.ldw + c;
-    if (n >= 4) {
-      v4f_any x = *(const v4f_any*)w;
+    v4f y;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(a.keep, x[e], a.step * v[e]);
-      *(v4f_any*)w = x;
+    for (int e = 0; e < 4; ++e) y[e] = __builtin_fmaf(a.keep, x[e], a.step * v[e]);
+    if (n >= 4) {
+      *(v4f_any*)w = y;
     } else {
-      for (int e = 0; e < n; ++e) w[e] = __builtin_fmaf(a.keep, w[e], a.step * v[e]);
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < n) w[e] = y[e];
     }
   } else if (a.x_bf16) {
     bf16_t* y = (bf16_t*)a.Y + (long long)g * a.sY + (long long)r * a.ldy + c;
@@ -548,8 +586,14 @@ __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_apply(Ort
         const int r = a.flip ? q0 + q : p0 + p, c = a.flip ? p0 + p : q0 + q;
         const int left = r < a.M ? a.N - c : 0;
         const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
-        result(a, g, r, c, left, lo);
-        result(a, g, r, c + 4, left - 4, hi);
+        v4f wl = {}, wh = {};
+        if (a.W) {
+          const float* w = a.W + (long long)g * a.sW + (long long)r * a.ldw + c;
+          wl = load4(w, left);
+          wh = load4(w + 4, left - 4);
+        }
+        result(a, g, r, c, left, lo, wl);
+        result(a, g, r, c + 4, left - 4, hi, wh);
       } else {
         if (q0 + q >= a.np || p0 + p >= a.mp) continue;
         f16x8 h, w;
@@ -573,6 +617,7 @@ __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_apply(Ort
 // with zeros to multiples of 32, a wavefront works on 32 x 32 blocks.
 constexpr int kSmallThreads = 512, kSmallWaves = kSmallThreads / 64, kSmallMost = 128;
 constexpr int kSmallBlocks = 5;  // of X a wavefront
+constexpr int kSmallFours = 20;  // of X a thread (LDS holds fewer than 20 * 512 * 4 values)
 constexpr size_t kSmallLds = 160 * 1024;
 __host__ __device__ constexpr int pitch(int n) { return n + 8; }
 constexpr size_t small_lds(int mp, int np) {
@@ -580,6 +625,17 @@ constexpr size_t small_lds(int mp, int np) {
 }
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+struct Place {  // of a row's four neighbours
+  int r, c;
+  __device__ __forceinline__ void next(int dr, int dc, int quads) {
+    r += dr;
+    c += dc;
+    if (c >= quads) {
+      c -= quads;
+      ++r;
+    }
+  }
+};
 struct Plane2 {  // a matrix's two pieces in LDS
   _Float16* p[2];
   int ld;
@@ -590,9 +646,11 @@ template <bool COLS, class Mac>
 __device__ __forceinline__ void block_product(const Plane2& F, int r0, const Plane2& S, int c0,
                                               int K, int lr, int lq,
                                               typename Mac::Acc (&acc)[2][2]) {
-#pragma unroll 1
-  for (int k = 0; k < K; k += 32) {
+  struct Frags {
     f16x8 f[2][2], g[2][2];
+  };
+  auto read = [&](int k) __attribute__((always_inline)) {
+    Frags x;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -603,20 +661,32 @@ __device__ __forceinline__ void block_product(const Plane2& F, int r0, const Pla
           using L = __attribute__((address_space(3))) s16x4;
           const _Float16* b =
               F.p[w] + (k + 8 * lq + (lr >> 2)) * F.ld + r0 + i * 16 + 4 * (lr & 3);
-          const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)b);
-          const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(b + 4 * F.ld));
-          f[i][w] = __builtin_bit_cast(
-              f16x8, s16x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)b);
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((L*)(b + 4 * F.ld));
+          x.f[i][w] = __builtin_bit_cast(
+              f16x8, s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
         } else {
-          f[i][w] = *(const f16x8*)(F.p[w] + (r0 + i * 16 + lr) * F.ld + k + 8 * lq);
+          x.f[i][w] = *(const f16x8*)(F.p[w] + (r0 + i * 16 + lr) * F.ld + k + 8 * lq);
         }
-        g[i][w] = *(const f16x8*)(S.p[w] + (c0 + i * 16 + lr) * S.ld + k + 8 * lq);
+        x.g[i][w] = *(const f16x8*)(S.p[w] + (c0 + i * 16 + lr) * S.ld + k + 8 * lq);
       }
+    return x;
+  };
+  auto mac = [&](const Frags& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) Mac::mac(acc[i][j], f[i][0], f[i][1], g[j][0], g[j][1]);
+      for (int j = 0; j < 2; ++j)
+        Mac::mac(acc[i][j], x.f[i][0], x.f[i][1], x.g[j][0], x.g[j][1]);
+  };
+  Frags x = read(0);  // the next fragments are on their way while these are multiplied
+#pragma unroll 1
+  for (int k = 32; k < K; k += 32) {
+    const Frags next = read(k);
+    mac(x);
+    x = next;
   }
+  mac(x);
 }
 
 __global__ __launch_bounds__(kSmallThreads) void k_ortho_small(OrthoArgs a, int mp, int np) {
@@ -633,16 +703,38 @@ __global__ __launch_bounds__(kSmallThreads) void k_ortho_small(OrthoArgs a, int 
   A.p[0] = X.p[1] + mp * X.ld;
   A.p[1] = A.p[0] + mp * A.ld;
 
-  // the norm, an update's momentum step with it, in the place of A
-  double* red = (double*)A.p[0];
-  const int quads = (a.N + 3) / 4;
-  double s = 0;
-  for (int u = tid; u < a.M * quads; u += kSmallThreads) {
-    const int r = u / quads, c = u % quads * 4;
-    const v4f d = direction<true>(a, g, r, c, a.N - c);
+  // the whole matrix into registers, all loads at once, an update's momentum step with it
+  const int quads = (a.N + 3) / 4, total = a.M * quads;
+  const int dr = kSmallThreads / quads, dc = kSmallThreads % quads;
+  v4f d[kSmallFours];
+  Place at{tid / quads, tid % quads};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s += (double)d[e] * (double)d[e];
-  }
+  for (int i = 0; i < kSmallFours; i += 4)
+    if (i * kSmallThreads < total) {
+      Fetched f[4];
+      Place was[4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        was[h] = at;
+        if (at.r < a.M) f[h] = fetch<true>(a, g, at.r, at.c * 4, a.N - at.c * 4);
+        at.next(dr, dc, quads);
+      }
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        d[i + h] = v4f{};
+        if (was[h].r < a.M)
+          d[i + h] = take<true>(a, g, was[h].r, was[h].c * 4, a.N - was[h].c * 4, f[h]);
+      }
+    }
+  // the norm, in the place of A
+  double* red = (double*)A.p[0];
+  double s = 0;
+#pragma unroll
+  for (int i = 0; i < kSmallFours; ++i)
+    if (i * kSmallThreads < total) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += (double)d[i][e] * (double)d[i][e];
+    }
   red[tid] = s;
   for (int w = kSmallThreads / 2; w; w /= 2) {
     __syncthreads();
@@ -652,16 +744,18 @@ __global__ __launch_bounds__(kSmallThreads) void k_ortho_small(OrthoArgs a, int 
   const double norm = sqrt(red[0]), ratio = norm / (norm + (double)a.eps);
   const int k0 = ratio > 0 ? max(0, min(100, -ilogb(ratio))) : 0;  // see k_ortho_split
   const double inv = ldexp((double)a.scale_x, k0) / (norm + (double)a.eps);
-  // (each thread reads what it wrote itself above)
   const int rows = a.flip ? np : mp, cols = (a.flip ? mp : np) / 4;
-  for (int u = tid; u < a.M * quads; u += kSmallThreads) {
-    const int r = u / quads, c = u % quads * 4;
-    const v4f d = direction<false>(a, g, r, c, a.N - c);
+  at = Place{tid / quads, tid % quads};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int o = a.flip ? (c + e) * X.ld + r : r * X.ld + c + e;
-      split2((float)((double)d[e] * inv), X.p[0][o], X.p[1][o]);
+  for (int i = 0; i < kSmallFours; ++i) {
+    if (i * kSmallThreads < total && at.r < a.M) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = at.r, c = at.c * 4 + e, o = a.flip ? c * X.ld + r : r * X.ld + c;
+        split2((float)((double)d[i][e] * inv), X.p[0][o], X.p[1][o]);
+      }
     }
+    at.next(dr, dc, quads);
   }
   // zeros behind the last row and behind each row's last four
   for (int u = tid; u < rows * cols; u += kSmallThreads) {
@@ -782,16 +876,33 @@ __global__ __launch_bounds__(kSmallThreads) void k_ortho_small(OrthoArgs a, int 
     }
     __syncthreads();
   }
-  for (int u = tid; u < a.M * quads; u += kSmallThreads) {
-    const int r = u / quads, c = u % quads * 4;
-    float v[4];
+  // (an update's weights four fours at a time, as above)
+  at = Place{tid / quads, tid % quads};
+  while (at.r < a.M) {
+    v4f w[4];
+    Place was[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int o = a.flip ? (c + e) * X.ld + r : r * X.ld + c + e;
-      v[e] = __uint_as_float((uint32_t)((const uint16_t*)X.p[0])[o] << 16 |
-                             ((const uint16_t*)X.p[1])[o]);
+    for (int h = 0; h < 4; ++h) {
+      was[h] = at;
+      if (a.W && at.r < a.M)
+        w[h] = load4(a.W + (long long)g * a.sW + (long long)at.r * a.ldw + at.c * 4,
+                     a.N - at.c * 4);
+      at.next(dr, dc, quads);
     }
-    result(a, g, r, c, a.N - c, v);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      const int r = was[h].r, c = was[h].c * 4;
+      if (r < a.M) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int o = a.flip ? (c + e) * X.ld + r : r * X.ld + c + e;
+          v[e] = __uint_as_float((uint32_t)((const uint16_t*)X.p[0])[o] << 16 |
+                                 ((const uint16_t*)X.p[1])[o]);
+        }
+        result(a, g, r, c, a.N - c, v, w[h]);
+      }
+    }
   }
 }
 
