@@ -471,8 +471,9 @@ enum { LSGD_E4M3 = 0, LSGD_E5M2 = 1 };
  * with d_S [G][M][up(ceil(N / 128), 4)], blocks along N; and with d_Qt, the
  * transposes, d_Qt [G][N][up(M, 128)] with d_St [G][N][up(ceil(M / 128), 4)],
  * blocks along M. Either pair may be NULL (both pointers), not both pairs; one
- * call reads X once for the two. All padding is written. d_Q and d_Qt are
- * 16-byte aligned, X aligned to its elements, else LSGD_E_INVALID.
+ * call reads X once for the two. All padding is written. M, N <= 2^30, d_Q and
+ * d_Qt 16-byte aligned, X aligned to its elements, else LSGD_E_INVALID. What is
+ * written must not overlap X.
  */
 lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G,
                                  int32_t M, int32_t N, const void* d_X,
@@ -494,7 +495,7 @@ lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G,
  * multiples of 4) are the group strides; 0 shares one matrix among the groups.
  * d_A, d_B 16-byte, d_SA, d_SB 4-byte aligned. The bytes past Kd of a row
  * must be zeros, as lsgd_quantise_blocks leaves them, and its scale bytes
- * below 255. Kd <= 2^22. C is out_dtype LSGD_FP32 or LSGD_BF16 (rounded once), row pitch
+ * below 255. M, N <= 2^30, Kd <= 2^22. C is out_dtype LSGD_FP32 or LSGD_BF16 (rounded once), row pitch
  * ldc >= N, group stride sC >= M * ldc (any value for G == 1); nothing between
  * its rows is written. d_ws: workspace of
  * lsgd_grouped_gemm_blocks_workspace_bytes (for the same sizes; which may be 0; then NULL is
@@ -540,7 +541,8 @@ lsgd_status lsgd_orthogonalise_workspace_bytes(int32_t dtype, int32_t G,
                                                size_t* bytes);
 
 /* Y_g = O(X_g) for G matrices, X and Y of `dtype` (pitches and strides in
- * elements). Y may be X itself (same pitch and stride). */
+ * elements). Y may be X itself (same pitch and stride); else
+ * they must not overlap. */
 lsgd_status lsgd_orthogonalise(int32_t dtype, int32_t G, int32_t M, int32_t N,
                                const void* d_X, int64_t ldx, int64_t sX,
                                void* d_Y, int64_t ldy, int64_t sY,
@@ -553,7 +555,8 @@ lsgd_status lsgd_orthogonalise(int32_t dtype, int32_t G, int32_t M, int32_t N,
  *   w = (1 - lr wd) w - lr scale O(d).
  * gemm_dtype: the precision of O's products (as dtype above). Pointers may point into
  * the replicas' flat rows (a layer's W of every replica: sW the row length). lr,
- * weight_decay and scale finite, 0 <= momentum < 1, nesterov 0 or 1. */
+ * weight_decay and scale finite, 0 <= momentum < 1, nesterov 0 or 1. W, U and G must
+ * not overlap. */
 lsgd_status lsgd_orthogonal_update(int32_t gemm_dtype, int32_t G, int32_t M,
                                    int32_t N, float* d_W, int64_t ldw,
                                    int64_t sW, float* d_U, int64_t ldu,

@@ -467,7 +467,7 @@ __global__ __launch_bounds__((64 * (BP / WP) * (BQ / WQ)), 2) void k_gemm_tile(B
            t.wq, k0);
   v4f acc[T::FP][T::FQ] = {};
   t.run(st, steps, mac, acc);
-  if constexpr (T::kStage >= BQ / 2 * (BP * 4 + 16)) {
+  if constexpr (BP == 64) {  // the only tiles that are split
     if (a.splits > 1) {
       tile_out<false, T::kThreads>(t, acc, st[0], st[1], a.part,
                                    ((long long)sg * a.M + q0) * a.N + p0, a.N, a.N - p0, a.M - q0);

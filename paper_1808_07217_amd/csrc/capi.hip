@@ -279,6 +279,12 @@ Layout make_layout(const lsgd_config* c) {
 
 // Inner range of a product of blocks: a tile's rows are addressed by 32-bit offsets.
 constexpr int32_t kMaxInner = 1 << 22;
+// The most rows and columns of a matrix in blocks: whole tiles of them fit an int.
+constexpr int32_t kMaxBlockRows = 1 << 30;
+bool block_sizes(int32_t G, int32_t M, int32_t N, int32_t Kd) {
+  return G >= 1 && G <= 65535 && M >= 1 && M <= kMaxBlockRows && N >= 1 && N <= kMaxBlockRows &&
+         Kd >= 1 && Kd <= kMaxInner;
+}
 
 lsgd_status block_status(hipError_t e) {
   return e == hipSuccess ? LSGD_OK : (e == hipErrorInvalidValue ? LSGD_E_INVALID : LSGD_E_HIP);
@@ -1809,7 +1815,9 @@ lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G, int32
                                  uint8_t* d_S, uint8_t* d_Qt, uint8_t* d_St, void* stream) {
   if ((dtype != LSGD_FP32 && dtype != LSGD_BF16) || (format != LSGD_E4M3 && format != LSGD_E5M2))
     return LSGD_E_INVALID;
-  if (G < 1 || M < 1 || N < 1 || G > 65535 || !d_X || ldx < N || sX < 0) return LSGD_E_INVALID;
+  if (G < 1 || M < 1 || N < 1 || G > 65535 || M > kMaxBlockRows || N > kMaxBlockRows || !d_X ||
+      ldx < N || sX < 0)
+    return LSGD_E_INVALID;
   if ((uintptr_t)d_X % (dtype == LSGD_BF16 ? 2 : 4)) return LSGD_E_INVALID;
   if (!d_Q != !d_S || !d_Qt != !d_St || (!d_Q && !d_Qt)) return LSGD_E_INVALID;
   if ((uintptr_t)d_Q % 16 || (uintptr_t)d_Qt % 16) return LSGD_E_INVALID;
@@ -1821,8 +1829,7 @@ lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G, int32
 lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t out_dtype, int32_t G, int32_t M,
                                                      int32_t N, int32_t Kd, size_t* bytes) {
   if (out_dtype != LSGD_FP32 && out_dtype != LSGD_BF16) return LSGD_E_INVALID;
-  if (!bytes || G < 1 || M < 1 || N < 1 || Kd < 1 || G > 65535 || Kd > kMaxInner)
-    return LSGD_E_INVALID;
+  if (!bytes || !block_sizes(G, M, N, Kd)) return LSGD_E_INVALID;
   *bytes = lsgd::gemm_blocks_workspace_bytes(out_dtype == LSGD_BF16, G, M, N, Kd);
   return LSGD_OK;
 }
@@ -1837,7 +1844,7 @@ lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b, int32_t
       (format_b != LSGD_E4M3 && format_b != LSGD_E5M2) ||
       (out_dtype != LSGD_FP32 && out_dtype != LSGD_BF16))
     return LSGD_E_INVALID;
-  if (G < 1 || M < 1 || N < 1 || Kd < 1 || G > 65535 || Kd > kMaxInner) return LSGD_E_INVALID;
+  if (!block_sizes(G, M, N, Kd)) return LSGD_E_INVALID;
   if (!d_A || !d_SA || !d_B || !d_SB || !d_C || ldc < N) return LSGD_E_INVALID;
   if (sA < 0 || sB < 0 || sSA < 0 || sSB < 0 || sA % 16 || sB % 16 || sSA % 4 || sSB % 4)
     return LSGD_E_INVALID;

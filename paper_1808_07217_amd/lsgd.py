@@ -753,11 +753,13 @@ def orthogonal_update(W: torch.Tensor, U: torch.Tensor, G: torch.Tensor, lr: flo
     """In-place update of W [K][M][N] and its momentum U with gradient G (all
     float32, columns contiguous; views into the replicas' flat rows are fine):
     u = m u + g, d = g + m u (``nesterov``) or u, w = (1 - lr wd) w - lr scale O(d)
-    with O of ``orthogonalise`` (lsgd_orthogonal_update)."""
+    with O of ``orthogonalise`` (lsgd_orthogonal_update). They must not overlap."""
     (ldw, sW), (ldu, sU), (ldg, sG) = (_matrices("W", W, _FP32), _matrices("U", U, _FP32),
                                        _matrices("G", G, _FP32))
     if U.shape != W.shape or G.shape != W.shape:
         raise ValueError("W, U, G must have one shape")
+    if len({W.data_ptr(), U.data_ptr(), G.data_ptr()}) < 3:
+        raise ValueError("W, U, G must not overlap")
     _same_device(W, U, G)
     K, M, N = W.shape
     co = _coefficients(coefficients)

@@ -111,6 +111,24 @@ def test_grouped_gemm_blocks_refusals():
     assert call(**big, _19=nb.value - 1) == 2
 
 
+def test_blocks_refuse_more_rows_than_an_int_holds_tiles_of():
+    f, nb, lib = P(4096), ctypes.c_size_t(), _lib()
+    top = 2**31 - 1
+    for M, N in ((2**30 + 1, 1), (1, 2**30 + 1), (top, 1), (1, top)):
+        assert lib.lsgd_quantise_blocks(0, 0, 1, M, N, f, N, 0, f, f, None, None, None) == 1
+        assert lib.lsgd_quantise_blocks(0, 0, 1, M, N, f, N, 0, None, None, f, f, None) == 1
+        size = lib.lsgd_grouped_gemm_blocks_workspace_bytes
+        assert size(1, 1, M, N, 5, ctypes.byref(nb)) == 1
+        assert lib.lsgd_grouped_gemm_blocks(0, 0, 1, 1, M, N, 5, f, 0, f, 0, f, 0, f, 0, f, N, 0,
+                                            f, 1 << 40, None) == 1
+    assert size(1, 1, 2**30, 2**30, 5, ctypes.byref(nb)) == 0
+    # sizes that are allowed, but more tiles than a launch can number
+    M = N = 2**30
+    assert lib.lsgd_quantise_blocks(0, 0, 1, M, N, f, N, 0, f, f, None, None, None) == 1
+    assert lib.lsgd_grouped_gemm_blocks(0, 0, 1, 1, M, N, 5, f, 0, f, 0, f, 0, f, 0, f, N, 0, f,
+                                        1 << 40, None) == 1
+
+
 CO = (ctypes.c_float * 3)(3.4445, -4.7750, 2.0315)
 
 

@@ -184,6 +184,15 @@ def test_orthogonal_update_in_bf16_precision():
         assert np.abs(_np(W) - w).max() <= 0.1 * 4 * near + 2.0 ** -22 * np.abs(w).max()
 
 
+def test_orthogonal_update_refuses_one_tensor_twice():
+    L = _lsgd()
+    a, b = (torch.ones(2, 3, 4, device=device()) for _ in range(2))
+    for bad in ((a, a, b), (a, b, a), (a, b, b)):
+        with pytest.raises(ValueError, match="overlap"):
+            L.orthogonal_update(*bad, 0.1, 0.9)
+    assert (a == 1).all() and (b == 1).all()
+
+
 def test_updates_on_streams_and_in_graphs():
     """Two captured graphs with a workspace each, replayed in turn with eager calls
     between them, and a call on a side stream: the eager bits every time."""
@@ -251,3 +260,104 @@ def test_local_step_of_a_large_layer():
     mean = _np(flat).mean(axis=0)
     L.replica_average(flat)
     assert np.abs(_np(flat) - mean).max() <= 1e-6 * np.abs(mean).max()
+
+
+def _steps_on_device(X, pieces, eps=1e-7, coefficients=(3.4445, -4.7750, 2.0315), steps=5):
+    """The oracle's two functions for matrices too large for the host: exact in float64
+    (pieces = 0), or with the roundings of that many fp16 pieces and fp32 sums."""
+    a, b, c = (float(np.float32(v)) for v in coefficients)
+
+    def split(x, scale, n):
+        x = x * scale
+        hi = x.half().float()
+        return [hi, (x - hi).half().float()][:n]
+
+    def product(p, q):
+        r = p[0] @ q[0]
+        return r if min(len(p), len(q)) == 1 else r + (p[0] @ q[1] + p[1] @ q[0])
+
+    out = torch.empty(X.shape, device=X.device, dtype=torch.float64)
+    for g in range(X.shape[0]):
+        x = X[g].double()
+        flip = x.shape[0] > x.shape[1]
+        x = (x.T if flip else x).contiguous()
+        x = x / (x.norm() + float(np.float32(eps)))
+        if pieces == 0:
+            for _ in range(steps):
+                A = x @ x.T.contiguous()
+                x = a * x + (b * A + c * (A @ A)) @ x
+        else:
+            S, Sa, Sb = 2.0 ** np.floor(np.log2(np.sqrt(x.numel()))), 2.0 ** 15, 2.0 ** 14
+            X2 = split(x.float(), S, 2)
+            for _ in range(steps):
+                Xp = X2[:pieces]
+                A = split(product(Xp, [p.T.contiguous() for p in Xp]) * (Sa / S / S), 1.0, pieces)
+                Bm = split((b * sum(A) + c * (product(A, A) / Sa)) / Sa, Sb, pieces)
+                y = product(Bm, Xp) / Sb + a * sum(X2)
+                X2 = split(y, 1.0, 2)
+            x = y.double() / S
+        out[g] = x.T if flip else x
+    return out
+
+
+# Between them they take every cut that the products have, at ragged edges and with the
+# result's rows along either side: few or many matrices of hundreds of rows, of thousands.
+LARGE = [(100, 190, 200), (16, 500, 510), (2, 2040, 2030), (1, 4090, 1500), (1, 8190, 2040),
+         (1, 4000, 4090)]
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", LARGE)
+def test_large_matrices_match_float64(shape, precision):
+    """orthogonalise, and the update (whose result is not rounded to bf16), within the
+    module's tolerance."""
+    L = _lsgd()
+    print(f"large {shape} {precision}", flush=True)
+    K, M, N = shape
+    dt = torch.bfloat16 if precision == "bf16" else torch.float32
+    gen = torch.Generator(device=device()).manual_seed(M + N)
+    rand = lambda *s: torch.randn(*s, generator=gen, device=device())  # noqa: E731
+    r = max(1, min(M, N) // 16)
+    X = (rand(K, M, N) + torch.stack([rand(M, r) @ rand(r, N) for _ in range(K)]) / r ** 0.5).to(dt)
+    W, U = torch.zeros(K, M, N, device=device()), torch.zeros(K, M, N, device=device())
+    L.orthogonal_update(W, U, X.float(), -1.0, 0.0, gemm_dtype=dt)
+    assert torch.equal(U, X.float())
+    Y = L.orthogonalise(X)
+    pieces = 1 if precision == "bf16" else 2
+    for g in range(0, K, max(1, K // 3)):
+        want = _steps_on_device(X[g:g + 1], 0)[0]
+        near = (_steps_on_device(X[g:g + 1], pieces)[0] - want).abs()
+        # W = 0 * 1 + 1 * O rounds once, as orthogonalise's fp32 result does
+        for got, half in ((Y[g], torch.finfo(dt).eps / 2), (W[g], 2.0 ** -24)):
+            e, floor = (got.double() - want).abs(), half + 35 * 2.0 ** -24
+            tol = 4 * near.norm() + floor * want.norm()
+            assert e.norm() <= tol, (g, float(e.norm()), float(tol))
+            tol = 4 * near.max() + floor * want.abs().max()
+            assert e.max() <= tol, (g, float(e.max()), float(tol))
+
+
+def test_update_in_bf16_precision_of_a_large_layer_in_flat_rows():
+    """Momentum, decay and Nesterov on matrices that take the one-piece products, inside
+    rows that are longer than them."""
+    L = _lsgd()
+    print("update large flat", flush=True)
+    K, M, N = 2, 600, 401
+    gen = torch.Generator(device=device()).manual_seed(5)
+    flat = [torch.randn(K, M * N + 9, generator=gen, device=device()) for _ in range(3)]
+    W, U, G = (t[:, 5:5 + M * N].view(K, M, N) for t in flat)
+    kept = [(t[:, :5].clone(), t[:, 5 + M * N:].clone()) for t in flat]
+    f = lambda v: float(np.float32(v))  # noqa: E731
+    lr, m, wd = 0.05, 0.9, 0.1
+    w0, u0, g0 = W.double(), U.double(), G.double()
+    L.orthogonal_update(W, U, G, lr, m, wd, nesterov=True, gemm_dtype=torch.bfloat16)
+    u = f(m) * u0 + g0
+    d = g0 + f(m) * u
+    o = _steps_on_device(d, 0)
+    near = (_steps_on_device(d, 1) - o).abs().max()
+    w = (1 - f(lr) * f(wd)) * w0 - f(lr) * o
+    assert ((U.double() - u).abs() <= 2 * 2.0 ** -24 * (u0.abs() + g0.abs())).all()
+    tol = 3 * 2.0 ** -24 * (w0.abs() + lr * o.abs()) + lr * (
+        4 * near + 36 * 2.0 ** -24 * o.abs().max())
+    assert ((W.double() - w).abs() <= tol).all()
+    for t, (a, b) in zip(flat, kept):
+        assert torch.equal(t[:, :5], a) and torch.equal(t[:, 5 + M * N:], b)
