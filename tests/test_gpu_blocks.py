@@ -290,3 +290,58 @@ def test_blocks_on_a_side_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, L.grouped_gemm_blocks(L.quantise_blocks(X), w))
+
+
+def _tail(t, rows):
+    """The last rows of the last group, as blocks of their own."""
+    from paper_1808_07217_amd import lsgd as L
+    return L.Blocks(t.q[-1:, -rows:].contiguous(), t.scale[-1:, -rows:].contiguous(), t.n)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_quantise_tensors_past_the_caches(dtype, fmt):
+    """Hundreds of MB and more, whose values are streamed past the caches: the bits of the
+    same rows as small tensors, in either direction."""
+    L = _lsgd()
+    print(f"quantise streamed {dtype} {fmt}", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(3)
+    dt = torch.float32 if dtype == "fp32" else torch.bfloat16
+    X = torch.randn(3, 8190, 8195, generator=gen, device=device()).to(dt)
+    q, t = L.quantise_blocks(X, fmt, both=True)
+    alone = L.quantise_blocks(X, fmt)
+    assert torch.equal(alone.q.view(torch.uint8), q.q.view(torch.uint8))
+    assert torch.equal(alone.scale.view(torch.uint8), q.scale.view(torch.uint8))
+    for g, m, n in ((0, 0, 0), (1, 4096, 128), (2, 8064, 8064)):
+        part = X[g:g + 1, m:m + 128, n:]
+        a, _ = L.quantise_blocks(part, fmt, both=True)
+        _, b = L.quantise_blocks(X[g:g + 1, m:, n:n + 128], fmt, both=True)
+        assert torch.equal(q.q[g, m:m + 128, n:].view(torch.uint8), a.q[0].view(torch.uint8))
+        assert torch.equal(t.q[g, n:n + 128, m:].view(torch.uint8), b.q[0].view(torch.uint8))
+        for whole, own, first, blocks in ((q.scale[g, m:m + 128], a.scale, n // 128, 65 - n // 128),
+                                          (t.scale[g, n:n + 128], b.scale, m // 128, 64 - m // 128)):
+            assert torch.equal(whole[:, first:first + blocks].view(torch.uint8),
+                               own[0, :, :blocks].view(torch.uint8))
+
+
+def test_blocks_past_32_bit_offsets():
+    """Inputs, values and results of more than 2^32 bytes and 2^31 elements: the last rows
+    are those of the same rows alone."""
+    L = _lsgd()
+    print("blocks past 32 bits", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(4)
+    X = torch.randn(1, 131200, 33000, generator=gen, device=device(), dtype=torch.bfloat16)
+    a, t = L.quantise_blocks(X, both=True)
+    assert a.q.numel() > 2 ** 32 and t.q.numel() > 2 ** 32
+    _check_blocks(_tail(a, 65), _np(X[:, -65:]), "e4m3")
+    _check_blocks(_tail(t, 65), _np(X[:, :, -65:]).transpose(0, 2, 1), "e4m3")
+    b = L.quantise_blocks(X[:, :70])
+    del X
+    _check_product(L.grouped_gemm_blocks(a, b)[:, -65:], _tail(a, 65), b)
+    del t
+    # a result of 2.4e9 elements
+    rows = L.Blocks(a.q[:, :49000, :128].contiguous(), a.scale[:, :49000, :4].contiguous(), 128)
+    del a
+    for out in (torch.bfloat16, torch.float32):
+        C = L.grouped_gemm_blocks(rows, rows, out_dtype=out)
+        _check_product(C[:, -65:, -65:], _tail(rows, 65), _tail(rows, 65))

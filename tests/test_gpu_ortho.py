@@ -361,3 +361,20 @@ def test_update_in_bf16_precision_of_a_large_layer_in_flat_rows():
     assert ((W.double() - w).abs() <= tol).all()
     for t, (a, b) in zip(flat, kept):
         assert torch.equal(t[:, :5], a) and torch.equal(t[:, 5 + M * N:], b)
+
+
+def test_groups_past_32_bit_offsets():
+    """Three tall matrices, 3.2e9 elements: the last of them as a matrix alone."""
+    L = _lsgd()
+    print("orthogonalise past 32 bits", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(6)
+    X = torch.randn(3, 2 ** 20, 1024, generator=gen, device=device(), dtype=torch.bfloat16)
+    Y = L.orthogonalise(X)[2:]
+    X = X[2:].clone()
+    want = L.orthogonalise(X)
+    # (the cut of the products may differ, and with it the order of their sums: two results
+    # of one precision are each within the tolerance of the exact one)
+    exact, near = _steps_on_device(X, 0), _steps_on_device(X, 1)
+    tol = 4 * (near - exact).norm() + (2.0 ** -8 + 35 * 2.0 ** -24) * exact.norm()
+    for got in (Y, want):
+        assert (got.double() - exact).norm() <= tol
