@@ -213,6 +213,29 @@ def test_product_extreme_scales_and_specials():
         assert not np.isfinite(C[:3, 0]).any() and np.isfinite(C[:2, 1]).all()
 
 
+@pytest.mark.parametrize("fa", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+def test_product_at_the_smallest_scale(fa, out):
+    """Values around fp32's smallest normal number, whose blocks have the scale 2^-127,
+    times large ones: every sum here is of few bits, so results are exact; but a result in
+    fp32 takes values through bf16, whose numbers below 2^-126 are multiples of 2^-133:
+    each of the 256 values may be off by half of that, 2^-134, times 2^100."""
+    L = _lsgd()
+    print(f"product smallest scale {fa} {out}", flush=True)
+    e = np.arange(-134, -110)
+    A = np.repeat(np.exp2(e.astype(np.float64))[:, None], 256, axis=1)[None].astype(np.float32)
+    Bm = np.full((1, 5, 256), 2.0 ** 100, np.float32)
+    a, b = L.quantise_blocks(to_dev(A), fa), L.quantise_blocks(to_dev(Bm), "e4m3")
+    assert (a.scale.view(torch.uint8)[0, 0, :2] == 0).all()
+    want = B.values(_np(a.q), _np(a.scale)) @ B.values(_np(b.q), _np(b.scale)).transpose(0, 2, 1)
+    C = L.grouped_gemm_blocks(a, b, out_dtype=torch.bfloat16 if out == "bf16" else torch.float32)
+    assert want[0, 10, 0] > 0
+    # (the values from 2^-126 on, and all of them to bf16, exactly)
+    np.testing.assert_array_equal(_np(C)[:, 8 if out == "fp32" else 0:],
+                                  want[:, 8 if out == "fp32" else 0:])
+    assert np.abs(_np(C) - want).max() <= 256 * 2.0 ** -134 * 2.0 ** 100
+
+
 def test_product_shared_operands_and_strided_output():
     """One weight matrix for every group (expand), an output that is a view of
     padded rows: nothing between its rows changes; views at a row offset."""
