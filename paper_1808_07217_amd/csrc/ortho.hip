@@ -354,12 +354,12 @@ __device__ __forceinline__ void result(const OrthoArgs& a, int g, int r, int c, 
   }
 }
 
-// The square tiles: 256 x 256 with eight wavefronts of 128 x 64; 128 x 128 with four of a
-// quarter each, or, with four stages and so alone on a compute unit, eight of 64 x 32; 64 x
-// 64 with four.
+// The square tiles: 256 x 256 and 192 x 192 with eight wavefronts, two by four; 128 x 128
+// with four of a quarter each, or, with four stages and so alone on a compute unit, eight of
+// 64 x 32; 64 x 64 with four.
 template <int T, int S>
 struct Shape {
-  static constexpr bool kEight = T == 256 || (T == 128 && S == 4);
+  static constexpr bool kEight = T >= 192 || (T == 128 && S == 4);
   static constexpr int kWq = T / (kEight ? 4 : 2), kThreads = kEight ? 512 : 256;
 };
 
@@ -455,7 +455,7 @@ __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_gram(Orth
   t.init((const uint8_t*)src + (long long)p0 * ld, (const uint8_t*)src + (long long)q0 * ld, ld,
          a.mp - p0, a.mp - q0);
   // (256 x 256 tiles have no room for two; theirs are products of thousands both ways)
-  using Mac = MacHalf<P, P == 2 && !SECOND && BT <= 128>;
+  using Mac = MacHalf<P, P == 2 && !SECOND && BT <= 192>;
   Mac mac;
   typename Mac::Acc acc[T::FP][T::FQ] = {};
   t.run(st, ld / 128, mac, acc);
@@ -928,19 +928,22 @@ struct Cut {
 // takes per_cu workgroups at once (LDS), a round of them costs per_cu times `each`, and the
 // last round as much as a full one. `each` is what one tile took of a full round, in
 // units of about 10 us at an inner range of 2048 in fp32 precision, measured on 8 x
-// 2048^2 and 4096^2 with one cut forced for all products (16, 16, 44, 38, 133 us). At the
-// other end, with one workgroup to a unit, a product waits for loads and launches:
-// 512^2 takes 125 us in 64 x 64 tiles of four stages, 136 of three, 213 / 282 in 128 x 128
+// 2048^2 and 4096^2 with one cut forced for all products (16, 16, 44, 38, 84, 133 us). The
+// 192 x 192 tiles are for what 256 x 256 ones leave half of the units without: the triangles
+// of 4096 x 8192 in bf16 172 + 97 -> 150 + 78 us a step, 4 x 1500^2 1137 -> 993 us in all. At
+// the other end, with one workgroup to a unit, a product waits for loads and launches: 512^2
+// takes 125 us in 64 x 64 tiles of four stages, 136 of three, 213 / 282 in 128 x 128
 // tiles of four / two, 609 in 256 x 256 ones.
 constexpr int kCus = 256;
 template <class F>
 Cut best_cut(F tiles) {
-  const Cut cuts[5] = {{64, 4}, {64, 3}, {128, 4}, {128, 2}, {256, 2}};
-  const int per_cu[5] = {2, 3, 1, 2, 1};
-  const double each[5] = {1.6, 1.55, 4.3, 3.8, 12.6};
+  constexpr int kCuts = 6;
+  const Cut cuts[kCuts] = {{64, 4}, {64, 3}, {128, 4}, {128, 2}, {192, 2}, {256, 2}};
+  const int per_cu[kCuts] = {2, 3, 1, 2, 1, 1};
+  const double each[kCuts] = {1.6, 1.55, 4.3, 3.8, 8.4, 12.6};
   int at = 0;
   double least = 0;
-  for (int i = 0; i < 5; ++i) {
+  for (int i = 0; i < kCuts; ++i) {
     const double rounds = std::ceil((double)tiles(cuts[i].tile) / (kCus * per_cu[i]));
     const double t = rounds * per_cu[i] * each[i];
     if (i == 0 || t < least) {
@@ -960,6 +963,7 @@ void launch_gram(const OrthoArgs& a, int step, hipStream_t s) {
 template <int P, bool SECOND>
 void gram(Cut c, const OrthoArgs& a, int step, hipStream_t s) {
   if (c.tile == 256) return launch_gram<P, SECOND, 256, 2>(a, step, s);
+  if (c.tile == 192) return launch_gram<P, SECOND, 192, 2>(a, step, s);
   if (c.tile == 128 && c.stages == 2) return launch_gram<P, SECOND, 128, 2>(a, step, s);
   if (c.tile == 128) return launch_gram<P, SECOND, 128, 4>(a, step, s);
   if (c.stages == 3) return launch_gram<P, SECOND, 64, 3>(a, step, s);
@@ -974,6 +978,7 @@ void launch_apply(const OrthoArgs& a, int step, hipStream_t s) {
 template <int P, bool LAST>
 void apply(Cut c, const OrthoArgs& a, int step, hipStream_t s) {
   if (c.tile == 256) return launch_apply<P, LAST, 256, 2>(a, step, s);
+  if (c.tile == 192) return launch_apply<P, LAST, 192, 2>(a, step, s);
   if (c.tile == 128 && c.stages == 2) return launch_apply<P, LAST, 128, 2>(a, step, s);
   if (c.tile == 128) return launch_apply<P, LAST, 128, 4>(a, step, s);
   if (c.stages == 3) return launch_apply<P, LAST, 64, 3>(a, step, s);

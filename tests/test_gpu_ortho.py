@@ -303,7 +303,7 @@ def _steps_on_device(X, pieces, eps=1e-7, coefficients=(3.4445, -4.7750, 2.0315)
 # Between them they take every cut that the products have, at ragged edges and with the
 # result's rows along either side: few or many matrices of hundreds of rows, of thousands.
 LARGE = [(100, 190, 200), (16, 500, 510), (2, 2040, 2030), (1, 4090, 1500), (1, 8190, 2040),
-         (1, 4000, 4090)]
+         (1, 4000, 4090), (1, 4300, 4400), (4, 1500, 1490), (1, 1900, 4500)]
 
 
 @pytest.mark.parametrize("precision", ["fp32", "bf16"])
