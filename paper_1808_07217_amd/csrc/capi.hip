@@ -310,7 +310,9 @@ bool written_groups(int32_t G, int32_t M, int32_t N, const void* p, int64_t ld, 
 // The steps' coefficients and the powers of two that X, A and B are held at (see
 // ortho.hip): the largest singular value on the way, from 1 on, bounds every entry of X,
 // its square those of A and the largest |b t + c t^2| those of B; a power of two
-// puts the bound below fp16's largest value (0.9 of it, for rounding). X's is no
+// puts the bound below fp16's largest value (0.9 of it, for rounding). X's bound is at
+// least 2: a matrix that starts below 1, as all do by eps, is held at a norm in [1, 2)
+// (k(t) in ortho.hip). X's power of two is no
 // larger than sqrt(M N), which brings its entries to about 1 at the start: a
 // larger one would move nothing out of fp16's subnormal range that matters.
 bool ortho_numbers(lsgd::OrthoArgs& a, int32_t steps, const float* h, float eps) {
@@ -346,7 +348,7 @@ bool ortho_numbers(lsgd::OrthoArgs& a, int32_t steps, const float* h, float eps)
   a.grow = std::max(0, (int)std::ceil(std::log2(std::max(ratio, 1e-30))));
   const double room = 0.9 * 65504.0;
   auto pow2_below = [](double v) { return std::exp2(std::floor(std::log2(v))); };
-  const double sx = pow2_below(std::min(std::sqrt((double)a.M * a.N), room / top));
+  const double sx = pow2_below(std::min(std::sqrt((double)a.M * a.N), room / std::max(top, 2.0)));
   const double sa = pow2_below(room / t);
   const double sb = pow2_below(room / std::max(poly, 1.0));
   a.steps = steps;

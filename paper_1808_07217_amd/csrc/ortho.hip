@@ -19,7 +19,9 @@
 // and each is stored on both sides. All three products are tiles of tile_loop.h.
 // A matrix whose norm is small against eps starts that much below 1 and grows by at
 // most a known factor a step; X of step t is held 2^k(t) higher, k(t) = max(0,
-// k(0) - t * grow), so that it too has all of its bits.
+// k(0) - t * grow), so that it too has all of its bits: k(0) takes the norm r, 0 < r < 1,
+// to 1 <= 2^k(0) r < 2, which the scale of X leaves room for (r = 1 - 1e-7, nearly every
+// matrix's, to almost 2).
 // The steps work on m = min(M, N) rows. X lies in memory both ways, [m][n] for X X^T
 // and [n][m] for B X, rows padded with zeros to a multiple of 64 so that no product
 // has a tail; a zero row or column stays zero through the steps. In fp32 precision the two

@@ -378,3 +378,32 @@ def test_groups_past_32_bit_offsets():
     tol = 4 * (near - exact).norm() + (2.0 ** -8 + 35 * 2.0 ** -24) * exact.norm()
     for got in (Y, want):
         assert (got.double() - exact).norm() <= tol
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(2 ** 20, 1024), (1024, 2 ** 20)])
+def test_one_entry_holds_the_norm_of_the_largest_matrix(shape, dtype):
+    """2^30 elements, all but one of them zero: that one is held as high as any entry can be,
+    and the result is its singular value's course, s := s (a + b s^2 + c s^4), at its place.
+
+    From 1 on the course is 0.70, 1.11, 0.72, 1.09, 0.70, and an error of one step grows by
+    |a + 3 b s^2 + 5 c s^4| <= 1.3 in each of the next, to below 2 in all. One step's own: in
+    fp32 precision 35 2^-24 (see the top); with operands of 11 bits, off by u = 2^-12, A is off
+    by 3 u (two X, A itself), A A by 6 u, B by one more, B X by yet another, so at s = 1.12
+    5 |b| s^3 + 8 |c| s^5 = 62 u."""
+    L = _lsgd()
+    print(f"one entry {shape} {dtype}", flush=True)
+    M, N = shape
+    X = torch.zeros(1, M, N, device=device(),
+                    dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
+    X[0, M - 3, 7] = -1.0
+    Y = L.orthogonalise(X)
+    s = -1.0 / (1.0 + float(np.float32(1e-7)))
+    a, b, c = (float(np.float32(v)) for v in (3.4445, -4.7750, 2.0315))
+    for _ in range(5):
+        s = s * (a + b * s ** 2 + c * s ** 4)
+    got = float(Y[0, M - 3, 7])
+    step = 35 * 2.0 ** -24 if dtype == "fp32" else 62 * 2.0 ** -12 + 2.0 ** -8
+    assert abs(got - s) <= 5 * 2 * step, (got, s)
+    Y[0, M - 3, 7] = 0
+    assert bool((Y == 0).all())
