@@ -33,11 +33,11 @@ constexpr long long kNtBytesCaller = 320LL << 20;
 
 typedef uint16_t bf16_t;  // bfloat16 bit pattern
 
-// fp32 -> bf16, round to nearest even (finite inputs; overflow gives inf).
+// fp32 -> bf16, round to nearest even; overflow gives inf, a NaN of any pattern a quiet
+// NaN. The hardware's conversion, whose bits for all 2^32 inputs but NaN are those of
+// (b + 0x7fff + (b >> 16 & 1)) >> 16; that sum carries a NaN's payload into its sign.
 __device__ __forceinline__ bf16_t f32_to_bf16(float x) {
-  uint32_t b = __float_as_uint(x);
-  b += 0x7FFFu + ((b >> 16) & 1u);
-  return (bf16_t)(b >> 16);
+  return __builtin_bit_cast(bf16_t, (__bf16)x);
 }
 __device__ __forceinline__ float bf16_to_f32(bf16_t h) {
   return __uint_as_float(((uint32_t)h) << 16);

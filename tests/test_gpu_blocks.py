@@ -368,3 +368,37 @@ def test_blocks_past_32_bit_offsets():
     for out in (torch.bfloat16, torch.float32):
         C = L.grouped_gemm_blocks(rows, rows, out_dtype=out)
         _check_product(C[:, -65:, -65:], _tail(rows, 65), _tail(rows, 65))
+
+
+@pytest.mark.parametrize("shape", [(4, 3, 256), (64, 64, 8192), (1500, 2050, 260)])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_product_specials_to_bf16(shape, fmt):
+    """NaN of several patterns and infinities in single results' operands, small, split and
+    in large tiles: they show in their rows and columns of a bf16 result, nowhere else. Scales
+    of 2^100 and 2^-100 meet in it as well."""
+    L = _lsgd()
+    print(f"product specials {shape} {fmt}", flush=True)
+    M, N, K = shape
+    if K == 8192:
+        assert L._gemm_blocks_workspace(1, 1, M, N, K) > 0
+    # powers of two: every sum is exact in fp32 (K < 2^24) but for the result's rounding
+    A, Bm = torch.ones(1, M, K, device=device()), torch.ones(1, N, K, device=device())
+    A[0, 1] = 2.0 ** 100
+    Bm[0, 1] = 2.0 ** -100
+    want = (A[0, :, :1].double() * Bm[0, :, 0].double() * K).to(torch.bfloat16)
+    for bits in (0x7FC00000, 0x7FFFFFFF, -1, 0x7F800001):
+        a, b = A.clone(), Bm.clone()
+        a.view(torch.int32)[0, 3, K // 2] = bits
+        b[0, 2, 5] = float("inf")
+        b[0, 0, K - 1] = float("-inf")
+        C = L.grouped_gemm_blocks(L.quantise_blocks(a, fmt), L.quantise_blocks(b, fmt),
+                                  out_dtype=torch.bfloat16)[0]
+        assert torch.isnan(C[3]).all()
+        rows = [m for m in range(M) if m != 3]
+        if fmt == "e4m3":
+            assert torch.isnan(C[:, [0, 2]]).all()
+        else:
+            assert (C[rows][:, 2] == float("inf")).all()
+            assert (C[rows][:, 0] == float("-inf")).all()
+        cols = [n for n in range(N) if n not in (0, 2)]
+        assert torch.equal(C[rows][:, cols], want[rows][:, cols])

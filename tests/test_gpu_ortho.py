@@ -407,3 +407,20 @@ def test_one_entry_holds_the_norm_of_the_largest_matrix(shape, dtype):
     assert abs(got - s) <= 5 * 2 * step, (got, s)
     Y[0, M - 3, 7] = 0
     assert bool((Y == 0).all())
+
+
+@pytest.mark.parametrize("shape", [(4, 20, 30), (4, 200, 150), (4, 400, 500)])
+@pytest.mark.parametrize("bits", [0x7FC0, 0x7FFF, -1, 0x7F81, 0x7F80])
+def test_specials_in_bf16(shape, bits):
+    """A NaN of any pattern or an infinity makes its own bf16 matrix NaN in every entry,
+    whichever kernels it takes, and leaves the other groups' bits alone; zeros stay."""
+    L = _lsgd()
+    print(f"specials bf16 {shape} {bits:x}", flush=True)
+    X = to_dev(_matrices(np.random.default_rng(6), *shape).astype(np.float32)).to(torch.bfloat16)
+    clean = L.orthogonalise(X)
+    X[1] = 0
+    X.view(torch.int16)[2, 3, 5] = bits
+    Y = L.orthogonalise(X)
+    assert torch.equal(Y[0], clean[0]) and torch.equal(Y[3], clean[3])
+    assert (Y[1] == 0).all()
+    assert torch.isnan(Y[2]).all()
