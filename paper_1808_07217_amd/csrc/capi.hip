@@ -1847,12 +1847,12 @@ lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b, int32_t
       (out_dtype != LSGD_FP32 && out_dtype != LSGD_BF16))
     return LSGD_E_INVALID;
   if (!block_sizes(G, M, N, Kd)) return LSGD_E_INVALID;
-  if (!d_A || !d_SA || !d_B || !d_SB || !d_C || ldc < N) return LSGD_E_INVALID;
+  const size_t esz = out_dtype == LSGD_BF16 ? 2 : 4;
+  if (!d_A || !d_SA || !d_B || !d_SB || !written_groups(G, M, N, d_C, ldc, sC, esz))
+    return LSGD_E_INVALID;
   if (sA < 0 || sB < 0 || sSA < 0 || sSB < 0 || sA % 16 || sB % 16 || sSA % 4 || sSB % 4)
     return LSGD_E_INVALID;
-  if (G > 1 && sC / M < ldc) return LSGD_E_INVALID;
-  if ((uintptr_t)d_A % 16 || (uintptr_t)d_B % 16 || (uintptr_t)d_SA % 4 || (uintptr_t)d_SB % 4 ||
-      (uintptr_t)d_C % (out_dtype == LSGD_BF16 ? 2 : 4))
+  if ((uintptr_t)d_A % 16 || (uintptr_t)d_B % 16 || (uintptr_t)d_SA % 4 || (uintptr_t)d_SB % 4)
     return LSGD_E_INVALID;
   const size_t need = lsgd::gemm_blocks_workspace_bytes(out_dtype == LSGD_BF16, G, M, N, Kd);
   if (need && ((uintptr_t)d_ws % 16 || !d_ws)) return LSGD_E_INVALID;

@@ -214,3 +214,18 @@ def test_binding_refuses_host_tensors_and_shapes():
                 L.Blocks(q, s, 5)):
         with pytest.raises(ValueError):
             L.grouped_gemm_blocks(bad, bad)
+
+
+def test_product_refuses_groups_that_overlap():
+    """Group strides that would let two groups of C share an element; nothing is
+    launched."""
+    f, lib = P(4096), _lib()
+    M, N, ld = 3, 4, 6
+
+    def call(G, ldc, sC):
+        return lib.lsgd_grouped_gemm_blocks(0, 0, 0, G, M, N, 5, f, 384, f, 12, f, 512, f, 16, f,
+                                            ldc, sC, f, 1 << 40, None)
+
+    for G, ldc, sC in ((2, ld, 2 * ld + N - 1), (2, ld, 3), (2, ld, 0), (2, ld, -ld * M),
+                       (2, 2 * N - 1, N), (3, 3 * N - 1, N), (2, ld, ld)):
+        assert call(G, ldc, sC) == 1, (G, ldc, sC)

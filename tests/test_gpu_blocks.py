@@ -402,3 +402,28 @@ def test_product_specials_to_bf16(shape, fmt):
             assert (C[rows][:, 0] == float("-inf")).all()
         cols = [n for n in range(N) if n not in (0, 2)]
         assert torch.equal(C[rows][:, cols], want[rows][:, cols])
+
+
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 40, 70, 200), (2, 64, 64, 8192)])
+def test_product_into_groups_that_end_early_or_lie_side_by_side(shape, out):
+    """Groups closer than M row pitches: the last row of a padded group ends where the next
+    group begins, and rows that hold every group's row. Nothing else is written."""
+    L = _lsgd()
+    print(f"product into close groups {shape} {out}", flush=True)
+    G, M, N, K = shape
+    dt = torch.bfloat16 if out == "bf16" else torch.float32
+    a, b = _operands(L, np.random.default_rng(9), *shape, "e4m3", "e4m3")
+    want = L.grouped_gemm_blocks(a, b, out_dtype=dt)
+    ld = N + 5
+    each = (M - 1) * ld + N
+    flat = torch.full((G * each + 9,), 7.0, device=device(), dtype=dt)
+    close = flat.as_strided((G, M, N), (each, ld, 1), 4)
+    assert torch.equal(L.grouped_gemm_blocks(a, b, out=close), want)
+    close.fill_(7.0)
+    assert (flat == 7.0).all()
+    room = torch.full((M, G, N + 3), 7.0, device=device(), dtype=dt)
+    side = room[:, :, :N].transpose(0, 1)
+    assert torch.equal(L.grouped_gemm_blocks(a, b, out=side), want)
+    side.fill_(7.0)
+    assert (room == 7.0).all()
