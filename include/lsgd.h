@@ -499,7 +499,7 @@ lsgd_status lsgd_quantise_blocks(int32_t dtype, int32_t format, int32_t G,
  * below 255. M, N <= 2^30, Kd <= 2^22. C is out_dtype LSGD_FP32 or LSGD_BF16 (rounded once), row pitch
  * ldc >= N, and its groups must not overlap: sC at least a group's extent (M - 1) ldc + N,
  * or rows of at least G groups side by side (any value for G == 1); nothing between
- * its rows is written. d_ws: workspace of
+ * its rows is written. C must not overlap A, B or their scales. d_ws: workspace of
  * lsgd_grouped_gemm_blocks_workspace_bytes (for the same sizes; which may be 0; then NULL is
  * allowed), 16-byte aligned, LSGD_E_WORKSPACE if smaller. A result does not
  * depend on what the workspace held.

@@ -594,6 +594,36 @@ def _matrices(name: str, X: torch.Tensor, dtypes) -> Tuple[int, int]:
     return (sM if M > 1 else N), (sG if G > 1 else 0)
 
 
+def _span(t: torch.Tensor) -> Tuple[int, int]:
+    """The first byte of a 3-D tensor of contiguous columns, and the one behind its last."""
+    G, M, N = t.shape
+    sG, sM, _ = t.stride()
+    at = t.data_ptr()
+    return at, at + ((G - 1) * sG + (M - 1) * sM + N) * t.element_size()
+
+
+def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether two such tensors share a byte: by their spans where those are apart, and else
+    (views into one buffer) by their rows."""
+    a0, a1 = _span(a)
+    b0, b1 = _span(b)
+    if a1 <= b0 or b1 <= a0:
+        return False
+
+    def rows(t):  # where the runs without a gap start, sorted, and their length
+        G, M, N = t.shape
+        sG, sM, _ = t.stride()
+        if sM == N:
+            M, N = 1, M * N
+        at = (torch.arange(G) * sG)[:, None] + torch.arange(M) * sM
+        return (at.flatten() * t.element_size() + t.data_ptr()).sort()[0], N * t.element_size()
+
+    (ra, na), (rb, nb) = rows(a), rows(b)
+    # of a's runs that start before a run of b ends, the last one ends last
+    before = torch.searchsorted(ra, rb + nb)
+    return bool(((before > 0) & (ra[(before - 1).clamp_min(0)] + na > rb)).any())
+
+
 def _same_device(*ts):
     if any(t.device != ts[0].device for t in ts[1:]):
         raise ValueError("all tensors must be on one device")
@@ -660,7 +690,8 @@ def grouped_gemm_blocks(A: Blocks, B: Blocks, out: Optional[torch.Tensor] = None
     dimension (lsgd_grouped_gemm_blocks), C float32 (products in bf16, exact, summed
     in fp32) or bfloat16 (the 8-bit matrix instruction, twice as fast). y = x w takes
     x and w's transpose, dy w^T takes dy and w, and x^T dy the transposes of x and
-    dy. A group stride of 0 (``expand``) shares a matrix among the groups."""
+    dy. A group stride of 0 (``expand``) shares a matrix among the groups. ``out``
+    (whose type counts then, not ``out_dtype``) must not overlap A or B."""
     fa, G, M, sA, sSA = _block_operand("A", A)
     fb, Gb, N, sB, sSB = _block_operand("B", B)
     n, dev = A.n, A.q.device
@@ -675,6 +706,8 @@ def grouped_gemm_blocks(A: Blocks, B: Blocks, out: Optional[torch.Tensor] = None
         ldc, sC = _matrices("out", out, _FLOATS)
         if out.shape != (G, M, N):
             raise ValueError("out must be [G][M][N]")
+        if any(_overlap(out, t) for t in (A.q, A.scale, B.q, B.scale)):
+            raise ValueError("out must not overlap A or B")
     if not (A.scale.device == dev and B.q.device == dev and B.scale.device == dev
             and out.device == dev):
         raise ValueError("all tensors must be on one device")
@@ -729,7 +762,7 @@ def orthogonalise(X: torch.Tensor, steps: int = 5, coefficients: Sequence[float]
                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The matrices X [G][M][N] (float32 or bfloat16) taken towards their
     orthogonal factors by Newton-Schulz steps (lsgd_orthogonalise); ``out`` may be
-    X itself."""
+    X itself, and else must not overlap it."""
     ldx, sX = _matrices("X", X, _FLOATS)
     G, M, N = X.shape
     out = torch.empty((G, M, N), dtype=X.dtype, device=X.device) if out is None else out
@@ -737,6 +770,8 @@ def orthogonalise(X: torch.Tensor, steps: int = 5, coefficients: Sequence[float]
     if out.shape != X.shape:
         raise ValueError("out must have X's shape")
     _same_device(X, out)
+    if (out.data_ptr(), ldy, sY) != (X.data_ptr(), ldx, sX) and _overlap(out, X):
+        raise ValueError("out must be X itself or not overlap it")
     co = _coefficients(coefficients)
     ws = _workspace_for(workspace, G, M, N, X.dtype, X.device)
     _enqueue(X.device, _lib.lsgd_orthogonalise, _precision(X.dtype), G, M, N, X.data_ptr(), ldx,
@@ -758,9 +793,9 @@ def orthogonal_update(W: torch.Tensor, U: torch.Tensor, G: torch.Tensor, lr: flo
                                        _matrices("G", G, _FP32))
     if U.shape != W.shape or G.shape != W.shape:
         raise ValueError("W, U, G must have one shape")
-    if len({W.data_ptr(), U.data_ptr(), G.data_ptr()}) < 3:
-        raise ValueError("W, U, G must not overlap")
     _same_device(W, U, G)
+    if _overlap(W, U) or _overlap(W, G) or _overlap(U, G):
+        raise ValueError("W, U, G must not overlap")
     K, M, N = W.shape
     co = _coefficients(coefficients)
     ws = _workspace_for(workspace, K, M, N, gemm_dtype, W.device)

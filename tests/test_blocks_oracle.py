@@ -229,3 +229,34 @@ def test_product_refuses_groups_that_overlap():
     for G, ldc, sC in ((2, ld, 2 * ld + N - 1), (2, ld, 3), (2, ld, 0), (2, ld, -ld * M),
                        (2, 2 * N - 1, N), (3, 3 * N - 1, N), (2, ld, ld)):
         assert call(G, ldc, sC) == 1, (G, ldc, sC)
+
+
+def test_binding_finds_overlaps_exactly():
+    """Random pairs of views into one buffer, of any pitches and strides, types and shared
+    groups, against the set of their bytes."""
+    from paper_1808_07217_amd import lsgd as L
+    rng = np.random.default_rng(1)
+    buf = torch.zeros(4096, dtype=torch.uint8)
+    seen = {False: 0, True: 0}
+
+    def view():
+        t = buf.view([torch.float32, torch.bfloat16, torch.float8_e4m3fn][rng.integers(3)])
+        G, M, N = (int(v) for v in rng.integers(1, 6, 3))
+        ld = N + int(rng.integers(0, 30)) * int(rng.integers(0, 2))
+        s = int(rng.choice([0, N, M * ld, M * ld + 40, (M - 1) * ld + N, 90]))
+        extent = (G - 1) * s + (M - 1) * ld + N
+        return t.as_strided((G, M, N), (s, ld, 1), int(rng.integers(0, t.numel() - extent + 1)))
+
+    def bytes_of(t):
+        e = t.element_size()
+        return {t.data_ptr() + e * (g * t.stride(0) + m * t.stride(1) + n) + k
+                for g in range(t.shape[0]) for m in range(t.shape[1]) for n in range(t.shape[2])
+                for k in range(e)}
+
+    for _ in range(3000):
+        a, b = view(), view()
+        want = bool(bytes_of(a) & bytes_of(b))
+        assert L._overlap(a, b) == want == L._overlap(b, a)
+        seen[want] += L._span(a)[0] < L._span(b)[1] and L._span(b)[0] < L._span(a)[1]
+    # of both kinds among pairs whose spans are not apart
+    assert min(seen.values()) > 100, seen

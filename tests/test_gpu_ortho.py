@@ -424,3 +424,31 @@ def test_specials_in_bf16(shape, bits):
     assert torch.equal(Y[0], clean[0]) and torch.equal(Y[3], clean[3])
     assert (Y[1] == 0).all()
     assert torch.isnan(Y[2]).all()
+
+
+def test_overlapping_tensors_are_refused():
+    """Views that share some elements, and an ``out`` that is neither X itself nor apart from
+    it: refused before anything is written. Rows that lie between each other's are not."""
+    L = _lsgd()
+    print("overlaps", flush=True)
+    buf = torch.ones(2, 200, device=device())
+    view = lambda at: buf[:, at:at + 60].view(2, 6, 10)  # noqa: E731
+    for at in ((0, 59, 130), (0, 70, 129), (70, 129, 0), (5, 70, 0)):
+        with pytest.raises(ValueError, match="overlap"):
+            L.orthogonal_update(*(view(v) for v in at), 0.1, 0.9)
+    for bad in (view(59), buf[:1, :60].view(1, 6, 10).expand(2, 6, 10),
+                buf.as_strided((2, 6, 10), (100, 11, 1))):
+        with pytest.raises(ValueError, match="overlap"):
+            L.orthogonalise(view(0), out=bad)
+    blocks = L.quantise_blocks(view(0))
+    room = torch.zeros(2, 6, 128, device=device(), dtype=torch.uint8)
+    inside = L.Blocks(room.view(torch.float8_e4m3fn), blocks.scale, 10)
+    with pytest.raises(ValueError, match="overlap"):
+        L.grouped_gemm_blocks(inside, blocks, out=room.view(torch.float32)[:, :, :6])
+    assert (buf == 1).all() and (room == 0).all()
+    G = to_dev(_matrices(np.random.default_rng(3), 2, 6, 10).astype(np.float32))
+    W, U = view(0), view(60)
+    want = [W.clone(), U.clone()]
+    L.orthogonal_update(*want, G, 0.1, 0.9)
+    L.orthogonal_update(W, U, G, 0.1, 0.9)
+    assert torch.equal(W, want[0]) and torch.equal(U, want[1])
