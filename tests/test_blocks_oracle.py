@@ -257,6 +257,9 @@ def test_binding_finds_overlaps_exactly():
         a, b = view(), view()
         want = bool(bytes_of(a) & bytes_of(b))
         assert L._overlap(a, b) == want == L._overlap(b, a)
-        seen[want] += L._span(a)[0] < L._span(b)[1] and L._span(b)[0] < L._span(a)[1]
+        size = lambda t: max(bytes_of(t)) + 1 - t.data_ptr()  # noqa: E731
+        apart = L._apart(a.data_ptr(), size(a), b.data_ptr(), size(b))
+        assert not (apart and want)
+        seen[want] += not apart
     # of both kinds among pairs whose spans are not apart
     assert min(seen.values()) > 100, seen
