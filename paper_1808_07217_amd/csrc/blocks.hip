@@ -260,7 +260,7 @@ hipError_t quantise(const QuantArgs& a, hipStream_t s) {
 // 2^-15 of it on normal data, well below bf16's own 2^-9. That is too coarse for a
 // result in fp32, which instead widens the values, scale and all, to bf16 (exact: 4
 // bits of a value, and 2^e is in bf16's range; only a value below 2^-126 becomes a
-// multiple of bf16's 2^-133) as they reach the registers and takes
+// multiple of bf16's 2^-133, and 2^128, to which only fp32's last values round, an infinity) as they reach the registers and takes
 // v_mfma_f32_16x16x32_bf16, half as fast: exact products, fp32 sums.
 // Lane l holds 32 of a block's 128 k for row l % 16; which 32 is free, the scale being
 // one for all: two vectors of 16 bytes, 64 apart. The first operand is B's rows, so that a

@@ -427,3 +427,25 @@ def test_product_into_groups_that_end_early_or_lie_side_by_side(shape, out):
     assert torch.equal(L.grouped_gemm_blocks(a, b, out=side), want)
     side.fill_(7.0)
     assert (room == 7.0).all()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_product_of_values_that_round_to_two_to_the_128(fmt):
+    """The top of fp32's range rounds to 2^128 in 8 bits. The 8-bit instruction takes it as it
+    is; a result in fp32 takes values through bf16, which has no such number: an infinity, as
+    the value itself is in fp32. What rounds below it stays exact in both."""
+    L = _lsgd()
+    print(f"product at 2^128 {fmt}", flush=True)
+    first = {"e4m3": 1.9375, "e5m2": 1.875}[fmt]  # half way between the value below and 2^128
+    A = np.zeros((1, 3, 128), np.float32)
+    A[0, 0, 0] = first * 2.0 ** 127
+    A[0, 1, 0] = np.nextafter(A[0, 0, 0], np.float32(0))
+    A[0, 2, 0] = -np.finfo(np.float32).max
+    Bm = np.full((1, 2, 128), 2.0 ** -20, np.float32)
+    a, b = L.quantise_blocks(to_dev(A), fmt), L.quantise_blocks(to_dev(Bm))
+    below = {"e4m3": 1.875, "e5m2": 1.75}[fmt] * 2.0 ** 107
+    C = _np(L.grouped_gemm_blocks(a, b, out_dtype=torch.bfloat16))
+    np.testing.assert_array_equal(C[0, :, 0], [2.0 ** 108, below, -(2.0 ** 108)])
+    for x, y, pick in ((a, b, lambda C: C[0, :, 1]), (b, a, lambda C: C[0, 1])):
+        np.testing.assert_array_equal(pick(_np(L.grouped_gemm_blocks(x, y))),
+                                      [np.inf, below, -np.inf])
