@@ -509,6 +509,10 @@ lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t out_dtype,
                                                      int32_t G, int32_t M,
                                                      int32_t N, int32_t Kd,
                                                      size_t* bytes);
+/* How that product is cut, for tests and profiles: cut[0] the tile's rows and columns,
+ * cut[1] the stages of loads, cut[2] the ranges of the inner dimension. */
+lsgd_status lsgd_grouped_gemm_blocks_cut(int32_t out_dtype, int32_t G, int32_t M, int32_t N,
+                                         int32_t Kd, int32_t cut[3]);
 lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b,
                                      int32_t out_dtype, int32_t G, int32_t M,
                                      int32_t N, int32_t Kd, const uint8_t* d_A,

@@ -544,7 +544,8 @@ int splits_of(bool bf16, int G, int M, int N, int Kd) {
 struct BlockCut {
   int tile, stages;
 };
-BlockCut block_cut(bool bf16, int G, int M, int N) {
+BlockCut block_cut(bool bf16, int G, int M, int N, int splits) {
+  if (splits > 1) return BlockCut{64, 4};
   const BlockCut cuts[4] = {{64, 4}, {128, 4}, {128, 2}, {256, 2}};
   const int per_cu[4] = {2, 1, 2, 1};
   const double each[2][4] = {{1.6, 5.3, 4.5, 0.0}, {1.6, 4.5, 3.8, 12.6}};
@@ -577,7 +578,7 @@ hipError_t gemm_blocks(BlockGemmArgs a, hipStream_t s) {
   a.splits = splits_of(OUTBF, a.G, a.M, a.N, a.Kd);
   const int nb = (a.Kd + 127) / 128;
   a.chunk = (nb + 4 * a.splits - 1) / (4 * a.splits) * 4;
-  const BlockCut c = a.splits > 1 ? BlockCut{64, 4} : block_cut(OUTBF, a.G, a.M, a.N);
+  const BlockCut c = block_cut(OUTBF, a.G, a.M, a.N, a.splits);
   hipError_t e;
   if (c.tile == 64)
     e = launch_tile<FA, FB, OUTBF, 64, 32, 4>(a, s);
@@ -610,6 +611,13 @@ hipError_t launch_quantise(int bf16, int fmt, const QuantArgs& a, hipStream_t s)
 size_t gemm_blocks_workspace_bytes(int bf16, int G, int M, int N, int Kd) {
   const int s = splits_of(bf16, G, M, N, Kd);
   return s == 1 ? 0 : (size_t)s * G * M * N * sizeof(float);
+}
+
+void gemm_blocks_cut(int bf16, int G, int M, int N, int Kd, int cut[3]) {
+  cut[2] = splits_of(bf16, G, M, N, Kd);
+  const BlockCut c = block_cut(bf16, G, M, N, cut[2]);
+  cut[0] = c.tile;
+  cut[1] = c.stages;
 }
 
 hipError_t launch_gemm_blocks(int fmt_a, int fmt_b, const BlockGemmArgs& a, hipStream_t s) {

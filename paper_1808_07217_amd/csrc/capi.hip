@@ -1836,6 +1836,14 @@ lsgd_status lsgd_grouped_gemm_blocks_workspace_bytes(int32_t out_dtype, int32_t 
   return LSGD_OK;
 }
 
+lsgd_status lsgd_grouped_gemm_blocks_cut(int32_t out_dtype, int32_t G, int32_t M, int32_t N,
+                                         int32_t Kd, int32_t cut[3]) {
+  if (out_dtype != LSGD_FP32 && out_dtype != LSGD_BF16) return LSGD_E_INVALID;
+  if (!cut || !block_sizes(G, M, N, Kd)) return LSGD_E_INVALID;
+  lsgd::gemm_blocks_cut(out_dtype == LSGD_BF16, G, M, N, Kd, cut);
+  return LSGD_OK;
+}
+
 lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b, int32_t out_dtype,
                                      int32_t G, int32_t M, int32_t N, int32_t Kd,
                                      const uint8_t* d_A, int64_t sA, const uint8_t* d_SA,

@@ -158,6 +158,7 @@ struct BlockGemmArgs {
   int splits, chunk;
 };
 size_t gemm_blocks_workspace_bytes(int bf16, int G, int M, int N, int Kd);
+void gemm_blocks_cut(int bf16, int G, int M, int N, int Kd, int cut[3]);  // tile, stages, ranges
 hipError_t launch_gemm_blocks(int fmt_a, int fmt_b, const BlockGemmArgs& a, hipStream_t s);
 
 // ------------------------------------------------- orthogonalised momentum

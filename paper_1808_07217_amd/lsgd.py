@@ -102,6 +102,7 @@ _SIGS = {
                         _c.c_float, _c.c_int32, _P],
     "lsgd_quantise_blocks": [_I, _I, _I, _I, _I, _P, _L, _L, _P, _P, _P, _P, _P],
     "lsgd_grouped_gemm_blocks_workspace_bytes": [_I, _I, _I, _I, _I, _c.POINTER(_c.c_size_t)],
+    "lsgd_grouped_gemm_blocks_cut": [_I, _I, _I, _I, _I, _P],
     "lsgd_grouped_gemm_blocks": [_I, _I, _I, _I, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _L,
                                  _P, _L, _L, _P, _c.c_size_t, _P],
     "lsgd_orthogonalise_workspace_bytes": [_I, _I, _I, _I, _c.POINTER(_c.c_size_t)],

@@ -263,3 +263,13 @@ def test_binding_finds_overlaps_exactly():
         seen[want] += not apart
     # of both kinds among pairs whose spans are not apart
     assert min(seen.values()) > 100, seen
+
+
+def test_product_cut_refusals():
+    cut, lib = (ctypes.c_int32 * 3)(), _lib()
+    f = lib.lsgd_grouped_gemm_blocks_cut
+    assert f(0, 1, 2, 3, 4, None) == 1
+    for bad in ((2, 1, 2, 3, 4), (0, 0, 2, 3, 4), (0, 1, 0, 3, 4), (0, 1, 2, 2**31 - 1, 4),
+                (1, 1, 2, 3, 2**22 + 1)):
+        assert f(*bad, cut) == 1, bad
+    assert f(1, 1, 2, 3, 4, cut) == 0 and list(cut) == [64, 4, 1]

@@ -1,5 +1,7 @@
 """GPU tests of tensors in 8-bit blocks and their grouped product against the
 float64 oracle."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -159,8 +161,7 @@ def test_product_split_over_the_inner_dimension(shape):
         assert torch.equal(C, L.grouped_gemm_blocks(a, b, out_dtype=dt))
 
 
-# the sizes at which every cut of a product is taken: 64, 128 (two and four stages) and
-# 256, their last tiles ragged
+# tiles of 64 and of 128 (two and four stages), the last ones ragged; every cut: CUTS below
 @pytest.mark.parametrize("out", ["fp32", "bf16"])
 @pytest.mark.parametrize("shape", [(1, 2000, 2040, 500), (1, 4100, 3900, 260), (3, 1537, 771, 384),
                                    (1, 260, 8200, 1100)])
@@ -449,3 +450,60 @@ def test_product_of_values_that_round_to_two_to_the_128(fmt):
     for x, y, pick in ((a, b, lambda C: C[0, :, 1]), (b, a, lambda C: C[0, 1])):
         np.testing.assert_array_equal(pick(_np(L.grouped_gemm_blocks(x, y))),
                                       [np.inf, below, -np.inf])
+
+
+# (G, M, N): the cut that a product of theirs takes: the tile's side, and its stages of loads
+CUTS = {(3, 150, 331): (64, 4), (1, 1501, 1487): (128, 4), (1, 2503, 2291): (128, 2),
+        (10, 378, 2492): (256, 2)}
+
+
+@pytest.mark.parametrize("fa", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("fb", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", CUTS)
+def test_product_cuts(shape, out, fa, fb):
+    """Every tile with every pair of formats, over one step to nine (each remainder of the
+    unrolled loop, scale bytes of either parity, a last block that is not whole), into a
+    view of padded rows; every element against float64 (there products of 8-bit values and
+    powers of two are exact, and sums of 1037 of them to 2^-42 of their size)."""
+    L = _lsgd()
+    G, M, N = shape
+    dt = torch.bfloat16 if out == "bf16" else torch.float32
+    cut = (ctypes.c_int32 * 3)()
+    gen = torch.Generator(device=device()).manual_seed(M)
+    rand = lambda *s: torch.randn(*s, generator=gen, device=device())  # noqa: E731
+    # the 256-wide tiles are for bf16 results alone
+    tile = CUTS[shape] if (shape, out) != ((10, 378, 2492), "fp32") else (128, 4)
+
+    def val(t):
+        q = t.q.to(torch.float64).view(*t.q.shape[:2], -1, 128)
+        return (q * t.scale.to(torch.float64)[:, :, :q.shape[2], None]).flatten(2)
+
+    for K in (100, 250, 384, 500, 600, 1037):
+        print(f"product cut {shape} {K} {out} {fa} {fb}", flush=True)
+        assert L._lib.lsgd_grouped_gemm_blocks_cut(int(out == "bf16"), G, M, N, K, cut) == 0
+        assert tuple(cut) == (*tile, 1)
+        a = L.quantise_blocks(rand(G, M, K) * torch.exp(rand(1, M, 1)), fa)
+        b = L.quantise_blocks(rand(G, N, K) * torch.exp(rand(1, 1, K)), fb)
+        room = torch.full((G, M + 1, N + 3), 7.0, device=device(), dtype=dt)
+        C = L.grouped_gemm_blocks(a, b, out=room[:, 1:, 2:N + 2])
+        va, vb = val(a), val(b).transpose(1, 2).contiguous()
+        ref, size = va @ vb, va.abs() @ vb.abs()
+        # as in _check_product
+        bound = gamma(K + 1) * size + 1e-38
+        if out == "bf16":
+            bound += 2.0 ** -10 * size
+            bound += 2.0 ** -8 * (ref.abs() + bound)
+        assert bool(((C.double() - ref).abs() <= bound).all()), K
+        C.fill_(7.0)
+        assert bool((room == 7.0).all())
+
+
+@pytest.mark.parametrize("fa", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("fb", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("shape", [(2, 70, 90, 300), (1, 3, 200, 2000), (1, 64, 64, 8192)])
+def test_product_formats_to_bf16(shape, fa, fb):
+    L = _lsgd()
+    print(f"product to bf16 {shape} {fa} {fb}", flush=True)
+    a, b = _operands(L, np.random.default_rng(3), *shape, fa, fb)
+    _check_product(L.grouped_gemm_blocks(a, b, out_dtype=torch.bfloat16), a, b)
