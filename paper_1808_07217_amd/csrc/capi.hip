@@ -1895,6 +1895,14 @@ lsgd_status lsgd_orthogonalise_workspace_bytes(int32_t dtype, int32_t G, int32_t
   return LSGD_OK;
 }
 
+lsgd_status lsgd_orthogonalise_cut(int32_t dtype, int32_t G, int32_t M, int32_t N,
+                                   int32_t cut[5]) {
+  if (!cut || (dtype != LSGD_FP32 && dtype != LSGD_BF16) || !ortho_sizes(G, M, N))
+    return LSGD_E_INVALID;
+  lsgd::ortho_cut(dtype == LSGD_BF16, G, M, N, cut);
+  return LSGD_OK;
+}
+
 lsgd_status lsgd_orthogonalise(int32_t dtype, int32_t G, int32_t M, int32_t N, const void* d_X,
                                int64_t ldx, int64_t sX, void* d_Y, int64_t ldy, int64_t sY,
                                int32_t steps, const float* h_coefficients, float eps, void* d_ws,

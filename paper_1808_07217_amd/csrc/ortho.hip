@@ -27,6 +27,7 @@
 // has a tail; a zero row or column stays zero through the steps. In fp32 precision the two
 // pieces of 32 neighbours share a line of 128 bytes, first pieces, then second ones; in
 // the bf16 form each piece is a matrix of its own, and only the first is multiplied.
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <type_traits>
@@ -983,7 +984,10 @@ void apply(Cut c, const OrthoArgs& a, int step, hipStream_t s) {
   if (c.tile == 192) return launch_apply<P, LAST, 192, 2>(a, step, s);
   if (c.tile == 128 && c.stages == 2) return launch_apply<P, LAST, 128, 2>(a, step, s);
   if (c.tile == 128) return launch_apply<P, LAST, 128, 4>(a, step, s);
-  if (c.stages == 3) return launch_apply<P, LAST, 64, 3>(a, step, s);
+  // (of matrices of kOnePieceFrom rows and more, whose 64 x 64 tiles are three times as many as
+  // their 128 x 128 ones, no count makes three stages of the small ones the cheapest)
+  if constexpr (P == 2)
+    if (c.stages == 3) return launch_apply<P, LAST, 64, 3>(a, step, s);
   return launch_apply<P, LAST, 64, 4>(a, step, s);
 }
 
@@ -1032,6 +1036,18 @@ OrthoPlan ortho_plan(bool bf16, int G, int M, int N) {
   return p;
 }
 
+Cut gram_cut(const OrthoPlan& p, int G) {
+  return best_cut([&](int T) {
+    const long long r = (p.mp + T - 1) / T;
+    return r * (r + 1) / 2 * G;
+  });
+}
+Cut apply_cut(const OrthoPlan& p, int G) {
+  return best_cut([&](int T) {
+    return (long long)((p.mp + T - 1) / T) * ((p.np + T - 1) / T) * G;
+  });
+}
+
 template <int P>
 hipError_t ortho(const OrthoArgs& a, const OrthoPlan& p, hipStream_t s) {
   // (64 x 64 tiles are the most there are of anything)
@@ -1041,11 +1057,7 @@ hipError_t ortho(const OrthoArgs& a, const OrthoPlan& p, hipStream_t s) {
                      p.chunks);
   hipLaunchKernelGGL(k_ortho_split<P>, grid_of(tiles * a.G), dim3(kThreads), 0, s, a, p.chunks,
                      p.mp / 64, p.np / 64);
-  auto across = [](long long r, int T) { return (r + T - 1) / T; };
-  const Cut cg = best_cut([&](int T) {
-    return across(p.mp, T) * (across(p.mp, T) + 1) / 2 * a.G;
-  });
-  const Cut ca = best_cut([&](int T) { return across(p.mp, T) * across(p.np, T) * a.G; });
+  const Cut cg = gram_cut(p, a.G), ca = apply_cut(p, a.G);
   for (int t = 0; t < a.steps; ++t) {
     gram<P, false>(cg, a, t, s);
     gram<P, true>(cg, a, t, s);
@@ -1062,6 +1074,13 @@ hipError_t ortho(const OrthoArgs& a, const OrthoPlan& p, hipStream_t s) {
 
 size_t ortho_workspace_bytes(int bf16, int G, int M, int N) {
   return ortho_plan(bf16, G, M, N).total;
+}
+
+void ortho_cut(int bf16, int G, int M, int N, int cut[5]) {
+  const OrthoPlan p = ortho_plan(bf16, G, M, N);
+  const Cut g = p.small ? Cut{0, 0} : gram_cut(p, G), a = p.small ? Cut{0, 0} : apply_cut(p, G);
+  const int v[5] = {p.small ? 0 : p.pieces, g.tile, g.stages, a.tile, a.stages};
+  std::copy(v, v + 5, cut);
 }
 
 hipError_t launch_ortho(int bf16, OrthoArgs a, void* ws, hipStream_t s) {

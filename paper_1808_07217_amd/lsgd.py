@@ -106,6 +106,7 @@ _SIGS = {
     "lsgd_grouped_gemm_blocks": [_I, _I, _I, _I, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _L,
                                  _P, _L, _L, _P, _c.c_size_t, _P],
     "lsgd_orthogonalise_workspace_bytes": [_I, _I, _I, _I, _c.POINTER(_c.c_size_t)],
+    "lsgd_orthogonalise_cut": [_I, _I, _I, _I, _P],
     "lsgd_orthogonalise": [_I, _I, _I, _I, _P, _L, _L, _P, _L, _L, _I, _c.POINTER(_c.c_float),
                            _c.c_float, _P, _c.c_size_t, _P],
     "lsgd_orthogonal_update": [_I, _I, _I, _I, _P, _L, _L, _P, _L, _L, _P, _L, _L, _c.c_float,

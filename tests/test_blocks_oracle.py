@@ -273,3 +273,29 @@ def test_product_cut_refusals():
                 (1, 1, 2, 3, 2**22 + 1)):
         assert f(*bad, cut) == 1, bad
     assert f(1, 1, 2, 3, 4, cut) == 0 and list(cut) == [64, 4, 1]
+
+
+def test_every_cut_of_the_orthogonalisation_is_tested():
+    """The shapes of the GPU tests, which run each in both precisions, against all the cuts that
+    matrices of up to 32 x 32 tiles of 64, in any number up to 800, take."""
+    import test_gpu_ortho as T
+    cut, f = (ctypes.c_int32 * 5)(), _lib().lsgd_orthogonalise_cut
+
+    def cuts(shapes):
+        seen = set()
+        for G, M, N in shapes:
+            for dtype in (0, 1):
+                assert f(dtype, G, M, N, cut) == 0
+                if cut[0]:
+                    seen |= {("A", cut[0], cut[1], cut[2]), ("X", cut[0], cut[3], cut[4])}
+        return seen
+
+    tested = cuts(T.SHAPES + T.LARGE + T.CUTS)
+    tiles = (1, 2, 3, 4, 5, 6, 7, 8, 9, 11, 14, 18, 24, 32)
+    assert tested == cuts((G, 64 * m, 64 * n + 600 * (n == 1)) for m in tiles for n in tiles
+                          for G in (*range(1, 60), *range(60, 800, 7)))
+    assert len(tested) == 23
+
+    assert f(2, 1, 64, 64, cut) == 1 and f(0, 0, 64, 64, cut) == 1 and f(0, 1, 64, 0, cut) == 1
+    assert f(0, 1, 64, 64, None) == 1
+    assert f(0, 1, 64, 64, cut) == 0 and list(cut) == [0] * 5

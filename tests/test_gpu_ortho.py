@@ -300,8 +300,8 @@ def _steps_on_device(X, pieces, eps=1e-7, coefficients=(3.4445, -4.7750, 2.0315)
     return out
 
 
-# Between them they take every cut that the products have, at ragged edges and with the
-# result's rows along either side: few or many matrices of hundreds of rows, of thousands.
+# Ragged edges and the result's rows along either side: few or many matrices of hundreds of
+# rows, of thousands. (SHAPES, these and CUTS take every cut that the products have.)
 LARGE = [(100, 190, 200), (16, 500, 510), (2, 2040, 2030), (1, 4090, 1500), (1, 8190, 2040),
          (1, 4000, 4090), (1, 4300, 4400), (4, 1500, 1490), (1, 1900, 4500)]
 
@@ -452,3 +452,13 @@ def test_overlapping_tensors_are_refused():
     L.orthogonal_update(*want, G, 0.1, 0.9)
     L.orthogonal_update(W, U, G, 0.1, 0.9)
     assert torch.equal(W, want[0]) and torch.equal(U, want[1])
+
+
+# Few wide or many small matrices, whose products take 64 x 64 tiles of three or four stages
+CUTS = [(15, 18, 2318), (15, 2318, 18), (26, 400, 448), (26, 448, 400), (1, 450, 500)]
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", CUTS)
+def test_small_tiles_match_float64(shape, precision):
+    test_large_matrices_match_float64(shape, precision)
