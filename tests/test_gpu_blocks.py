@@ -507,3 +507,81 @@ def test_product_formats_to_bf16(shape, fa, fb):
     print(f"product to bf16 {shape} {fa} {fb}", flush=True)
     a, b = _operands(L, np.random.default_rng(3), *shape, fa, fb)
     _check_product(L.grouped_gemm_blocks(a, b, out_dtype=torch.bfloat16), a, b)
+
+
+@pytest.mark.parametrize("shape", [(1, 64, 64, 8192), (2, 3, 130, 20001), (1, 70, 33, 4100)])
+@pytest.mark.parametrize("out", ["fp32", "bf16"])
+def test_product_whatever_the_workspace_holds(shape, out):
+    """The caller's own workspace, of exactly the size asked for and full of NaN, zeros or what
+    the last call left: the same bits, and nothing behind its end written."""
+    L = _lsgd()
+    print(f"product workspace {shape} {out}", flush=True)
+    G, M, N, K = shape
+    dt, code = (torch.bfloat16, 1) if out == "bf16" else (torch.float32, 0)
+    a, b = _operands(L, np.random.default_rng(5), *shape, "e4m3", "e5m2")
+    want = L.grouped_gemm_blocks(a, b, out_dtype=dt)
+    nb = L._gemm_blocks_workspace(code, G, M, N, K)
+    assert nb > 0 and nb % 4 == 0
+    ws = torch.full((nb + 64,), 255, device=device(), dtype=torch.uint8)
+    assert torch.isnan(ws.view(torch.float32)).all()
+    for fill in (None, 0, 255):
+        if fill is not None:
+            ws.fill_(fill)
+        ws[nb:] = 77
+        C = torch.full((G, M, N), 7.0, device=device(), dtype=dt)
+        assert L._lib.lsgd_grouped_gemm_blocks(
+            0, 1, code, G, M, N, K, a.q.data_ptr(), a.q.stride(0), a.scale.data_ptr(),
+            a.scale.stride(0), b.q.data_ptr(), b.q.stride(0), b.scale.data_ptr(),
+            b.scale.stride(0), C.data_ptr(), N, M * N, ws.data_ptr(), nb,
+            torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(C, want)
+        assert (ws[nb:] == 77).all()
+        if K == 8192:  # (the last sums are still there: the workspace is used)
+            assert not (ws[:nb] == 255).all()
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 1), (2, 130, 257), (3, 127, 641)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_transpose_alone(shape, dtype):
+    """The C entry point without the rows' pair: the transposes' bytes as with it, every one
+    of them written."""
+    L = _lsgd()
+    print(f"transpose alone {shape} {dtype}", flush=True)
+    G, M, N = shape
+    X = to_dev(np.random.default_rng(2).standard_normal(shape).astype(np.float32))
+    X = X.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    for code, fmt in ((0, "e4m3"), (1, "e5m2")):
+        _, t = L.quantise_blocks(X, fmt, both=True)
+        q, s = torch.full_like(t.q.view(torch.uint8), 99), torch.full_like(
+            t.scale.view(torch.uint8), 99)
+        assert L._lib.lsgd_quantise_blocks(
+            int(dtype == "bf16"), code, G, M, N, X.data_ptr(), N, M * N, None, None, q.data_ptr(),
+            s.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+        assert torch.equal(q, t.q.view(torch.uint8)) and torch.equal(s, t.scale.view(torch.uint8))
+
+
+def test_weight_gradient_against_difference_quotients():
+    """dw = x^T dy of the kernels, at many entries, against the quotient of sum(y dy) in w: y is
+    linear in w, so a step of 1 leaves the quotient exact but for float64's rounding of the sums
+    (1e-12 of the sum of absolute values). x and dy are what 8 bits hold, so the operands are
+    exact and dw is off by its fp32 sums alone."""
+    L = _lsgd()
+    print("weight gradient quotients", flush=True)
+    rng = np.random.default_rng(12)
+    T, I, O = 150, 40, 70
+    # three bits of a value and two binades: exact in e4m3 and, of two bits, in e5m2
+    x = to_dev((rng.integers(-7, 8, (1, T, I)) * 2.0 ** rng.integers(-1, 1, (1, T, I)))
+               .astype(np.float32))
+    dy = to_dev((rng.integers(-3, 4, (1, T, O)) * 2.0 ** rng.integers(-2, 1, (1, T, O)))
+                .astype(np.float32))
+    w = to_dev(rng.standard_normal((1, I, O)).astype(np.float32))
+    (_, xt), (_, dt) = L.quantise_blocks(x, both=True), L.quantise_blocks(dy, "e5m2", both=True)
+    dw = _np(L.grouped_gemm_blocks(xt, dt))[0]
+    vx, vd, vw = _np(x)[0], _np(dy)[0], _np(w)[0]
+    for i, o in zip(rng.integers(0, I, 60), rng.integers(0, O, 60)):
+        w2 = vw.copy()
+        w2[i, o] += 1.0
+        quotient = ((vx @ w2) * vd).sum() - ((vx @ vw) * vd).sum()
+        size = np.abs((np.abs(vx) @ np.abs(w2)) * np.abs(vd)).sum()
+        bound = gamma(T + 1) * (np.abs(vx[:, i]) * np.abs(vd[:, o])).sum() + 1e-12 * size
+        assert abs(dw[i, o] - quotient) <= bound, (i, o)

@@ -462,3 +462,22 @@ CUTS = [(15, 18, 2318), (15, 2318, 18), (26, 400, 448), (26, 448, 400), (1, 450,
 @pytest.mark.parametrize("shape", CUTS)
 def test_small_tiles_match_float64(shape, precision):
     test_large_matrices_match_float64(shape, precision)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 141, 300), (2, 450, 390)])
+def test_whatever_the_workspace_holds(shape, dtype):
+    """Full of NaN, of zeros, or of what a call on another matrix left: the same bits."""
+    L = _lsgd()
+    print(f"workspace {shape} {dtype}", flush=True)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rng = np.random.default_rng(9)
+    X, other = (to_dev(_matrices(rng, *shape).astype(np.float32)).to(dt) for _ in range(2))
+    want = L.orthogonalise(X)
+    ws = L.orthogonalise_workspace(*shape, dtype=dt)
+    assert ws.numel() > 0
+    for before in (lambda: ws.fill_(255), lambda: ws.zero_(),
+                   lambda: L.orthogonalise(other, workspace=ws),
+                   lambda: L.orthogonalise(other * float("nan"), workspace=ws)):
+        before()
+        assert torch.equal(L.orthogonalise(X, workspace=ws), want)
