@@ -549,10 +549,10 @@ lsgd_status lsgd_orthogonalise_workspace_bytes(int32_t dtype, int32_t G,
 
 /* How the steps of such matrices are cut, for tests and profiles: cut[0] the pieces of an
  * operand, 0 where one launch does all steps (the rest is 0 then); cut[1], cut[2] the tile's
- * rows and columns and the stages of loads of the products A and A A, cut[3], cut[4] those
- * of B X. */
+ * rows and columns and the stages of loads of X X^T, cut[3], cut[4] those of A A, cut[5],
+ * cut[6] those of B X. */
 lsgd_status lsgd_orthogonalise_cut(int32_t dtype, int32_t G, int32_t M, int32_t N,
-                                   int32_t cut[5]);
+                                   int32_t cut[7]);
 
 /* Y_g = O(X_g) for G matrices, X and Y of `dtype` (pitches and strides in
  * elements). Y may be X itself (same pitch and stride); else

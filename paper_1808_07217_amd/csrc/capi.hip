@@ -1896,7 +1896,7 @@ lsgd_status lsgd_orthogonalise_workspace_bytes(int32_t dtype, int32_t G, int32_t
 }
 
 lsgd_status lsgd_orthogonalise_cut(int32_t dtype, int32_t G, int32_t M, int32_t N,
-                                   int32_t cut[5]) {
+                                   int32_t cut[7]) {
   if (!cut || (dtype != LSGD_FP32 && dtype != LSGD_BF16) || !ortho_sizes(G, M, N))
     return LSGD_E_INVALID;
   lsgd::ortho_cut(dtype == LSGD_BF16, G, M, N, cut);

@@ -190,8 +190,8 @@ struct OrthoArgs {
 };
 // `bf16`: the products' precision. Workspace 256-byte aligned.
 size_t ortho_workspace_bytes(int bf16, int G, int M, int N);
-// pieces an operand (0: all steps in one launch), tile and stages of A and B, of B X
-void ortho_cut(int bf16, int G, int M, int N, int cut[5]);
+// pieces an operand (0: all steps in one launch), tile and stages of X X^T, A A and B X
+void ortho_cut(int bf16, int G, int M, int N, int cut[7]);
 hipError_t launch_ortho(int bf16, OrthoArgs a, void* ws, hipStream_t s);
 
 // ---------------------------------------------------------------- head

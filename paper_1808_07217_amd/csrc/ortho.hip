@@ -457,7 +457,7 @@ __global__ __launch_bounds__((Shape<BT, S>::kThreads), 2) void k_ortho_gram(Orth
   const int ld = K * P * 2;
   t.init((const uint8_t*)src + (long long)p0 * ld, (const uint8_t*)src + (long long)q0 * ld, ld,
          a.mp - p0, a.mp - q0);
-  // (256 x 256 tiles have no room for two; theirs are products of thousands both ways)
+  // (256 x 256 tiles have no room for two: see x_cut)
   using Mac = MacHalf<P, P == 2 && !SECOND && BT <= 192>;
   Mac mac;
   typename Mac::Acc acc[T::FP][T::FQ] = {};
@@ -938,15 +938,15 @@ struct Cut {
 // takes 125 us in 64 x 64 tiles of four stages, 136 of three, 213 / 282 in 128 x 128
 // tiles of four / two, 609 in 256 x 256 ones.
 constexpr int kCus = 256;
+constexpr int kCuts = 6;
 template <class F>
-Cut best_cut(F tiles) {
-  constexpr int kCuts = 6;
+Cut best_cut(F tiles, int n = kCuts) {
   const Cut cuts[kCuts] = {{64, 4}, {64, 3}, {128, 4}, {128, 2}, {192, 2}, {256, 2}};
   const int per_cu[kCuts] = {2, 3, 1, 2, 1, 1};
   const double each[kCuts] = {1.6, 1.55, 4.3, 3.8, 8.4, 12.6};
   int at = 0;
   double least = 0;
-  for (int i = 0; i < kCuts; ++i) {
+  for (int i = 0; i < n; ++i) {
     const double rounds = std::ceil((double)tiles(cuts[i].tile) / (kCus * per_cu[i]));
     const double t = rounds * per_cu[i] * each[i];
     if (i == 0 || t < least) {
@@ -1036,11 +1036,18 @@ OrthoPlan ortho_plan(bool bf16, int G, int M, int N) {
   return p;
 }
 
-Cut gram_cut(const OrthoPlan& p, int G) {
+Cut gram_cut(const OrthoPlan& p, int G, int n = kCuts) {
   return best_cut([&](int T) {
     const long long r = (p.mp + T - 1) / T;
     return r * (r + 1) / 2 * G;
-  });
+  }, n);
+}
+// X X^T of few rows takes no 256 x 256 tiles, the last of the cuts, which keep its sums in one:
+// 256 of 256 x 4096 off by 3.8e-6 in those and 2.6e-6 in others at the same speed (6566 and
+// 6498 us in all; 256 x 512 1161 and 1217 us, 1.8e-6 and 1.7e-6). From 512 rows on the other
+// products' errors are as large (80 of 512 x 8192 2.2e-6 and 1.8e-6) and the tiles gain 1 to 7%.
+Cut x_cut(const OrthoPlan& p, int G) {
+  return gram_cut(p, G, p.mp < kOnePieceFrom ? kCuts - 1 : kCuts);
 }
 Cut apply_cut(const OrthoPlan& p, int G) {
   return best_cut([&](int T) {
@@ -1057,9 +1064,9 @@ hipError_t ortho(const OrthoArgs& a, const OrthoPlan& p, hipStream_t s) {
                      p.chunks);
   hipLaunchKernelGGL(k_ortho_split<P>, grid_of(tiles * a.G), dim3(kThreads), 0, s, a, p.chunks,
                      p.mp / 64, p.np / 64);
-  const Cut cg = gram_cut(p, a.G), ca = apply_cut(p, a.G);
+  const Cut cx = x_cut(p, a.G), cg = gram_cut(p, a.G), ca = apply_cut(p, a.G);
   for (int t = 0; t < a.steps; ++t) {
-    gram<P, false>(cg, a, t, s);
+    gram<P, false>(cx, a, t, s);
     gram<P, true>(cg, a, t, s);
     if (t + 1 < a.steps)
       apply<P, false>(ca, a, t, s);
@@ -1076,11 +1083,13 @@ size_t ortho_workspace_bytes(int bf16, int G, int M, int N) {
   return ortho_plan(bf16, G, M, N).total;
 }
 
-void ortho_cut(int bf16, int G, int M, int N, int cut[5]) {
+void ortho_cut(int bf16, int G, int M, int N, int cut[7]) {
   const OrthoPlan p = ortho_plan(bf16, G, M, N);
-  const Cut g = p.small ? Cut{0, 0} : gram_cut(p, G), a = p.small ? Cut{0, 0} : apply_cut(p, G);
-  const int v[5] = {p.small ? 0 : p.pieces, g.tile, g.stages, a.tile, a.stages};
-  std::copy(v, v + 5, cut);
+  std::fill(cut, cut + 7, 0);
+  if (p.small) return;
+  const Cut x = x_cut(p, G), g = gram_cut(p, G), a = apply_cut(p, G);
+  const int v[7] = {p.pieces, x.tile, x.stages, g.tile, g.stages, a.tile, a.stages};
+  std::copy(v, v + 7, cut);
 }
 
 hipError_t launch_ortho(int bf16, OrthoArgs a, void* ws, hipStream_t s) {

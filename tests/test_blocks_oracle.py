@@ -279,7 +279,7 @@ def test_every_cut_of_the_orthogonalisation_is_tested():
     """The shapes of the GPU tests, which run each in both precisions, against all the cuts that
     matrices of up to 32 x 32 tiles of 64, in any number up to 800, take."""
     import test_gpu_ortho as T
-    cut, f = (ctypes.c_int32 * 5)(), _lib().lsgd_orthogonalise_cut
+    cut, f = (ctypes.c_int32 * 7)(), _lib().lsgd_orthogonalise_cut
 
     def cuts(shapes):
         seen = set()
@@ -287,15 +287,28 @@ def test_every_cut_of_the_orthogonalisation_is_tested():
             for dtype in (0, 1):
                 assert f(dtype, G, M, N, cut) == 0
                 if cut[0]:
-                    seen |= {("A", cut[0], cut[1], cut[2]), ("X", cut[0], cut[3], cut[4])}
+                    seen |= {(cut[0], i, cut[i], cut[i + 1]) for i in (1, 3, 5)}
         return seen
 
     tested = cuts(T.SHAPES + T.LARGE + T.CUTS)
     tiles = (1, 2, 3, 4, 5, 6, 7, 8, 9, 11, 14, 18, 24, 32)
     assert tested == cuts((G, 64 * m, 64 * n + 600 * (n == 1)) for m in tiles for n in tiles
                           for G in (*range(1, 60), *range(60, 800, 7)))
-    assert len(tested) == 23
+    assert len(tested) == 35
 
     assert f(2, 1, 64, 64, cut) == 1 and f(0, 0, 64, 64, cut) == 1 and f(0, 1, 64, 0, cut) == 1
     assert f(0, 1, 64, 64, None) == 1
-    assert f(0, 1, 64, 64, cut) == 0 and list(cut) == [0] * 5
+    assert f(0, 1, 64, 64, cut) == 0 and list(cut) == [0] * 7
+
+
+def test_few_rows_keep_two_sums():
+    """X X^T of matrices of fewer than 385 rows never takes the tiles that keep one sum."""
+    cut, f = (ctypes.c_int32 * 7)(), _lib().lsgd_orthogonalise_cut
+    one = 0
+    for m in range(64, 449, 64):
+        for n in (m, 600, 4096):
+            for G in range(1, 700, 3):
+                assert f(0, G, m, n, cut) == 0
+                one += cut[3] == 256
+                assert m >= 385 or cut[1] < 256, (G, m, n)
+    assert one > 0

@@ -481,3 +481,20 @@ def test_whatever_the_workspace_holds(shape, dtype):
                    lambda: L.orthogonalise(other * float("nan"), workspace=ws)):
         before()
         assert torch.equal(L.orthogonalise(X, workspace=ws), want)
+
+
+def test_precision_does_not_depend_on_the_number_of_matrices():
+    """Few long rows, alone and as one of many, where the products take other tiles: sums of as
+    many roundings, in another order, are off by as much (their rms over 10^6 results; a
+    quarter for chance. With one sum in place of two X X^T alone would round sqrt(3) times
+    as far)."""
+    L = _lsgd()
+    print("precision in a crowd", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(3)
+    rand = lambda *s: torch.randn(*s, generator=gen, device=device())  # noqa: E731
+    X = rand(1, 256, 4096) + 0.5 * rand(1, 256, 16) @ rand(1, 16, 4096)
+    want = _steps_on_device(X, 0)
+    alone = (L.orthogonalise(X).double() - want).norm()
+    for G in (200, 256):
+        many = (L.orthogonalise(X.expand(G, 256, 4096))[G - 1:].double() - want).norm()
+        assert many <= 1.25 * alone, (G, float(many / alone))
