@@ -569,7 +569,7 @@ lsgd_status lsgd_orthogonalise(int32_t dtype, int32_t G, int32_t M, int32_t N,
  *   w = (1 - lr wd) w - lr scale O(d).
  * gemm_dtype: the precision of O's products (as dtype above). Pointers may point into
  * the replicas' flat rows (a layer's W of every replica: sW the row length). lr,
- * weight_decay and scale finite, 0 <= momentum < 1, nesterov 0 or 1. W, U and G must
+ * weight_decay and scale and their products finite in fp32, 0 <= momentum < 1, nesterov 0 or 1. W, U and G must
  * not overlap. */
 lsgd_status lsgd_orthogonal_update(int32_t gemm_dtype, int32_t G, int32_t M,
                                    int32_t N, float* d_W, int64_t ldw,

@@ -1958,6 +1958,8 @@ lsgd_status lsgd_orthogonal_update(int32_t gemm_dtype, int32_t G, int32_t M, int
   a.nesterov = nesterov;
   a.keep = (float)(1.0 - (double)lr * weight_decay);
   a.step = (float)(-(double)lr * scale);
+  // (an infinite factor would make NaN of every zero it meets)
+  if (!std::isfinite(a.keep) || !std::isfinite(a.step)) return LSGD_E_INVALID;
   return ortho_launch(gemm_dtype, a, d_ws, ws_bytes, stream);
 }
 

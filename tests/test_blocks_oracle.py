@@ -312,3 +312,11 @@ def test_few_rows_keep_two_sums():
                 one += cut[3] == 256
                 assert m >= 385 or cut[1] < 256, (G, m, n)
     assert one > 0
+
+
+def test_update_refuses_factors_that_overflow():
+    f, c = P(4096), ctypes.c_float
+    for lr, wd, scale in ((1e30, 0.0, 1e30), (1e30, 1e30, 1.0), (-3e38, 0.0, 2.0)):
+        assert _lib().lsgd_orthogonal_update(
+            0, 1, 3, 4, f, 4, 0, f, 4, 0, f, 4, 0, c(lr), c(0.9), c(wd), 0, c(scale), 5, CO,
+            c(1e-7), None, 0, None) == 1

@@ -498,3 +498,23 @@ def test_precision_does_not_depend_on_the_number_of_matrices():
     for G in (200, 256):
         many = (L.orthogonalise(X.expand(G, 256, 4096))[G - 1:].double() - want).norm()
         assert many <= 1.25 * alone, (G, float(many / alone))
+
+
+@pytest.mark.parametrize("shape", [(3, 30, 41), (3, 150, 141)])
+def test_update_with_a_shared_gradient_and_replicas_side_by_side(shape):
+    """One gradient for every replica (expand), W and U in rows that hold all replicas' rows:
+    the bits of separate contiguous tensors."""
+    L = _lsgd()
+    print(f"update shared {shape}", flush=True)
+    K, M, N = shape
+    rng = np.random.default_rng(2)
+    room = to_dev(rng.standard_normal((2, M, K, N + 2)).astype(np.float32))
+    W, U = (t[:, :, 1:N + 1].transpose(0, 1) for t in room)
+    g = to_dev(_matrices(rng, 1, M, N).astype(np.float32))
+    w, u, before = W.contiguous(), U.contiguous(), room.clone()
+    L.orthogonal_update(w, u, g.expand(K, M, N).contiguous(), 0.1, 0.9, 0.01, nesterov=True)
+    L.orthogonal_update(W, U, g.expand(K, M, N), 0.1, 0.9, 0.01, nesterov=True)
+    assert torch.equal(W, w) and torch.equal(U, u)
+    for i, t in enumerate((w, u)):
+        before[i][:, :, 1:N + 1] = t.transpose(0, 1)
+    assert torch.equal(room, before)
