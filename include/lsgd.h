@@ -530,7 +530,8 @@ lsgd_status lsgd_grouped_gemm_blocks(int32_t format_a, int32_t format_b,
  * (on X^T where M > N), h_coefficients = {a, b, c} (host). The products
  * take fp32 precision for dtype LSGD_FP32 (two fp16 pieces of each operand on
  * the matrix cores); for LSGD_BF16 operands of 11 significant bits do where
- * min(M, N) > 384 (X itself is held in two pieces all the same). A zero matrix stays zero; an
+ * min(M, N) > 384 (X itself is held in two pieces all the same): a result off by 2.0e-3 to
+ * 2.3e-3 of its norm, where rounding it to bf16 alone takes 1.7e-3. A zero matrix stays zero; an
  * infinity or a NaN makes the whole result NaN.
  *
  * Arguments, else LSGD_E_INVALID: 1 <= G <= 65535, 1 <= M, N <= 2^20 with

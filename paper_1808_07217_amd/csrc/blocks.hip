@@ -227,8 +227,9 @@ __global__ __launch_bounds__(kThreads) void k_quantise(QuantArgs a, int tm, int 
 }
 
 // From kNtBytesCaller of input and output on the values are streamed: 16384 x 8192 in bf16
-// both ways (537 MB) 156 -> 116 us; with 268 MB (8192^2) the call itself gains as much, but
-// the product that reads the values next loses more (506 -> 519 us together).
+// both ways (537 MB), repeated on one input, 156 -> 119 us; with 268 MB (8192^2) the call
+// itself gains as much, but the product that reads the values next loses more (506 -> 519 us
+// together).
 template <bool BF, int FMT>
 hipError_t quantise(const QuantArgs& a, hipStream_t s) {
   const double bytes = (double)a.M * a.N * a.G *
@@ -257,7 +258,7 @@ hipError_t quantise(const QuantArgs& a, hipStream_t s) {
 // scale operands are the blocks' bytes. It sums eight neighbouring products at a
 // time with 13 bits below the largest of them (probed: 2^10 + 2^-3 is exact, 2^10 +
 // 2^-4 is 2^10) and those sums in fp32: an error of 2^-10 sum |a b| at worst and about
-// 2^-15 of it on normal data, well below bf16's own 2^-9. That is too coarse for a
+// 2^-15 of it on normal data, well below bf16's own 2^-8. That is too coarse for a
 // result in fp32, which instead widens the values, scale and all, to bf16 (exact: 4
 // bits of a value, and 2^e is in bf16's range; only a value below 2^-126 becomes a
 // multiple of bf16's 2^-133, and 2^128, to which only fp32's last values round, an infinity) as they reach the registers and takes
@@ -539,8 +540,10 @@ int splits_of(bool bf16, int G, int M, int N, int Kd) {
 }
 
 // Tile sizes and stages, by estimated time: see ortho.hip's for what the numbers mean;
-// these are from 4096^3 and 8192^3 (us, to bf16 112 / 82 / 73 / 62 and 886 / 597 / 492 / 404;
-// to fp32 170 / 147 / 125 and 1294 / 1031 / 889).
+// these are from 4096^3 and 8192^3 (us, repeated on one input, to bf16 112 / 82 / 73 / 62 and
+// 886 / 597 / 492 / 404; to fp32 170 / 147 / 125 and 1294 / 1031 / 889; under the kernel trace,
+// whose pauses let the clock change, 117 / 79 / 68 / 57 and 1027 / 688 / 614 / 490, 194 / 155 /
+// 130 and 1351 / 1125 / 979).
 struct BlockCut {
   int tile, stages;
 };

@@ -9,11 +9,10 @@
 // x = x1 + x2 (22 to 24 significant bits), and fp32 products are x1 y1 + x1 y2 + x2 y1,
 // each exact in fp32; what is left out is 2^-24 |x y| at worst. In the bf16 form
 // the products of matrices of kOnePieceFrom rows and more take the first piece alone
-// (2^-12, an eighth of bf16's own rounding; the fewer rows, the less its errors average
-// out: the result was off by 2.0e-3 at 2048 rows and 2.5e-3 at 160, rounding to bf16
-// alone 1.7e-3). X keeps both pieces there too, because a X passes on the small
-// singular directions, which the steps amplify by a each time: rounding X itself to
-// 11 bits loses them (error 1.8e-2 instead of 1.7e-3 for matrices of low rank in noise).
+// (2^-11 at worst, an eighth of bf16's own rounding; see kOnePieceFrom). X keeps both
+// pieces there too, because a X passes on the small singular directions, which the steps
+// amplify by a each time: rounding X itself to 11 bits loses them (error 1.8e-2 instead of
+// 1.7e-3 for matrices of low rank in noise).
 //
 // A and B are symmetric: only their tiles on and below the diagonal are computed,
 // and each is stored on both sides. All three products are tiles of tile_loop.h.
@@ -929,14 +928,18 @@ struct Cut {
 };
 // The cut of least estimated time; tiles(T): how many tiles of T there are. A compute unit
 // takes per_cu workgroups at once (LDS), a round of them costs per_cu times `each`, and the
-// last round as much as a full one. `each` is what one tile took of a full round, in
-// units of about 10 us at an inner range of 2048 in fp32 precision, measured on 8 x
-// 2048^2 and 4096^2 with one cut forced for all products (16, 16, 44, 38, 84, 133 us). The
-// 192 x 192 tiles are for what 256 x 256 ones leave half of the units without: the triangles
-// of 4096 x 8192 in bf16 172 + 97 -> 150 + 78 us a step, 4 x 1500^2 1137 -> 993 us in all. At
-// the other end, with one workgroup to a unit, a product waits for loads and launches: 512^2
-// takes 125 us in 64 x 64 tiles of four stages, 136 of three, 213 / 282 in 128 x 128
-// tiles of four / two, 609 in 256 x 256 ones.
+// last round as much as a full one. `each` is the cost of one tile relative to the others,
+// fitted to products with one cut forced for all of them. Measured since, B X in fp32
+// precision, us for one tile on each unit and an inner range of 2048, in the order of `cuts`:
+//   4096^2:     14, 14, 42, 43, 87, 145      8 x 2048^2:   18, 18, 56, 55, 107, 181
+// and the whole products, of which the table picks the fastest each time:
+//   4096^2, X X^T:   333, 322, 221, 231, 172, 224      B X:   454, 449, 335, 342, 348, 291
+//   8 x 2048^2:      312, 309, 243, 243, 260, 269             576, 574, 452, 443, 429, 362
+// The 192 x 192 tiles are for what 256 x 256 ones leave half of the units without: the
+// triangles of 4096 x 8192 in bf16 172 + 97 -> 150 + 78 us a step, 4 x 1500^2 1137 -> 993 us
+// in all. At the other end, with one workgroup to a unit, a product waits for loads and
+// launches: 512^2 takes 125 us in 64 x 64 tiles of four stages, 136 of three, 213 / 282 in
+// 128 x 128 tiles of four / two, 609 in 256 x 256 ones.
 constexpr int kCus = 256;
 constexpr int kCuts = 6;
 template <class F>
@@ -1000,6 +1003,15 @@ int norm_chunks(int M, int N) {
   return (int)(c > 1024 ? 1024 : c);
 }
 
+// From this many rows on the bf16 form multiplies first pieces alone. The fewer rows, the less
+// their errors average out: the bf16 result of that many rows is off by (1e-3; 1.66 is its
+// rounding alone, and all there is with two pieces)
+//   130 to 160: 2.3 to 2.5, 256: 2.3 to 2.4, 384: 2.2 to 2.4, 448 and 512: 2.1 to 2.3, 2048: 2.0
+// and the two pieces' time is, with the single ones' in brackets, for eight matrices in us
+//   256 x 256: 106 (89), 256 x 1000: 143 (112), 384 x 384: 132 (99), 384 x 1000: 177 (129),
+//   448 x 1000: 185 (143).
+// There is no step in either: small matrices keep their precision, where it costs 20 to 40 us,
+// large ones, which wait for the matrix cores, do not.
 constexpr int kOnePieceFrom = 385;
 
 struct OrthoPlan {

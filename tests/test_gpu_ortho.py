@@ -388,7 +388,7 @@ def test_one_entry_holds_the_norm_of_the_largest_matrix(shape, dtype):
 
     From 1 on the course is 0.70, 1.11, 0.72, 1.09, 0.70, and an error of one step grows by
     |a + 3 b s^2 + 5 c s^4| <= 1.3 in each of the next, to below 2 in all. One step's own: in
-    fp32 precision 35 2^-24 (see the top); with operands of 11 bits, off by u = 2^-12, A is off
+    fp32 precision 35 2^-24 (see the top); with operands of 11 bits, off by u = 2^-11, A is off
     by 3 u (two X, A itself), A A by 6 u, B by one more, B X by yet another, so at s = 1.12
     5 |b| s^3 + 8 |c| s^5 = 62 u."""
     L = _lsgd()
@@ -403,7 +403,7 @@ def test_one_entry_holds_the_norm_of_the_largest_matrix(shape, dtype):
     for _ in range(5):
         s = s * (a + b * s ** 2 + c * s ** 4)
     got = float(Y[0, M - 3, 7])
-    step = 35 * 2.0 ** -24 if dtype == "fp32" else 62 * 2.0 ** -12 + 2.0 ** -8
+    step = 35 * 2.0 ** -24 if dtype == "fp32" else 62 * 2.0 ** -11 + 2.0 ** -8
     assert abs(got - s) <= 5 * 2 * step, (got, s)
     Y[0, M - 3, 7] = 0
     assert bool((Y == 0).all())
