@@ -582,6 +582,141 @@ lsgd_status lsgd_orthogonal_update(int32_t gemm_dtype, int32_t G, int32_t M,
                                    const float* h_coefficients, float eps,
                                    void* d_ws, size_t ws_bytes, void* stream);
 
+/*
+ * Matrices in 8-bit integers with an fp32 scale for each row: the operands of
+ * lsgd_grouped_gemm_rows. A row of n values takes up(n, 128) bytes, zeros past the
+ * n-th, and one scale s: max |x| / 127 rounded to fp32, at least 2^-126; 1 for a row of
+ * zeros; a NaN for a row that holds an infinity or a NaN, whose integers are zeros. A value x
+ * is held as the integer nearest to x / s, ties to even, |q| <= 127.
+ */
+
+/*
+ * Writes G matrices X_g [M][N] (dtype LSGD_FP32 or LSGD_BF16, row pitch
+ * ldx >= N, group stride sX >= 0 in elements) in rows: d_Q [G][M][up(N, 128)]
+ * with d_S [G][M]; and with d_Qt and d_St (NULL: not wanted) the transposes, a scale for
+ * each column of X: d_Qt [G][N][up(M, 128)] with d_St [G][N]. All padding is written.
+ * G <= 65535, M, N <= 2^30, d_Q and d_Qt 16-byte aligned, the rest aligned to its
+ * elements, else LSGD_E_INVALID. With the transposes: a workspace of
+ * lsgd_quantise_rows_workspace_bytes, 4-byte aligned (LSGD_E_WORKSPACE if smaller),
+ * one call's at a time; without them NULL is allowed. What is written must not overlap
+ * X, the workspace or another result.
+ */
+lsgd_status lsgd_quantise_rows_workspace_bytes(int32_t G, int32_t M, int32_t N,
+                                               size_t* bytes);
+lsgd_status lsgd_quantise_rows(int32_t dtype, int32_t G, int32_t M, int32_t N,
+                               const void* d_X, int64_t ldx, int64_t sX,
+                               int8_t* d_Q, float* d_S, int8_t* d_Qt,
+                               float* d_St, void* d_ws, size_t ws_bytes,
+                               void* stream);
+
+/*
+ * Grouped product of matrices in rows along the contracted dimension:
+ *   C_g[m][n] = S_A[m] S_B[n] sum_k A_g[m][k] B_g[n][k] + bias_g[n]
+ * The sum of integers is exact; it is rounded to fp32, as are its two products with the
+ * scales (the last together with the bias), and once more to LSGD_BF16 (out_dtype). A_g is
+ * M rows, B_g N rows of Kd integers in the layout above: the forward product y = x w + b
+ * takes x and the transpose of w, the input gradient dy w^T takes dy and w, the weight
+ * gradient x^T dy the transposes of both. Group strides sA, sB (bytes, multiples
+ * of 16), sSA, sSB and sbias (elements) may be 0: a matrix shared among the groups. d_A, d_B
+ * 16-byte aligned; the bytes past Kd of a row must be zeros, as lsgd_quantise_rows
+ * leaves them; any integer from -128 to 127 and any positive scale will do. d_bias fp32
+ * [G][N] or NULL. G <= 65535, M, N <= 2^30, Kd <= 2^22. C's pitch and group stride and the workspace (of
+ * lsgd_grouped_gemm_rows_workspace_bytes, 16-byte aligned) as lsgd_grouped_gemm_blocks
+ * has them. C must not overlap anything that is read.
+ */
+lsgd_status lsgd_grouped_gemm_rows_workspace_bytes(int32_t out_dtype, int32_t G,
+                                                   int32_t M, int32_t N,
+                                                   int32_t Kd, size_t* bytes);
+/* How that product is cut, for tests and profiles: cut[0] the tile's rows and columns,
+ * cut[1] the stages of loads, cut[2] the ranges of the inner dimension. */
+lsgd_status lsgd_grouped_gemm_rows_cut(int32_t out_dtype, int32_t G, int32_t M,
+                                       int32_t N, int32_t Kd, int32_t cut[3]);
+lsgd_status lsgd_grouped_gemm_rows(int32_t out_dtype, int32_t G, int32_t M,
+                                   int32_t N, int32_t Kd, const int8_t* d_A,
+                                   int64_t sA, const float* d_SA, int64_t sSA,
+                                   const int8_t* d_B, int64_t sB,
+                                   const float* d_SB, int64_t sSB,
+                                   const float* d_bias, int64_t sbias,
+                                   void* d_C, int64_t ldc, int64_t sC,
+                                   void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * Layer norm of the rows of G matrices X_g [M][N] (dtype), each with a weight and a bias
+ * of its own (fp32 [G][N], group strides sw, sb >= 0; NULL: ones, zeros):
+ *   mean = sum x / N, rstd = (sum (x - mean)^2 / N + eps)^-1/2,
+ *   Y = (x - mean) rstd w + b (out_dtype, rounded once), d_mean, d_rstd fp32 [G][M].
+ * The sums are held in fp64. A NaN or an infinity in a row makes the row NaN. X's pitch
+ * ldx >= N and stride sX >= 0 in elements; Y's groups must not overlap (as C of
+ * lsgd_grouped_gemm_blocks). eps finite and > 0. G <= 65535, M, N <= 2^30, else
+ * LSGD_E_INVALID. Results must not overlap anything that is read.
+ */
+lsgd_status lsgd_layer_norm(int32_t dtype, int32_t out_dtype, int32_t G,
+                            int32_t M, int32_t N, const void* d_X, int64_t ldx,
+                            int64_t sX, const float* d_w, int64_t sw,
+                            const float* d_b, int64_t sb, float eps, void* d_Y,
+                            int64_t ldy, int64_t sY, float* d_mean,
+                            float* d_rstd, void* stream);
+
+/*
+ * Its gradients, from dY (out_dtype), X (dtype) and the mean and rstd that
+ * lsgd_layer_norm wrote: with n = (x - mean) rstd and e = dy w,
+ *   dX = rstd (e - sum e / N - n sum (e n) / N) (dtype),
+ *   dw = sum over the group's rows of dy n, db = sum of dy (fp32 [G][N], group strides sdw,
+ *   sdb >= N; both NULL: not wanted).
+ * The sums over rows are added in an order that the sizes alone decide. Workspace
+ * (not without dw and db): lsgd_layer_norm_backward_workspace_bytes, 16-byte aligned (LSGD_E_WORKSPACE
+ * if smaller; 0 for few rows; then NULL is allowed), one call's at a time. Limits as
+ * above. Results must not overlap each other or anything that is read.
+ */
+lsgd_status lsgd_layer_norm_backward_workspace_bytes(int32_t G, int32_t M,
+                                                     int32_t N, size_t* bytes);
+lsgd_status lsgd_layer_norm_backward(int32_t dtype, int32_t out_dtype, int32_t G,
+                                     int32_t M, int32_t N, const void* d_dY,
+                                     int64_t ldg, int64_t sG, const void* d_X,
+                                     int64_t ldx, int64_t sX,
+                                     const float* d_mean, const float* d_rstd,
+                                     const float* d_w, int64_t sw, void* d_dX,
+                                     int64_t ldd, int64_t sD, float* d_dw,
+                                     int64_t sdw, float* d_db, int64_t sdb,
+                                     void* d_ws, size_t ws_bytes, void* stream);
+
+/*
+ * The gradients of K replicas: `count` tensors, of each replica a matrix [M][N] (dtype
+ * LSGD_FP32 or LSGD_BF16, row pitch ld >= N, replica stride s >= 0 in elements; a
+ * replica's flat row holds one at an offset, s the row length). The array is read
+ * before the call returns.
+ */
+typedef struct lsgd_tensor {
+  void* d_data;
+  int64_t M, N, ld, s;
+  int32_t dtype;
+  int32_t reserved; /* 0 */
+} lsgd_tensor;
+#define LSGD_MAX_TENSORS 65536
+
+/*
+ * lsgd_gradient_norm: d_norm[k] (fp32 [K]) = the root of the sum of squares over all values of
+ * replica k's tensors, squares and sum in fp64, in an order that the sizes alone decide (a tensor
+ * listed twice counts twice). lsgd_clip_gradients also multiplies the values of each replica
+ * whose norm is above max_norm (finite, > 0) by max_norm / norm, the factor and the product in
+ * fp64, rounded once; the others' stay as they are, as do those of a replica whose norm is not finite.
+ * d_norm holds the norms before clipping. K <= 65535, count <= LSGD_MAX_TENSORS, M and N at
+ * least 1, M N, M ld, s <= 2^44, else LSGD_E_INVALID. Clipped tensors' replicas must not overlap
+ * (s >= (M - 1) ld + N, or rows of all K side by side), nor two tensors, nor d_norm. Workspace of
+ * lsgd_gradient_norm_workspace_bytes, 8-byte aligned (LSGD_E_WORKSPACE if smaller), one call's
+ * at a time.
+ */
+lsgd_status lsgd_gradient_norm_workspace_bytes(int32_t K, int32_t count,
+                                               const lsgd_tensor* h_tensors,
+                                               size_t* bytes);
+lsgd_status lsgd_gradient_norm(int32_t K, int32_t count,
+                               const lsgd_tensor* h_tensors, float* d_norm,
+                               void* d_ws, size_t ws_bytes, void* stream);
+lsgd_status lsgd_clip_gradients(int32_t K, int32_t count,
+                                const lsgd_tensor* h_tensors, double max_norm,
+                                float* d_norm, void* d_ws, size_t ws_bytes,
+                                void* stream);
+
 #ifdef __cplusplus
 }
 #endif

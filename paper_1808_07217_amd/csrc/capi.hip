@@ -290,6 +290,19 @@ lsgd_status block_status(hipError_t e) {
   return e == hipSuccess ? LSGD_OK : (e == hipErrorInvalidValue ? LSGD_E_INVALID : LSGD_E_HIP);
 }
 
+// Groups, rows and columns of an operator on rows.
+bool row_sizes(int32_t G, int32_t M, int32_t N) {
+  return G >= 1 && G <= 65535 && M >= 1 && M <= kMaxBlockRows && N >= 1 && N <= kMaxBlockRows;
+}
+bool float_type(int32_t dtype) { return dtype == LSGD_FP32 || dtype == LSGD_BF16; }
+size_t float_size(int32_t dtype) { return dtype == LSGD_BF16 ? 2 : 4; }
+// A matrix that a call reads.
+bool read_groups(const void* p, int32_t N, int64_t ld, int64_t s, size_t esz) {
+  return p && ld >= N && s >= 0 && (uintptr_t)p % esz == 0;
+}
+// The vectors [G][N] of a layer norm: nullptr, or fp32 at any stride.
+bool read_vectors(const float* p, int64_t s) { return !p || (s >= 0 && (uintptr_t)p % 4 == 0); }
+
 bool ortho_sizes(int32_t G, int32_t M, int32_t N) {
   // (rows of a tile are addressed by 32-bit offsets: 256 rows of 2^20 values in 4 bytes)
   if (G < 1 || G > 65535 || M < 1 || N < 1 || M > (1 << 20) || N > (1 << 20)) return false;
@@ -361,6 +374,43 @@ bool ortho_numbers(lsgd::OrthoArgs& a, int32_t steps, const float* h, float eps)
   a.f_out = (float)(1.0 / (sb * sx));
   a.f_x = h[0];
   return true;
+}
+
+// The tensors of a clip, as launch_clip takes them; written: the call changes them.
+bool clip_tensors(int32_t K, int32_t count, const lsgd_tensor* h, bool written,
+                  std::vector<lsgd::ClipTensor>& to) {
+  if (K < 1 || K > 65535 || count < 1 || count > LSGD_MAX_TENSORS || !h) return false;
+  constexpr int64_t kMost = 1LL << 44;
+  to.resize(count);
+  for (int i = 0; i < count; ++i) {
+    const lsgd_tensor& t = h[i];
+    if (!float_type(t.dtype) || t.reserved || !t.d_data || (uintptr_t)t.d_data % float_size(t.dtype))
+      return false;
+    if (t.M < 1 || t.N < 1 || t.M > kMost / t.N || t.ld < t.N || t.ld > kMost / t.M || t.s < 0 || t.s > kMost)
+      return false;
+    // replicas that do not overlap, one after the other or side by side in rows
+    if (written && K > 1 &&
+        (t.s < t.N || !((t.s - t.N) / t.ld >= t.M - 1 || (t.ld - t.N) / t.s >= K - 1)))
+      return false;
+    to[i] = lsgd::ClipTensor{t.d_data, t.M, t.N, t.ld, t.s, t.dtype == LSGD_BF16, 0};
+  }
+  return true;
+}
+
+lsgd_status clip_call(int32_t K, int32_t count, const lsgd_tensor* h, bool scale, double most,
+                      float* d_norm, void* d_ws, size_t ws_bytes, void* stream) {
+  if (!d_norm || (uintptr_t)d_norm % 4 || !(most > 0.0) || !std::isfinite(most)) return LSGD_E_INVALID;
+  try {
+    std::vector<lsgd::ClipTensor> t;
+    if (!clip_tensors(K, count, h, scale, t)) return LSGD_E_INVALID;
+    const size_t need = lsgd::clip_workspace_bytes(K, count, t.data());
+    if (need && (!d_ws || (uintptr_t)d_ws % 8)) return LSGD_E_INVALID;
+    if (ws_bytes < need) return LSGD_E_WORKSPACE;
+    return block_status(
+        lsgd::launch_clip(K, count, t.data(), scale, most, d_norm, d_ws, (hipStream_t)stream));
+  } catch (...) {
+    return LSGD_E_INVALID;
+  }
 }
 
 lsgd_status ortho_launch(int32_t dtype, const lsgd::OrthoArgs& a, void* d_ws, size_t ws_bytes,
@@ -1961,6 +2011,204 @@ lsgd_status lsgd_orthogonal_update(int32_t gemm_dtype, int32_t G, int32_t M, int
   // (an infinite factor would make NaN of every zero it meets)
   if (!std::isfinite(a.keep) || !std::isfinite(a.step)) return LSGD_E_INVALID;
   return ortho_launch(gemm_dtype, a, d_ws, ws_bytes, stream);
+}
+
+// ------------------------------------- tensors in 8-bit integers, rows
+lsgd_status lsgd_quantise_rows_workspace_bytes(int32_t G, int32_t M, int32_t N, size_t* bytes) {
+  if (!bytes || !row_sizes(G, M, N)) return LSGD_E_INVALID;
+  *bytes = lsgd::rows_quantise_workspace_bytes(G, M, N);
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_quantise_rows(int32_t dtype, int32_t G, int32_t M, int32_t N, const void* d_X,
+                               int64_t ldx, int64_t sX, int8_t* d_Q, float* d_S, int8_t* d_Qt,
+                               float* d_St, void* d_ws, size_t ws_bytes, void* stream) {
+  if (!float_type(dtype) || !row_sizes(G, M, N) || !read_groups(d_X, N, ldx, sX, float_size(dtype)))
+    return LSGD_E_INVALID;
+  if (!d_Q || !d_S || !d_Qt != !d_St || (uintptr_t)d_Q % 16 || (uintptr_t)d_Qt % 16 ||
+      (uintptr_t)d_S % 4 || (uintptr_t)d_St % 4)
+    return LSGD_E_INVALID;
+  if (d_Qt) {
+    if (!d_ws || (uintptr_t)d_ws % 4) return LSGD_E_INVALID;
+    if (ws_bytes < lsgd::rows_quantise_workspace_bytes(G, M, N)) return LSGD_E_WORKSPACE;
+  }
+  lsgd::RowQuantArgs a{};
+  a.G = G;
+  a.M = M;
+  a.N = N;
+  a.X = d_X;
+  a.ldx = ldx;
+  a.sX = sX;
+  a.Q = (uint8_t*)d_Q;
+  a.S = d_S;
+  a.Qt = (uint8_t*)d_Qt;
+  a.St = d_St;
+  return block_status(
+      lsgd::launch_quantise_rows(dtype == LSGD_BF16, a, d_ws, (hipStream_t)stream));
+}
+
+lsgd_status lsgd_grouped_gemm_rows_workspace_bytes(int32_t out_dtype, int32_t G, int32_t M,
+                                                   int32_t N, int32_t Kd, size_t* bytes) {
+  if (!float_type(out_dtype) || !bytes || !block_sizes(G, M, N, Kd)) return LSGD_E_INVALID;
+  *bytes = lsgd::gemm_rows_workspace_bytes(out_dtype == LSGD_BF16, G, M, N, Kd);
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_grouped_gemm_rows_cut(int32_t out_dtype, int32_t G, int32_t M, int32_t N,
+                                       int32_t Kd, int32_t cut[3]) {
+  if (!float_type(out_dtype) || !cut || !block_sizes(G, M, N, Kd)) return LSGD_E_INVALID;
+  lsgd::gemm_rows_cut(out_dtype == LSGD_BF16, G, M, N, Kd, cut);
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_grouped_gemm_rows(int32_t out_dtype, int32_t G, int32_t M, int32_t N, int32_t Kd,
+                                   const int8_t* d_A, int64_t sA, const float* d_SA, int64_t sSA,
+                                   const int8_t* d_B, int64_t sB, const float* d_SB, int64_t sSB,
+                                   const float* d_bias, int64_t sbias, void* d_C, int64_t ldc,
+                                   int64_t sC, void* d_ws, size_t ws_bytes, void* stream) {
+  if (!float_type(out_dtype) || !block_sizes(G, M, N, Kd)) return LSGD_E_INVALID;
+  if (!d_A || !d_SA || !d_B || !d_SB ||
+      !written_groups(G, M, N, d_C, ldc, sC, float_size(out_dtype)))
+    return LSGD_E_INVALID;
+  if (sA < 0 || sB < 0 || sSA < 0 || sSB < 0 || sA % 16 || sB % 16 || (uintptr_t)d_A % 16 ||
+      (uintptr_t)d_B % 16 || (uintptr_t)d_SA % 4 || (uintptr_t)d_SB % 4 ||
+      !read_vectors(d_bias, sbias))
+    return LSGD_E_INVALID;
+  const size_t need = lsgd::gemm_rows_workspace_bytes(out_dtype == LSGD_BF16, G, M, N, Kd);
+  if (need && (!d_ws || (uintptr_t)d_ws % 16)) return LSGD_E_INVALID;
+  if (ws_bytes < need) return LSGD_E_WORKSPACE;
+  lsgd::RowGemmArgs a{};
+  a.G = G;
+  a.M = M;
+  a.N = N;
+  a.Kd = Kd;
+  a.A = (const uint8_t*)d_A;
+  a.sA = sA;
+  a.SA = d_SA;
+  a.sSA = sSA;
+  a.B = (const uint8_t*)d_B;
+  a.sB = sB;
+  a.SB = d_SB;
+  a.sSB = sSB;
+  a.bias = d_bias;
+  a.sbias = sbias;
+  a.C = d_C;
+  a.ldc = ldc;
+  a.sC = sC;
+  a.out_bf16 = out_dtype == LSGD_BF16;
+  a.part = d_ws;
+  return block_status(lsgd::launch_gemm_rows(a, (hipStream_t)stream));
+}
+
+// ------------------------------------------------------------ layer norm
+lsgd_status lsgd_layer_norm(int32_t dtype, int32_t out_dtype, int32_t G, int32_t M, int32_t N,
+                            const void* d_X, int64_t ldx, int64_t sX, const float* d_w, int64_t sw,
+                            const float* d_b, int64_t sb, float eps, void* d_Y, int64_t ldy,
+                            int64_t sY, float* d_mean, float* d_rstd, void* stream) {
+  if (!float_type(dtype) || !float_type(out_dtype) || !row_sizes(G, M, N)) return LSGD_E_INVALID;
+  if (!read_groups(d_X, N, ldx, sX, float_size(dtype)) || !read_vectors(d_w, sw) ||
+      !read_vectors(d_b, sb) || !written_groups(G, M, N, d_Y, ldy, sY, float_size(out_dtype)))
+    return LSGD_E_INVALID;
+  if (!std::isfinite(eps) || !(eps > 0.f) || !d_mean || !d_rstd || (uintptr_t)d_mean % 4 ||
+      (uintptr_t)d_rstd % 4)
+    return LSGD_E_INVALID;
+  lsgd::NormArgs a{};
+  a.G = G;
+  a.M = M;
+  a.N = N;
+  a.X = d_X;
+  a.ldx = ldx;
+  a.sX = sX;
+  a.w = d_w;
+  a.b = d_b;
+  a.sw = sw;
+  a.sb = sb;
+  a.eps = eps;
+  a.Y = d_Y;
+  a.ldy = ldy;
+  a.sY = sY;
+  a.mean = d_mean;
+  a.rstd = d_rstd;
+  return block_status(lsgd::launch_norm(dtype == LSGD_BF16, out_dtype == LSGD_BF16, a,
+                                        (hipStream_t)stream));
+}
+
+lsgd_status lsgd_layer_norm_backward_workspace_bytes(int32_t G, int32_t M, int32_t N,
+                                                     size_t* bytes) {
+  if (!bytes || !row_sizes(G, M, N)) return LSGD_E_INVALID;
+  *bytes = lsgd::norm_back_workspace_bytes(G, M, N);
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_layer_norm_backward(int32_t dtype, int32_t out_dtype, int32_t G, int32_t M,
+                                     int32_t N, const void* d_dY, int64_t ldg, int64_t sG,
+                                     const void* d_X, int64_t ldx, int64_t sX, const float* d_mean,
+                                     const float* d_rstd, const float* d_w, int64_t sw, void* d_dX,
+                                     int64_t ldd, int64_t sD, float* d_dw, int64_t sdw,
+                                     float* d_db, int64_t sdb, void* d_ws, size_t ws_bytes,
+                                     void* stream) {
+  if (!float_type(dtype) || !float_type(out_dtype) || !row_sizes(G, M, N)) return LSGD_E_INVALID;
+  if (!read_groups(d_dY, N, ldg, sG, float_size(out_dtype)) ||
+      !read_groups(d_X, N, ldx, sX, float_size(dtype)) || !read_vectors(d_w, sw) ||
+      !written_groups(G, M, N, d_dX, ldd, sD, float_size(dtype)))
+    return LSGD_E_INVALID;
+  if (!d_mean || !d_rstd || (uintptr_t)d_mean % 4 || (uintptr_t)d_rstd % 4 || !d_dw != !d_db)
+    return LSGD_E_INVALID;
+  if (d_dw && (!written_groups(G, 1, N, d_dw, N, sdw, 4) || !written_groups(G, 1, N, d_db, N, sdb, 4)))
+    return LSGD_E_INVALID;
+  if (d_dw) {
+    const size_t need = lsgd::norm_back_workspace_bytes(G, M, N);
+    if (need && (!d_ws || (uintptr_t)d_ws % 16)) return LSGD_E_INVALID;
+    if (ws_bytes < need) return LSGD_E_WORKSPACE;
+  }
+  lsgd::NormBackArgs a{};
+  a.G = G;
+  a.M = M;
+  a.N = N;
+  a.dY = d_dY;
+  a.ldg = ldg;
+  a.sg = sG;
+  a.X = d_X;
+  a.ldx = ldx;
+  a.sX = sX;
+  a.mean = d_mean;
+  a.rstd = d_rstd;
+  a.w = d_w;
+  a.sw = sw;
+  a.dX = d_dX;
+  a.ldd = ldd;
+  a.sd = sD;
+  a.dw = d_dw;
+  a.sdw = sdw;
+  a.db = d_db;
+  a.sdb = sdb;
+  return block_status(lsgd::launch_norm_back(dtype == LSGD_BF16, out_dtype == LSGD_BF16, a, d_ws,
+                                             (hipStream_t)stream));
+}
+
+// -------------------------------------------------------------- clipping
+lsgd_status lsgd_gradient_norm_workspace_bytes(int32_t K, int32_t count,
+                                               const lsgd_tensor* h_tensors, size_t* bytes) {
+  if (!bytes) return LSGD_E_INVALID;
+  try {
+    std::vector<lsgd::ClipTensor> t;
+    if (!clip_tensors(K, count, h_tensors, false, t)) return LSGD_E_INVALID;
+    *bytes = lsgd::clip_workspace_bytes(K, count, t.data());
+  } catch (...) {
+    return LSGD_E_INVALID;
+  }
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_gradient_norm(int32_t K, int32_t count, const lsgd_tensor* h_tensors,
+                               float* d_norm, void* d_ws, size_t ws_bytes, void* stream) {
+  return clip_call(K, count, h_tensors, false, 1.0, d_norm, d_ws, ws_bytes, stream);
+}
+
+lsgd_status lsgd_clip_gradients(int32_t K, int32_t count, const lsgd_tensor* h_tensors,
+                                double max_norm, float* d_norm, void* d_ws, size_t ws_bytes,
+                                void* stream) {
+  return clip_call(K, count, h_tensors, true, max_norm, d_norm, d_ws, ws_bytes, stream);
 }
 
 }  // extern "C"

@@ -161,6 +161,98 @@ size_t gemm_blocks_workspace_bytes(int bf16, int G, int M, int N, int Kd);
 void gemm_blocks_cut(int bf16, int G, int M, int N, int Kd, int cut[3]);  // tile, stages, ranges
 hipError_t launch_gemm_blocks(int fmt_a, int fmt_b, const BlockGemmArgs& a, hipStream_t s);
 
+// ---------------------------------------------- tensors in 8-bit integers, rows
+// (rows.hip) An 8-bit matrix of R rows and n columns: rows of up(n, 128) bytes, zeros
+// past column n, and an fp32 scale for each row.
+struct RowQuantArgs {
+  int G, M, N;
+  const void* X;      // [G][M][N], row pitch ldx, group stride sX (elements)
+  long long ldx, sX;
+  uint8_t* Q;         // [G][M][up(N, 128)]
+  float* S;           // [G][M]
+  uint8_t* Qt;        // the transposes, [G][N][up(M, 128)]; nullptr: not wanted
+  float* St;
+  // set by launch_quantise_rows: strips' largest magnitudes [G][tn][M], [G][tm][N]
+  uint32_t *rowmost, *colmost;
+};
+size_t rows_quantise_workspace_bytes(int G, int M, int N);  // with the transposes
+hipError_t launch_quantise_rows(int bf16, const RowQuantArgs& a, void* ws, hipStream_t s);
+// C[g] = A[g] B[g]^T over Kd (strides as BlockGemmArgs's; of scales and biases in elements).
+struct RowGemmArgs {
+  int G, M, N, Kd;
+  const uint8_t* A;
+  long long sA;
+  const float* SA;
+  long long sSA;
+  const uint8_t* B;
+  long long sB;
+  const float* SB;
+  long long sSB;
+  const float* bias;  // [G][N], group stride sbias; nullptr: none
+  long long sbias;
+  void* C;
+  long long ldc, sC;
+  int out_bf16;
+  void* part;  // workspace: the ranges' sums [splits][G][M][N]
+  // set by launch_gemm_rows: ranges of `chunk` steps of 128
+  int splits, chunk;
+};
+size_t gemm_rows_workspace_bytes(int bf16, int G, int M, int N, int Kd);
+void gemm_rows_cut(int bf16, int G, int M, int N, int Kd, int cut[3]);  // tile, stages, ranges
+hipError_t launch_gemm_rows(RowGemmArgs a, hipStream_t s);
+
+// ---------------------------------------------------------------- layer norm
+// (norm.hip) Rows of X [G][M][N] normalised; weight and bias [G][N] (group strides; nullptr:
+// 1 and 0), mean and 1 / deviation [G][M].
+struct NormArgs {
+  int G, M, N;
+  const void* X;
+  long long ldx, sX;
+  const float *w, *b;
+  long long sw, sb;
+  float eps;
+  void* Y;
+  long long ldy, sY;
+  float *mean, *rstd;
+  int strip;  // set by launch_norm: rows a workgroup takes
+};
+hipError_t launch_norm(int x_bf16, int y_bf16, const NormArgs& a, hipStream_t s);
+// The gradients; dw and db (both or neither) [G][N].
+struct NormBackArgs {
+  int G, M, N;
+  const void* dY;     // of Y's type
+  long long ldg, sg;
+  const void* X;
+  long long ldx, sX;
+  const float *mean, *rstd;
+  const float* w;
+  long long sw;
+  void* dX;           // of X's type
+  long long ldd, sd;
+  float *dw, *db;
+  long long sdw, sdb;
+  // set by launch_norm_back: rows a workgroup takes, their number in a group, and its sums
+  // [G][strips][2][N]
+  int strip, strips;
+  float* part;
+};
+size_t norm_back_workspace_bytes(int G, int M, int N);
+hipError_t launch_norm_back(int x_bf16, int y_bf16, const NormBackArgs& a, void* ws, hipStream_t s);
+
+// ---------------------------------------------------------------- clipping
+// (clip.hip) A tensor of each of K replicas: matrices [M][N], row pitch ld, replica stride s.
+struct ClipTensor {
+  void* p;
+  long long M, N, ld, s;
+  int bf16;
+  int first;  // set by launch_clip: its first chunk of a replica's
+};
+size_t clip_workspace_bytes(int K, int count, const ClipTensor* t);
+// norm[k]: the root of the sum of squares over all the tensors of replica k; scale: where it is
+// finite and above `most`, they are multiplied by most / norm.
+hipError_t launch_clip(int K, int count, const ClipTensor* t, bool scale, double most, float* norm,
+                       void* ws, hipStream_t s);
+
 // ------------------------------------------------- orthogonalised momentum
 // (ortho.hip) G matrices [M][N] taken to their orthogonal factors; U set: the
 // update of W by the momentum U and the gradient X, else Y = O(X).

@@ -1,0 +1,452 @@
+// Layer norm of the rows of G matrices and its gradients.
+//
+// Forward: mean = sum x / N, d = x - mean, rstd = (sum d^2 / N + eps)^-1/2, y = d rstd w + b.
+// Both sums are held in fp64, and the mean in two floats: rows far from zero and
+// values whose squares leave fp32's range come out as exactly as others.
+// Backward, from the mean and rstd that the forward pass wrote: n = (x - mean) rstd, e = dy w,
+// dx = rstd (e - sum e / N - n sum (e n) / N), dw = sum over rows of dy n, db of dy.
+#include <algorithm>
+#include <type_traits>
+
+#include "device_common.h"
+#include "row_io.h"
+
+namespace lsgd {
+namespace {
+
+constexpr int kThreads = 256;
+
+// The sum over T threads of a row (T a power of two; wavefronts of a row's own from 64
+// on, all of the workgroup's above 64), in all of them; `room`: of K sums, a wavefront's each.
+template <int T, int K, class A>
+__device__ __forceinline__ void row_sums(A (&v)[K], A (*room)[K]) {
+#pragma unroll
+  for (int d = (T < 64 ? T : 64) / 2; d; d /= 2)
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d, 64);
+  if constexpr (T > 64) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();  // the last sums have been read
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < K; ++k) room[wave][k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      v[k] = room[0][k];
+#pragma unroll
+      for (int w = 1; w < T / 64; ++w) v[k] += room[w][k];
+    }
+  }
+}
+
+struct Moments {
+  float hi, lo, rstd;
+};
+__device__ __forceinline__ void split_mean(double mean, Moments& s) {
+  s.hi = (float)mean;
+  s.lo = (float)(mean - s.hi);
+}
+__device__ __forceinline__ float inverse_root(double mean_square, float eps) {
+  return (float)(1.0 / sqrt(mean_square + eps));
+}
+
+// A strip of rows a workgroup, T threads a row, V vectors of eight values each, in registers.
+template <bool XBF, bool YBF, int T, int V>
+__global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm(NormArgs a, int strips,
+                                                                      long long total) {
+  constexpr int kBlock = T < kThreads ? kThreads : T, kRows = kBlock / T;
+  __shared__ double room[kBlock / 64][1];
+  const unsigned id = workgroup_id();
+  if (id >= total) return;
+  const int g = id / strips, m0 = (id - g * strips) * a.strip;
+  const int t = threadIdx.x % T, end = min(a.M, m0 + a.strip);
+  float w[V][8], b[V][8];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int n = (t + i * T) * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[i][e] = 1.f, b[i][e] = 0.f;
+    if (a.w) load8<false>(a.w, g * a.sw + n, a.N - n, w[i]);
+    if (a.b) load8<false>(a.b, g * a.sb + n, a.N - n, b[i]);
+  }
+  for (int r = m0; r < end; r += kRows) {
+    const int m = r + threadIdx.x / T;
+    const bool in = m < end;
+    float x[V][8];
+    double s[1] = {0.0};
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int n = (t + i * T) * 8;
+      load8<XBF>(a.X, g * a.sX + m * a.ldx + n, in ? a.N - n : 0, x[i]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[0] += x[i][e];
+    }
+    row_sums<T>(s, room);
+    Moments mo;
+    const double mean = s[0] / a.N;
+    split_mean(mean, mo);
+    s[0] = 0.0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int n = (t + i * T) * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[i][e] = n + e < a.N ? (x[i][e] - mo.hi) - mo.lo : 0.f;
+        s[0] += (double)x[i][e] * x[i][e];
+      }
+    }
+    row_sums<T>(s, room);
+    mo.rstd = inverse_root(s[0] / a.N, a.eps);
+    if (in) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int n = (t + i * T) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] = __builtin_fmaf(x[i][e] * mo.rstd, w[i][e], b[i][e]);
+        store8<YBF>(a.Y, g * a.sY + m * a.ldy + n, a.N - n, x[i]);
+      }
+      if (t == 0) {
+        a.mean[(long long)g * a.M + m] = mo.hi;
+        a.rstd[(long long)g * a.M + m] = mo.rstd;
+      }
+    }
+  }
+}
+
+// Rows of any length: three passes over a row.
+constexpr int kLong = 1024;
+template <bool XBF, bool YBF>
+__global__ __launch_bounds__(kLong) void k_norm_long(NormArgs a, long long total) {
+  __shared__ double room[kLong / 64][1];
+  const unsigned id = workgroup_id();
+  if (id >= total) return;
+  const int g = id / a.M, m = id - g * a.M;
+  const long long x0 = g * a.sX + m * a.ldx;
+  float x[8];
+  double s[1] = {0.0};
+  for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
+    load8<XBF>(a.X, x0 + n, a.N - n, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[0] += x[e];
+  }
+  row_sums<kLong>(s, room);
+  Moments mo;
+  split_mean(s[0] / a.N, mo);
+  s[0] = 0.0;
+  for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
+    load8<XBF>(a.X, x0 + n, a.N - n, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float d = n + e < a.N ? (x[e] - mo.hi) - mo.lo : 0.f;
+      s[0] += (double)d * d;
+    }
+  }
+  row_sums<kLong>(s, room);
+  mo.rstd = inverse_root(s[0] / a.N, a.eps);
+  for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
+    float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, b[8] = {};
+    load8<XBF>(a.X, x0 + n, a.N - n, x);
+    if (a.w) load8<false>(a.w, g * a.sw + n, a.N - n, w);
+    if (a.b) load8<false>(a.b, g * a.sb + n, a.N - n, b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      x[e] = __builtin_fmaf(((x[e] - mo.hi) - mo.lo) * mo.rstd, w[e], b[e]);
+    store8<YBF>(a.Y, g * a.sY + m * a.ldy + n, a.N - n, x);
+  }
+  if (threadIdx.x == 0) {
+    a.mean[(long long)g * a.M + m] = mo.hi;
+    a.rstd[(long long)g * a.M + m] = mo.rstd;
+  }
+}
+
+// ---------------------------------------------------------------- backward
+// A strip of rows a workgroup; a thread keeps the sums of its columns over them. A: the
+// arithmetic of a row. Of rows of few columns little is left beside the two directions that are
+// taken out (of two columns eps / variance of e): those in fp64.
+constexpr int kNarrow = 8;
+template <bool XBF, bool YBF, int T, int V, class A>
+__global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm_back(NormBackArgs a,
+                                                                           long long total) {
+  constexpr int kBlock = T < kThreads ? kThreads : T, kRows = kBlock / T, kCols = T * V * 8;
+  __shared__ A room[kBlock / 64][2];
+  __shared__ float slots[kRows > 1 ? kRows * kCols : 1];
+  const unsigned id = workgroup_id();
+  if (id >= total) return;
+  const int g = id / a.strips, strip = id - g * a.strips, m0 = strip * a.strip;
+  const int t = threadIdx.x % T, slot = threadIdx.x / T, end = min(a.M, m0 + a.strip);
+  float w[V][8], dw[V][8], db[V][8];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int n = (t + i * T) * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[i][e] = 1.f, dw[i][e] = db[i][e] = 0.f;
+    if (a.w) load8<false>(a.w, g * a.sw + n, a.N - n, w[i]);
+  }
+  for (int r = m0; r < end; r += kRows) {
+    const int m = r + slot;
+    const bool in = m < end;
+    A x[V][8], dy[V][8];
+    A s[2] = {0, 0};
+    const A mean = in ? a.mean[(long long)g * a.M + m] : 0.f;
+    const A rstd = in ? a.rstd[(long long)g * a.M + m] : 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int n = (t + i * T) * 8;
+      float xf[8], df[8];
+      load8<XBF>(a.X, g * a.sX + m * a.ldx + n, in ? a.N - n : 0, xf);
+      load8<YBF>(a.dY, g * a.sg + m * a.ldg + n, in ? a.N - n : 0, df);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[i][e] = ((A)xf[e] - mean) * rstd;
+        dw[i][e] += df[e] * (float)x[i][e];
+        db[i][e] += df[e];
+        dy[i][e] = (A)df[e] * w[i][e];
+        s[0] += dy[i][e];
+        s[1] += dy[i][e] * x[i][e];
+      }
+    }
+    row_sums<T>(s, room);
+    const A c1 = s[0] / a.N, c2 = s[1] / a.N;
+    if (in) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int n = (t + i * T) * 8;
+        float d[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = (float)(rstd * (dy[i][e] - c1 - x[i][e] * c2));
+        store8<XBF>(a.dX, g * a.sd + m * a.ldd + n, a.N - n, d);
+      }
+    }
+  }
+  if (!a.dw) return;
+  // the rows' slots joined in order; one strip is the result itself
+  float* to_w = a.strips == 1 ? a.dw + g * a.sdw : a.part + (long long)id * 2 * a.N;
+  float* to_b = a.strips == 1 ? a.db + g * a.sdb : a.part + ((long long)id * 2 + 1) * a.N;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float* to = h ? to_b : to_w;
+    if constexpr (kRows == 1) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        store8<false>(to, (t + i * T) * 8, a.N - (t + i * T) * 8, h ? db[i] : dw[i]);
+    } else {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          slots[slot * kCols + (t + i * T) * 8 + e] = h ? db[i][e] : dw[i][e];
+      __syncthreads();
+      for (int n = threadIdx.x; n < a.N; n += kBlock) {
+        float sum = slots[n];
+#pragma unroll
+        for (int k = 1; k < kRows; ++k) sum += slots[k * kCols + n];
+        to[n] = sum;
+      }
+    }
+  }
+}
+
+// dw, db = the strips' sums in order: 64 columns a workgroup, a quarter of the strips a
+// wavefront. Columns g, (dw then db), n.
+__global__ __launch_bounds__(kThreads) void k_norm_join(NormBackArgs a, int tiles, long long total) {
+  __shared__ double room[4][64];
+  const unsigned id = workgroup_id();
+  if (id >= total) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int gh = id / tiles, g = gh / 2, h = gh & 1, n = (id - gh * tiles) * 64 + lane;
+  const int each = (a.strips + 3) / 4, k0 = wave * each, k1 = min(a.strips, k0 + each);
+  double sum = 0.0;
+  if (n < a.N)
+    for (int k = k0; k < k1; ++k) sum += a.part[(((long long)g * a.strips + k) * 2 + h) * a.N + n];
+  room[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && n < a.N)
+    (h ? a.db + g * a.sdb : a.dw + g * a.sdw)[n] =
+        (float)((room[0][lane] + room[1][lane]) + (room[2][lane] + room[3][lane]));
+}
+
+// Rows of any length: dx in two passes over a row, dw and db from a third, by columns.
+template <bool XBF, bool YBF>
+__global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long long total) {
+  __shared__ float room[kLong / 64][2];
+  const unsigned id = workgroup_id();
+  if (id >= total) return;
+  const int g = id / a.M, m = id - g * a.M;
+  const long long x0 = g * a.sX + m * a.ldx, d0 = g * a.sg + m * a.ldg;
+  const float mean = a.mean[id], rstd = a.rstd[id];
+  float s[2] = {0.f, 0.f}, x[8], dy[8];
+  auto take = [&](int n) __attribute__((always_inline)) {
+    float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    load8<XBF>(a.X, x0 + n, a.N - n, x);
+    load8<YBF>(a.dY, d0 + n, a.N - n, dy);
+    if (a.w) load8<false>(a.w, g * a.sw + n, a.N - n, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = (x[e] - mean) * rstd;
+      dy[e] *= w[e];
+    }
+  };
+  for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
+    take(n);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s[0] += dy[e];
+      s[1] += dy[e] * x[e];
+    }
+  }
+  row_sums<kLong>(s, room);
+  const float c1 = s[0] / a.N, c2 = s[1] / a.N;
+  for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
+    take(n);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = rstd * (dy[e] - c1 - x[e] * c2);
+    store8<XBF>(a.dX, g * a.sd + m * a.ldd + n, a.N - n, x);
+  }
+}
+// 512 columns of a strip a workgroup, every fourth row a wavefront.
+template <bool XBF, bool YBF>
+__global__ __launch_bounds__(kThreads) void k_norm_params(NormBackArgs a, int tiles, long long total) {
+  __shared__ float room[2][4][512];
+  const unsigned id = workgroup_id();
+  if (id >= total) return;
+  const int gs = id / tiles, g = gs / a.strips, m0 = (gs - g * a.strips) * a.strip;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, end = min(a.M, m0 + a.strip);
+  const int n0 = (id - gs * tiles) * 512, n = n0 + lane * 8;
+  float dw[8] = {}, db[8] = {};
+  for (int m = m0 + wave; m < end; m += 4) {
+    const float mean = a.mean[(long long)g * a.M + m], rstd = a.rstd[(long long)g * a.M + m];
+    float x[8], dy[8];
+    load8<XBF>(a.X, g * a.sX + m * a.ldx + n, a.N - n, x);
+    load8<YBF>(a.dY, g * a.sg + m * a.ldg + n, a.N - n, dy);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      dw[e] += dy[e] * ((x[e] - mean) * rstd);
+      db[e] += dy[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    room[0][wave][lane * 8 + e] = dw[e];
+    room[1][wave][lane * 8 + e] = db[e];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float* to = a.strips == 1 ? (h ? a.db + g * a.sdb : a.dw + g * a.sdw)
+                              : a.part + ((long long)gs * 2 + h) * a.N;
+    for (int c = threadIdx.x; c < 512 && n0 + c < a.N; c += kThreads)
+      to[n0 + c] = (room[h][0][c] + room[h][1][c]) + (room[h][2][c] + room[h][3][c]);
+  }
+}
+
+// ------------------------------------------------------------------ launches
+// Threads and vectors a row of N values takes; T == 0: any length.
+struct RowShape {
+  int T, V;
+};
+RowShape row_shape(int N) {
+  if (N <= 128) return {16, 1};
+  if (N <= 512) return {64, 1};
+  if (N <= 1024) return {64, 2};
+  if (N <= 2048) return {256, 1};
+  if (N <= 4096) return {256, 2};
+  if (N <= 8192) return {512, 2};
+  if (N <= 16384) return {1024, 2};
+  return {0, 0};
+}
+template <int T, int V>
+struct Shape {
+  static constexpr int t = T, v = V;
+};
+template <class F>
+hipError_t with_shape(int N, F f) {
+  const RowShape s = row_shape(N);
+  if (s.T == 16) return f(Shape<16, 1>{});
+  if (s.T == 64) return s.V == 1 ? f(Shape<64, 1>{}) : f(Shape<64, 2>{});
+  if (s.T == 256) return s.V == 1 ? f(Shape<256, 1>{}) : f(Shape<256, 2>{});
+  if (s.T == 512) return f(Shape<512, 2>{});
+  return f(Shape<1024, 2>{});
+}
+// Rows of a strip: about kStrips strips in all, of whole sets of rows at work at one time.
+constexpr long long kStrips = 1024;
+int strip_rows(int G, int M, int N) {
+  const RowShape s = row_shape(N);
+  const int each = s.T == 0 ? 4 : std::max(1, kThreads / s.T);
+  const long long strips = std::max(1LL, kStrips / G);
+  const long long rows = (M + strips - 1) / strips;
+  return (int)((rows + each - 1) / each * each);
+}
+
+template <bool XBF, bool YBF>
+hipError_t norm(NormArgs a, hipStream_t s) {
+  if (row_shape(a.N).T == 0) {
+    const long long total = (long long)a.G * a.M;
+    if (total > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((k_norm_long<XBF, YBF>), grid_of(total), dim3(kLong), 0, s, a, total);
+    return hipGetLastError();
+  }
+  a.strip = strip_rows(a.G, a.M, a.N);
+  const int strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
+  const long long total = (long long)strips * a.G;
+  return with_shape(a.N, [&](auto z) {
+    constexpr int T = decltype(z)::t, V = decltype(z)::v;
+    hipLaunchKernelGGL((k_norm<XBF, YBF, T, V>), grid_of(total), dim3(T < kThreads ? kThreads : T),
+                       0, s, a, strips, total);
+    return hipGetLastError();
+  });
+}
+
+template <bool XBF, bool YBF>
+hipError_t norm_back(NormBackArgs a, void* ws, hipStream_t s) {
+  a.strip = strip_rows(a.G, a.M, a.N);
+  a.strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
+  a.part = (float*)ws;
+  const long long strips = (long long)a.strips * a.G;
+  hipError_t e;
+  if (row_shape(a.N).T == 0) {
+    const long long total = (long long)a.G * a.M, tiles = (a.N + 511LL) / 512;
+    if (total > 0x7fffffffLL || tiles * strips > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((k_norm_back_long<XBF, YBF>), grid_of(total), dim3(kLong), 0, s, a, total);
+    if ((e = hipGetLastError()) != hipSuccess || !a.dw) return e;
+    hipLaunchKernelGGL((k_norm_params<XBF, YBF>), grid_of(tiles * strips), dim3(kThreads), 0, s, a,
+                       (int)tiles, tiles * strips);
+    e = hipGetLastError();
+  } else if (a.N <= kNarrow) {
+    hipLaunchKernelGGL((k_norm_back<XBF, YBF, 16, 1, double>), grid_of(strips), dim3(kThreads), 0, s,
+                       a, strips);
+    e = hipGetLastError();
+  } else {
+    e = with_shape(a.N, [&](auto z) {
+      constexpr int T = decltype(z)::t, V = decltype(z)::v;
+      hipLaunchKernelGGL((k_norm_back<XBF, YBF, T, V, float>), grid_of(strips),
+                         dim3(T < kThreads ? kThreads : T), 0, s, a, strips);
+      return hipGetLastError();
+    });
+  }
+  if (e != hipSuccess || !a.dw || a.strips == 1) return e;
+  const long long tiles = (a.N + 63LL) / 64, total = tiles * 2 * a.G;
+  if (total > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k_norm_join, grid_of(total), dim3(kThreads), 0, s, a, (int)tiles, total);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm(int x_bf16, int y_bf16, const NormArgs& a, hipStream_t s) {
+  if (x_bf16) return y_bf16 ? norm<true, true>(a, s) : norm<true, false>(a, s);
+  return y_bf16 ? norm<false, true>(a, s) : norm<false, false>(a, s);
+}
+
+size_t norm_back_workspace_bytes(int G, int M, int N) {
+  const long long strip = strip_rows(G, M, N), strips = (M + strip - 1) / strip;
+  return strips == 1 ? 0 : (size_t)G * strips * 2 * N * sizeof(float);
+}
+
+hipError_t launch_norm_back(int x_bf16, int y_bf16, const NormBackArgs& a, void* ws, hipStream_t s) {
+  if (x_bf16) return y_bf16 ? norm_back<true, true>(a, ws, s) : norm_back<true, false>(a, ws, s);
+  return y_bf16 ? norm_back<false, true>(a, ws, s) : norm_back<false, false>(a, ws, s);
+}
+
+}  // namespace lsgd

@@ -1,0 +1,561 @@
+// Tensors in 8-bit integers with an fp32 scale for each row, and the grouped product
+// of two of them.
+//
+// A row's scale s is max |x| / 127, rounded to fp32, at least 2^-126 (then 1 / s and
+// s / 2 are exact enough to work with), 1 for a row of zeros, and a NaN for a row that
+// holds an infinity or a NaN, whose integers are zeros: every product that reads the
+// row shows it. An element is the integer nearest to x / s, ties to even.
+#include <algorithm>
+#include <cmath>
+
+#include "row_io.h"
+#include "tile_loop.h"
+
+namespace lsgd {
+namespace {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// vectors at any element's alignment
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+constexpr int kThreads = 256;
+constexpr uint32_t kInf = 0x7f800000u;
+
+// ---------------------------------------------------------------- quantise
+// Magnitudes are compared as the bits of |x|: infinities and NaN are then the largest.
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ float scale_of(uint32_t most) {
+  if (most == 0) return 1.f;
+  if (most >= kInf) return __uint_as_float(0x7fc00000u);
+  return fmaxf(__uint_as_float(most) / 127.f, 0x1p-126f);
+}
+// The integers nearest to v / s. x (1 / s) is off by less than 2^-15, so that it rounds to the
+// wrong neighbour only next to the middle between two, and there the remainder
+// x - q s, which is exact in fp32 (|x| and s below 2^128, at most 24 bits between its
+// first and last), is at least s / 2: then, rarely, the tie or the neighbour is settled.
+// Everything is zero for a NaN in place of s.
+__device__ __forceinline__ u32x2 pack8(const float (&v)[8], float s) {
+  const float r = 1.f / s, half = 0.5f * s;
+  float q[8], far = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    q[i] = __builtin_rintf(v[i] * r);
+    far = fmaxf(far, fabsf(__builtin_fmaf(-q[i], s, v[i])));
+  }
+  if (far >= half) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float rest = __builtin_fmaf(-q[i], s, v[i]);
+      const bool odd = ((int)q[i] & 1) != 0;
+      if (fabsf(rest) > half || (fabsf(rest) == half && odd)) q[i] += rest > 0.f ? 1.f : -1.f;
+    }
+  }
+  const bool none = !(s == s);
+  u32x2 w = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)(int)q[i] & 255u) << (8 * (i % 4));
+  return none ? u32x2{0u, 0u} : w;
+}
+
+// The largest of T lanes' values (T a power of two up to 64), in all of them.
+template <int T>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t m) {
+#pragma unroll
+  for (int d = T / 2; d; d /= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d, T));
+  return m;
+}
+
+// Rows alone: T threads a row, V vectors of eight values each, all in registers, or
+// (V == 0) in two passes of any length.
+template <bool BF, int T, int V>
+__global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_rows(RowQuantArgs a,
+                                                                      long long rows) {
+  constexpr int kBlock = T < kThreads ? kThreads : T, kRows = kBlock / T, kWaves = kBlock / 64;
+  __shared__ uint32_t most[T > 64 ? kWaves : 1];
+  const int t = threadIdx.x % T;
+  const long long row = (long long)workgroup_id() * kRows + threadIdx.x / T;
+  if (T >= 64 && row >= rows) return;  // (whole wavefronts, and all of a row's)
+  const long long g = row / a.M, m = row - g * a.M;
+  const long long x = g * a.sX + m * a.ldx;
+  const int vecs = (a.N + 127) / 128 * 16;  // of eight
+  const bool in = row < rows;
+  uint32_t top = 0;
+  float v[V ? V : 1][8];
+  auto take = [&](int k, float(&w)[8]) __attribute__((always_inline)) {
+    load8<BF>(a.X, x + k * 8LL, in ? a.N - k * 8 : 0, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude(w[i]));
+  };
+  if constexpr (V > 0) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) take(t + i * T, v[i]);
+  } else {
+    for (int k = t; k < vecs; k += T) take(k, v[0]);
+  }
+  top = lanes_max<(T < 64 ? T : 64)>(top);
+  if constexpr (T > 64) {
+    if (threadIdx.x % 64 == 0) most[threadIdx.x / 64] = top;
+    __syncthreads();
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) top = max(top, most[i]);
+  }
+  const float s = scale_of(top);
+  if (!in) return;
+  u32x2* q = (u32x2*)(a.Q + row * (vecs * 8LL));
+  if constexpr (V > 0) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (t + i * T < vecs) q[t + i * T] = pack8(v[i], s);
+  } else {
+    for (int k = t; k < vecs; k += T) {
+      load8<BF>(a.X, x + k * 8LL, a.N - k * 8, v[0]);
+      q[k] = pack8(v[0], s);
+    }
+  }
+  if (t == 0) a.S[row] = s;
+}
+
+// Both ways, in three launches: the largest magnitudes of strips of kStripRows rows by 512
+// columns, the scales from those, and the integers of 128 x 128 tiles from a second
+// read of X.
+constexpr int kStripRows = 512, kStripCols = 512;
+
+// Wavefront w of a strip takes its rows w, w + 4, ..., a lane eight columns.
+template <bool BF>
+__global__ __launch_bounds__(kThreads) void k_rows_most(RowQuantArgs a, int tm, int tn, int total) {
+  __shared__ uint32_t most[4][kStripCols];
+  const unsigned id = workgroup_id();
+  if (id >= (unsigned)total) return;
+  const int g = id / (tm * tn), mt = id % (tm * tn) / tn, nt = id % tn;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int n = nt * kStripCols + lane * 8, m0 = mt * kStripRows;
+  const int end = min(a.M, m0 + kStripRows);
+  uint32_t cm[8] = {};
+  for (int m = m0 + wave; m < end; m += 4) {
+    float v[8];
+    load8<BF>(a.X, g * a.sX + m * a.ldx + n, a.N - n, v);
+    uint32_t rm = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t b = magnitude(v[i]);
+      rm = max(rm, b);
+      cm[i] = max(cm[i], b);
+    }
+    rm = lanes_max<64>(rm);
+    if (lane == 0) a.rowmost[((long long)g * tn + nt) * a.M + m] = rm;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most[wave][lane * 8 + i] = cm[i];
+  __syncthreads();
+  for (int c = threadIdx.x; c < kStripCols; c += kThreads)
+    if (nt * kStripCols + c < a.N)
+      a.colmost[((long long)g * tm + mt) * a.N + nt * kStripCols + c] =
+          max(max(most[0][c], most[1][c]), max(most[2][c], most[3][c]));
+}
+
+// The scales of the rows (g, m), then of the columns (g, n).
+__global__ __launch_bounds__(kThreads) void k_rows_scales(RowQuantArgs a, int tm, int tn) {
+  const long long i = (long long)workgroup_id() * kThreads + threadIdx.x;
+  const long long rows = (long long)a.G * a.M, cols = (long long)a.G * a.N;
+  if (i >= rows + cols) return;
+  const bool row = i < rows;
+  const long long j = row ? i : i - rows;
+  const int each = row ? a.M : a.N, parts = row ? tn : tm;
+  const long long g = j / each;
+  const uint32_t* p = (row ? a.rowmost : a.colmost) + g * parts * each + (j - g * each);
+  uint32_t top = 0;
+  for (int k = 0; k < parts; ++k) top = max(top, p[(long long)k * each]);
+  (row ? a.S : a.St)[j] = scale_of(top);
+}
+
+// Rows of 128 bytes; piece k of 16 lies in slot k ^ (row / 8 % 8), which spreads the rows,
+// eight apart, that a wavefront writes at once over the banks.
+__device__ __forceinline__ int turned(int row, int byte) {
+  return row * 128 + (byte ^ (row / 8 % 8 * 16));
+}
+// A tile of 128 x 128: thread t holds eight rows from 8 (t / 16) and eight columns from
+// 8 (t % 16); the transpose's bytes are turned in LDS, so that each of its rows leaves
+// as a whole line.
+template <bool BF>
+__global__ __launch_bounds__(kThreads) void k_rows_both(RowQuantArgs a, int tm, int tn, int total) {
+  __shared__ __align__(16) uint8_t turn[128 * 128];
+  const unsigned id = workgroup_id();
+  if (id >= (unsigned)total) return;
+  const int l = xcd_order(id, total);
+  const int g = l / (tm * tn), mt = l % (tm * tn) / tn, nt = l % tn;
+  const int tid = threadIdx.x, c = tid & 15, rg = tid >> 4;
+  const int n0 = nt * 128, m0 = mt * 128, n = n0 + c * 8, r0 = m0 + rg * 8;
+  float v[8][8];
+#pragma unroll
+  for (int p = 0; p < 8; ++p)
+    load8<BF>(a.X, g * a.sX + (r0 + p) * a.ldx + n, r0 + p < a.M ? a.N - n : 0, v[p]);
+  const long long ldq = (a.N + 127) / 128 * 128, ldt = (a.M + 127) / 128 * 128;
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    if (r0 + p >= a.M) continue;
+    const long long row = (long long)g * a.M + r0 + p;
+    *(u32x2*)(a.Q + row * ldq + n) = pack8(v[p], a.S[row]);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float w[8] = {v[0][i], v[1][i], v[2][i], v[3][i], v[4][i], v[5][i], v[6][i], v[7][i]};
+    const float s = a.St[(long long)g * a.N + min(n + i, a.N - 1)];
+    *(u32x2*)(turn + turned(c * 8 + i, rg * 8)) = pack8(w, s);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int at = i * kThreads + tid, j = at >> 3, k = (at & 7) * 16;
+    if (n0 + j < a.N)
+      *(u32x4*)(a.Qt + ((long long)g * a.N + n0 + j) * ldt + m0 + k) =
+          *(const u32x4*)(turn + turned(j, k));
+  }
+}
+
+template <bool BF>
+hipError_t quantise(RowQuantArgs a, void* ws, hipStream_t s) {
+  if (!a.Qt) {
+    const long long rows = (long long)a.G * a.M;
+    auto launch = [&](auto kernel, int per, int threads) {
+      const long long n = (rows + per - 1) / per;
+      if (n > 0x7fffffffLL) return hipErrorInvalidValue;
+      hipLaunchKernelGGL(kernel, grid_of(n), dim3(threads), 0, s, a, rows);
+      return hipGetLastError();
+    };
+    if (a.N <= 128) return launch(k_rows<BF, 16, 1>, 16, 256);
+    if (a.N <= 512) return launch(k_rows<BF, 64, 1>, 4, 256);
+    if (a.N <= 1024) return launch(k_rows<BF, 64, 2>, 4, 256);
+    if (a.N <= 2048) return launch(k_rows<BF, 64, 4>, 4, 256);
+    if (a.N <= 4096) return launch(k_rows<BF, 256, 2>, 1, 256);
+    if (a.N <= 8192) return launch(k_rows<BF, 256, 4>, 1, 256);
+    if (a.N <= 16384) return launch(k_rows<BF, 1024, 2>, 1, 1024);
+    return launch(k_rows<BF, 1024, 0>, 1, 1024);
+  }
+  const long long tm = (a.M + kStripRows - 1LL) / kStripRows, tn = (a.N + kStripCols - 1LL) / kStripCols;
+  const long long bm = (a.M + 127LL) / 128, bn = (a.N + 127LL) / 128;
+  if (bm * bn > 0x7fffffffLL / a.G) return hipErrorInvalidValue;
+  a.rowmost = (uint32_t*)ws;
+  a.colmost = a.rowmost + a.G * tn * a.M;
+  hipLaunchKernelGGL((k_rows_most<BF>), grid_of(tm * tn * a.G), dim3(kThreads), 0, s, a, (int)tm,
+                     (int)tn, (int)(tm * tn * a.G));
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const long long scales = (long long)a.G * ((long long)a.M + a.N);
+  hipLaunchKernelGGL(k_rows_scales, grid_of((scales + kThreads - 1) / kThreads), dim3(kThreads), 0,
+                     s, a, (int)tm, (int)tn);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL((k_rows_both<BF>), grid_of(bm * bn * a.G), dim3(kThreads), 0, s, a, (int)bm,
+                     (int)bn, (int)(bm * bn * a.G));
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------ product
+// v_mfma_i32_16x16x64_i8 twice a step of 128: exact sums in 32 bits. |q| <= 128, so a sum of
+// 2^17 - 1 products fits; a longer inner dimension is cut into ranges whose sums are joined in
+// 64 bits. Lane l holds 16 of a step half's 64 k for row l % 16, the same ones of both operands. The
+// first operand is B's rows, so that a lane's four results are neighbours in a row of C.
+constexpr int kMostSteps = 1020;  // of 128: below 2^17, a multiple of four
+
+struct MacRows {
+  struct Next {};
+  typedef Frag P;
+  typedef Frag Q;
+  typedef v4i Acc;
+  static constexpr int kEvenLoads = 0;
+  __device__ __forceinline__ void load(uint8_t*, int, bool) const {}
+  __device__ __forceinline__ void begin(const uint8_t*, int, Next&) const {}
+  __device__ __forceinline__ void take(const Next&) const {}
+  __device__ __forceinline__ void last(bool) const {}
+  template <int PH>
+  __device__ __forceinline__ P p(const Frag& f, int) const { return f; }
+  template <int PH>
+  __device__ __forceinline__ Q q(const Frag& f, int, const Next&) const { return f; }
+  template <int PH>
+  __device__ __forceinline__ void mac(v4i& c, const P& p, int, const Q& q, int) const {
+    c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_shufflevector(p, p, 0, 1, 2, 3),
+                                              __builtin_shufflevector(q, q, 0, 1, 2, 3), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_shufflevector(p, p, 4, 5, 6, 7),
+                                              __builtin_shufflevector(q, q, 4, 5, 6, 7), c, 0, 0, 0);
+  }
+};
+
+// sum sa sb + bias. The smaller scale comes first: a sum of integers times it stays in
+// range wherever the result does. (Both scales are taken once, a NaN among them too.)
+__device__ __forceinline__ float scaled(float sum, float sa, float sb, float bias) {
+  const float lo = sa < sb ? sa : sb, hi = sa < sb ? sb : sa;
+  return __builtin_fmaf(sum * lo, hi, bias);
+}
+
+// Eight neighbours of a row of C from LDS, n of them.
+template <int SIZE>
+__device__ __forceinline__ void copy8(void* C, long long at, const uint8_t* from, int n) {
+  if constexpr (SIZE == 2) {
+    bf16_t* c = (bf16_t*)C + at;
+    if (n >= 8) {
+      *(u32x4_any*)c = *(const u32x4*)from;
+    } else {
+      for (int e = 0; e < n; ++e) c[e] = ((const bf16_t*)from)[e];
+    }
+  } else {
+    float* c = (float*)C + at;
+    if (n >= 8) {
+      *(v4f_any*)c = *(const v4f*)from;
+      *(v4f_any*)(c + 4) = *(const v4f*)(from + 16);
+    } else {
+      for (int e = 0; e < n; ++e) c[e] = ((const float*)from)[e];
+    }
+  }
+}
+
+enum { kOutFp32 = 0, kOutBf16 = 1, kOutSums = 2 };
+
+// Tiles of C by way of LDS, so that whole rows of a tile leave at once: a group of each
+// wavefront's columns at a time, half of their rows in each of two stages (a pitch of 16
+// bytes more than a row spreads the sixteen rows that a wavefront writes at once over the banks).
+// `ends`: the scales of B's rows, their biases, the scales of A's rows.
+template <int OUT, int THREADS, class T>
+__device__ __forceinline__ void tile_out(const T& t, const v4i (&acc)[T::FP][T::FQ],
+                                         const float* ends, uint8_t* s0, uint8_t* s1, void* C,
+                                         long long row0, long long ldc, int np, int nq) {
+  constexpr int kSize = OUT == kOutBf16 ? 2 : 4, kPitch = T::kP * kSize + 16;
+  constexpr int kAcross = T::kQ / (T::FQ * 16);  // wavefronts along A's rows
+  constexpr int kFit = T::kStage / kPitch * 2 / (kAcross * 16);
+  constexpr int kGroup = kFit >= T::FQ ? T::FQ : (kFit >= 2 ? 2 : 1);  // columns of blocks at a time
+  constexpr int kRows = kAcross * kGroup * 16, kHalf = kRows / 2;
+  static_assert(kHalf * kPitch <= T::kStage && T::FQ % kGroup == 0, "half a group fits a stage");
+  auto at = [&](int r, int p) __attribute__((always_inline)) {
+    return (r < kHalf ? s0 : s1) + r % kHalf * kPitch + p * kSize;
+  };
+  const int lane = t.lane, p0 = t.wp + (lane >> 4) * 4, side = t.wq / (T::FQ * 16);
+#pragma unroll
+  for (int j0 = 0; j0 < T::FQ; j0 += kGroup) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int j = j0; j < j0 + kGroup; ++j) {
+      const float sa = ends[2 * T::kP + t.wq + j * 16 + (lane & 15)];
+#pragma unroll
+      for (int i = 0; i < T::FP; ++i) {
+        uint8_t* to = at((side * kGroup + j - j0) * 16 + (lane & 15), p0 + i * 16);
+        const v4i v = acc[i][j];
+        if constexpr (OUT == kOutSums) {
+          *(v4i*)to = v;
+        } else {
+          const v4f sb = *(const v4f*)(ends + p0 + i * 16);
+          const v4f b = *(const v4f*)(ends + T::kP + p0 + i * 16);
+          v4f f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = scaled((float)v[e], sa, sb[e], b[e]);
+          if constexpr (OUT == kOutBf16)
+            *(u32x2*)to = u32x2{f32_to_bf16(f[0]) | (uint32_t)f32_to_bf16(f[1]) << 16,
+                                f32_to_bf16(f[2]) | (uint32_t)f32_to_bf16(f[3]) << 16};
+          else
+            *(v4f*)to = f;
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll 2
+    for (int u = threadIdx.x; u < T::kP * kRows / 8; u += THREADS) {
+      const int r = u / (T::kP / 8), p = u % (T::kP / 8) * 8;
+      const int q = r / (kGroup * 16) * T::FQ * 16 + j0 * 16 + r % (kGroup * 16);
+      if (q < nq && p < np) copy8<kSize>(C, row0 + (long long)q * ldc + p, at(r, p), np - p);
+    }
+  }
+}
+
+// The tile of BP rows of B and BQ rows of A, over one of `splits` ranges of the inner
+// dimension (chunk steps each); OUT == kOutSums: a range's sums go to `part`.
+template <int OUT, int BP, int BQ, int WP, int WQ, int S>
+__global__ __launch_bounds__((64 * (BP / WP) * (BQ / WQ)), 2) void k_rows_tile(RowGemmArgs a, int tp,
+                                                                               int tq, int total) {
+  using T = TileLoop<BP, BQ, WP, WQ, S>;
+  LSGD_TILE_STAGES(st, S, T::kStage);
+  __shared__ __align__(16) float ends[2 * BP + BQ];
+  const unsigned id = workgroup_id();
+  if (id >= (unsigned)total) return;
+  int l = xcd_order(id, total);
+  const int sg = l / (tp * tq), g = sg % a.G, split = sg / a.G;
+  int pt, qt;
+  band_order(l % (tp * tq), tp, tq, pt, qt);
+  const int p0 = pt * BP, q0 = qt * BQ;
+  const int nb = (a.Kd + 127) / 128, ld = nb * 128;
+  const int k0 = split * a.chunk, steps = min(a.chunk, nb - k0);
+  T t;
+  t.init(a.B + (long long)g * a.sB + (long long)p0 * ld, a.A + (long long)g * a.sA + (long long)q0 * ld,
+         ld, a.N - p0, a.M - q0);
+  t.skip(k0);
+  if constexpr (OUT != kOutSums) {
+    // scales and biases straight to LDS, ahead of the tiles (loads return in order); zeros
+    // past the last row, and for no bias
+    constexpr int kParts = (2 * BP + BQ) / 64;
+#pragma unroll
+    for (int i = 0; i < (kParts + T::kWaves - 1) / T::kWaves; ++i) {
+      const int part = t.wave + i * T::kWaves;
+      if (part < kParts) {
+        const int at = part * 64;
+        const float* from = at < BP ? a.SB + g * a.sSB + p0
+                                    : (at < 2 * BP ? a.bias + g * a.sbias + p0 : a.SA + g * a.sSA + q0);
+        const int skip = at < BP ? at : (at < 2 * BP ? at - BP : at - 2 * BP);
+        int left = (at < 2 * BP ? min(a.N - p0, BP) : min(a.M - q0, BQ)) - skip;
+        if (at >= BP && at < 2 * BP && !a.bias) left = 0;
+        const __amdgpu_buffer_rsrc_t b = __builtin_amdgcn_make_buffer_rsrc(
+            (void*)(from + skip), 0, max(left, 0) * 4, kRsrcRaw);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            b, (__attribute__((address_space(3))) void*)(ends + at), 4, t.lane * 4, 0, 0, 0);
+      }
+    }
+  }
+  MacRows mac;
+  v4i acc[T::FP][T::FQ] = {};
+  t.run(st, steps, mac, acc);
+  if constexpr (OUT == kOutSums)
+    tile_out<OUT, T::kThreads>(t, acc, ends, st[0], st[1], a.part,
+                               ((long long)sg * a.M + q0) * a.N + p0, a.N, a.N - p0, a.M - q0);
+  else
+    tile_out<OUT, T::kThreads>(t, acc, ends, st[0], st[1], a.C,
+                               (long long)g * a.sC + (long long)q0 * a.ldc + p0, a.ldc, a.N - p0,
+                               a.M - q0);
+}
+
+// C = the ranges' sums, four neighbours a thread.
+template <bool OUTBF>
+__global__ __launch_bounds__(kThreads) void k_rows_join(RowGemmArgs a, int quads, long long total) {
+  const long long i = (long long)workgroup_id() * kThreads + threadIdx.x;
+  if (i >= total) return;
+  const long long row = i / quads, g = row / a.M, m = row - g * a.M;
+  const int n = (int)(i - row * quads) * 4, left = min(4, a.N - n);
+  const long long each = (long long)a.G * a.M * a.N;
+  const int* p = (const int*)a.part + row * a.N + n;
+  long long sum[4] = {};
+  for (int s = 0; s < a.splits; ++s, p += each)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) sum[e] += p[e];
+  const float sa = a.SA[g * a.sSA + m];
+  const long long at = g * a.sC + m * a.ldc + n;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e >= left) break;
+    const float f = scaled((float)sum[e], sa, a.SB[g * a.sSB + n + e],
+                           a.bias ? a.bias[g * a.sbias + n + e] : 0.f);
+    if constexpr (OUTBF)
+      ((bf16_t*)a.C)[at + e] = f32_to_bf16(f);
+    else
+      ((float*)a.C)[at + e] = f;
+  }
+}
+
+// ------------------------------------------------------------------ launches
+constexpr int kCus = 256;
+long long tiles_of(int G, int M, int N, long long b) {
+  return (N + b - 1) / b * ((M + b - 1) / b) * G;
+}
+
+// Ranges of the inner dimension: as many as leave the least estimated time where 64 x 64
+// tiles leave compute units idle (see blocks.hip's), and as many as its length needs.
+struct RowCut {
+  int tile, stages, splits, chunk;
+};
+RowCut row_cut(bool bf16, int G, int M, int N, int Kd) {
+  const int nb = (Kd + 127) / 128;
+  RowCut c{0, 0, 1, nb};
+  const long long tiles = tiles_of(G, M, N, 64);
+  const double bytes = (double)G * ((double)M + N) * nb * 128 / 5e6;
+  const double sums = 2.0 * G * M * N * sizeof(int) / 4e6;
+  double least = std::max(0.18 * nb, bytes);
+  for (int s = 2; s <= 64 && tiles * s <= 2 * kCus && nb >= 4 * s; s *= 2) {
+    const double t = std::max(0.18 * nb / s, bytes) + 4 + sums * s;
+    if (t < least) {
+      c.splits = s;
+      least = t;
+    }
+  }
+  const bool few = c.splits > 1;
+  c.splits = std::max(c.splits, (nb + kMostSteps - 1) / kMostSteps);
+  c.chunk = (nb + c.splits - 1) / c.splits;
+  c.splits = (nb + c.chunk - 1) / c.chunk;
+  const RowCut cuts[4] = {{64, 4}, {128, 4}, {128, 2}, {256, 2}};
+  const int per_cu[4] = {2, 1, 2, 1};
+  const double each[4] = {1.6, 4.5, 3.8, 12.6};
+  int at = 0;
+  for (int i = 0; i < (few ? 1 : 4); ++i) {
+    const double rounds = std::ceil((double)tiles_of(G, M, N, cuts[i].tile) * c.splits /
+                                    (kCus * per_cu[i]));
+    const double t = rounds * per_cu[i] * each[i];
+    if (i == 0 || t < least) {
+      at = i;
+      least = t;
+    }
+  }
+  c.tile = cuts[at].tile;
+  c.stages = cuts[at].stages;
+  return c;
+}
+
+template <int OUT, int B, int W, int S>
+hipError_t launch_tile(const RowGemmArgs& a, hipStream_t s) {
+  constexpr int WP = B == 256 ? 128 : B / 2;
+  const long long tp = (a.N + B - 1LL) / B, tq = (a.M + B - 1LL) / B;
+  if (tp * tq > 0x7fffffffLL / a.G / a.splits) return hipErrorInvalidValue;
+  const long long total = tp * tq * a.G * a.splits;
+  hipLaunchKernelGGL((k_rows_tile<OUT, B, B, WP, W, S>), grid_of(total),
+                     dim3(64 * (B / WP) * (B / W)), 0, s, a, (int)tp, (int)tq, (int)total);
+  return hipGetLastError();
+}
+template <int OUT>
+hipError_t gemm_tiles(const RowGemmArgs& a, const RowCut& c, hipStream_t s) {
+  if (c.tile == 64) return launch_tile<OUT, 64, 32, 4>(a, s);
+  if (c.tile == 128 && c.stages == 4) return launch_tile<OUT, 128, 32, 4>(a, s);
+  if (c.tile == 128) return launch_tile<OUT, 128, 64, 2>(a, s);
+  return launch_tile<OUT, 256, 64, 2>(a, s);
+}
+
+}  // namespace
+
+size_t rows_quantise_workspace_bytes(int G, int M, int N) {
+  const size_t tm = ((size_t)M + kStripRows - 1) / kStripRows;
+  const size_t tn = ((size_t)N + kStripCols - 1) / kStripCols;
+  return ((size_t)G * tn * M + (size_t)G * tm * N) * sizeof(uint32_t);
+}
+
+hipError_t launch_quantise_rows(int bf16, const RowQuantArgs& a, void* ws, hipStream_t s) {
+  return bf16 ? quantise<true>(a, ws, s) : quantise<false>(a, ws, s);
+}
+
+size_t gemm_rows_workspace_bytes(int bf16, int G, int M, int N, int Kd) {
+  const RowCut c = row_cut(bf16, G, M, N, Kd);
+  return c.splits == 1 ? 0 : (size_t)c.splits * G * M * N * sizeof(int);
+}
+
+void gemm_rows_cut(int bf16, int G, int M, int N, int Kd, int cut[3]) {
+  const RowCut c = row_cut(bf16, G, M, N, Kd);
+  cut[0] = c.tile;
+  cut[1] = c.stages;
+  cut[2] = c.splits;
+}
+
+hipError_t launch_gemm_rows(RowGemmArgs a, hipStream_t s) {
+  const RowCut c = row_cut(a.out_bf16, a.G, a.M, a.N, a.Kd);
+  a.splits = c.splits;
+  a.chunk = c.chunk;
+  if (a.splits == 1)
+    return a.out_bf16 ? gemm_tiles<kOutBf16>(a, c, s) : gemm_tiles<kOutFp32>(a, c, s);
+  const hipError_t e = gemm_tiles<kOutSums>(a, c, s);
+  if (e != hipSuccess) return e;
+  const int quads = (a.N + 3) / 4;
+  const long long total = (long long)a.G * a.M * quads;
+  if ((total + kThreads - 1) / kThreads > 0x7fffffffLL) return hipErrorInvalidValue;
+  if (a.out_bf16)
+    hipLaunchKernelGGL((k_rows_join<true>), grid_of((total + kThreads - 1) / kThreads),
+                       dim3(kThreads), 0, s, a, quads, total);
+  else
+    hipLaunchKernelGGL((k_rows_join<false>), grid_of((total + kThreads - 1) / kThreads),
+                       dim3(kThreads), 0, s, a, quads, total);
+  return hipGetLastError();
+}
+
+}  // namespace lsgd

@@ -112,6 +112,20 @@ _SIGS = {
     "lsgd_orthogonal_update": [_I, _I, _I, _I, _P, _L, _L, _P, _L, _L, _P, _L, _L, _c.c_float,
                                _c.c_float, _c.c_float, _I, _c.c_float, _I,
                                _c.POINTER(_c.c_float), _c.c_float, _P, _c.c_size_t, _P],
+    "lsgd_quantise_rows_workspace_bytes": [_I, _I, _I, _c.POINTER(_c.c_size_t)],
+    "lsgd_quantise_rows": [_I, _I, _I, _I, _P, _L, _L, _P, _P, _P, _P, _P, _c.c_size_t, _P],
+    "lsgd_grouped_gemm_rows_workspace_bytes": [_I, _I, _I, _I, _I, _c.POINTER(_c.c_size_t)],
+    "lsgd_grouped_gemm_rows_cut": [_I, _I, _I, _I, _I, _P],
+    "lsgd_grouped_gemm_rows": [_I, _I, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P, _L, _P, _L,
+                               _P, _L, _L, _P, _c.c_size_t, _P],
+    "lsgd_layer_norm": [_I, _I, _I, _I, _I, _P, _L, _L, _P, _L, _P, _L, _c.c_float, _P, _L, _L,
+                        _P, _P, _P],
+    "lsgd_layer_norm_backward_workspace_bytes": [_I, _I, _I, _c.POINTER(_c.c_size_t)],
+    "lsgd_layer_norm_backward": [_I, _I, _I, _I, _I, _P, _L, _L, _P, _L, _L, _P, _P, _P, _L,
+                                 _P, _L, _L, _P, _L, _P, _L, _P, _c.c_size_t, _P],
+    "lsgd_gradient_norm_workspace_bytes": [_I, _I, _P, _c.POINTER(_c.c_size_t)],
+    "lsgd_gradient_norm": [_I, _I, _P, _P, _P, _c.c_size_t, _P],
+    "lsgd_clip_gradients": [_I, _I, _P, _c.c_double, _P, _P, _c.c_size_t, _P],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -825,3 +839,319 @@ def orthogonal_update(W: torch.Tensor, U: torch.Tensor, G: torch.Tensor, lr: flo
              w, ldw, sW, u, ldu, sU, g, ldg, sG, float(lr),
              float(momentum), float(weight_decay), int(bool(nesterov)), float(scale), int(steps),
              co, float(eps), ws.data_ptr(), ws.numel())
+
+
+# -- large layers: products in 8-bit integers, layer norm, clipping --------
+class Rows(NamedTuple):
+    """G matrices of M rows and n columns in 8-bit integers with a scale for each row (the
+    layout of lsgd_quantise_rows): q [G][M][up(n, 128)], int8, zeros past column n, and
+    scale [G][M], float32."""
+    q: torch.Tensor
+    scale: torch.Tensor
+    n: int
+
+
+@functools.lru_cache(maxsize=4096)
+def _rows_workspace(G: int, M: int, N: int) -> int:
+    nb = _c.c_size_t()
+    _check(_lib.lsgd_quantise_rows_workspace_bytes(G, M, N, _c.byref(nb)))
+    return nb.value
+
+
+def quantise_rows(X: torch.Tensor, both: bool = False) -> Union[Rows, Tuple[Rows, Rows]]:
+    """X [G][M][N] (float32 or bfloat16, columns contiguous) in 8-bit integers with a scale
+    for each row (lsgd_quantise_rows); ``both``: (X's rows, its transpose's, whose
+    scales are those of X's columns)."""
+    ldx, sX = _matrices("X", X, _FLOATS)
+    G, M, N = X.shape
+    dev = X.device
+    q = torch.empty((G, M, _up(N, 128)), dtype=torch.int8, device=dev)
+    s = torch.empty((G, M), dtype=torch.float32, device=dev)
+    dt = BF16 if X.dtype == torch.bfloat16 else FP32
+    if not both:
+        _enqueue(dev, _lib.lsgd_quantise_rows, dt, G, M, N, X.data_ptr(), ldx, sX, q.data_ptr(),
+                 s.data_ptr(), None, None, None, 0)
+        return Rows(q, s, N)
+    qt = torch.empty((G, N, _up(M, 128)), dtype=torch.int8, device=dev)
+    st = torch.empty((G, N), dtype=torch.float32, device=dev)
+    nb = _rows_workspace(G, M, N)
+    ws = torch.empty(nb, dtype=torch.uint8, device=dev)
+    _enqueue(dev, _lib.lsgd_quantise_rows, dt, G, M, N, X.data_ptr(), ldx, sX, q.data_ptr(),
+             s.data_ptr(), qt.data_ptr(), st.data_ptr(), ws.data_ptr(), nb)
+    return Rows(q, s, N), Rows(qt, st, M)
+
+
+def _row_operand(name: str, X: Rows) -> Tuple[int, int, int, int]:
+    """Groups, rows and the two group strides of an operand."""
+    q, s, n = X
+    shape = q.shape
+    if len(shape) != 3 or q.dtype != torch.int8 or s.dtype != torch.float32:
+        raise ValueError(f"{name} must hold 3-D int8 values and float32 scales")
+    G, M, L = shape
+    if n < 1 or L != _up(n, 128) or s.shape != (G, M) or not (G and M):
+        raise ValueError(f"{name}: shapes do not match the row layout of {n} columns")
+    if not (q.is_cuda and s.is_cuda):
+        raise ValueError(f"{name} must be on a CUDA (HIP) device")
+    if q.is_contiguous() and s.is_contiguous():
+        return G, M, M * L, M
+    if q.stride(2) != 1 or (M > 1 and (q.stride(1) != L or s.stride(1) != 1)):
+        raise ValueError(f"{name}: rows must be contiguous and unpadded")
+    return G, M, (q.stride(0) if G > 1 else 0), (s.stride(0) if G > 1 else 0)
+
+
+def _vectors(name: str, v: torch.Tensor, G: int, N: int) -> int:
+    """Group stride of a float32 [G][N] device tensor whose columns are contiguous."""
+    if v.dtype != torch.float32 or v.shape != (G, N):
+        raise ValueError(f"{name} must be float32 [G][N] = [{G}][{N}]")
+    if not v.is_cuda:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    sG, sN = v.stride()
+    if N > 1 and sN != 1:
+        raise ValueError(f"{name}'s columns must be contiguous")
+    return sG if G > 1 else 0
+
+
+def _not_over(out: torch.Tensor, what: str, *read) -> None:
+    """Refuses a result that shares a byte with one of ``read`` (1-D to 3-D tensors)."""
+    def three(t):
+        return t if t.dim() == 3 else t.unsqueeze(1) if t.dim() == 2 else t.view(1, 1, -1)
+    for t in read:
+        if t is not None and _overlap(three(out), three(t)):
+            raise ValueError(what)
+
+
+@functools.lru_cache(maxsize=4096)
+def _gemm_rows_workspace(out: int, G: int, M: int, N: int, n: int) -> int:
+    nb = _c.c_size_t()
+    _check(_lib.lsgd_grouped_gemm_rows_workspace_bytes(out, G, M, N, n, _c.byref(nb)))
+    return nb.value
+
+
+def grouped_gemm_rows(A: Rows, B: Rows, bias: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None,
+                      out_dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """C[g] = A[g] @ B[g]^T + bias[g] of two tensors in rows along the contracted dimension
+    (lsgd_grouped_gemm_rows): an exact sum of integers times the rows' scales, C float32 or
+    bfloat16, ``bias`` float32 [G][N]. y = x w + b takes x and w's transpose, dy w^T takes
+    dy and w, and x^T dy the transposes of x and dy. A group stride of 0 (``expand``)
+    shares a matrix or a bias among the groups. ``out`` (whose type counts then, not
+    ``out_dtype``) must not overlap what is read."""
+    G, M, sA, sSA = _row_operand("A", A)
+    Gb, N, sB, sSB = _row_operand("B", B)
+    n, dev = A.n, A.q.device
+    if n != B.n or G != Gb:
+        raise ValueError("A and B must have the same groups and inner dimension")
+    sbias = 0 if bias is None else _vectors("bias", bias, G, N)
+    if out is None:
+        if out_dtype not in _FLOATS:
+            raise ValueError("out_dtype must be float32 or bfloat16")
+        out = torch.empty((G, M, N), dtype=out_dtype, device=dev)
+        ldc, sC = N, M * N
+    else:
+        ldc, sC = _matrices("out", out, _FLOATS)
+        if out.shape != (G, M, N):
+            raise ValueError("out must be [G][M][N]")
+        _not_over(out, "out must not overlap A, B or bias", A.q, A.scale, B.q, B.scale, bias)
+    if not (A.scale.device == dev and B.q.device == dev and B.scale.device == dev
+            and out.device == dev and (bias is None or bias.device == dev)):
+        raise ValueError("all tensors must be on one device")
+    dt = BF16 if out.dtype == torch.bfloat16 else FP32
+    nb = _gemm_rows_workspace(dt, G, M, N, n)
+    ws = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
+    _enqueue(dev, _lib.lsgd_grouped_gemm_rows, dt, G, M, N, n, A.q.data_ptr(), sA,
+             A.scale.data_ptr(), sSA, B.q.data_ptr(), sB, B.scale.data_ptr(), sSB,
+             None if bias is None else bias.data_ptr(), sbias, out.data_ptr(), ldc, sC,
+             ws.data_ptr() if nb else None, nb)
+    return out
+
+
+def layer_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None,
+               bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+               out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None
+               ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(Y, mean, rstd) of the layer norm of X's rows (lsgd_layer_norm): X [G][M][N] float32
+    or bfloat16, columns contiguous, ``weight`` and ``bias`` float32 [G][N] (views into
+    the replicas' flat rows are fine; one for all groups: ``expand``; None: ones, zeros), Y of
+    X's type or ``out_dtype``, mean and rstd float32 [G][M]. ``out`` (whose type counts
+    then) must not overlap what is read."""
+    ldx, sX = _matrices("X", X, _FLOATS)
+    G, M, N = X.shape
+    dev = X.device
+    sw = 0 if weight is None else _vectors("weight", weight, G, N)
+    sb = 0 if bias is None else _vectors("bias", bias, G, N)
+    if out is None:
+        if out_dtype is None:
+            out_dtype = X.dtype
+        elif out_dtype not in _FLOATS:
+            raise ValueError("out_dtype must be float32 or bfloat16")
+        out = torch.empty((G, M, N), dtype=out_dtype, device=dev)
+        ldy, sY = N, M * N
+    else:
+        ldy, sY = _matrices("out", out, _FLOATS)
+        if out.shape != X.shape:
+            raise ValueError("out must have X's shape")
+        _not_over(out, "out must not overlap X, weight or bias", X, weight, bias)
+    if out.device != dev or (weight is not None and weight.device != dev) or (
+            bias is not None and bias.device != dev):
+        raise ValueError("all tensors must be on one device")
+    stats = torch.empty((2, G, M), dtype=torch.float32, device=dev)
+    mean, rstd = stats[0], stats[1]
+    _enqueue(dev, _lib.lsgd_layer_norm, BF16 if X.dtype == torch.bfloat16 else FP32,
+             BF16 if out.dtype == torch.bfloat16 else FP32, G, M, N, X.data_ptr(), ldx, sX,
+             None if weight is None else weight.data_ptr(), sw,
+             None if bias is None else bias.data_ptr(), sb, float(eps), out.data_ptr(), ldy, sY,
+             mean.data_ptr(), rstd.data_ptr())
+    return out, mean, rstd
+
+
+@functools.lru_cache(maxsize=4096)
+def _norm_workspace(G: int, M: int, N: int) -> int:
+    nb = _c.c_size_t()
+    _check(_lib.lsgd_layer_norm_backward_workspace_bytes(G, M, N, _c.byref(nb)))
+    return nb.value
+
+
+def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
+                        rstd: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                        parameters: bool = True, out: Optional[torch.Tensor] = None,
+                        dweight: Optional[torch.Tensor] = None,
+                        dbias: Optional[torch.Tensor] = None
+                        ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """(dX, dweight, dbias) of ``layer_norm`` from the gradient dY of its result, its X,
+    mean, rstd and weight (lsgd_layer_norm_backward). dX has X's type, the others are float32
+    [G][N], or None without ``parameters``. ``out``, ``dweight`` and ``dbias`` take the
+    results (the last two, views into flat rows of gradients for instance, with any group
+    stride) and must not overlap each other or what is read."""
+    ldg, sG = _matrices("dY", dY, _FLOATS)
+    ldx, sX = _matrices("X", X, _FLOATS)
+    if dY.shape != X.shape:
+        raise ValueError("dY must have X's shape")
+    G, M, N = X.shape
+    dev = X.device
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.dtype != torch.float32 or t.shape != (G, M) or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous float32 [G][M] = [{G}][{M}]")
+    sw = 0 if weight is None else _vectors("weight", weight, G, N)
+    if not parameters and (dweight is not None or dbias is not None):
+        raise ValueError("dweight and dbias are not computed without parameters")
+    read = (dY, X, mean, rstd, weight)
+    given = []
+    if out is None:
+        out = torch.empty((G, M, N), dtype=X.dtype, device=dev)
+        ldd, sD = N, M * N
+    else:
+        ldd, sD = _matrices("out", out, (X.dtype,))
+        if out.shape != X.shape:
+            raise ValueError("out must have X's shape")
+        given.append(out)
+    sdw = sdb = N
+    if parameters:
+        if dweight is None:
+            dweight = torch.empty((G, N), dtype=torch.float32, device=dev)
+        else:
+            sdw = _vectors("dweight", dweight, G, N)
+            given.append(dweight)
+        if dbias is None:
+            dbias = torch.empty((G, N), dtype=torch.float32, device=dev)
+        else:
+            sdb = _vectors("dbias", dbias, G, N)
+            given.append(dbias)
+    for i, t in enumerate(given):
+        _not_over(t, "results must not overlap each other or what is read", *read, *given[:i])
+    for t in (dY, mean, rstd, weight, out, dweight, dbias):
+        if t is not None and t.device != dev:
+            raise ValueError("all tensors must be on one device")
+    nb = _norm_workspace(G, M, N) if parameters else 0
+    ws = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
+    _enqueue(dev, _lib.lsgd_layer_norm_backward, BF16 if X.dtype == torch.bfloat16 else FP32,
+             BF16 if dY.dtype == torch.bfloat16 else FP32, G, M, N, dY.data_ptr(), ldg, sG,
+             X.data_ptr(), ldx, sX, mean.data_ptr(), rstd.data_ptr(),
+             None if weight is None else weight.data_ptr(), sw, out.data_ptr(), ldd, sD,
+             dweight.data_ptr() if parameters else None, sdw,
+             dbias.data_ptr() if parameters else None, sdb, ws.data_ptr() if nb else None, nb)
+    return out, dweight, dbias
+
+
+def _tensor_table(tensors: Sequence[torch.Tensor]):
+    """(replicas, device, [(address, M, N, ld, s, type code), ...]) of tensors [K][...]."""
+    if isinstance(tensors, torch.Tensor) or not len(tensors):
+        raise ValueError("tensors must be a non-empty sequence of tensors")
+    table, K, dev = [], None, tensors[0].device
+    for t in tensors:
+        shape, stride, n = t.shape, t.stride(), t.dim()
+        if t.dtype not in _FLOATS or not n or not t.numel():
+            raise ValueError("tensors must be non-empty float32 or bfloat16 [K][...]")
+        if K is None:
+            K = shape[0]
+        if not t.is_cuda or t.device != dev:
+            raise ValueError("tensors must be on one CUDA (HIP) device")
+        if shape[0] != K:
+            raise ValueError("tensors must have one number of replicas")
+        if n == 3:
+            M, N = shape[1], shape[2]
+            ld, one = (stride[1] if M > 1 else N), (stride[2] if N > 1 else 1)
+        else:
+            M, N, one = 1, t.numel() // K, 1
+            ld, run = N, 1  # a replica's values: one run without gaps
+            for d in range(n - 1, 0, -1):
+                if shape[d] > 1 and stride[d] != run:
+                    one = 0
+                run *= shape[d]
+        if one != 1 or ld < N:
+            raise ValueError("a replica's values must be contiguous, or [M][N] of contiguous rows")
+        table.append((t.data_ptr(), M, N, ld, stride[0] if K > 1 else 0,
+                      BF16 if t.dtype == torch.bfloat16 else FP32))
+    return K, dev, table
+
+
+def _runs_apart(K: int, table) -> bool:
+    """Whether no two of the tensors share a byte (each replica's own being apart)."""
+    size = (4, 2)
+    runs = sorted((p, p + ((M - 1) * ld + N) * size[d], s * size[d]) for p, M, N, ld, s, d in table)
+    # tensors one after the other
+    if all(a[1] + (K - 1) * a[2] <= b[0] for a, b in zip(runs, runs[1:])):
+        return True
+    # replicas in rows of one length, in each of them the tensors one after the other
+    if all(a[1] <= b[0] and a[2] == b[2] for a, b in zip(runs, runs[1:])) and (
+            runs[-1][1] - runs[0][0] <= runs[0][2]):
+        return True
+    starts, ends = [], []
+    for p, M, N, ld, s, d in table:
+        if ld == N:
+            M, N = 1, M * N
+        at = (torch.arange(K) * (s * size[d]))[:, None] + torch.arange(M) * (ld * size[d]) + p
+        starts.append(at.flatten())
+        ends.append(starts[-1] + N * size[d])
+    start, order = torch.cat(starts).sort()
+    end = torch.cat(ends)[order].cummax(0)[0]
+    return bool((start[1:] >= end[:-1]).all())
+
+
+def _clip_call(tensors, written: bool, *bound) -> torch.Tensor:
+    K, dev, table = _tensor_table(tensors)
+    if written and not _runs_apart(K, table):
+        raise ValueError("tensors must not overlap")
+    n = len(table)
+    h = (_L * (6 * n))(*[v for row in table for v in row])
+    nb = _c.c_size_t()
+    _check(_lib.lsgd_gradient_norm_workspace_bytes(K, n, h, _c.byref(nb)))
+    ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
+    norm = torch.empty(K, dtype=torch.float32, device=dev)
+    _enqueue(dev, _lib.lsgd_clip_gradients if written else _lib.lsgd_gradient_norm, K, n, h, *bound,
+             norm.data_ptr(), ws.data_ptr(), nb.value)
+    return norm
+
+
+def gradient_norm(tensors: Sequence[torch.Tensor]) -> torch.Tensor:
+    """The norm of each replica's values over all ``tensors`` [K][...] (float32 or bfloat16; a
+    replica's values contiguous, or [M][N] of contiguous rows; views into flat rows are
+    fine): float32 [K] (lsgd_gradient_norm). One norm over everything: views [1][...]."""
+    return _clip_call(tensors, False)
+
+
+def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float) -> torch.Tensor:
+    """In place: the ``tensors`` of each replica whose ``gradient_norm`` is above ``max_norm``
+    (finite, > 0), times max_norm / norm; the others, and those of a replica whose norm
+    is not finite, stay as they are. Returns the norms before clipping
+    (lsgd_clip_gradients). The tensors must not overlap."""
+    return _clip_call(tensors, True, float(max_norm))

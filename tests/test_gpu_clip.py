@@ -1,0 +1,268 @@
+"""GPU tests of gradient norms and clipping against the float64 oracle, and of the
+operators around a large layer in one step."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer_oracle as O
+from gpu_util import U32, device, gamma, to_dev
+
+pytestmark = pytest.mark.gpu
+
+
+def _lsgd():
+    from paper_1808_07217_amd import lsgd as L
+    return L
+
+
+def _np(t):
+    return t.to(torch.float32).cpu().numpy().astype(np.float64)
+
+
+def _tensors(K, shapes, seed=0, spread=1.0):
+    rng = np.random.default_rng(seed)
+    size = np.exp(spread * rng.standard_normal(K))
+    out = []
+    for i, (dt, *s) in enumerate(shapes):
+        x = rng.standard_normal((K, *s)) * size.reshape((K,) + (1,) * len(s))
+        out.append(to_dev(x.astype(np.float32)).to(torch.bfloat16 if dt == "b" else torch.float32))
+    return out
+
+
+def _check(ts, bound):
+    """Squares and sums are in fp64 (2^-53 each, against the bound's u = 2^-24): the norm is
+    rounded once, a value's product with the factor once to its type."""
+    L = _lsgd()
+    before = [_np(t) for t in ts]
+    copies = [t.clone() for t in ts]
+    norm, want = O.clip(before, bound)
+    only = L.gradient_norm(ts)
+    got = L.clip_gradients(ts, bound)
+    assert torch.equal(only, got)
+    assert np.all(np.abs(_np(got) - norm) <= 1.001 * U32 * norm)
+    kept = ~(norm > bound)
+    for t, c, w in zip(ts, copies, want):
+        half = 2.0 ** -8 if t.dtype == torch.bfloat16 else U32
+        assert np.all(np.abs(_np(t) - w) <= 1.001 * half * np.abs(w) + 2.0 ** -134)
+        assert torch.equal(t[torch.from_numpy(kept)], c[torch.from_numpy(kept)])
+    return norm
+
+
+LISTS = {
+    "one value": (1, [("f", 1)]),
+    "scalars": (3, [("f",), ("b",)]),
+    "softmax": (4, [("f", 64, 10), ("f", 10)]),
+    "mixed": (5, [("b", 33, 7), ("f", 129), ("b", 1), ("f", 3, 5, 2, 11), ("b", 4097), ("f", 1, 1)]),
+    "one replica": (1, [("f", 300, 500), ("b", 7, 9)]),
+    "many": (3, [("f" if i % 3 else "b", i % 7 + 1, 13 * (i % 5) + 1) for i in range(150)]),
+    "large": (2, [("f", 2000, 3001), ("b", 1500, 2003), ("f", 5)]),
+    "many replicas": (700, [("f", 5, 9), ("b", 31)]),
+}
+
+
+@pytest.mark.parametrize("name", LISTS)
+@pytest.mark.parametrize("bound", [1e-3, 20.0, 1e9])
+def test_matches_oracle(name, bound):
+    print(f"clip {name} {bound}", flush=True)
+    _check(_tensors(*LISTS[name]), bound)
+
+
+def test_some_replicas_above_the_bound():
+    print("clip some", flush=True)
+    ts = _tensors(16, [("f", 100, 70), ("f", 70), ("b", 33)], spread=2.0)
+    norm = O.clip([_np(t) for t in ts], 1e30)[0]
+    _check(ts, float(np.median(norm)))
+    # a bound that is the norm itself leaves everything, one below it clips
+    ts = [to_dev(np.array([[3.0, 4.0], [6.0, 8.0]], np.float32))]
+    _check(ts, 5.0)
+    assert ts[0].tolist() == [[3.0, 4.0], [3.0, 4.0]]
+
+
+def test_extremes():
+    """Squares that leave fp32's range on both sides, subnormals, zeros, a norm past fp32, and
+    infinities and NaN, whose replicas stay as they are."""
+    L = _lsgd()
+    print("clip extremes", flush=True)
+    x = np.zeros((8, 300), np.float32)
+    x[0] = 1e25
+    x[1] = -1e-25
+    x[2] = 1e-44
+    x[4] = np.finfo(np.float32).max
+    x[5, ::7], x[5, 3] = 2.0, np.nan
+    x[6, ::7], x[6, 290] = 2.0, -np.inf
+    x[7] = 1.0
+    for dt in (torch.float32, torch.bfloat16):
+        t = to_dev(x).to(dt)
+        c = t.clone()
+        v = _np(t)
+        with np.errstate(over="ignore"):
+            norm, want = O.clip([v[[0, 1, 2, 3, 4, 7]]], 1e-30)
+            norm = norm.astype(np.float32)
+        got = L.clip_gradients([t], 1e-30)
+        a, b = _np(got)[[0, 1, 2, 3, 4, 7]], norm.astype(np.float64)
+        assert np.isinf(a[4]) and np.isinf(b[4])
+        np.testing.assert_allclose(np.delete(a, 4), np.delete(b, 4), rtol=1.3e-7, atol=2.0 ** -149)
+        half = 2.0 ** -8 if dt == torch.bfloat16 else U32
+        # (fp32's largest value is an infinity in bf16: its replica stays as it is there)
+        now, (want,) = _np(t)[[0, 1, 2, 3, 4, 7]], want
+        with np.errstate(invalid="ignore"):
+            near = np.abs(now - want) <= 1.001 * half * np.abs(want) + 2.0 ** -134
+        assert np.all(near | (now == want)) and np.isfinite(now[4]).all() == (dt == torch.float32)
+        assert np.isnan(_np(got)[5]) and np.isinf(_np(got)[6])
+        bits = torch.int16 if dt == torch.bfloat16 else torch.int32
+        assert torch.equal(t[5:7].view(bits), c[5:7].view(bits))
+        assert torch.equal(t[2:4], c[2:4])
+
+
+def test_flat_rows_and_views():
+    """Tensors inside the replicas' flat rows and rows with a pitch: nothing beside them
+    changes."""
+    print("clip views", flush=True)
+    K = 5
+    rng = np.random.default_rng(2)
+    for dt in (torch.float32, torch.bfloat16):
+        flat = to_dev(rng.standard_normal((K, 2000)).astype(np.float32)).to(dt)
+        room = to_dev(rng.standard_normal((K, 40, 77)).astype(np.float32)).to(dt)
+        side = to_dev(rng.standard_normal((9, K, 300)).astype(np.float32)).to(dt)
+        tall = to_dev(rng.standard_normal((K, 3000, 5)).astype(np.float32)).to(dt)
+        ts = [flat[:, 3:3 + 33 * 40].view(K, 33, 40), flat[:, 1323:1364], flat[:, 1999:],
+              room[:, 3:33, 5:70], room[:, 33:, :1], side[:, :, 7:290].transpose(0, 1),
+              tall[:, 1:, 1:4]]
+        kept = [(t, t.clone()) for t in (flat, room, side, tall)]
+        _check(ts, 3.0)
+        for t in ts:
+            t.zero_()
+        for t, c in kept:
+            for v in ([flat[:, 3:3 + 33 * 40], *ts[1:3]] if t is flat else
+                      ts[3:5] if t is room else [ts[5]] if t is side else [ts[6]]):
+                off = v.storage_offset()
+                c.as_strided(v.shape, v.stride(), off).zero_()
+            assert torch.equal(t, c)
+
+
+def test_norms_of_shared_and_repeated_tensors():
+    """The norm reads: replicas of one matrix (expand), a tensor twice."""
+    L = _lsgd()
+    print("norm shared", flush=True)
+    t = _tensors(1, [("f", 20, 30)])[0]
+    e = t.expand(3, 20, 30)
+    got = _np(L.gradient_norm([e, e]))
+    want = np.sqrt(2 * (_np(t) ** 2).sum())
+    assert np.all(np.abs(got - want) <= 1.001 * U32 * want)
+    for bad in ([e], [t, t], [t, t[:, 3:5]], [t, t.view(1, -1)[:, 590:]], [t[:, ::2], t[:, 2:3]]):
+        with pytest.raises((ValueError, L.LsgdError)):
+            L.clip_gradients(bad, 1.0)
+    L.clip_gradients([t[:, ::2], t[:, 1::2]], 1.0)
+    for bad in ([t, t.expand(3, 20, 30)], [t.transpose(1, 2)], [t[:, :, ::2]],
+                [torch.zeros(1, 2, 3, 8, device=device())[..., :4]],
+                [t[:, :1].expand(1, 20, 30)]):
+        with pytest.raises((ValueError, L.LsgdError)):
+            L.gradient_norm(bad)
+    for bound in (0.0, -1.0, float("inf"), float("nan")):
+        with pytest.raises(L.LsgdError):
+            L.clip_gradients([t], bound)
+
+
+def test_on_a_side_stream_and_in_a_graph():
+    L = _lsgd()
+    print("clip stream and graph", flush=True)
+    src = _tensors(4, [("f", 100, 300), ("b", 77), ("f", 5000)])
+    work = [t.clone() for t in src]
+
+    def step():
+        for a, b in zip(work, src):
+            a.copy_(b)
+        return L.clip_gradients(work, 7.0)
+
+    want, values = step(), [t.clone() for t in work]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step()
+    side.synchronize()
+    assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(work, values))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm = step()
+    for k in range(4):
+        for t in src:
+            t.copy_(torch.randn(t.shape, device=device()) * (k + 1) / 50)
+        graph.replay()
+        torch.cuda.synchronize()
+        held = [t.clone() for t in work]
+        eager = step()
+        assert torch.equal(norm, eager) and all(torch.equal(a, b) for a, b in zip(work, held))
+
+
+def test_past_32_bit_offsets():
+    """A tensor of more than 2^32 bytes, contiguous and with a pitch."""
+    L = _lsgd()
+    print("clip past 32 bits", flush=True)
+    t = torch.zeros(1, 2 ** 16, 2 ** 15 + 64, device=device(), dtype=torch.bfloat16)
+    t[0, 0, 0], t[0, -1, -1], t[0, -1, 2 ** 15 - 1] = 3.0, 4.0, 12.0
+    assert L.gradient_norm([t]).tolist() == [13.0]
+    assert L.clip_gradients([t[:, :, :2 ** 15]], 153.0 ** 0.5 / 3).item() == np.float32(153.0 ** 0.5)
+    assert t[0, 0, 0] == 1.0 and t[0, -1, -1] == 4.0 and t[0, -1, 2 ** 15 - 1] == 4.0
+    assert L.clip_gradients([t], 1.0).item() == np.float32(33.0 ** 0.5)
+    assert abs(t[0, -1, -1].item() - 4 / 33.0 ** 0.5) <= 2.0 ** -8
+
+
+def test_a_layer_s_local_step():
+    """A step of two replicas of x -> layer norm -> layer in 8-bit integers, parameters and
+    gradients in flat rows: forward, all gradients, clipping, update and average, against
+    the formulas in float64 on what each operator was given."""
+    L = _lsgd()
+    print("layer step", flush=True)
+    rng = np.random.default_rng(21)
+    K, T, I, F, lr, bound = 2, 60, 200, 130, 0.1, 0.5
+    f32 = lambda *s: to_dev(rng.standard_normal(s).astype(np.float32))  # noqa: E731
+    P = O.up(2 * I + I * F + F, 64)
+    params, grads, moms = f32(K, P), torch.zeros(K, P, device=device()), torch.zeros(K, P, device=device())
+
+    def views(flat):
+        return (flat[:, :I], flat[:, I:2 * I], flat[:, 2 * I:2 * I + I * F].view(K, I, F),
+                flat[:, 2 * I + I * F:2 * I + I * F + F])
+
+    (gw, gb, w, b), (dgw, dgb, dw, db) = views(params), views(grads)
+    x, dy = f32(K, T, I), f32(K, T, F)
+    h, mean, rstd = L.layer_norm(x, gw, gb)
+    (hq, ht), (wq, wt), (dq, dt) = (L.quantise_rows(t, both=True) for t in (h, w, dy))
+    y = L.grouped_gemm_rows(hq, wt, b)
+    L.grouped_gemm_rows(ht, dt, out=dw)
+    dh = L.grouped_gemm_rows(dq, wq)
+    db.copy_(dy.sum(1))
+    dx, _, _ = L.layer_norm_backward(dh, x, mean, rstd, gw, dweight=dgw, dbias=dgb)
+    before = _np(grads)
+    norm = L.clip_gradients([dgw, dgb, dw, db], bound)
+    start = _np(params)
+    L.sgd_update(params, moms, grads, lr, 0.0, 0.0)
+    L.replica_average(params)
+
+    # forward and gradients by the formulas; 8 bits move a product's operand by half a scale
+    yy, mm, rr = O.layer_norm(_np(x), start[:, :I], start[:, I:2 * I], 1e-5)
+    np.testing.assert_allclose(_np(h), yy, rtol=0, atol=16 * U32 * np.abs(yy).max())
+    wv, dv = start[:, 2 * I:2 * I + I * F].reshape(K, I, F), _np(dy)
+
+    def near(got, p, q, ep, eq):
+        exact = p @ q
+        off = (np.abs(p) + ep) @ (np.abs(q) + eq) - np.abs(p) @ np.abs(q)
+        assert np.all(np.abs(got - exact) <= 1.001 * off + 1e-5), np.max(np.abs(got - exact) / off)
+
+    half = lambda t, axis: np.abs(t).max(axis, keepdims=True) / 254  # noqa: E731
+    near(_np(y) - start[:, None, 2 * I + I * F:2 * I + I * F + F], yy, wv, half(yy, 2), half(wv, 1))
+    near(before[:, 2 * I:2 * I + I * F].reshape(K, I, F), yy.transpose(0, 2, 1), dv,
+         half(yy, 1).transpose(0, 2, 1), half(dv, 1))
+    near(_np(dh), dv, wv.transpose(0, 2, 1), half(dv, 2), half(wv, 2).transpose(0, 2, 1))
+    rx, rw, rb = O.layer_norm_backward(_np(dh), _np(x), _np(mean), _np(rstd), start[:, :I])
+    np.testing.assert_allclose(_np(dx), rx, rtol=0, atol=gamma(60) * np.abs(rx).max() * 20)
+    np.testing.assert_allclose(before[:, :I], rw, rtol=0, atol=gamma(100) * np.abs(rw).max() * 20)
+    np.testing.assert_allclose(before[:, I:2 * I], rb, rtol=0, atol=gamma(100) * np.abs(rb).max() * 20)
+    # clipping, update and average, from the gradients as they were
+    used = before[:, :2 * I + I * F + F]
+    want, (clipped,) = O.clip([used], bound)
+    assert np.all(want > bound)
+    np.testing.assert_allclose(_np(norm), want, rtol=1.001 * U32)
+    new = start.copy()
+    new[:, :used.shape[1]] -= float(np.float32(lr)) * clipped
+    np.testing.assert_allclose(_np(params), np.repeat(new.mean(0, keepdims=True), K, 0), rtol=0,
+                               atol=6 * U32 * np.abs(new).max())
