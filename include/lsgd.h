@@ -703,8 +703,8 @@ typedef struct lsgd_tensor {
  * d_norm holds the norms before clipping. K <= 65535, count <= LSGD_MAX_TENSORS, M and N at
  * least 1, M N, M ld, s <= 2^44, else LSGD_E_INVALID. Clipped tensors' replicas must not overlap
  * (s >= (M - 1) ld + N, or rows of all K side by side), nor two tensors, nor d_norm. Workspace of
- * lsgd_gradient_norm_workspace_bytes, 8-byte aligned (LSGD_E_WORKSPACE if smaller), one call's
- * at a time.
+ * lsgd_gradient_norm_workspace_bytes, 8-byte aligned (LSGD_E_WORKSPACE if smaller; 0 for few
+ * values; then NULL is allowed), one call's at a time.
  */
 lsgd_status lsgd_gradient_norm_workspace_bytes(int32_t K, int32_t count,
                                                const lsgd_tensor* h_tensors,

@@ -172,7 +172,9 @@ struct RowQuantArgs {
   float* S;           // [G][M]
   uint8_t* Qt;        // the transposes, [G][N][up(M, 128)]; nullptr: not wanted
   float* St;
-  // set by launch_quantise_rows: strips' largest magnitudes [G][tn][M], [G][tm][N]
+  // set by launch_quantise_rows: a strip's rows, and strips' largest magnitudes [G][tn][M],
+  // [G][tm][N]
+  int strip;
   uint32_t *rowmost, *colmost;
 };
 size_t rows_quantise_workspace_bytes(int G, int M, int N);  // with the transposes

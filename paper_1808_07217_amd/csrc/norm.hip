@@ -16,8 +16,9 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// The sum over T threads of a row (T a power of two; wavefronts of a row's own from 64
-// on, all of the workgroup's above 64), in all of them; `room`: of K sums, a wavefront's each.
+// The sums over T threads of a row (T a power of two; wavefronts of a row's own from 64
+// on, all of the workgroup's above 64), in all of them; `room`: a wavefront's sums each, another
+// room than the last call's (whose sums may still be read by some).
 template <int T, int K, class A>
 __device__ __forceinline__ void row_sums(A (&v)[K], A (*room)[K]) {
 #pragma unroll
@@ -25,11 +26,9 @@ __device__ __forceinline__ void row_sums(A (&v)[K], A (*room)[K]) {
 #pragma unroll
     for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d, 64);
   if constexpr (T > 64) {
-    const int wave = threadIdx.x >> 6;
-    __syncthreads();  // the last sums have been read
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-      for (int k = 0; k < K; ++k) room[wave][k] = v[k];
+      for (int k = 0; k < K; ++k) room[threadIdx.x >> 6][k] = v[k];
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -51,38 +50,48 @@ __device__ __forceinline__ float inverse_root(double mean_square, float eps) {
   return (float)(1.0 / sqrt(mean_square + eps));
 }
 
-// A strip of rows a workgroup, T threads a row, V vectors of eight values each, in registers.
+// A strip of rows a workgroup, T threads a row, V vectors of eight values each, in registers;
+// the next row is on its way while one is summed.
 template <bool XBF, bool YBF, int T, int V>
 __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm(NormArgs a, int strips,
                                                                       long long total) {
   constexpr int kBlock = T < kThreads ? kThreads : T, kRows = kBlock / T;
-  __shared__ double room[kBlock / 64][1];
+  __shared__ double room[2][kBlock / 64][1];
   const unsigned id = workgroup_id();
   if (id >= total) return;
   const int g = id / strips, m0 = (id - g * strips) * a.strip;
-  const int t = threadIdx.x % T, end = min(a.M, m0 + a.strip);
+  const int t = threadIdx.x % T, slot = threadIdx.x / T, end = min(a.M, m0 + a.strip);
+  Raw8<XBF> raw[V];
+  auto fetch = [&](int m) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int n = (t + i * T) * 8;
+      fetch8<XBF, T == 16>(a.X, g * a.sX + m * a.ldx, n, m < end ? a.N : 0, raw[i]);
+    }
+  };
+  fetch(m0 + slot);
   float w[V][8], b[V][8];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int n = (t + i * T) * 8;
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[i][e] = 1.f, b[i][e] = 0.f;
-    if (a.w) load8<false>(a.w, g * a.sw + n, a.N - n, w[i]);
-    if (a.b) load8<false>(a.b, g * a.sb + n, a.N - n, b[i]);
+    if (a.w) load8<false, T == 16>(a.w, g * a.sw, n, a.N, w[i]);
+    if (a.b) load8<false, T == 16>(a.b, g * a.sb, n, a.N, b[i]);
   }
   for (int r = m0; r < end; r += kRows) {
-    const int m = r + threadIdx.x / T;
-    const bool in = m < end;
+    const int m = r + slot;
     float x[V][8];
     double s[1] = {0.0};
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int n = (t + i * T) * 8;
-      load8<XBF>(a.X, g * a.sX + m * a.ldx + n, in ? a.N - n : 0, x[i]);
+    for (int i = 0; i < V; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[0] += x[i][e];
-    }
-    row_sums<T>(s, room);
+      for (int e = 0; e < 8; ++e) {
+        x[i][e] = raw[i][e];
+        s[0] += x[i][e];
+      }
+    if (r + kRows < end) fetch(m + kRows);
+    row_sums<T>(s, room[0]);
     Moments mo;
     const double mean = s[0] / a.N;
     split_mean(mean, mo);
@@ -96,15 +105,15 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm(NormArgs a
         s[0] += (double)x[i][e] * x[i][e];
       }
     }
-    row_sums<T>(s, room);
+    row_sums<T>(s, room[1]);
     mo.rstd = inverse_root(s[0] / a.N, a.eps);
-    if (in) {
+    if (m < end) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int n = (t + i * T) * 8;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[i][e] = __builtin_fmaf(x[i][e] * mo.rstd, w[i][e], b[i][e]);
-        store8<YBF>(a.Y, g * a.sY + m * a.ldy + n, a.N - n, x[i]);
+        store8<YBF>(a.Y, g * a.sY + m * a.ldy, n, a.N, x[i]);
       }
       if (t == 0) {
         a.mean[(long long)g * a.M + m] = mo.hi;
@@ -118,7 +127,7 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm(NormArgs a
 constexpr int kLong = 1024;
 template <bool XBF, bool YBF>
 __global__ __launch_bounds__(kLong) void k_norm_long(NormArgs a, long long total) {
-  __shared__ double room[kLong / 64][1];
+  __shared__ double room[2][kLong / 64][1];
   const unsigned id = workgroup_id();
   if (id >= total) return;
   const int g = id / a.M, m = id - g * a.M;
@@ -126,33 +135,33 @@ __global__ __launch_bounds__(kLong) void k_norm_long(NormArgs a, long long total
   float x[8];
   double s[1] = {0.0};
   for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
-    load8<XBF>(a.X, x0 + n, a.N - n, x);
+    load8<XBF>(a.X, x0, n, a.N, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[0] += x[e];
   }
-  row_sums<kLong>(s, room);
+  row_sums<kLong>(s, room[0]);
   Moments mo;
   split_mean(s[0] / a.N, mo);
   s[0] = 0.0;
   for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
-    load8<XBF>(a.X, x0 + n, a.N - n, x);
+    load8<XBF>(a.X, x0, n, a.N, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float d = n + e < a.N ? (x[e] - mo.hi) - mo.lo : 0.f;
       s[0] += (double)d * d;
     }
   }
-  row_sums<kLong>(s, room);
+  row_sums<kLong>(s, room[1]);
   mo.rstd = inverse_root(s[0] / a.N, a.eps);
   for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
     float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, b[8] = {};
-    load8<XBF>(a.X, x0 + n, a.N - n, x);
-    if (a.w) load8<false>(a.w, g * a.sw + n, a.N - n, w);
-    if (a.b) load8<false>(a.b, g * a.sb + n, a.N - n, b);
+    load8<XBF>(a.X, x0, n, a.N, x);
+    if (a.w) load8<false>(a.w, g * a.sw, n, a.N, w);
+    if (a.b) load8<false>(a.b, g * a.sb, n, a.N, b);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       x[e] = __builtin_fmaf(((x[e] - mo.hi) - mo.lo) * mo.rstd, w[e], b[e]);
-    store8<YBF>(a.Y, g * a.sY + m * a.ldy + n, a.N - n, x);
+    store8<YBF>(a.Y, g * a.sY + m * a.ldy, n, a.N, x);
   }
   if (threadIdx.x == 0) {
     a.mean[(long long)g * a.M + m] = mo.hi;
@@ -161,6 +170,13 @@ __global__ __launch_bounds__(kLong) void k_norm_long(NormArgs a, long long total
 }
 
 // ---------------------------------------------------------------- backward
+// What is computed from these values is computed anew behind this.
+template <bool BF>
+__device__ __forceinline__ void opaque(Raw8<BF>& v) {
+#pragma unroll
+  for (int i = 0; i < Raw8<BF>::kDwords; ++i) asm volatile("" : "+v"(v.w[i]));
+}
+
 // A strip of rows a workgroup; a thread keeps the sums of its columns over them. A: the
 // arithmetic of a row. Of rows of few columns little is left beside the two directions that are
 // taken out (of two columns eps / variance of e): those in fp64.
@@ -169,53 +185,75 @@ template <bool XBF, bool YBF, int T, int V, class A>
 __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm_back(NormBackArgs a,
                                                                            long long total) {
   constexpr int kBlock = T < kThreads ? kThreads : T, kRows = kBlock / T, kCols = T * V * 8;
-  __shared__ A room[kBlock / 64][2];
+  __shared__ A room[2][kBlock / 64][2];
   __shared__ float slots[kRows > 1 ? kRows * kCols : 1];
   const unsigned id = workgroup_id();
   if (id >= total) return;
   const int g = id / a.strips, strip = id - g * a.strips, m0 = strip * a.strip;
   const int t = threadIdx.x % T, slot = threadIdx.x / T, end = min(a.M, m0 + a.strip);
+  // a row as it was read, and the next one on its way
+  Raw8<XBF> xr[V], xn[V];
+  Raw8<YBF> dr[V], dn[V];
+  float mean_next = 0.f, rstd_next = 0.f;
+  auto fetch = [&](int m) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int n = (t + i * T) * 8, N = m < end ? a.N : 0;
+      fetch8<XBF, T == 16>(a.X, g * a.sX + m * a.ldx, n, N, xn[i]);
+      fetch8<YBF, T == 16>(a.dY, g * a.sg + m * a.ldg, n, N, dn[i]);
+    }
+    mean_next = m < end ? a.mean[(long long)g * a.M + m] : 0.f;
+    rstd_next = m < end ? a.rstd[(long long)g * a.M + m] : 0.f;
+  };
+  fetch(m0 + slot);
   float w[V][8], dw[V][8], db[V][8];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int n = (t + i * T) * 8;
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[i][e] = 1.f, dw[i][e] = db[i][e] = 0.f;
-    if (a.w) load8<false>(a.w, g * a.sw + n, a.N - n, w[i]);
+    if (a.w) load8<false, T == 16>(a.w, g * a.sw, n, a.N, w[i]);
   }
-  for (int r = m0; r < end; r += kRows) {
+  int odd = 0;
+  for (int r = m0; r < end; r += kRows, odd ^= 1) {
     const int m = r + slot;
-    const bool in = m < end;
-    A x[V][8], dy[V][8];
     A s[2] = {0, 0};
-    const A mean = in ? a.mean[(long long)g * a.M + m] : 0.f;
-    const A rstd = in ? a.rstd[(long long)g * a.M + m] : 0.f;
+    const A mean = mean_next, rstd = rstd_next;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int n = (t + i * T) * 8;
-      float xf[8], df[8];
-      load8<XBF>(a.X, g * a.sX + m * a.ldx + n, in ? a.N - n : 0, xf);
-      load8<YBF>(a.dY, g * a.sg + m * a.ldg + n, in ? a.N - n : 0, df);
+      xr[i] = xn[i];
+      dr[i] = dn[i];
+    }
+    if (r + kRows < end) fetch(m + kRows);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        x[i][e] = ((A)xf[e] - mean) * rstd;
-        dw[i][e] += df[e] * (float)x[i][e];
-        db[i][e] += df[e];
-        dy[i][e] = (A)df[e] * w[i][e];
-        s[0] += dy[i][e];
-        s[1] += dy[i][e] * x[i][e];
+        const A x = ((A)xr[i][e] - mean) * rstd, dy = (A)dr[i][e] * w[i][e];
+        dw[i][e] += dr[i][e] * (float)x;
+        db[i][e] += dr[i][e];
+        s[0] += dy;
+        s[1] += dy * x;
       }
+      __builtin_amdgcn_sched_barrier(0);  // (a vector at a time: fewer registers)
     }
-    row_sums<T>(s, room);
+    row_sums<T>(s, room[odd]);
     const A c1 = s[0] / a.N, c2 = s[1] / a.N;
-    if (in) {
+    if (m < end) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int n = (t + i * T) * 8;
+        // (computed again: what is kept instead takes the registers of a second workgroup)
+        opaque(xr[i]);
+        opaque(dr[i]);
         float d[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = (float)(rstd * (dy[i][e] - c1 - x[i][e] * c2));
-        store8<XBF>(a.dX, g * a.sd + m * a.ldd + n, a.N - n, d);
+        for (int e = 0; e < 8; ++e) {
+          const A x = ((A)xr[i][e] - mean) * rstd, dy = (A)dr[i][e] * w[i][e];
+          d[e] = (float)(rstd * (dy - c1 - x * c2));
+        }
+        store8<XBF>(a.dX, g * a.sd + m * a.ldd, n, a.N, d);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
@@ -229,7 +267,7 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm_back(NormB
     if constexpr (kRows == 1) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        store8<false>(to, (t + i * T) * 8, a.N - (t + i * T) * 8, h ? db[i] : dw[i]);
+        store8<false>(to, 0, (t + i * T) * 8, a.N, h ? db[i] : dw[i]);
     } else {
       __syncthreads();
 #pragma unroll
@@ -248,23 +286,31 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm_back(NormB
   }
 }
 
-// dw, db = the strips' sums in order: 64 columns a workgroup, a quarter of the strips a
+// dw, db = the strips' sums in order: 64 columns a workgroup, a sixteenth of the strips a
 // wavefront. Columns g, (dw then db), n.
-__global__ __launch_bounds__(kThreads) void k_norm_join(NormBackArgs a, int tiles, long long total) {
-  __shared__ double room[4][64];
+constexpr int kJoin = 1024;
+__global__ __launch_bounds__(kJoin) void k_norm_join(NormBackArgs a, int tiles, long long total) {
+  constexpr int kWaves = kJoin / 64;
+  __shared__ double room[kWaves][64];
   const unsigned id = workgroup_id();
   if (id >= total) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int gh = id / tiles, g = gh / 2, h = gh & 1, n = (id - gh * tiles) * 64 + lane;
-  const int each = (a.strips + 3) / 4, k0 = wave * each, k1 = min(a.strips, k0 + each);
+  const int each = (a.strips + kWaves - 1) / kWaves;
+  const int k0 = wave * each, k1 = min(a.strips, k0 + each);
   double sum = 0.0;
-  if (n < a.N)
-    for (int k = k0; k < k1; ++k) sum += a.part[(((long long)g * a.strips + k) * 2 + h) * a.N + n];
+  if (n < a.N) {
+    const float* p = a.part + (((long long)g * a.strips + k0) * 2 + h) * a.N + n;
+#pragma unroll 8
+    for (int k = k0; k < k1; ++k, p += 2LL * a.N) sum += *p;
+  }
   room[wave][lane] = sum;
   __syncthreads();
-  if (wave == 0 && n < a.N)
-    (h ? a.db + g * a.sdb : a.dw + g * a.sdw)[n] =
-        (float)((room[0][lane] + room[1][lane]) + (room[2][lane] + room[3][lane]));
+  if (wave == 0 && n < a.N) {
+#pragma unroll
+    for (int k = 1; k < kWaves; ++k) sum += room[k][lane];
+    (h ? a.db + g * a.sdb : a.dw + g * a.sdw)[n] = (float)sum;
+  }
 }
 
 // Rows of any length: dx in two passes over a row, dw and db from a third, by columns.
@@ -279,9 +325,9 @@ __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long l
   float s[2] = {0.f, 0.f}, x[8], dy[8];
   auto take = [&](int n) __attribute__((always_inline)) {
     float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-    load8<XBF>(a.X, x0 + n, a.N - n, x);
-    load8<YBF>(a.dY, d0 + n, a.N - n, dy);
-    if (a.w) load8<false>(a.w, g * a.sw + n, a.N - n, w);
+    load8<XBF>(a.X, x0, n, a.N, x);
+    load8<YBF>(a.dY, d0, n, a.N, dy);
+    if (a.w) load8<false>(a.w, g * a.sw, n, a.N, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       x[e] = (x[e] - mean) * rstd;
@@ -302,7 +348,7 @@ __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long l
     take(n);
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = rstd * (dy[e] - c1 - x[e] * c2);
-    store8<XBF>(a.dX, g * a.sd + m * a.ldd + n, a.N - n, x);
+    store8<XBF>(a.dX, g * a.sd + m * a.ldd, n, a.N, x);
   }
 }
 // 512 columns of a strip a workgroup, every fourth row a wavefront.
@@ -318,8 +364,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_params(NormBackArgs a, int ti
   for (int m = m0 + wave; m < end; m += 4) {
     const float mean = a.mean[(long long)g * a.M + m], rstd = a.rstd[(long long)g * a.M + m];
     float x[8], dy[8];
-    load8<XBF>(a.X, g * a.sX + m * a.ldx + n, a.N - n, x);
-    load8<YBF>(a.dY, g * a.sg + m * a.ldg + n, a.N - n, dy);
+    load8<XBF>(a.X, g * a.sX + m * a.ldx, n, a.N, x);
+    load8<YBF>(a.dY, g * a.sg + m * a.ldg, n, a.N, dy);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       dw[e] += dy[e] * ((x[e] - mean) * rstd);
@@ -369,12 +415,12 @@ hipError_t with_shape(int N, F f) {
   if (s.T == 512) return f(Shape<512, 2>{});
   return f(Shape<1024, 2>{});
 }
-// Rows of a strip: about kStrips strips in all, of whole sets of rows at work at one time.
-constexpr long long kStrips = 1024;
-int strip_rows(int G, int M, int N) {
+// Rows of a strip: about `strips` strips in all, of whole sets of rows at work at one time.
+constexpr long long kStrips = 1024, kBackStrips = 256;
+int strip_rows(long long strips, int G, int M, int N) {
   const RowShape s = row_shape(N);
   const int each = s.T == 0 ? 4 : std::max(1, kThreads / s.T);
-  const long long strips = std::max(1LL, kStrips / G);
+  strips = std::max(1LL, strips / G);
   const long long rows = (M + strips - 1) / strips;
   return (int)((rows + each - 1) / each * each);
 }
@@ -387,7 +433,7 @@ hipError_t norm(NormArgs a, hipStream_t s) {
     hipLaunchKernelGGL((k_norm_long<XBF, YBF>), grid_of(total), dim3(kLong), 0, s, a, total);
     return hipGetLastError();
   }
-  a.strip = strip_rows(a.G, a.M, a.N);
+  a.strip = strip_rows(kStrips, a.G, a.M, a.N);
   const int strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
   const long long total = (long long)strips * a.G;
   return with_shape(a.N, [&](auto z) {
@@ -400,7 +446,7 @@ hipError_t norm(NormArgs a, hipStream_t s) {
 
 template <bool XBF, bool YBF>
 hipError_t norm_back(NormBackArgs a, void* ws, hipStream_t s) {
-  a.strip = strip_rows(a.G, a.M, a.N);
+  a.strip = strip_rows(kBackStrips, a.G, a.M, a.N);
   a.strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
   a.part = (float*)ws;
   const long long strips = (long long)a.strips * a.G;
@@ -428,7 +474,7 @@ hipError_t norm_back(NormBackArgs a, void* ws, hipStream_t s) {
   if (e != hipSuccess || !a.dw || a.strips == 1) return e;
   const long long tiles = (a.N + 63LL) / 64, total = tiles * 2 * a.G;
   if (total > 0x7fffffffLL) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(k_norm_join, grid_of(total), dim3(kThreads), 0, s, a, (int)tiles, total);
+  hipLaunchKernelGGL(k_norm_join, grid_of(total), dim3(kJoin), 0, s, a, (int)tiles, total);
   return hipGetLastError();
 }
 
@@ -440,7 +486,7 @@ hipError_t launch_norm(int x_bf16, int y_bf16, const NormArgs& a, hipStream_t s)
 }
 
 size_t norm_back_workspace_bytes(int G, int M, int N) {
-  const long long strip = strip_rows(G, M, N), strips = (M + strip - 1) / strip;
+  const long long strip = strip_rows(kBackStrips, G, M, N), strips = (M + strip - 1) / strip;
   return strips == 1 ? 0 : (size_t)G * strips * 2 * N * sizeof(float);
 }
 

@@ -24,39 +24,83 @@ constexpr int kThreads = 256;
 constexpr uint32_t kInf = 0x7f800000u;
 
 // ---------------------------------------------------------------- quantise
-// Magnitudes are compared as the bits of |x|: infinities and NaN are then the largest.
-__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// Magnitudes are compared as the bits of |x|: infinities and NaN are then the largest. Of
+// bfloat16 two in a dword, of floats one.
+template <bool BF>
+struct Most8 {
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  static constexpr uint32_t kMask = BF ? 0x7fff7fffu : 0x7fffffffu;
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    if constexpr (BF)
+      return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                                    __builtin_bit_cast(u16x2, b)));
+    else
+      return max(a, b);
+  }
+  // the magnitude in a dword's half (BF), as a float's bits
+  static __device__ __forceinline__ uint32_t bits(uint32_t w, int half) {
+    return BF ? (half ? w & 0xffff0000u : w << 16) : w;
+  }
+  static __device__ __forceinline__ uint32_t most(uint32_t w) {
+    return BF ? max(bits(w, 0), bits(w, 1)) : w;
+  }
+};
+// The largest magnitude of eight values, and each of them kept if larger than a column's.
+template <bool BF, bool COLS>
+__device__ __forceinline__ uint32_t most8(const Raw8<BF>& v, uint32_t (&cols)[Raw8<BF>::kDwords]) {
+  typedef Most8<BF> L;
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < Raw8<BF>::kDwords; ++i) {
+    const uint32_t w = v.w[i] & L::kMask;
+    top = L::larger(top, w);
+    if constexpr (COLS) cols[i] = L::larger(cols[i], w);
+  }
+  return L::most(top);
+}
 __device__ __forceinline__ float scale_of(uint32_t most) {
   if (most == 0) return 1.f;
   if (most >= kInf) return __uint_as_float(0x7fc00000u);
   return fmaxf(__uint_as_float(most) / 127.f, 0x1p-126f);
 }
-// The integers nearest to v / s. x (1 / s) is off by less than 2^-15, so that it rounds to the
-// wrong neighbour only next to the middle between two, and there the remainder
-// x - q s, which is exact in fp32 (|x| and s below 2^128, at most 24 bits between its
-// first and last), is at least s / 2: then, rarely, the tie or the neighbour is settled.
-// Everything is zero for a NaN in place of s.
-__device__ __forceinline__ u32x2 pack8(const float (&v)[8], float s) {
-  const float r = 1.f / s, half = 0.5f * s;
+// The integers nearest to v / s. x (1 / s) + 1.5 2^23 rounds to a float whose last byte is the
+// integer. The product is off by less than 2^-15, so that it rounds to the wrong neighbour only
+// next to the middle between two, and there the remainder x - q s, which is exact in fp32
+// (|x| and s below 2^128, at most 24 bits between its first and last), is at least s / 2:
+// then, rarely, the tie or the neighbour is settled. Zeros for a NaN in place of s.
+__device__ __forceinline__ u32x2 pack8(const float (&v)[8], float s, float r) {
+  constexpr float kShift = 12582912.f;
   float q[8], far = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    q[i] = __builtin_rintf(v[i] * r);
-    far = fmaxf(far, fabsf(__builtin_fmaf(-q[i], s, v[i])));
+    q[i] = __builtin_fmaf(v[i], r, kShift);
+    far = fmaxf(far, fabsf(__builtin_fmaf(kShift - q[i], s, v[i])));
   }
-  if (far >= half) {
+  if (far >= 0.5f * s) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float rest = __builtin_fmaf(-q[i], s, v[i]);
-      const bool odd = ((int)q[i] & 1) != 0;
-      if (fabsf(rest) > half || (fabsf(rest) == half && odd)) q[i] += rest > 0.f ? 1.f : -1.f;
+      const float rest = __builtin_fmaf(kShift - q[i], s, v[i]);
+      const bool odd = (__float_as_uint(q[i]) & 1) != 0;
+      if (fabsf(rest) > 0.5f * s || (fabsf(rest) == 0.5f * s && odd)) q[i] += rest > 0.f ? 1.f : -1.f;
     }
   }
-  const bool none = !(s == s);
-  u32x2 w = {0u, 0u};
+  u32x2 w;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i / 4] |= ((uint32_t)(int)q[i] & 255u) << (8 * (i % 4));
-  return none ? u32x2{0u, 0u} : w;
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t lo = __builtin_amdgcn_perm(__float_as_uint(q[4 * h + 1]),
+                                              __float_as_uint(q[4 * h]), 0x0c0c0400u);
+    const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(q[4 * h + 3]),
+                                              __float_as_uint(q[4 * h + 2]), 0x0c0c0400u);
+    w[h] = s == s ? lo | hi << 16 : 0u;
+  }
+  return w;
+}
+template <bool BF>
+__device__ __forceinline__ u32x2 pack8(const Raw8<BF>& raw, float s, float r) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = raw[i];
+  return pack8(v, s, r);
 }
 
 // The largest of T lanes' values (T a power of two up to 64), in all of them.
@@ -73,6 +117,7 @@ template <bool BF, int T, int V>
 __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_rows(RowQuantArgs a,
                                                                       long long rows) {
   constexpr int kBlock = T < kThreads ? kThreads : T, kRows = kBlock / T, kWaves = kBlock / 64;
+  constexpr bool kSmall = T == 16;
   __shared__ uint32_t most[T > 64 ? kWaves : 1];
   const int t = threadIdx.x % T;
   const long long row = (long long)workgroup_id() * kRows + threadIdx.x / T;
@@ -81,18 +126,18 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_rows(RowQuantAr
   const long long x = g * a.sX + m * a.ldx;
   const int vecs = (a.N + 127) / 128 * 16;  // of eight
   const bool in = row < rows;
-  uint32_t top = 0;
-  float v[V ? V : 1][8];
-  auto take = [&](int k, float(&w)[8]) __attribute__((always_inline)) {
-    load8<BF>(a.X, x + k * 8LL, in ? a.N - k * 8 : 0, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, magnitude(w[i]));
-  };
+  uint32_t top = 0, none[Raw8<BF>::kDwords];
+  Raw8<BF> v[V ? V : 1];
   if constexpr (V > 0) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) take(t + i * T, v[i]);
+    for (int i = 0; i < V; ++i) fetch8<BF, kSmall>(a.X, x, (t + i * T) * 8, in ? a.N : 0, v[i]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) top = max(top, most8<BF, false>(v[i], none));
   } else {
-    for (int k = t; k < vecs; k += T) take(k, v[0]);
+    for (int k = t; k < vecs; k += T) {
+      fetch8<BF>(a.X, x, k * 8, a.N, v[0]);
+      top = max(top, most8<BF, false>(v[0], none));
+    }
   }
   top = lanes_max<(T < 64 ? T : 64)>(top);
   if constexpr (T > 64) {
@@ -102,73 +147,64 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_rows(RowQuantAr
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) top = max(top, most[i]);
   }
-  const float s = scale_of(top);
+  const float s = scale_of(top), r = 1.f / s;
   if (!in) return;
   u32x2* q = (u32x2*)(a.Q + row * (vecs * 8LL));
   if constexpr (V > 0) {
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (t + i * T < vecs) q[t + i * T] = pack8(v[i], s);
+      if (t + i * T < vecs) q[t + i * T] = pack8<BF>(v[i], s, r);
   } else {
     for (int k = t; k < vecs; k += T) {
-      load8<BF>(a.X, x + k * 8LL, a.N - k * 8, v[0]);
-      q[k] = pack8(v[0], s);
+      fetch8<BF>(a.X, x, k * 8, a.N, v[0]);
+      q[k] = pack8<BF>(v[0], s, r);
     }
   }
   if (t == 0) a.S[row] = s;
 }
 
-// Both ways, in three launches: the largest magnitudes of strips of kStripRows rows by 512
-// columns, the scales from those, and the integers of 128 x 128 tiles from a second
-// read of X.
-constexpr int kStripRows = 512, kStripCols = 512;
+// Both ways, in two launches: the largest magnitudes of strips of rows by 512 columns, and from
+// those and a second read of X the scales and the integers of 128 x 128 tiles, from the last
+// tile to the first: what the first launch read last is in the last-level cache still.
+constexpr int kMostThreads = 1024, kMostWaves = kMostThreads / 64, kMostCols = 512;
+constexpr int kMostRows = 8;  // of a wavefront in flight
 
-// Wavefront w of a strip takes its rows w, w + 4, ..., a lane eight columns.
-template <bool BF>
-__global__ __launch_bounds__(kThreads) void k_rows_most(RowQuantArgs a, int tm, int tn, int total) {
-  __shared__ uint32_t most[4][kStripCols];
+// Wavefront w of a strip takes its rows w, w + 16, ..., a lane eight columns.
+template <bool BF, bool SMALL>
+__global__ __launch_bounds__(kMostThreads) void k_rows_most(RowQuantArgs a, int tm, int tn,
+                                                            int total) {
+  typedef Most8<BF> L;
+  __shared__ uint32_t most[kMostWaves][kMostCols];
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
   const int g = id / (tm * tn), mt = id % (tm * tn) / tn, nt = id % tn;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int n = nt * kStripCols + lane * 8, m0 = mt * kStripRows;
-  const int end = min(a.M, m0 + kStripRows);
-  uint32_t cm[8] = {};
-  for (int m = m0 + wave; m < end; m += 4) {
-    float v[8];
-    load8<BF>(a.X, g * a.sX + m * a.ldx + n, a.N - n, v);
-    uint32_t rm = 0;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = nt * kMostCols + lane * 8, m0 = mt * a.strip, end = min(a.M, m0 + a.strip);
+  uint32_t cm[Raw8<BF>::kDwords] = {};
+  for (int m = m0 + wave; m < end; m += kMostWaves * kMostRows) {
+    Raw8<BF> v[kMostRows];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t b = magnitude(v[i]);
-      rm = max(rm, b);
-      cm[i] = max(cm[i], b);
+    for (int k = 0; k < kMostRows; ++k) {
+      const int mk = m + k * kMostWaves;
+      fetch8<BF, SMALL>(a.X, g * a.sX + mk * a.ldx, n, mk < end ? a.N : 0, v[k]);
     }
-    rm = lanes_max<64>(rm);
-    if (lane == 0) a.rowmost[((long long)g * tn + nt) * a.M + m] = rm;
+#pragma unroll
+    for (int k = 0; k < kMostRows; ++k) {
+      const int mk = m + k * kMostWaves;
+      const uint32_t rm = lanes_max<64>(most8<BF, true>(v[k], cm));
+      if (lane == 0 && mk < end) a.rowmost[((long long)g * tn + nt) * a.M + mk] = rm;
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) most[wave][lane * 8 + i] = cm[i];
+  for (int i = 0; i < 8; ++i) most[wave][lane * 8 + i] = L::bits(cm[BF ? i / 2 : i], i % 2);
   __syncthreads();
-  for (int c = threadIdx.x; c < kStripCols; c += kThreads)
-    if (nt * kStripCols + c < a.N)
-      a.colmost[((long long)g * tm + mt) * a.N + nt * kStripCols + c] =
-          max(max(most[0][c], most[1][c]), max(most[2][c], most[3][c]));
-}
-
-// The scales of the rows (g, m), then of the columns (g, n).
-__global__ __launch_bounds__(kThreads) void k_rows_scales(RowQuantArgs a, int tm, int tn) {
-  const long long i = (long long)workgroup_id() * kThreads + threadIdx.x;
-  const long long rows = (long long)a.G * a.M, cols = (long long)a.G * a.N;
-  if (i >= rows + cols) return;
-  const bool row = i < rows;
-  const long long j = row ? i : i - rows;
-  const int each = row ? a.M : a.N, parts = row ? tn : tm;
-  const long long g = j / each;
-  const uint32_t* p = (row ? a.rowmost : a.colmost) + g * parts * each + (j - g * each);
-  uint32_t top = 0;
-  for (int k = 0; k < parts; ++k) top = max(top, p[(long long)k * each]);
-  (row ? a.S : a.St)[j] = scale_of(top);
+  const int c = threadIdx.x;
+  if (c < kMostCols && nt * kMostCols + c < a.N) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int w = 0; w < kMostWaves; ++w) top = max(top, most[w][c]);
+    a.colmost[((long long)g * tm + mt) * a.N + nt * kMostCols + c] = top;
+  }
 }
 
 // Rows of 128 bytes; piece k of 16 lies in slot k ^ (row / 8 % 8), which spreads the rows,
@@ -178,78 +214,118 @@ __device__ __forceinline__ int turned(int row, int byte) {
 }
 // A tile of 128 x 128: thread t holds eight rows from 8 (t / 16) and eight columns from
 // 8 (t % 16); the transpose's bytes are turned in LDS, so that each of its rows leaves
-// as a whole line.
-template <bool BF>
-__global__ __launch_bounds__(kThreads) void k_rows_both(RowQuantArgs a, int tm, int tn, int total) {
+// as a whole line. Thread t < 128 finds the scale of the tile's row t, the others a column's.
+template <bool BF, bool SMALL, bool STREAM>
+__global__ __launch_bounds__(kThreads) void k_rows_both(RowQuantArgs a, int tm, int tn, int sm,
+                                                        int sn, int total) {
   __shared__ __align__(16) uint8_t turn[128 * 128];
+  __shared__ __align__(16) float scale[256], inverse[256];
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
-  const int l = xcd_order(id, total);
+  const int l = total - 1 - (int)id;
   const int g = l / (tm * tn), mt = l % (tm * tn) / tn, nt = l % tn;
   const int tid = threadIdx.x, c = tid & 15, rg = tid >> 4;
   const int n0 = nt * 128, m0 = mt * 128, n = n0 + c * 8, r0 = m0 + rg * 8;
-  float v[8][8];
+  Raw8<BF> v[8];
 #pragma unroll
   for (int p = 0; p < 8; ++p)
-    load8<BF>(a.X, g * a.sX + (r0 + p) * a.ldx + n, r0 + p < a.M ? a.N - n : 0, v[p]);
+    fetch8<BF, SMALL>(a.X, g * a.sX + (r0 + p) * a.ldx, n, r0 + p < a.M ? a.N : 0, v[p]);
+  {
+    const bool row = tid < 128;
+    const int at = row ? m0 + tid : n0 + tid - 128, each = row ? a.M : a.N, parts = row ? sn : sm;
+    const uint32_t* p = (row ? a.rowmost : a.colmost) + (long long)g * parts * each + at;
+    uint32_t top = 0;
+    if (at < each) {
+#pragma unroll 8
+      for (int k = 0; k < parts; ++k) top = max(top, p[(long long)k * each]);
+    }
+    const float s = scale_of(top);
+    scale[tid] = s;
+    inverse[tid] = 1.f / s;
+    if (at < each && (row ? nt : mt) == 0) (row ? a.S : a.St)[(long long)g * each + at] = s;
+  }
+  __syncthreads();
+  auto put = [&](auto value, auto* to) __attribute__((always_inline)) {
+    if constexpr (STREAM)
+      __builtin_nontemporal_store(value, to);
+    else
+      *to = value;
+  };
   const long long ldq = (a.N + 127) / 128 * 128, ldt = (a.M + 127) / 128 * 128;
 #pragma unroll
   for (int p = 0; p < 8; ++p) {
     if (r0 + p >= a.M) continue;
     const long long row = (long long)g * a.M + r0 + p;
-    *(u32x2*)(a.Q + row * ldq + n) = pack8(v[p], a.S[row]);
+    put(pack8<BF>(v[p], scale[rg * 8 + p], inverse[rg * 8 + p]), (u32x2*)(a.Q + row * ldq + n));
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float w[8] = {v[0][i], v[1][i], v[2][i], v[3][i], v[4][i], v[5][i], v[6][i], v[7][i]};
-    const float s = a.St[(long long)g * a.N + min(n + i, a.N - 1)];
-    *(u32x2*)(turn + turned(c * 8 + i, rg * 8)) = pack8(w, s);
+    *(u32x2*)(turn + turned(c * 8 + i, rg * 8)) =
+        pack8(w, scale[128 + c * 8 + i], inverse[128 + c * 8 + i]);
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int at = i * kThreads + tid, j = at >> 3, k = (at & 7) * 16;
     if (n0 + j < a.N)
-      *(u32x4*)(a.Qt + ((long long)g * a.N + n0 + j) * ldt + m0 + k) =
-          *(const u32x4*)(turn + turned(j, k));
+      put(*(const u32x4*)(turn + turned(j, k)),
+          (u32x4*)(a.Qt + ((long long)g * a.N + n0 + j) * ldt + m0 + k));
   }
 }
 
-template <bool BF>
-hipError_t quantise(RowQuantArgs a, void* ws, hipStream_t s) {
-  if (!a.Qt) {
-    const long long rows = (long long)a.G * a.M;
-    auto launch = [&](auto kernel, int per, int threads) {
-      const long long n = (rows + per - 1) / per;
-      if (n > 0x7fffffffLL) return hipErrorInvalidValue;
-      hipLaunchKernelGGL(kernel, grid_of(n), dim3(threads), 0, s, a, rows);
-      return hipGetLastError();
-    };
-    if (a.N <= 128) return launch(k_rows<BF, 16, 1>, 16, 256);
-    if (a.N <= 512) return launch(k_rows<BF, 64, 1>, 4, 256);
-    if (a.N <= 1024) return launch(k_rows<BF, 64, 2>, 4, 256);
-    if (a.N <= 2048) return launch(k_rows<BF, 64, 4>, 4, 256);
-    if (a.N <= 4096) return launch(k_rows<BF, 256, 2>, 1, 256);
-    if (a.N <= 8192) return launch(k_rows<BF, 256, 4>, 1, 256);
-    if (a.N <= 16384) return launch(k_rows<BF, 1024, 2>, 1, 1024);
-    return launch(k_rows<BF, 1024, 0>, 1, 1024);
-  }
-  const long long tm = (a.M + kStripRows - 1LL) / kStripRows, tn = (a.N + kStripCols - 1LL) / kStripCols;
+// Rows of a strip, whole sets of what a workgroup has in flight: long strips leave few column
+// maxima to read again, up to kStripRows, short ones fill the card.
+constexpr int kStripRows = 1024;
+int strip_rows(int G, int M, int N) {
+  constexpr int kSet = kMostWaves * kMostRows;
+  const long long across = ((long long)N + kMostCols - 1) / kMostCols * G;
+  const long long strips = std::max(1LL, 256 / across);
+  const long long rows = ((M + strips - 1) / strips + kSet - 1) / kSet * kSet;
+  return (int)std::min<long long>(rows, kStripRows);
+}
+
+template <bool BF, bool SMALL, bool STREAM>
+hipError_t quantise_both(RowQuantArgs a, void* ws, hipStream_t s) {
+  a.strip = strip_rows(a.G, a.M, a.N);
+  const long long tm = ((long long)a.M + a.strip - 1) / a.strip;
+  const long long tn = (a.N + kMostCols - 1LL) / kMostCols;
   const long long bm = (a.M + 127LL) / 128, bn = (a.N + 127LL) / 128;
   if (bm * bn > 0x7fffffffLL / a.G) return hipErrorInvalidValue;
   a.rowmost = (uint32_t*)ws;
   a.colmost = a.rowmost + a.G * tn * a.M;
-  hipLaunchKernelGGL((k_rows_most<BF>), grid_of(tm * tn * a.G), dim3(kThreads), 0, s, a, (int)tm,
-                     (int)tn, (int)(tm * tn * a.G));
-  hipError_t e = hipGetLastError();
+  hipLaunchKernelGGL((k_rows_most<BF, SMALL>), grid_of(tm * tn * a.G), dim3(kMostThreads), 0, s, a,
+                     (int)tm, (int)tn, (int)(tm * tn * a.G));
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const long long scales = (long long)a.G * ((long long)a.M + a.N);
-  hipLaunchKernelGGL(k_rows_scales, grid_of((scales + kThreads - 1) / kThreads), dim3(kThreads), 0,
-                     s, a, (int)tm, (int)tn);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL((k_rows_both<BF>), grid_of(bm * bn * a.G), dim3(kThreads), 0, s, a, (int)bm,
-                     (int)bn, (int)(bm * bn * a.G));
+  hipLaunchKernelGGL((k_rows_both<BF, SMALL, STREAM>), grid_of(bm * bn * a.G), dim3(kThreads), 0, s,
+                     a, (int)bm, (int)bn, (int)tm, (int)tn, (int)(bm * bn * a.G));
   return hipGetLastError();
+}
+
+template <bool BF>
+hipError_t quantise(const RowQuantArgs& a, void* ws, hipStream_t s) {
+  if (a.Qt) {
+    const double bytes = (double)a.M * a.N * a.G * ((BF ? 2 : 4) + 2);
+    if (bytes >= (double)kNtBytesCaller)
+      return a.N < 8 ? quantise_both<BF, true, true>(a, ws, s) : quantise_both<BF, false, true>(a, ws, s);
+    return a.N < 8 ? quantise_both<BF, true, false>(a, ws, s) : quantise_both<BF, false, false>(a, ws, s);
+  }
+  const long long rows = (long long)a.G * a.M;
+  auto launch = [&](auto kernel, int per, int threads) {
+    const long long n = (rows + per - 1) / per;
+    if (n > 0x7fffffffLL) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kernel, grid_of(n), dim3(threads), 0, s, a, rows);
+    return hipGetLastError();
+  };
+  if (a.N <= 128) return launch(k_rows<BF, 16, 1>, 16, 256);
+  if (a.N <= 512) return launch(k_rows<BF, 64, 1>, 4, 256);
+  if (a.N <= 1024) return launch(k_rows<BF, 64, 2>, 4, 256);
+  if (a.N <= 2048) return launch(k_rows<BF, 64, 4>, 4, 256);
+  if (a.N <= 4096) return launch(k_rows<BF, 256, 2>, 1, 256);
+  if (a.N <= 8192) return launch(k_rows<BF, 256, 4>, 1, 256);
+  if (a.N <= 16384) return launch(k_rows<BF, 1024, 2>, 1, 1024);
+  return launch(k_rows<BF, 1024, 0>, 1, 1024);
 }
 
 // ------------------------------------------------------------------ product
@@ -517,8 +593,8 @@ hipError_t gemm_tiles(const RowGemmArgs& a, const RowCut& c, hipStream_t s) {
 }  // namespace
 
 size_t rows_quantise_workspace_bytes(int G, int M, int N) {
-  const size_t tm = ((size_t)M + kStripRows - 1) / kStripRows;
-  const size_t tn = ((size_t)N + kStripCols - 1) / kStripCols;
+  const size_t strip = strip_rows(G, M, N), tm = ((size_t)M + strip - 1) / strip;
+  const size_t tn = ((size_t)N + kMostCols - 1) / kMostCols;
   return ((size_t)G * tn * M + (size_t)G * tm * N) * sizeof(uint32_t);
 }
 

@@ -1135,10 +1135,10 @@ def _clip_call(tensors, written: bool, *bound) -> torch.Tensor:
     h = (_L * (6 * n))(*[v for row in table for v in row])
     nb = _c.c_size_t()
     _check(_lib.lsgd_gradient_norm_workspace_bytes(K, n, h, _c.byref(nb)))
-    ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
+    ws = torch.empty(nb.value, dtype=torch.uint8, device=dev) if nb.value else None
     norm = torch.empty(K, dtype=torch.float32, device=dev)
     _enqueue(dev, _lib.lsgd_clip_gradients if written else _lib.lsgd_gradient_norm, K, n, h, *bound,
-             norm.data_ptr(), ws.data_ptr(), nb.value)
+             norm.data_ptr(), None if ws is None else ws.data_ptr(), nb.value)
     return norm
 
 
