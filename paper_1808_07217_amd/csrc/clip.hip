@@ -10,6 +10,7 @@
 #include <cmath>
 
 #include "device_common.h"
+#include "lanes.h"
 #include "row_io.h"
 
 namespace lsgd {
@@ -30,8 +31,7 @@ struct ClipArgs {
 // The sum over a workgroup's WAVES wavefronts, in a fixed order, in every thread.
 template <int WAVES>
 __device__ __forceinline__ double block_sum(double v, double (&room)[WAVES]) {
-#pragma unroll
-  for (int d = 32; d; d /= 2) v += __shfl_xor(v, d, 64);
+  v = lanes_sum<64>(v);
   if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
   __syncthreads();
   v = room[0];

@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "device_common.h"
+#include "lanes.h"
 #include "row_io.h"
 
 namespace lsgd {
@@ -22,9 +23,7 @@ constexpr int kThreads = 256;
 template <int T, int K, class A>
 __device__ __forceinline__ void row_sums(A (&v)[K], A (*room)[K]) {
 #pragma unroll
-  for (int d = (T < 64 ? T : 64) / 2; d; d /= 2)
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], d, 64);
+  for (int k = 0; k < K; ++k) v[k] = lanes_sum<(T < 64 ? T : 64)>(v[k]);
   if constexpr (T > 64) {
     if ((threadIdx.x & 63) == 0)
 #pragma unroll

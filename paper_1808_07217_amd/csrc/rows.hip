@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "lanes.h"
 #include "row_io.h"
 #include "tile_loop.h"
 
@@ -103,12 +104,9 @@ __device__ __forceinline__ u32x2 pack8(const Raw8<BF>& raw, float s, float r) {
   return pack8(v, s, r);
 }
 
-// The largest of T lanes' values (T a power of two up to 64), in all of them.
 template <int T>
 __device__ __forceinline__ uint32_t lanes_max(uint32_t m) {
-#pragma unroll
-  for (int d = T / 2; d; d /= 2) m = max(m, (uint32_t)__shfl_xor((int)m, d, T));
-  return m;
+  return over_lanes<T>(m, [](uint32_t a, uint32_t b) __attribute__((always_inline)) { return max(a, b); });
 }
 
 // Rows alone: T threads a row, V vectors of eight values each, all in registers, or
@@ -226,19 +224,27 @@ __global__ __launch_bounds__(kThreads) void k_rows_both(RowQuantArgs a, int tm, 
   const int g = l / (tm * tn), mt = l % (tm * tn) / tn, nt = l % tn;
   const int tid = threadIdx.x, c = tid & 15, rg = tid >> 4;
   const int n0 = nt * 128, m0 = mt * 128, n = n0 + c * 8, r0 = m0 + rg * 8;
+  // the strips' maxima first: the scales are found while X is on its way
+  constexpr int kAhead = 16;
+  const bool row = tid < 128;
+  const int at = row ? m0 + tid : n0 + tid - 128, each = row ? a.M : a.N, parts = row ? sn : sm;
+  const uint32_t* part = (row ? a.rowmost : a.colmost) + (long long)g * parts * each + at;
+  uint32_t tops[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    tops[k] = 0;
+    if (k < parts && at < each) tops[k] = part[(long long)k * each];
+  }
   Raw8<BF> v[8];
 #pragma unroll
   for (int p = 0; p < 8; ++p)
     fetch8<BF, SMALL>(a.X, g * a.sX + (r0 + p) * a.ldx, n, r0 + p < a.M ? a.N : 0, v[p]);
   {
-    const bool row = tid < 128;
-    const int at = row ? m0 + tid : n0 + tid - 128, each = row ? a.M : a.N, parts = row ? sn : sm;
-    const uint32_t* p = (row ? a.rowmost : a.colmost) + (long long)g * parts * each + at;
     uint32_t top = 0;
-    if (at < each) {
-#pragma unroll 8
-      for (int k = 0; k < parts; ++k) top = max(top, p[(long long)k * each]);
-    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) top = max(top, tops[k]);
+    if (at < each)
+      for (int k = kAhead; k < parts; ++k) top = max(top, part[(long long)k * each]);
     const float s = scale_of(top);
     scale[tid] = s;
     inverse[tid] = 1.f / s;
@@ -255,8 +261,8 @@ __global__ __launch_bounds__(kThreads) void k_rows_both(RowQuantArgs a, int tm, 
 #pragma unroll
   for (int p = 0; p < 8; ++p) {
     if (r0 + p >= a.M) continue;
-    const long long row = (long long)g * a.M + r0 + p;
-    put(pack8<BF>(v[p], scale[rg * 8 + p], inverse[rg * 8 + p]), (u32x2*)(a.Q + row * ldq + n));
+    const long long to = (long long)g * a.M + r0 + p;
+    put(pack8<BF>(v[p], scale[rg * 8 + p], inverse[rg * 8 + p]), (u32x2*)(a.Q + to * ldq + n));
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
