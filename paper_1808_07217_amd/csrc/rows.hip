@@ -371,9 +371,10 @@ __device__ __forceinline__ float scaled(float sum, float sa, float sb, float bia
   return __builtin_fmaf(sum * lo, hi, bias);
 }
 
-// Eight neighbours of a row of C from LDS, n of them.
+// Eight neighbours of a row of C from LDS (`second`: from the fifth on), n of them.
 template <int SIZE>
-__device__ __forceinline__ void copy8(void* C, long long at, const uint8_t* from, int n) {
+__device__ __forceinline__ void copy8(void* C, long long at, const uint8_t* from,
+                                      const uint8_t* second, int n) {
   if constexpr (SIZE == 2) {
     bf16_t* c = (bf16_t*)C + at;
     if (n >= 8) {
@@ -385,9 +386,9 @@ __device__ __forceinline__ void copy8(void* C, long long at, const uint8_t* from
     float* c = (float*)C + at;
     if (n >= 8) {
       *(v4f_any*)c = *(const v4f*)from;
-      *(v4f_any*)(c + 4) = *(const v4f*)(from + 16);
+      *(v4f_any*)(c + 4) = *(const v4f*)second;
     } else {
-      for (int e = 0; e < n; ++e) c[e] = ((const float*)from)[e];
+      for (int e = 0; e < n; ++e) c[e] = ((const float*)(e < 4 ? from : second))[e % 4];
     }
   }
 }
@@ -395,21 +396,23 @@ __device__ __forceinline__ void copy8(void* C, long long at, const uint8_t* from
 enum { kOutFp32 = 0, kOutBf16 = 1, kOutSums = 2 };
 
 // Tiles of C by way of LDS, so that whole rows of a tile leave at once: a group of each
-// wavefront's columns at a time, half of their rows in each of two stages (a pitch of 16
-// bytes more than a row spreads the sixteen rows that a wavefront writes at once over the banks).
+// wavefront's columns at a time, half of their rows in each of two stages. Piece k of 16 bytes of
+// row r lies in slot k ^ (r % 16) (or as many as a row has), which spreads the rows that a wavefront
+// writes at once over the banks.
 // `ends`: the scales of B's rows, their biases, the scales of A's rows.
 template <int OUT, int THREADS, class T>
 __device__ __forceinline__ void tile_out(const T& t, const v4i (&acc)[T::FP][T::FQ],
                                          const float* ends, uint8_t* s0, uint8_t* s1, void* C,
                                          long long row0, long long ldc, int np, int nq) {
-  constexpr int kSize = OUT == kOutBf16 ? 2 : 4, kPitch = T::kP * kSize + 16;
+  constexpr int kSize = OUT == kOutBf16 ? 2 : 4, kPitch = T::kP * kSize;
+  constexpr int kSpread = (kPitch < 256 ? kPitch : 256) - 16;
   constexpr int kAcross = T::kQ / (T::FQ * 16);  // wavefronts along A's rows
   constexpr int kFit = T::kStage / kPitch * 2 / (kAcross * 16);
   constexpr int kGroup = kFit >= T::FQ ? T::FQ : (kFit >= 2 ? 2 : 1);  // columns of blocks at a time
   constexpr int kRows = kAcross * kGroup * 16, kHalf = kRows / 2;
   static_assert(kHalf * kPitch <= T::kStage && T::FQ % kGroup == 0, "half a group fits a stage");
   auto at = [&](int r, int p) __attribute__((always_inline)) {
-    return (r < kHalf ? s0 : s1) + r % kHalf * kPitch + p * kSize;
+    return (r < kHalf ? s0 : s1) + r % kHalf * kPitch + (p * kSize ^ (r * 16 & kSpread));
   };
   const int lane = t.lane, p0 = t.wp + (lane >> 4) * 4, side = t.wq / (T::FQ * 16);
 #pragma unroll
@@ -444,7 +447,7 @@ __device__ __forceinline__ void tile_out(const T& t, const v4i (&acc)[T::FP][T::
     for (int u = threadIdx.x; u < T::kP * kRows / 8; u += THREADS) {
       const int r = u / (T::kP / 8), p = u % (T::kP / 8) * 8;
       const int q = r / (kGroup * 16) * T::FQ * 16 + j0 * 16 + r % (kGroup * 16);
-      if (q < nq && p < np) copy8<kSize>(C, row0 + (long long)q * ldc + p, at(r, p), np - p);
+      if (q < nq && p < np) copy8<kSize>(C, row0 + (long long)q * ldc + p, at(r, p), at(r, p + 4), np - p);
     }
   }
 }
