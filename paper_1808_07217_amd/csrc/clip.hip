@@ -25,6 +25,7 @@ struct ClipArgs {
   long long each;                // values a chunk
   double most;
   double* part;                  // [K][all]
+  double* wide;                  // [K]: the norms; nullptr: found by who needs them
   float* norm;
 };
 
@@ -40,72 +41,111 @@ __device__ __forceinline__ double block_sum(double v, double (&room)[WAVES]) {
   return v;
 }
 
-// f(value) of every value of chunk c of replica k by T threads, `tid` of them this one; WRITE: the
-// value becomes f's. Eights, U of a thread in flight, where rows lie side by side, one by one
-// otherwise.
-template <bool BF, bool WRITE, int T, class F>
-__device__ __forceinline__ void each_value(const ClipTensor& t, long long k, long long c,
-                                           long long each, int tid, F f) {
-  constexpr int U = 4;
-  const long long n = t.M * t.N, e0 = c * each, e1 = min(n, e0 + each);
-  if (t.M == 1 || t.ld == t.N) {
-    const long long x = k * t.s + e0;
-    const int values = (int)(e1 - e0), whole = values / 8 * 8;
-    for (int e = tid * 8; e < whole; e += T * 8 * U) {
-      Raw8<BF> v[U];
+// The values of a chunk of one replica's tensor as T threads take them, `tid` of them this
+// one: eights, U of a thread in flight, where rows lie side by side (run(), from a set that start()
+// has on its way), one by one otherwise. f(value) for every one; WRITE: the value becomes f's.
+constexpr int kFlight = 4;
+template <bool BF, int T>
+struct Chunk {
+  static constexpr int U = kFlight;
+  const ClipTensor& t;
+  long long x, e0;  // the replica's first value; the chunk's first, of the replica's
+  int values, tid;
+  bool flat;
+  Raw8<BF> v[U];
+  __device__ __forceinline__ Chunk(const ClipTensor& t, long long k, long long c, long long each,
+                                   int tid)
+      : t(t), x(k * t.s), e0(c * each), tid(tid) {
+    values = (int)min(t.M * t.N - e0, each);
+    flat = t.M == 1 || t.ld == t.N;
+  }
+  __device__ __forceinline__ float read(long long at) const {
+    return BF ? bf16_to_f32(((const bf16_t*)t.p)[at]) : ((const float*)t.p)[at];
+  }
+  __device__ __forceinline__ void write(long long at, float w) const {
+    if constexpr (BF)
+      ((bf16_t*)t.p)[at] = f32_to_bf16(w);
+    else
+      ((float*)t.p)[at] = w;
+  }
+  __device__ __forceinline__ void fetch(int e) {
+    const int whole = values / 8 * 8;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (e + u * T * 8 < whole) fetch8<BF>(t.p, x + e + u * T * 8, 0, 8, v[u]);
+    for (int u = 0; u < U; ++u)
+      if (e + u * T * 8 < whole) fetch8<BF>(t.p, x + e0 + e + u * T * 8, 0, 8, v[u]);
+  }
+  __device__ __forceinline__ void start() {
+    if (flat) fetch(tid * 8);
+  }
+  template <bool WRITE, class F>
+  __device__ __forceinline__ void run(F f) {
+    if (flat) {
+      const int whole = values / 8 * 8;
+      for (int e = tid * 8; e < whole; e += T * 8 * U) {
+        if (e != tid * 8) fetch(e);
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (e + u * T * 8 < whole) {
-          float w[8];
+        for (int u = 0; u < U; ++u)
+          if (e + u * T * 8 < whole) {
+            float w[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) w[i] = f(v[u][i]);
-          if constexpr (WRITE) store8<BF>(t.p, x + e + u * T * 8, 0, 8, w);
+            for (int i = 0; i < 8; ++i) w[i] = f(v[u][i]);
+            if constexpr (WRITE) store8<BF>(t.p, x + e0 + e + u * T * 8, 0, 8, w);
+          }
+      }
+      if (tid < values - whole) {
+        const long long at = x + e0 + whole + tid;
+        const float w = f(read(at));
+        if constexpr (WRITE) write(at, w);
+      }
+    } else {
+      const long long dm = T / t.N, dn = T - dm * t.N;
+      long long m = (e0 + tid) / t.N, j = e0 + tid - m * t.N;
+      for (int e = tid; e < values; e += T) {
+        const long long at = x + m * t.ld + j;
+        const float w = f(read(at));
+        if constexpr (WRITE) write(at, w);
+        m += dm;
+        j += dn;
+        if (j >= t.N) {
+          j -= t.N;
+          ++m;
         }
-    }
-    if (tid < values - whole) {
-      const long long at = x + whole + tid;
-      const float w = f(BF ? bf16_to_f32(((const bf16_t*)t.p)[at]) : ((const float*)t.p)[at]);
-      if constexpr (WRITE) {
-        if constexpr (BF)
-          ((bf16_t*)t.p)[at] = f32_to_bf16(w);
-        else
-          ((float*)t.p)[at] = w;
-      }
-    }
-  } else {
-    const long long dm = T / t.N, dn = T - dm * t.N;
-    long long m = (e0 + tid) / t.N, j = e0 + tid - m * t.N;
-    for (long long e = e0 + tid; e < e1; e += T) {
-      const long long at = k * t.s + m * t.ld + j;
-      const float w = f(BF ? bf16_to_f32(((const bf16_t*)t.p)[at]) : ((const float*)t.p)[at]);
-      if constexpr (WRITE) {
-        if constexpr (BF)
-          ((bf16_t*)t.p)[at] = f32_to_bf16(w);
-        else
-          ((float*)t.p)[at] = w;
-      }
-      m += dm;
-      j += dn;
-      if (j >= t.N) {
-        j -= t.N;
-        ++m;
       }
     }
   }
+};
+// Which of the launch's tensors holds a replica's chunk c: one comparison a lane.
+__device__ __forceinline__ int tensor_of(const ClipArgs& a, int c) {
+  static_assert(kBatch == 64, "a tensor a lane");
+  const int lane = threadIdx.x & 63;
+  const bool starts = lane < a.count && a.t[lane].first <= c;
+  return __popcll(__ballot(starts)) - 1;
 }
-template <bool WRITE, int T, class F>
-__device__ __forceinline__ void each_of(const ClipArgs& a, int k, int c, int tid, F f) {
-  int i = 0;
-  for (int step = kBatch / 2; step; step /= 2)  // the last tensor that starts at c or before
-    if (i + step < a.count && a.t[i + step].first <= c) i += step;
-  const ClipTensor& t = a.t[i];
-  if (t.bf16)
-    each_value<true, WRITE, T>(t, k, c - t.first, a.each, tid, f);
-  else
-    each_value<false, WRITE, T>(t, k, c - t.first, a.each, tid, f);
+// body(chunk) for the chunk c of replica k.
+template <int T, class B>
+__device__ __forceinline__ void with_chunk(const ClipArgs& a, int k, int c, int tid, B body) {
+  const ClipTensor& t = a.t[tensor_of(a, c)];
+  if (t.bf16) {
+    Chunk<true, T> chunk(t, k, c - t.first, a.each, tid);
+    body(chunk);
+  } else {
+    Chunk<false, T> chunk(t, k, c - t.first, a.each, tid);
+    body(chunk);
+  }
+}
+struct Squares {
+  double sum = 0.0;
+  __device__ __forceinline__ float operator()(float v) {
+    sum = __builtin_fma((double)v, (double)v, sum);
+    return v;
+  }
+};
+template <class C>
+__device__ __forceinline__ double squares_of(C& chunk) {
+  Squares q;
+  chunk.start();
+  chunk.template run<false>([&](float v) __attribute__((always_inline)) { return q(v); });
+  return q.sum;
 }
 
 __global__ __launch_bounds__(kThreads) void k_clip_sums(ClipArgs a, long long total) {
@@ -114,10 +154,7 @@ __global__ __launch_bounds__(kThreads) void k_clip_sums(ClipArgs a, long long to
   if (id >= total) return;
   const int k = id / a.chunks, c = id - k * a.chunks;
   double sum = 0.0;
-  each_of<false, kThreads>(a, k, c, threadIdx.x, [&](float v) {
-    sum = __builtin_fma((double)v, (double)v, sum);
-    return v;
-  });
+  with_chunk<kThreads>(a, k, c, threadIdx.x, [&](auto& chunk) { sum = squares_of(chunk); });
   sum = block_sum(sum, room);
   if (threadIdx.x == 0) a.part[(long long)k * a.all + a.base + c] = sum;
 }
@@ -131,48 +168,61 @@ __global__ __launch_bounds__(kOneThreads) void k_clip_one(ClipArgs a, int scale)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   double sum = 0.0;
   for (int c = wave; c < a.chunks; c += kOneThreads / 64)
-    each_of<false, 64>(a, k, c, lane, [&](float v) {
-      sum = __builtin_fma((double)v, (double)v, sum);
-      return v;
-    });
+    with_chunk<64>(a, k, c, lane, [&](auto& chunk) { sum += squares_of(chunk); });
   const double norm = sqrt(block_sum(sum, room));
   if (threadIdx.x == 0) a.norm[k] = (float)norm;
   if (!scale || !(norm > a.most) || norm == __builtin_inf()) return;
   const double f = a.most / norm;
   for (int c = wave; c < a.chunks; c += kOneThreads / 64)
-    each_of<true, 64>(a, k, c, lane, [&](float v) { return (float)(v * f); });
+    with_chunk<64>(a, k, c, lane, [&](auto& chunk) {
+      chunk.start();
+      chunk.template run<true>([&](float v) { return (float)(v * f); });
+    });
 }
 
-__device__ __forceinline__ double norm_of(const ClipArgs& a, int k,
-                                          double (&room)[kThreads / 64]) {
+template <int T>
+__device__ __forceinline__ double norm_of(const ClipArgs& a, int k, double (&room)[T / 64]) {
   double sum = 0.0;
-  for (int i = threadIdx.x; i < a.all; i += kThreads) sum += a.part[(long long)k * a.all + i];
+  const double* p = a.part + (long long)k * a.all;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < a.all; i += T) sum += p[i];
   return sqrt(block_sum(sum, room));
 }
 
-__global__ __launch_bounds__(kThreads) void k_clip_norm(ClipArgs a) {
-  __shared__ double room[kThreads / 64];
+constexpr int kNormThreads = 1024;
+__global__ __launch_bounds__(kNormThreads) void k_clip_norm(ClipArgs a) {
+  __shared__ double room[kNormThreads / 64];
   const unsigned k = workgroup_id();
-  const double norm = norm_of(a, k, room);
-  if (threadIdx.x == 0) a.norm[k] = (float)norm;
+  const double norm = norm_of<kNormThreads>(a, k, room);
+  if (threadIdx.x != 0) return;
+  a.norm[k] = (float)norm;
+  if (a.wide) a.wide[k] = norm;
 }
 
+// The chunks from the last to the first, eight by eight: what the launch before read last is in
+// the caches still, a chunk's in that of the XCD that both launches give it to.
 __global__ __launch_bounds__(kThreads) void k_clip_scale(ClipArgs a, long long total) {
   __shared__ double room[kThreads / 64];
-  const unsigned first = workgroup_id();
-  if (first >= total) return;
-  const unsigned id = (unsigned)(total - 1 - first);
+  const unsigned first = workgroup_id(), eights = (unsigned)((total + kXcds - 1) / kXcds);
+  if (first >= eights * kXcds) return;
+  const unsigned id = (eights - 1 - first / kXcds) * kXcds + first % kXcds;
+  if (id >= total) return;
   const int k = id / a.chunks, c = id - k * a.chunks;
-  const double norm = norm_of(a, k, room);
-  if (a.base + c == 0 && threadIdx.x == 0) a.norm[k] = (float)norm;
-  // (a norm that is infinite or no number leaves the values as they are)
-  if (!(norm > a.most) || norm == __builtin_inf()) return;
-  const double f = a.most / norm;
-  each_of<true, kThreads>(a, k, c, threadIdx.x, [&](float v) { return (float)(v * f); });
+  with_chunk<kThreads>(a, k, c, threadIdx.x, [&](auto& chunk) {
+    chunk.start();  // on its way while the norm is found
+    const double norm = a.wide ? a.wide[k] : norm_of<kThreads>(a, k, room);
+    if (!a.wide && a.base + c == 0 && threadIdx.x == 0) a.norm[k] = (float)norm;
+    // (a norm that is infinite or no number leaves the values as they are)
+    if (!(norm > a.most) || norm == __builtin_inf()) return;
+    const double f = a.most / norm;
+    chunk.template run<true>([&](float v) { return (float)(v * f); });
+  });
 }
 
-// The cut: values a chunk (about kChunks chunks in all), and a replica's chunks.
-constexpr long long kChunks = 2048, kLeast = 4096;
+// The cut: values a chunk, for about kChunks chunks in all and at least kLeast values; and a
+// replica's chunks. From kWide of them on their sums are added by a launch of its own.
+constexpr long long kChunks = 16384, kLeast = 6144, kStep = 2048;
+constexpr int kWide = 512;
 double values_of(int count, const ClipTensor* t) {
   double values = 0;
   for (int i = 0; i < count; ++i) values += (double)t[i].M * t[i].N;
@@ -184,7 +234,7 @@ bool in_one(int count, const ClipTensor* t) {
 long long chunk_values(int K, int count, const ClipTensor* t) {
   if (in_one(count, t)) return kOneChunk;
   const double each = values_of(count, t) * K / kChunks;
-  return std::min(((long long)(each / kLeast) + 1) * kLeast, 1LL << 30);
+  return std::min(std::max(((long long)(each / kStep) + 1) * kStep, kLeast), 1LL << 30);
 }
 long long chunks_of(const ClipTensor& t, long long each) { return (t.M * t.N + each - 1) / each; }
 
@@ -195,7 +245,7 @@ size_t clip_workspace_bytes(int K, int count, const ClipTensor* t) {
   const long long each = chunk_values(K, count, t);
   size_t all = 0;
   for (int i = 0; i < count; ++i) all += chunks_of(t[i], each);
-  return all * K * sizeof(double);
+  return (all + 1) * K * sizeof(double);
 }
 
 hipError_t launch_clip(int K, int count, const ClipTensor* t, bool scale, double most, float* norm,
@@ -221,11 +271,12 @@ hipError_t launch_clip(int K, int count, const ClipTensor* t, bool scale, double
     hipLaunchKernelGGL(k_clip_one, dim3(K), dim3(kOneThreads), 0, s, a, (int)scale);
     return hipGetLastError();
   }
+  a.wide = scale && all >= kWide ? a.part + (size_t)all * K : nullptr;
   // the tensors in batches, in the second pass from the last to the first
   const int batches = (count + kBatch - 1) / kBatch;
-  for (int pass = 0; pass < (scale ? 2 : 1); ++pass)
+  auto pass = [&](auto launch, bool reverse) {
     for (int n = 0; n < batches; ++n) {
-      const int from = (pass ? batches - 1 - n : n) * kBatch;
+      const int from = (reverse ? batches - 1 - n : n) * kBatch;
       a.count = std::min(kBatch, count - from);
       long long base = 0, chunks = 0;
       for (int i = 0; i < from; ++i) base += chunks_of(t[i], a.each);
@@ -236,19 +287,24 @@ hipError_t launch_clip(int K, int count, const ClipTensor* t, bool scale, double
       }
       a.base = (int)base;
       a.chunks = (int)chunks;
-      const long long total = chunks * K;
-      if (pass)
-        hipLaunchKernelGGL(k_clip_scale, grid_of(total), dim3(kThreads), 0, s, a, total);
-      else
-        hipLaunchKernelGGL(k_clip_sums, grid_of(total), dim3(kThreads), 0, s, a, total);
+      launch(chunks * K);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-  if (!scale) {
-    hipLaunchKernelGGL(k_clip_norm, dim3(K), dim3(kThreads), 0, s, a);
-    return hipGetLastError();
+    return hipSuccess;
+  };
+  hipError_t e = pass([&](long long total) {
+    hipLaunchKernelGGL(k_clip_sums, grid_of(total), dim3(kThreads), 0, s, a, total);
+  }, false);
+  if (e != hipSuccess) return e;
+  if (!scale || a.wide) {
+    hipLaunchKernelGGL(k_clip_norm, dim3(K), dim3(kNormThreads), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess || !scale) return e;
   }
-  return hipSuccess;
+  return pass([&](long long total) {
+    hipLaunchKernelGGL(k_clip_scale, grid_of((total + kXcds - 1) / kXcds * kXcds), dim3(kThreads), 0,
+                       s, a, total);
+  }, true);
 }
 
 }  // namespace lsgd

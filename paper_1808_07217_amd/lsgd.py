@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import itertools
 import os
 from typing import NamedTuple, Optional, Sequence, Tuple, Union
 
@@ -1072,48 +1073,58 @@ def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
     return out, dweight, dbias
 
 
+_CODE = {torch.float32: FP32, torch.bfloat16: BF16}
+
+
 def _tensor_table(tensors: Sequence[torch.Tensor]):
     """(replicas, device, [(address, M, N, ld, s, type code), ...]) of tensors [K][...]."""
     if isinstance(tensors, torch.Tensor) or not len(tensors):
         raise ValueError("tensors must be a non-empty sequence of tensors")
-    table, K, dev = [], None, tensors[0].device
+    table, K, index = [], 0, tensors[0].get_device()
+    if index < 0:
+        raise ValueError("tensors must be on a CUDA (HIP) device")
     for t in tensors:
-        shape, stride, n = t.shape, t.stride(), t.dim()
-        if t.dtype not in _FLOATS or not n or not t.numel():
-            raise ValueError("tensors must be non-empty float32 or bfloat16 [K][...]")
-        if K is None:
-            K = shape[0]
-        if not t.is_cuda or t.device != dev:
-            raise ValueError("tensors must be on one CUDA (HIP) device")
+        shape, code = t.shape, _CODE.get(t.dtype)
+        n = len(shape)
+        if code is None or not n:
+            raise ValueError("tensors must be float32 or bfloat16 [K][...]")
+        if t.get_device() != index:
+            raise ValueError("tensors must be on one device")
         if shape[0] != K:
-            raise ValueError("tensors must have one number of replicas")
+            if table or not shape[0]:
+                raise ValueError("tensors must have one number of replicas, at least 1")
+            K = shape[0]
+        stride = t.stride()
         if n == 3:
-            M, N = shape[1], shape[2]
+            _, M, N = shape
             ld, one = (stride[1] if M > 1 else N), (stride[2] if N > 1 else 1)
         else:
-            M, N, one = 1, t.numel() // K, 1
-            ld, run = N, 1  # a replica's values: one run without gaps
+            M = N = one = 1  # a replica's values: one run without gaps
             for d in range(n - 1, 0, -1):
-                if shape[d] > 1 and stride[d] != run:
+                if shape[d] != 1 and stride[d] != N:
                     one = 0
-                run *= shape[d]
+                N *= shape[d]
+            ld = N
+        if not M * N:
+            raise ValueError("tensors must not be empty")
         if one != 1 or ld < N:
             raise ValueError("a replica's values must be contiguous, or [M][N] of contiguous rows")
-        table.append((t.data_ptr(), M, N, ld, stride[0] if K > 1 else 0,
-                      BF16 if t.dtype == torch.bfloat16 else FP32))
-    return K, dev, table
+        table.append((t.data_ptr(), M, N, ld, stride[0] if K > 1 else 0, code))
+    return K, torch.device("cuda", index), table
 
 
 def _runs_apart(K: int, table) -> bool:
     """Whether no two of the tensors share a byte (each replica's own being apart)."""
     size = (4, 2)
-    runs = sorted((p, p + ((M - 1) * ld + N) * size[d], s * size[d]) for p, M, N, ld, s, d in table)
-    # tensors one after the other
-    if all(a[1] + (K - 1) * a[2] <= b[0] for a, b in zip(runs, runs[1:])):
-        return True
-    # replicas in rows of one length, in each of them the tensors one after the other
-    if all(a[1] <= b[0] and a[2] == b[2] for a, b in zip(runs, runs[1:])) and (
-            runs[-1][1] - runs[0][0] <= runs[0][2]):
+    runs = sorted([(p, p + ((M - 1) * ld + N) * size[d], s * size[d]) for p, M, N, ld, s, d in table])
+    one = flat = True
+    first, end, step = runs[0]
+    row = step
+    for p, e, s in runs[1:]:
+        one = one and end + (K - 1) * step <= p   # tensors one after the other
+        flat = flat and end <= p and s == row     # in each replica's row of one length
+        end, step = e, s
+    if one or (flat and end - first <= row):
         return True
     starts, ends = [], []
     for p, M, N, ld, s, d in table:
@@ -1132,7 +1143,7 @@ def _clip_call(tensors, written: bool, *bound) -> torch.Tensor:
     if written and not _runs_apart(K, table):
         raise ValueError("tensors must not overlap")
     n = len(table)
-    h = (_L * (6 * n))(*[v for row in table for v in row])
+    h = (_L * (6 * n))(*itertools.chain.from_iterable(table))
     nb = _c.c_size_t()
     _check(_lib.lsgd_gradient_norm_workspace_bytes(K, n, h, _c.byref(nb)))
     ws = torch.empty(nb.value, dtype=torch.uint8, device=dev) if nb.value else None
