@@ -18,24 +18,30 @@ namespace {
 constexpr int kThreads = 256;
 
 // The sums over T threads of a row (T a power of two; wavefronts of a row's own from 64
-// on, all of the workgroup's above 64), in all of them; `room`: a wavefront's sums each, another
-// room than the last call's (whose sums may still be read by some).
+// on), in all of them; `room`: a wavefront's sums each, another room than the last call's (whose
+// sums may still be read by some). From T = 128 on every thread of the workgroup calls it.
 template <int T, int K, class A>
 __device__ __forceinline__ void row_sums(A (&v)[K], A (*room)[K]) {
 #pragma unroll
   for (int k = 0; k < K; ++k) v[k] = lanes_sum<(T < 64 ? T : 64)>(v[k]);
   if constexpr (T > 64) {
+    const int wave = threadIdx.x >> 6, first = wave / (T / 64) * (T / 64);
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-      for (int k = 0; k < K; ++k) room[threadIdx.x >> 6][k] = v[k];
+      for (int k = 0; k < K; ++k) room[wave][k] = v[k];
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      v[k] = room[0][k];
+      v[k] = room[first][k];
 #pragma unroll
-      for (int w = 1; w < T / 64; ++w) v[k] += room[w][k];
+      for (int w = 1; w < T / 64; ++w) v[k] += room[first + w][k];
     }
   }
+}
+// Which of a workgroup's rows a thread works on (the same in a whole wavefront from T = 64 on).
+template <int T>
+__device__ __forceinline__ int slot_of() {
+  return T < 64 ? threadIdx.x / T : __builtin_amdgcn_readfirstlane(threadIdx.x / T);
 }
 
 struct Moments {
@@ -51,15 +57,14 @@ __device__ __forceinline__ float inverse_root(double mean_square, float eps) {
 
 // A strip of rows a workgroup, T threads a row, V vectors of eight values each, in registers;
 // the next row is on its way while one is summed.
-template <bool XBF, bool YBF, int T, int V>
-__global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm(NormArgs a, int strips,
-                                                                      long long total) {
-  constexpr int kBlock = T < kThreads ? kThreads : T, kRows = kBlock / T;
+template <bool XBF, bool YBF, int T, int V, int B>
+__global__ __launch_bounds__(B) void k_norm(NormArgs a, int strips, long long total) {
+  constexpr int kBlock = B, kRows = kBlock / T;
   __shared__ double room[2][kBlock / 64][1];
   const unsigned id = workgroup_id();
   if (id >= total) return;
   const int g = id / strips, m0 = (id - g * strips) * a.strip;
-  const int t = threadIdx.x % T, slot = threadIdx.x / T, end = min(a.M, m0 + a.strip);
+  const int t = threadIdx.x % T, slot = slot_of<T>(), end = min(a.M, m0 + a.strip);
   Raw8<XBF> raw[V];
   auto fetch = [&](int m) __attribute__((always_inline)) {
 #pragma unroll
@@ -180,17 +185,17 @@ __device__ __forceinline__ void opaque(Raw8<BF>& v) {
 // arithmetic of a row. Of rows of few columns little is left beside the two directions that are
 // taken out (of two columns eps / variance of e): those in fp64.
 constexpr int kNarrow = 8;
-template <bool XBF, bool YBF, int T, int V, class A>
-__global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm_back(NormBackArgs a,
-                                                                           long long total) {
-  constexpr int kBlock = T < kThreads ? kThreads : T, kRows = kBlock / T, kCols = T * V * 8;
+template <bool XBF, bool YBF, int T, int V, int B, class A>
+__global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total) {
+  constexpr int kBlock = B, kRows = kBlock / T, kCols = T * V * 8;
   __shared__ A room[2][kBlock / 64][2];
   __shared__ float slots[kRows > 1 ? kRows * kCols : 1];
   const unsigned id = workgroup_id();
   if (id >= total) return;
   const int g = id / a.strips, strip = id - g * a.strips, m0 = strip * a.strip;
-  const int t = threadIdx.x % T, slot = threadIdx.x / T, end = min(a.M, m0 + a.strip);
-  // a row as it was read, and the next one on its way
+  const int t = threadIdx.x % T, slot = slot_of<T>(), end = min(a.M, m0 + a.strip);
+  // a row as it was read, and the next one on its way (which four vectors leave no registers for)
+  constexpr bool kAhead = V < 4;
   Raw8<XBF> xr[V], xn[V];
   Raw8<YBF> dr[V], dn[V];
   float mean_next = 0.f, rstd_next = 0.f;
@@ -204,7 +209,7 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm_back(NormB
     mean_next = m < end ? a.mean[(long long)g * a.M + m] : 0.f;
     rstd_next = m < end ? a.rstd[(long long)g * a.M + m] : 0.f;
   };
-  fetch(m0 + slot);
+  if (kAhead) fetch(m0 + slot);
   float w[V][8], dw[V][8], db[V][8];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
@@ -217,13 +222,14 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_norm_back(NormB
   for (int r = m0; r < end; r += kRows, odd ^= 1) {
     const int m = r + slot;
     A s[2] = {0, 0};
+    if (!kAhead) fetch(m);
     const A mean = mean_next, rstd = rstd_next;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       xr[i] = xn[i];
       dr[i] = dn[i];
     }
-    if (r + kRows < end) fetch(m + kRows);
+    if (kAhead && r + kRows < end) fetch(m + kRows);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
@@ -387,89 +393,96 @@ __global__ __launch_bounds__(kThreads) void k_norm_params(NormBackArgs a, int ti
 }
 
 // ------------------------------------------------------------------ launches
-// Threads and vectors a row of N values takes; T == 0: any length.
-struct RowShape {
-  int T, V;
-};
-RowShape row_shape(int N) {
-  if (N <= 128) return {16, 1};
-  if (N <= 512) return {64, 1};
-  if (N <= 1024) return {64, 2};
-  if (N <= 2048) return {256, 1};
-  if (N <= 4096) return {256, 2};
-  if (N <= 8192) return {512, 2};
-  if (N <= 16384) return {1024, 2};
-  return {0, 0};
-}
-template <int T, int V>
+// Threads and vectors a row of N values takes, and threads of a workgroup; T == 0: any length.
+template <int T_, int V_, int B_>
 struct Shape {
-  static constexpr int t = T, v = V;
+  static constexpr int T = T_, V = V_, B = B_;
 };
 template <class F>
-hipError_t with_shape(int N, F f) {
-  const RowShape s = row_shape(N);
-  if (s.T == 16) return f(Shape<16, 1>{});
-  if (s.T == 64) return s.V == 1 ? f(Shape<64, 1>{}) : f(Shape<64, 2>{});
-  if (s.T == 256) return s.V == 1 ? f(Shape<256, 1>{}) : f(Shape<256, 2>{});
-  if (s.T == 512) return f(Shape<512, 2>{});
-  return f(Shape<1024, 2>{});
+auto with_shape(int N, F f) {
+  if (N <= 128) return f(Shape<16, 1, 256>{});
+  if (N <= 512) return f(Shape<64, 1, 256>{});
+  if (N <= 1024) return f(Shape<64, 2, 256>{});
+  if (N <= 2048) return f(Shape<256, 1, 256>{});
+  if (N <= 4096) return f(Shape<256, 2, 256>{});
+  if (N <= 8192) return f(Shape<512, 2, 512>{});
+  if (N <= 16384) return f(Shape<1024, 2, 1024>{});
+  return f(Shape<0, 0, 0>{});
 }
-// Rows of a strip: about `strips` strips in all, of whole sets of rows at work at one time.
-constexpr long long kStrips = 1024, kBackStrips = 256;
-int strip_rows(long long strips, int G, int M, int N) {
-  const RowShape s = row_shape(N);
-  const int each = s.T == 0 ? 4 : std::max(1, kThreads / s.T);
+// Backward, where sums of the columns stay in registers, and few strips leave few of them to add.
+template <class F>
+auto with_back_shape(int N, F f) {
+  if (N <= kNarrow) return f(Shape<16, 1, 256>{});
+  if (N <= 128) return f(Shape<16, 1, 1024>{});
+  if (N <= 512) return f(Shape<64, 1, 1024>{});
+  if (N <= 1024) return f(Shape<128, 1, 1024>{});
+  if (N <= 2048) return f(Shape<256, 1, 1024>{});
+  if (N <= 4096) return f(Shape<512, 1, 1024>{});
+  if (N <= 8192) return f(Shape<512, 2, 512>{});
+  if (N <= 16384) return f(Shape<512, 4, 512>{});
+  return f(Shape<0, 0, 0>{});
+}
+// Rows of a strip: about `strips` strips in all, of whole sets of `each` rows at work at one time.
+int strip_rows(long long strips, int each, int G, int M) {
   strips = std::max(1LL, strips / G);
   const long long rows = (M + strips - 1) / strips;
   return (int)((rows + each - 1) / each * each);
 }
+constexpr long long kStrips = 1024;
 
 template <bool XBF, bool YBF>
 hipError_t norm(NormArgs a, hipStream_t s) {
-  if (row_shape(a.N).T == 0) {
-    const long long total = (long long)a.G * a.M;
-    if (total > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_norm_long<XBF, YBF>), grid_of(total), dim3(kLong), 0, s, a, total);
-    return hipGetLastError();
-  }
-  a.strip = strip_rows(kStrips, a.G, a.M, a.N);
-  const int strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
-  const long long total = (long long)strips * a.G;
   return with_shape(a.N, [&](auto z) {
-    constexpr int T = decltype(z)::t, V = decltype(z)::v;
-    hipLaunchKernelGGL((k_norm<XBF, YBF, T, V>), grid_of(total), dim3(T < kThreads ? kThreads : T),
-                       0, s, a, strips, total);
+    constexpr int T = decltype(z)::T, V = decltype(z)::V, B = decltype(z)::B;
+    if constexpr (T == 0) {
+      const long long total = (long long)a.G * a.M;
+      if (total > 0x7fffffffLL) return hipErrorInvalidValue;
+      hipLaunchKernelGGL((k_norm_long<XBF, YBF>), grid_of(total), dim3(kLong), 0, s, a, total);
+    } else {
+      a.strip = strip_rows(kStrips, B / T, a.G, a.M);
+      const int strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
+      const long long total = (long long)strips * a.G;
+      hipLaunchKernelGGL((k_norm<XBF, YBF, T, V, B>), grid_of(total), dim3(B), 0, s, a, strips, total);
+    }
     return hipGetLastError();
+  });
+}
+
+// One strip, and no second launch, where each of a workgroup's places for rows gets few.
+constexpr int kFewRows = 16;
+constexpr long long kBackStrips = 256, kNarrowStrips = 1024;
+int back_strip_rows(int G, int M, int N) {
+  return with_back_shape(N, [&](auto z) {
+    constexpr int T = decltype(z)::T, B = decltype(z)::B;
+    constexpr int each = T == 0 ? 4 : B / (T == 0 ? 1 : T);
+    if (M <= kFewRows * each) return (M + each - 1) / each * each;
+    return strip_rows(N <= kNarrow ? kNarrowStrips : kBackStrips, each, G, M);
   });
 }
 
 template <bool XBF, bool YBF>
 hipError_t norm_back(NormBackArgs a, void* ws, hipStream_t s) {
-  a.strip = strip_rows(kBackStrips, a.G, a.M, a.N);
+  a.strip = back_strip_rows(a.G, a.M, a.N);
   a.strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
   a.part = (float*)ws;
   const long long strips = (long long)a.strips * a.G;
-  hipError_t e;
-  if (row_shape(a.N).T == 0) {
-    const long long total = (long long)a.G * a.M, tiles = (a.N + 511LL) / 512;
-    if (total > 0x7fffffffLL || tiles * strips > 0x7fffffffLL) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((k_norm_back_long<XBF, YBF>), grid_of(total), dim3(kLong), 0, s, a, total);
-    if ((e = hipGetLastError()) != hipSuccess || !a.dw) return e;
-    hipLaunchKernelGGL((k_norm_params<XBF, YBF>), grid_of(tiles * strips), dim3(kThreads), 0, s, a,
-                       (int)tiles, tiles * strips);
-    e = hipGetLastError();
-  } else if (a.N <= kNarrow) {
-    hipLaunchKernelGGL((k_norm_back<XBF, YBF, 16, 1, double>), grid_of(strips), dim3(kThreads), 0, s,
-                       a, strips);
-    e = hipGetLastError();
-  } else {
-    e = with_shape(a.N, [&](auto z) {
-      constexpr int T = decltype(z)::t, V = decltype(z)::v;
-      hipLaunchKernelGGL((k_norm_back<XBF, YBF, T, V, float>), grid_of(strips),
-                         dim3(T < kThreads ? kThreads : T), 0, s, a, strips);
-      return hipGetLastError();
-    });
-  }
+  hipError_t e = with_back_shape(a.N, [&](auto z) {
+    constexpr int T = decltype(z)::T, V = decltype(z)::V, B = decltype(z)::B;
+    if constexpr (T == 0) {
+      const long long total = (long long)a.G * a.M, tiles = (a.N + 511LL) / 512;
+      if (total > 0x7fffffffLL || tiles * strips > 0x7fffffffLL) return hipErrorInvalidValue;
+      hipLaunchKernelGGL((k_norm_back_long<XBF, YBF>), grid_of(total), dim3(kLong), 0, s, a, total);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess || !a.dw) return e;
+      hipLaunchKernelGGL((k_norm_params<XBF, YBF>), grid_of(tiles * strips), dim3(kThreads), 0, s, a,
+                         (int)tiles, tiles * strips);
+    } else {
+      typedef std::conditional_t<T == 16 && B == 256, double, float> A;
+      hipLaunchKernelGGL((k_norm_back<XBF, YBF, T, V, B, A>), grid_of(strips), dim3(B), 0, s, a,
+                         strips);
+    }
+    return hipGetLastError();
+  });
   if (e != hipSuccess || !a.dw || a.strips == 1) return e;
   const long long tiles = (a.N + 63LL) / 64, total = tiles * 2 * a.G;
   if (total > 0x7fffffffLL) return hipErrorInvalidValue;
@@ -485,7 +498,7 @@ hipError_t launch_norm(int x_bf16, int y_bf16, const NormArgs& a, hipStream_t s)
 }
 
 size_t norm_back_workspace_bytes(int G, int M, int N) {
-  const long long strip = strip_rows(kBackStrips, G, M, N), strips = (M + strip - 1) / strip;
+  const long long strip = back_strip_rows(G, M, N), strips = (M + strip - 1) / strip;
   return strips == 1 ? 0 : (size_t)G * strips * 2 * N * sizeof(float);
 }
 

@@ -585,7 +585,7 @@ def _enqueue(device: torch.device, call, *args) -> None:
     calling thread's. (The stream's raw handle: a torch.cuda.Stream object costs as
     much as the launch.)"""
     i = device.index
-    if i == torch.cuda.current_device():
+    if i == torch._C._cuda_getDevice():
         _check(call(*args, torch._C._cuda_getCurrentRawStream(i)))
     else:
         with torch.cuda.device(i):

@@ -48,8 +48,9 @@ def _check_forward(got, X, w, b):
 
 def _check_backward(got, dY, X, mean, rstd, w):
     """n rounds twice, e = dy w once. A row's sums are added along at most 40 + N / 1024
-    terms one after the other, a column's along at most a strip's rows and its slots. Rows of
-    up to 8 columns are computed in fp64."""
+    terms one after the other, a column's along the rows that a thread takes of a strip (at most 16,
+    or a 256th of all groups' rows) and up to 64 threads'. Rows of up to 8 columns are
+    computed in fp64."""
     dx, dw, db = got
     G, M, N = X.shape
     rx, rw, rb = O.layer_norm_backward(dY, X, mean, rstd, w)
@@ -68,7 +69,7 @@ def _check_backward(got, dY, X, mean, rstd, w):
     assert np.all(err <= bound), np.max(err / bound)
     if dw is None:
         return
-    R = min(M, -(-M // max(1, 256 // G)) + 16) + 20  # (of at least 256 strips in all)
+    R = min(M, -(-M // max(1, 256 // G)) + 16) + 64
     assert np.all(np.abs(_np(dw) - rw) <= gamma(R + 3) * np.abs(dY * n).sum(1) + 2.0 ** -140)
     assert np.all(np.abs(_np(db) - rb) <= gamma(R) * np.abs(dY).sum(1) + 2.0 ** -140)
 
@@ -269,7 +270,7 @@ def test_on_a_side_stream_and_in_a_graph():
         assert all(torch.equal(p, q) for p, q in zip(out, step()))
 
 
-@pytest.mark.parametrize("shape", [(1, 40000, 33), (2, 3000, 700), (1, 40, 17000)])
+@pytest.mark.parametrize("shape", [(1, 40000, 33), (2, 3000, 700), (1, 140, 17000)])
 def test_whatever_the_workspace_holds(shape):
     """The caller's own workspace of exactly the size asked for: the same bits, and nothing
     behind its end written."""
