@@ -428,7 +428,7 @@ int strip_rows(long long strips, int each, int G, int M) {
   const long long rows = (M + strips - 1) / strips;
   return (int)((rows + each - 1) / each * each);
 }
-constexpr long long kStrips = 1024;
+constexpr long long kStrips = 1024, kSmallStrips = 4096;  // of workgroups of 512 and more threads, of 256
 
 template <bool XBF, bool YBF>
 hipError_t norm(NormArgs a, hipStream_t s) {
@@ -439,7 +439,7 @@ hipError_t norm(NormArgs a, hipStream_t s) {
       if (total > 0x7fffffffLL) return hipErrorInvalidValue;
       hipLaunchKernelGGL((k_norm_long<XBF, YBF>), grid_of(total), dim3(kLong), 0, s, a, total);
     } else {
-      a.strip = strip_rows(kStrips, B / T, a.G, a.M);
+      a.strip = strip_rows(B == 256 ? kSmallStrips : kStrips, B / T, a.G, a.M);
       const int strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
       const long long total = (long long)strips * a.G;
       hipLaunchKernelGGL((k_norm<XBF, YBF, T, V, B>), grid_of(total), dim3(B), 0, s, a, strips, total);
