@@ -866,8 +866,8 @@ def quantise_rows(X: torch.Tensor, both: bool = False) -> Union[Rows, Tuple[Rows
     ldx, sX = _matrices("X", X, _FLOATS)
     G, M, N = X.shape
     dev = X.device
-    q = torch.empty((G, M, _up(N, 128)), dtype=torch.int8, device=dev)
-    s = torch.empty((G, M), dtype=torch.float32, device=dev)
+    q = X.new_empty((G, M, _up(N, 128)), dtype=torch.int8)
+    s = X.new_empty((G, M), dtype=torch.float32)
     dt = BF16 if X.dtype == torch.bfloat16 else FP32
     if not both:
         _enqueue(dev, _lib.lsgd_quantise_rows, dt, G, M, N, X.data_ptr(), ldx, sX, q.data_ptr(),
@@ -985,7 +985,7 @@ def layer_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None,
             out_dtype = X.dtype
         elif out_dtype not in _FLOATS:
             raise ValueError("out_dtype must be float32 or bfloat16")
-        out = torch.empty((G, M, N), dtype=out_dtype, device=dev)
+        out = X.new_empty((G, M, N), dtype=out_dtype)
         ldy, sY = N, M * N
     else:
         ldy, sY = _matrices("out", out, _FLOATS)
@@ -995,8 +995,7 @@ def layer_norm(X: torch.Tensor, weight: Optional[torch.Tensor] = None,
     if out.device != dev or (weight is not None and weight.device != dev) or (
             bias is not None and bias.device != dev):
         raise ValueError("all tensors must be on one device")
-    stats = torch.empty((2, G, M), dtype=torch.float32, device=dev)
-    mean, rstd = stats[0], stats[1]
+    mean, rstd = X.new_empty((2, G, M), dtype=torch.float32).unbind(0)
     _enqueue(dev, _lib.lsgd_layer_norm, BF16 if X.dtype == torch.bfloat16 else FP32,
              BF16 if out.dtype == torch.bfloat16 else FP32, G, M, N, X.data_ptr(), ldx, sX,
              None if weight is None else weight.data_ptr(), sw,
@@ -1035,10 +1034,9 @@ def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
     sw = 0 if weight is None else _vectors("weight", weight, G, N)
     if not parameters and (dweight is not None or dbias is not None):
         raise ValueError("dweight and dbias are not computed without parameters")
-    read = (dY, X, mean, rstd, weight)
     given = []
     if out is None:
-        out = torch.empty((G, M, N), dtype=X.dtype, device=dev)
+        out = X.new_empty((G, M, N))
         ldd, sD = N, M * N
     else:
         ldd, sD = _matrices("out", out, (X.dtype,))
@@ -1047,19 +1045,22 @@ def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
         given.append(out)
     sdw = sdb = N
     if parameters:
-        if dweight is None:
-            dweight = torch.empty((G, N), dtype=torch.float32, device=dev)
-        else:
+        if dweight is not None:
             sdw = _vectors("dweight", dweight, G, N)
             given.append(dweight)
-        if dbias is None:
-            dbias = torch.empty((G, N), dtype=torch.float32, device=dev)
-        else:
+        if dbias is not None:
             sdb = _vectors("dbias", dbias, G, N)
             given.append(dbias)
+        if dweight is None and dbias is None:
+            dweight, dbias = X.new_empty((2, G, N), dtype=torch.float32).unbind(0)
+        elif dweight is None:
+            dweight = X.new_empty((G, N), dtype=torch.float32)
+        elif dbias is None:
+            dbias = X.new_empty((G, N), dtype=torch.float32)
     for i, t in enumerate(given):
-        _not_over(t, "results must not overlap each other or what is read", *read, *given[:i])
-    for t in (dY, mean, rstd, weight, out, dweight, dbias):
+        _not_over(t, "results must not overlap each other or what is read", dY, X, mean, rstd, weight,
+                  *given[:i])
+    for t in (dY, mean, rstd, weight, *given):
         if t is not None and t.device != dev:
             raise ValueError("all tensors must be on one device")
     nb = _norm_workspace(G, M, N) if parameters else 0
