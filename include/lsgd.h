@@ -597,8 +597,8 @@ lsgd_status lsgd_orthogonal_update(int32_t gemm_dtype, int32_t G, int32_t M,
  * each column of X: d_Qt [G][N][up(M, 128)] with d_St [G][N]. All padding is written.
  * G <= 65535, M, N <= 2^30, d_Q and d_Qt 16-byte aligned, the rest aligned to its
  * elements, else LSGD_E_INVALID. With the transposes: a workspace of
- * lsgd_quantise_rows_workspace_bytes, 4-byte aligned (LSGD_E_WORKSPACE if smaller),
- * one call's at a time; without them NULL is allowed. What is written must not overlap
+ * lsgd_quantise_rows_workspace_bytes, 4-byte aligned (LSGD_E_WORKSPACE if smaller; 0 for
+ * small matrices), one call's at a time; without them, or for 0, NULL is allowed. What is written must not overlap
  * X, the workspace or another result.
  */
 lsgd_status lsgd_quantise_rows_workspace_bytes(int32_t G, int32_t M, int32_t N,
@@ -702,13 +702,17 @@ typedef struct lsgd_tensor {
  * fp64, rounded once; the others' stay as they are, as do those of a replica whose norm is not finite.
  * d_norm holds the norms before clipping. K <= 65535, count <= LSGD_MAX_TENSORS, M and N at
  * least 1, M N, M ld, s <= 2^44, else LSGD_E_INVALID. Clipped tensors' replicas must not overlap
- * (s >= (M - 1) ld + N, or rows of all K side by side), nor two tensors, nor d_norm. Workspace of
+ * (s >= (M - 1) ld + N, or rows of all K side by side), nor two tensors (lsgd_tensors_apart says
+ * whether they do, or where that would take over 2^24 runs of values, may), else LSGD_E_INVALID;
+ * nor d_norm or the workspace a tensor. Workspace of
  * lsgd_gradient_norm_workspace_bytes, 8-byte aligned (LSGD_E_WORKSPACE if smaller; 0 for few
  * values; then NULL is allowed), one call's at a time.
  */
 lsgd_status lsgd_gradient_norm_workspace_bytes(int32_t K, int32_t count,
                                                const lsgd_tensor* h_tensors,
                                                size_t* bytes);
+lsgd_status lsgd_tensors_apart(int32_t K, int32_t count,
+                               const lsgd_tensor* h_tensors, int32_t* apart);
 lsgd_status lsgd_gradient_norm(int32_t K, int32_t count,
                                const lsgd_tensor* h_tensors, float* d_norm,
                                void* d_ws, size_t ws_bytes, void* stream);

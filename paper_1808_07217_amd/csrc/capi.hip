@@ -397,12 +397,57 @@ bool clip_tensors(int32_t K, int32_t count, const lsgd_tensor* h, bool written,
   return true;
 }
 
+// Whether no two of the tensors share a byte (each one's own replicas being apart); false
+// too where telling would take more than kMostRuns runs of bytes.
+bool tensors_apart(int32_t K, const std::vector<lsgd::ClipTensor>& t) {
+  constexpr int64_t kMostRuns = 1 << 24;
+  struct Run {
+    uint64_t first, end;  // of a replica
+    uint64_t step;        // to the next one's
+  };
+  std::vector<Run> runs;
+  runs.reserve(t.size());
+  for (const auto& x : t) {
+    const uint64_t p = (uint64_t)(uintptr_t)x.p, e = x.bf16 ? 2 : 4;
+    runs.push_back({p, p + ((x.M - 1) * x.ld + x.N) * e, K > 1 ? x.s * e : 0});
+  }
+  std::sort(runs.begin(), runs.end(), [](const Run& a, const Run& b) { return a.first < b.first; });
+  // tensors one after the other, or so in each replica's row of one length
+  bool one = true, flat = true;
+  for (size_t i = 1; i < runs.size(); ++i) {
+    const Run &a = runs[i - 1], &b = runs[i];
+    one = one && a.end + (K - 1) * a.step <= b.first;
+    flat = flat && a.end <= b.first && a.step == b.step;
+  }
+  if (one || (flat && runs.back().end - runs[0].first <= runs[0].step)) return true;
+  // else run by run
+  int64_t total = 0;
+  for (const auto& x : t) {
+    total += (x.ld == x.N ? 1 : x.M) * K;
+    if (total > kMostRuns) return false;
+  }
+  runs.clear();
+  for (const auto& x : t) {
+    const uint64_t e = x.bf16 ? 2 : 4, M = x.ld == x.N ? 1 : x.M, N = x.M * x.N / M;
+    for (int32_t k = 0; k < K; ++k)
+      for (uint64_t m = 0; m < M; ++m) {
+        const uint64_t p = (uint64_t)(uintptr_t)x.p + (k * x.s + m * x.ld) * e;
+        runs.push_back({p, p + N * e, 0});
+      }
+  }
+  std::sort(runs.begin(), runs.end(), [](const Run& a, const Run& b) { return a.first < b.first; });
+  for (size_t i = 1; i < runs.size(); ++i)
+    if (runs[i - 1].end > runs[i].first) return false;  // (runs before that one end no later)
+  return true;
+}
+
 lsgd_status clip_call(int32_t K, int32_t count, const lsgd_tensor* h, bool scale, double most,
                       float* d_norm, void* d_ws, size_t ws_bytes, void* stream) {
   if (!d_norm || (uintptr_t)d_norm % 4 || !(most > 0.0) || !std::isfinite(most)) return LSGD_E_INVALID;
   try {
     std::vector<lsgd::ClipTensor> t;
-    if (!clip_tensors(K, count, h, scale, t)) return LSGD_E_INVALID;
+    if (!clip_tensors(K, count, h, scale, t) || (scale && !tensors_apart(K, t)))
+      return LSGD_E_INVALID;
     const size_t need = lsgd::clip_workspace_bytes(K, count, t.data());
     if (need && (!d_ws || (uintptr_t)d_ws % 8)) return LSGD_E_INVALID;
     if (ws_bytes < need) return LSGD_E_WORKSPACE;
@@ -2029,8 +2074,9 @@ lsgd_status lsgd_quantise_rows(int32_t dtype, int32_t G, int32_t M, int32_t N, c
       (uintptr_t)d_S % 4 || (uintptr_t)d_St % 4)
     return LSGD_E_INVALID;
   if (d_Qt) {
-    if (!d_ws || (uintptr_t)d_ws % 4) return LSGD_E_INVALID;
-    if (ws_bytes < lsgd::rows_quantise_workspace_bytes(G, M, N)) return LSGD_E_WORKSPACE;
+    const size_t need = lsgd::rows_quantise_workspace_bytes(G, M, N);
+    if (need && (!d_ws || (uintptr_t)d_ws % 4)) return LSGD_E_INVALID;
+    if (ws_bytes < need) return LSGD_E_WORKSPACE;
   }
   lsgd::RowQuantArgs a{};
   a.G = G;
@@ -2194,6 +2240,19 @@ lsgd_status lsgd_gradient_norm_workspace_bytes(int32_t K, int32_t count,
     std::vector<lsgd::ClipTensor> t;
     if (!clip_tensors(K, count, h_tensors, false, t)) return LSGD_E_INVALID;
     *bytes = lsgd::clip_workspace_bytes(K, count, t.data());
+  } catch (...) {
+    return LSGD_E_INVALID;
+  }
+  return LSGD_OK;
+}
+
+lsgd_status lsgd_tensors_apart(int32_t K, int32_t count, const lsgd_tensor* h_tensors,
+                               int32_t* apart) {
+  if (!apart) return LSGD_E_INVALID;
+  try {
+    std::vector<lsgd::ClipTensor> t;
+    if (!clip_tensors(K, count, h_tensors, true, t)) return LSGD_E_INVALID;
+    *apart = tensors_apart(K, t);
   } catch (...) {
     return LSGD_E_INVALID;
   }

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(B) void k_norm(NormArgs a, int strips, long long to
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int n = (t + i * T) * 8;
-      fetch8<XBF, T == 16>(a.X, g * a.sX + m * a.ldx, n, m < end ? a.N : 0, raw[i]);
+      fetch8<XBF, T == 1>(a.X, g * a.sX + m * a.ldx, n, m < end ? a.N : 0, raw[i]);
     }
   };
   fetch(m0 + slot);
@@ -80,8 +80,8 @@ __global__ __launch_bounds__(B) void k_norm(NormArgs a, int strips, long long to
     const int n = (t + i * T) * 8;
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[i][e] = 1.f, b[i][e] = 0.f;
-    if (a.w) load8<false, T == 16>(a.w, g * a.sw, n, a.N, w[i]);
-    if (a.b) load8<false, T == 16>(a.b, g * a.sb, n, a.N, b[i]);
+    if (a.w) load8<false, T == 1>(a.w, g * a.sw, n, a.N, w[i]);
+    if (a.b) load8<false, T == 1>(a.b, g * a.sb, n, a.N, b[i]);
   }
   for (int r = m0; r < end; r += kRows) {
     const int m = r + slot;
@@ -183,13 +183,14 @@ __device__ __forceinline__ void opaque(Raw8<BF>& v) {
 
 // A strip of rows a workgroup; a thread keeps the sums of its columns over them. A: the
 // arithmetic of a row. Of rows of few columns little is left beside the two directions that are
-// taken out (of two columns eps / variance of e): those in fp64.
-constexpr int kNarrow = 8;
+// taken out (of two columns eps / variance of e): those of up to eight, a thread's each, in fp64.
 template <bool XBF, bool YBF, int T, int V, int B, class A>
 __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total) {
   constexpr int kBlock = B, kRows = kBlock / T, kCols = T * V * 8;
   __shared__ A room[2][kBlock / 64][2];
-  __shared__ float slots[kRows > 1 ? kRows * kCols : 1];
+  // the columns' sums of several rows at work at one time: a wavefront's, or its rows' each
+  constexpr int kSlots = T < 64 ? kBlock / 64 : kRows;
+  __shared__ float slots[kSlots > 1 ? kSlots * kCols : 1];
   const unsigned id = workgroup_id();
   if (id >= total) return;
   const int g = id / a.strips, strip = id - g * a.strips, m0 = strip * a.strip;
@@ -203,8 +204,8 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int n = (t + i * T) * 8, N = m < end ? a.N : 0;
-      fetch8<XBF, T == 16>(a.X, g * a.sX + m * a.ldx, n, N, xn[i]);
-      fetch8<YBF, T == 16>(a.dY, g * a.sg + m * a.ldg, n, N, dn[i]);
+      fetch8<XBF, T == 1>(a.X, g * a.sX + m * a.ldx, n, N, xn[i]);
+      fetch8<YBF, T == 1>(a.dY, g * a.sg + m * a.ldg, n, N, dn[i]);
     }
     mean_next = m < end ? a.mean[(long long)g * a.M + m] : 0.f;
     rstd_next = m < end ? a.rstd[(long long)g * a.M + m] : 0.f;
@@ -216,7 +217,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
     const int n = (t + i * T) * 8;
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[i][e] = 1.f, dw[i][e] = db[i][e] = 0.f;
-    if (a.w) load8<false, T == 16>(a.w, g * a.sw, n, a.N, w[i]);
+    if (a.w) load8<false, T == 1>(a.w, g * a.sw, n, a.N, w[i]);
   }
   int odd = 0;
   for (int r = m0; r < end; r += kRows, odd ^= 1) {
@@ -263,28 +264,31 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
     }
   }
   if (!a.dw) return;
-  // the rows' slots joined in order; one strip is the result itself
+  // joined in order; one strip is the result itself
   float* to_w = a.strips == 1 ? a.dw + g * a.sdw : a.part + (long long)id * 2 * a.N;
   float* to_b = a.strips == 1 ? a.db + g * a.sdb : a.part + ((long long)id * 2 + 1) * a.N;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     float* to = h ? to_b : to_w;
-    if constexpr (kRows == 1) {
+    if constexpr (kSlots == 1) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
         store8<false>(to, 0, (t + i * T) * 8, a.N, h ? db[i] : dw[i]);
     } else {
+      const int mine = T < 64 ? threadIdx.x >> 6 : slot;
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          slots[slot * kCols + (t + i * T) * 8 + e] = h ? db[i][e] : dw[i][e];
+        for (int e = 0; e < 8; ++e) {
+          const float v = strided_sum<(T < 64 ? T : 64)>(h ? db[i][e] : dw[i][e]);
+          if (T >= 64 || (threadIdx.x & 63) < T) slots[mine * kCols + (t + i * T) * 8 + e] = v;
+        }
       __syncthreads();
       for (int n = threadIdx.x; n < a.N; n += kBlock) {
         float sum = slots[n];
 #pragma unroll
-        for (int k = 1; k < kRows; ++k) sum += slots[k * kCols + n];
+        for (int k = 1; k < kSlots; ++k) sum += slots[k * kCols + n];
         to[n] = sum;
       }
     }
@@ -400,6 +404,8 @@ struct Shape {
 };
 template <class F>
 auto with_shape(int N, F f) {
+  if (N <= 8) return f(Shape<1, 1, 256>{});
+  if (N <= 32) return f(Shape<4, 1, 256>{});
   if (N <= 128) return f(Shape<16, 1, 256>{});
   if (N <= 512) return f(Shape<64, 1, 256>{});
   if (N <= 1024) return f(Shape<64, 2, 256>{});
@@ -412,7 +418,8 @@ auto with_shape(int N, F f) {
 // Backward, where sums of the columns stay in registers, and few strips leave few of them to add.
 template <class F>
 auto with_back_shape(int N, F f) {
-  if (N <= kNarrow) return f(Shape<16, 1, 256>{});
+  if (N <= 8) return f(Shape<1, 1, 256>{});
+  if (N <= 32) return f(Shape<4, 1, 1024>{});
   if (N <= 128) return f(Shape<16, 1, 1024>{});
   if (N <= 512) return f(Shape<64, 1, 1024>{});
   if (N <= 1024) return f(Shape<128, 1, 1024>{});
@@ -449,14 +456,14 @@ hipError_t norm(NormArgs a, hipStream_t s) {
 }
 
 // One strip, and no second launch, where each of a workgroup's places for rows gets few.
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 8;
 constexpr long long kBackStrips = 256, kNarrowStrips = 1024;
 int back_strip_rows(int G, int M, int N) {
   return with_back_shape(N, [&](auto z) {
     constexpr int T = decltype(z)::T, B = decltype(z)::B;
     constexpr int each = T == 0 ? 4 : B / (T == 0 ? 1 : T);
     if (M <= kFewRows * each) return (M + each - 1) / each * each;
-    return strip_rows(N <= kNarrow ? kNarrowStrips : kBackStrips, each, G, M);
+    return strip_rows(T == 1 ? kNarrowStrips : kBackStrips, each, G, M);
   });
 }
 
@@ -477,7 +484,7 @@ hipError_t norm_back(NormBackArgs a, void* ws, hipStream_t s) {
       hipLaunchKernelGGL((k_norm_params<XBF, YBF>), grid_of(tiles * strips), dim3(kThreads), 0, s, a,
                          (int)tiles, tiles * strips);
     } else {
-      typedef std::conditional_t<T == 16 && B == 256, double, float> A;
+      typedef std::conditional_t<T == 1, double, float> A;
       hipLaunchKernelGGL((k_norm_back<XBF, YBF, T, V, B, A>), grid_of(strips), dim3(B), 0, s, a,
                          strips);
     }

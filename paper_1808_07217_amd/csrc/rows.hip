@@ -212,8 +212,9 @@ __device__ __forceinline__ int turned(int row, int byte) {
 }
 // A tile of 128 x 128: thread t holds eight rows from 8 (t / 16) and eight columns from
 // 8 (t % 16); the transpose's bytes are turned in LDS, so that each of its rows leaves
-// as a whole line. Thread t < 128 finds the scale of the tile's row t, the others a column's.
-template <bool BF, bool SMALL, bool STREAM>
+// as a whole line. Thread t < 128 finds the scale of the tile's row t, the others a column's,
+// from the strips' maxima; ONE: matrices of a single tile, from its own.
+template <bool BF, bool SMALL, bool STREAM, bool ONE>
 __global__ __launch_bounds__(kThreads) void k_rows_both(RowQuantArgs a, int tm, int tn, int sm,
                                                         int sn, int total) {
   __shared__ __align__(16) uint8_t turn[128 * 128];
@@ -228,31 +229,51 @@ __global__ __launch_bounds__(kThreads) void k_rows_both(RowQuantArgs a, int tm, 
   constexpr int kAhead = 16;
   const bool row = tid < 128;
   const int at = row ? m0 + tid : n0 + tid - 128, each = row ? a.M : a.N, parts = row ? sn : sm;
-  const uint32_t* part = (row ? a.rowmost : a.colmost) + (long long)g * parts * each + at;
-  uint32_t tops[kAhead];
-  auto ahead = [&](int k0) __attribute__((always_inline)) {
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      tops[k] = 0;
-      if (k0 + k < parts && at < each) tops[k] = part[(long long)(k0 + k) * each];
-    }
-  };
-  uint32_t top = 0;
+  uint32_t tops[kAhead], top = 0;
   auto larger = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) top = max(top, tops[k]);
   };
-  ahead(0);
-  for (int k0 = kAhead; k0 < parts; k0 += kAhead) {
-    larger();
-    ahead(k0);
+  if constexpr (!ONE) {
+    const uint32_t* part = (row ? a.rowmost : a.colmost) + (long long)g * parts * each + at;
+    auto ahead = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        tops[k] = 0;
+        if (k0 + k < parts && at < each) tops[k] = part[(long long)(k0 + k) * each];
+      }
+    };
+    ahead(0);
+    for (int k0 = kAhead; k0 < parts; k0 += kAhead) {
+      larger();
+      ahead(k0);
+    }
   }
   Raw8<BF> v[8];
 #pragma unroll
   for (int p = 0; p < 8; ++p)
     fetch8<BF, SMALL>(a.X, g * a.sX + (r0 + p) * a.ldx, n, r0 + p < a.M ? a.N : 0, v[p]);
-  {
+  if constexpr (ONE) {
+    __shared__ uint32_t rows[128], cols[4][128];
+    uint32_t cm[Raw8<BF>::kDwords] = {};
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      const uint32_t m = lanes_max<16>(most8<BF, true>(v[p], cm));
+      if (c == 0) rows[rg * 8 + p] = m;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t m = over_rows(Most8<BF>::bits(cm[BF ? i / 2 : i], i % 2),
+                                   [](uint32_t a, uint32_t b) __attribute__((always_inline)) { return max(a, b); });
+      if ((tid & 63) < 16) cols[tid >> 6][c * 8 + i] = m;
+    }
+    __syncthreads();
+    const int k = tid & 127;
+    top = row ? rows[k] : max(max(cols[0][k], cols[1][k]), max(cols[2][k], cols[3][k]));
+  } else {
     larger();
+  }
+  {
     const float s = scale_of(top);
     scale[tid] = s;
     inverse[tid] = 1.f / s;
@@ -299,12 +320,20 @@ int strip_rows(int G, int M, int N) {
   return (int)rows;
 }
 
+bool one_tile(int M, int N) { return M <= 128 && N <= 128; }
+
 template <bool BF, bool SMALL, bool STREAM>
 hipError_t quantise_both(RowQuantArgs a, void* ws, hipStream_t s) {
   a.strip = strip_rows(a.G, a.M, a.N);
   const long long tm = ((long long)a.M + a.strip - 1) / a.strip;
   const long long tn = (a.N + kMostCols - 1LL) / kMostCols;
   const long long bm = (a.M + 127LL) / 128, bn = (a.N + 127LL) / 128;
+  if (one_tile(a.M, a.N)) {
+    if constexpr (!STREAM)
+      hipLaunchKernelGGL((k_rows_both<BF, SMALL, false, true>), dim3(a.G), dim3(kThreads), 0, s, a, 1,
+                         1, 0, 0, a.G);
+    return hipGetLastError();
+  }
   if (bm * bn > 0x7fffffffLL / a.G) return hipErrorInvalidValue;
   a.rowmost = (uint32_t*)ws;
   a.colmost = a.rowmost + a.G * tn * a.M;
@@ -312,7 +341,7 @@ hipError_t quantise_both(RowQuantArgs a, void* ws, hipStream_t s) {
                      (int)tm, (int)tn, (int)(tm * tn * a.G));
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_rows_both<BF, SMALL, STREAM>), grid_of(bm * bn * a.G), dim3(kThreads), 0, s,
+  hipLaunchKernelGGL((k_rows_both<BF, SMALL, STREAM, false>), grid_of(bm * bn * a.G), dim3(kThreads), 0, s,
                      a, (int)bm, (int)bn, (int)tm, (int)tn, (int)(bm * bn * a.G));
   return hipGetLastError();
 }
@@ -321,7 +350,7 @@ template <bool BF>
 hipError_t quantise(const RowQuantArgs& a, void* ws, hipStream_t s) {
   if (a.Qt) {
     const double bytes = (double)a.M * a.N * a.G * ((BF ? 2 : 4) + 2);
-    if (bytes >= (double)kNtBytesCaller)
+    if (bytes >= (double)kNtBytesCaller && !one_tile(a.M, a.N))
       return a.N < 8 ? quantise_both<BF, true, true>(a, ws, s) : quantise_both<BF, false, true>(a, ws, s);
     return a.N < 8 ? quantise_both<BF, true, false>(a, ws, s) : quantise_both<BF, false, false>(a, ws, s);
   }
@@ -610,6 +639,7 @@ hipError_t gemm_tiles(const RowGemmArgs& a, const RowCut& c, hipStream_t s) {
 }  // namespace
 
 size_t rows_quantise_workspace_bytes(int G, int M, int N) {
+  if (one_tile(M, N)) return 0;
   const size_t strip = strip_rows(G, M, N), tm = ((size_t)M + strip - 1) / strip;
   const size_t tn = ((size_t)N + kMostCols - 1) / kMostCols;
   return ((size_t)G * tn * M + (size_t)G * tm * N) * sizeof(uint32_t);

@@ -9,8 +9,9 @@ from __future__ import annotations
 
 import ctypes
 import functools
-import itertools
 import os
+import struct
+import sys
 from typing import NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
@@ -125,6 +126,7 @@ _SIGS = {
     "lsgd_layer_norm_backward": [_I, _I, _I, _I, _I, _P, _L, _L, _P, _L, _L, _P, _P, _P, _L,
                                  _P, _L, _L, _P, _L, _P, _L, _P, _c.c_size_t, _P],
     "lsgd_gradient_norm_workspace_bytes": [_I, _I, _P, _c.POINTER(_c.c_size_t)],
+    "lsgd_tensors_apart": [_I, _I, _P, _c.POINTER(_c.c_int32)],
     "lsgd_gradient_norm": [_I, _I, _P, _P, _P, _c.c_size_t, _P],
     "lsgd_clip_gradients": [_I, _I, _P, _c.c_double, _P, _P, _c.c_size_t, _P],
 }
@@ -873,12 +875,12 @@ def quantise_rows(X: torch.Tensor, both: bool = False) -> Union[Rows, Tuple[Rows
         _enqueue(dev, _lib.lsgd_quantise_rows, dt, G, M, N, X.data_ptr(), ldx, sX, q.data_ptr(),
                  s.data_ptr(), None, None, None, 0)
         return Rows(q, s, N)
-    qt = torch.empty((G, N, _up(M, 128)), dtype=torch.int8, device=dev)
-    st = torch.empty((G, N), dtype=torch.float32, device=dev)
+    qt = X.new_empty((G, N, _up(M, 128)), dtype=torch.int8)
+    st = X.new_empty((G, N), dtype=torch.float32)
     nb = _rows_workspace(G, M, N)
-    ws = torch.empty(nb, dtype=torch.uint8, device=dev)
+    ws = torch.empty(nb, dtype=torch.uint8, device=dev) if nb else None
     _enqueue(dev, _lib.lsgd_quantise_rows, dt, G, M, N, X.data_ptr(), ldx, sX, q.data_ptr(),
-             s.data_ptr(), qt.data_ptr(), st.data_ptr(), ws.data_ptr(), nb)
+             s.data_ptr(), qt.data_ptr(), st.data_ptr(), ws.data_ptr() if nb else None, nb)
     return Rows(q, s, N), Rows(qt, st, M)
 
 
@@ -1077,80 +1079,55 @@ def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
 _CODE = {torch.float32: FP32, torch.bfloat16: BF16}
 
 
-def _tensor_table(tensors: Sequence[torch.Tensor]):
-    """(replicas, device, [(address, M, N, ld, s, type code), ...]) of tensors [K][...]."""
+@functools.lru_cache(maxsize=1 << 16)
+def _geometry(shape, stride, dtype) -> Tuple[int, bytes]:
+    """Replicas of a tensor [K][...], and all fields of its lsgd_tensor but the address."""
+    code, n = _CODE.get(dtype), len(shape)
+    if code is None or not n:
+        raise ValueError("tensors must be float32 or bfloat16 [K][...]")
+    if n == 3:
+        K, M, N = shape
+        ld, one = (stride[1] if M > 1 else N), (stride[2] if N > 1 else 1)
+    else:
+        K, M, N, one = shape[0], 1, 1, 1  # a replica's values: one run without gaps
+        for d in range(n - 1, 0, -1):
+            if shape[d] != 1 and stride[d] != N:
+                one = 0
+            N *= shape[d]
+        ld = N
+    if not K * M * N:
+        raise ValueError("tensors must not be empty")
+    if one != 1 or ld < N:
+        raise ValueError("a replica's values must be contiguous, or [M][N] of contiguous rows")
+    return K, struct.pack("=5q", M, N, ld, stride[0] if K > 1 else 0, code)
+
+
+def _clip_call(tensors, call, *bound) -> torch.Tensor:
     if isinstance(tensors, torch.Tensor) or not len(tensors):
         raise ValueError("tensors must be a non-empty sequence of tensors")
-    table, K, index = [], 0, tensors[0].get_device()
-    if index < 0:
-        raise ValueError("tensors must be on a CUDA (HIP) device")
+    index, fields, K = tensors[0].get_device(), [], None
     for t in tensors:
-        shape, code = t.shape, _CODE.get(t.dtype)
-        n = len(shape)
-        if code is None or not n:
-            raise ValueError("tensors must be float32 or bfloat16 [K][...]")
-        if t.get_device() != index:
-            raise ValueError("tensors must be on one device")
-        if shape[0] != K:
-            if table or not shape[0]:
-                raise ValueError("tensors must have one number of replicas, at least 1")
-            K = shape[0]
-        stride = t.stride()
-        if n == 3:
-            _, M, N = shape
-            ld, one = (stride[1] if M > 1 else N), (stride[2] if N > 1 else 1)
-        else:
-            M = N = one = 1  # a replica's values: one run without gaps
-            for d in range(n - 1, 0, -1):
-                if shape[d] != 1 and stride[d] != N:
-                    one = 0
-                N *= shape[d]
-            ld = N
-        if not M * N:
-            raise ValueError("tensors must not be empty")
-        if one != 1 or ld < N:
-            raise ValueError("a replica's values must be contiguous, or [M][N] of contiguous rows")
-        table.append((t.data_ptr(), M, N, ld, stride[0] if K > 1 else 0, code))
-    return K, torch.device("cuda", index), table
-
-
-def _runs_apart(K: int, table) -> bool:
-    """Whether no two of the tensors share a byte (each replica's own being apart)."""
-    size = (4, 2)
-    runs = sorted([(p, p + ((M - 1) * ld + N) * size[d], s * size[d]) for p, M, N, ld, s, d in table])
-    one = flat = True
-    first, end, step = runs[0]
-    row = step
-    for p, e, s in runs[1:]:
-        one = one and end + (K - 1) * step <= p   # tensors one after the other
-        flat = flat and end <= p and s == row     # in each replica's row of one length
-        end, step = e, s
-    if one or (flat and end - first <= row):
-        return True
-    starts, ends = [], []
-    for p, M, N, ld, s, d in table:
-        if ld == N:
-            M, N = 1, M * N
-        at = (torch.arange(K) * (s * size[d]))[:, None] + torch.arange(M) * (ld * size[d]) + p
-        starts.append(at.flatten())
-        ends.append(starts[-1] + N * size[d])
-    start, order = torch.cat(starts).sort()
-    end = torch.cat(ends)[order].cummax(0)[0]
-    return bool((start[1:] >= end[:-1]).all())
-
-
-def _clip_call(tensors, written: bool, *bound) -> torch.Tensor:
-    K, dev, table = _tensor_table(tensors)
-    if written and not _runs_apart(K, table):
-        raise ValueError("tensors must not overlap")
-    n = len(table)
-    h = (_L * (6 * n))(*itertools.chain.from_iterable(table))
-    nb = _c.c_size_t()
+        k, geometry = _geometry(t.shape, t.stride(), t.dtype)
+        if t.get_device() != index or index < 0:
+            raise ValueError("tensors must be on one CUDA (HIP) device")
+        if k != K:
+            if K is not None:
+                raise ValueError("tensors must have one number of replicas")
+            K = k
+        fields += (t.data_ptr().to_bytes(8, sys.byteorder), geometry)
+    n, h, nb = len(tensors), b"".join(fields), _c.c_size_t()
     _check(_lib.lsgd_gradient_norm_workspace_bytes(K, n, h, _c.byref(nb)))
-    ws = torch.empty(nb.value, dtype=torch.uint8, device=dev) if nb.value else None
-    norm = torch.empty(K, dtype=torch.float32, device=dev)
-    _enqueue(dev, _lib.lsgd_clip_gradients if written else _lib.lsgd_gradient_norm, K, n, h, *bound,
-             norm.data_ptr(), None if ws is None else ws.data_ptr(), nb.value)
+    t = tensors[0]
+    ws = t.new_empty(nb.value, dtype=torch.uint8) if nb.value else None
+    norm = t.new_empty(K, dtype=torch.float32)
+    try:
+        _enqueue(t.device, call, K, n, h, *bound, norm.data_ptr(),
+                 None if ws is None else ws.data_ptr(), nb.value)
+    except LsgdError:
+        apart = _c.c_int32()
+        if bound and not _lib.lsgd_tensors_apart(K, n, h, _c.byref(apart)) and not apart.value:
+            raise ValueError("tensors must not overlap") from None
+        raise
     return norm
 
 
@@ -1158,7 +1135,7 @@ def gradient_norm(tensors: Sequence[torch.Tensor]) -> torch.Tensor:
     """The norm of each replica's values over all ``tensors`` [K][...] (float32 or bfloat16; a
     replica's values contiguous, or [M][N] of contiguous rows; views into flat rows are
     fine): float32 [K] (lsgd_gradient_norm). One norm over everything: views [1][...]."""
-    return _clip_call(tensors, False)
+    return _clip_call(tensors, _lib.lsgd_gradient_norm)
 
 
 def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float) -> torch.Tensor:
@@ -1166,4 +1143,4 @@ def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float) -> torch.Te
     (finite, > 0), times max_norm / norm; the others, and those of a replica whose norm
     is not finite, stay as they are. Returns the norms before clipping
     (lsgd_clip_gradients). The tensors must not overlap."""
-    return _clip_call(tensors, True, float(max_norm))
+    return _clip_call(tensors, _lib.lsgd_clip_gradients, float(max_norm))

@@ -97,11 +97,12 @@ def test_quantise_rows_refusals():
     assert size(2, 3, 5, None) == 1
     for bad in ((0, 3, 5), (65536, 3, 5), (2, 0, 5), (2, 3, 0), (2, 2**30 + 1, 5), (2, 3, 2**30 + 1)):
         assert size(*bad, ctypes.byref(nb)) == 1, bad
-    assert size(2, 3, 5, ctypes.byref(nb)) == 0 and nb.value > 0
-    ok = [0, 2, 3, 5, f, 5, 15, f, f, f, f, f, nb.value, None]
+    assert size(2, 3, 5, ctypes.byref(nb)) == 0 and nb.value == 0  # (a single tile)
+    assert size(2, 3, 500, ctypes.byref(nb)) == 0 and nb.value > 0
+    ok = [0, 2, 3, 500, f, 500, 1500, f, f, f, f, f, nb.value, None]
     _refuses(lib.lsgd_quantise_rows, ok, (
         dict(_0=2), dict(_0=-1), dict(_1=0), dict(_1=65536), dict(_2=0), dict(_3=0), dict(_4=None),
-        dict(_4=P(4098)), dict(_5=4), dict(_6=-1), dict(_7=None), dict(_7=P(4104)), dict(_8=None),
+        dict(_4=P(4098)), dict(_5=499), dict(_6=-1), dict(_7=None), dict(_7=P(4104)), dict(_8=None),
         dict(_8=P(4098)), dict(_9=None), dict(_9=P(4104)), dict(_10=None), dict(_10=P(4097)),
         dict(_11=None), dict(_11=P(4098)), dict(_2=2**30 + 1), dict(_3=2**30 + 1, _5=2**31),
         # sizes that are allowed, but more rows or tiles than a launch can number
@@ -233,7 +234,7 @@ def test_binding_refuses_host_tensors_and_shapes():
     x, v = torch.zeros(2, 3, 4), torch.zeros(2, 4)
     for call in (lambda: L.quantise_rows(x), lambda: L.layer_norm(x, v, v),
                  lambda: L.layer_norm_backward(x, x, v[:, :3], v[:, :3], v),
-                 lambda: L.gradient_norm([x]), lambda: L.clip_gradients([x], 1.0)):
+                 lambda: L.gradient_norm([x]), lambda: L.clip_gradients([x], 1.0)):  # (host tensors)
         with pytest.raises(ValueError, match="CUDA"):
             call()
     for bad in (x[0], x.half(), x[:, :, :0], x.int()):
@@ -251,10 +252,16 @@ def test_binding_refuses_host_tensors_and_shapes():
                 call(bad)
 
 
-def test_binding_finds_tensors_that_overlap_exactly():
-    """Random lists of views into one buffer against the set of their bytes."""
-    from paper_1808_07217_amd import lsgd as L
-    rng = np.random.default_rng(4)
+def _apart(K, rows):
+    out = ctypes.c_int32(-1)
+    assert _lib().lsgd_tensors_apart(K, len(rows), _table(*rows), ctypes.byref(out)) == 0
+    return bool(out.value)
+
+
+def test_overlapping_tensors_are_found_exactly():
+    """Random lists of views into one buffer against the set of their bytes; those that overlap
+    are refused."""
+    lib, rng, f = _lib(), np.random.default_rng(4), P(1 << 40)
     seen = {False: 0, True: 0}
     for _ in range(3000):
         K, table, used, clash = int(rng.integers(1, 4)), [], set(), False
@@ -271,10 +278,21 @@ def test_binding_finds_tensors_that_overlap_exactly():
             clash |= bool(mine & used)
             used |= mine
             table.append((p, M, N, ld, s, d))
-        assert L._runs_apart(K, table) == (not clash), table
+        assert _apart(K, table) == (not clash), table
+        if clash:
+            assert lib.lsgd_clip_gradients(K, len(table), _table(*table), ctypes.c_double(1.0), f, f,
+                                           1 << 20, None) == 1
         seen[clash] += 1
     assert min(seen.values()) > 300, seen
     # tensors of flat rows side by side, in any order
     row = [(4096, 4, 6, 6, 64, 0), (4096 + 4 * 24, 1, 6, 6, 64, 0), (4096 + 4 * 30, 2, 17, 17, 64, 0)]
-    assert L._runs_apart(5, row) and L._runs_apart(5, row[::-1])
-    assert not L._runs_apart(5, row + [(4096 + 4 * 63, 1, 2, 2, 64, 0)])
+    assert _apart(5, row) and _apart(5, row[::-1])
+    assert not _apart(5, row + [(4096 + 4 * 63, 1, 2, 2, 64, 0)])
+    # two interleaved matrices of too many rows to look at
+    many = [(4096, 1 << 24, 3, 8, 0, 0), (4096 + 12, 1 << 24, 3, 8, 0, 0)]
+    assert not _apart(1, many) and _apart(1, [(p, 1 << 20, *r) for p, _, *r in many])
+    one = ctypes.c_int32()
+    assert lib.lsgd_tensors_apart(5, 3, _table(*row), None) == 1
+    assert lib.lsgd_tensors_apart(0, 3, _table(*row), ctypes.byref(one)) == 1
+    assert lib.lsgd_tensors_apart(5, 3, None, ctypes.byref(one)) == 1
+    assert lib.lsgd_tensors_apart(5, 1, _table((4096, 4, 6, 6, 20, 0)), ctypes.byref(one)) == 1
