@@ -88,12 +88,14 @@ __global__ __launch_bounds__(B) void k_norm(NormArgs a, int strips, long long to
     float x[V][8];
     double s[1] = {0.0};
 #pragma unroll
-    for (int i = 0; i < V; ++i)
+    for (int i = 0; i < V; ++i) {
+      settle8<XBF, T == 1>((t + i * T) * 8, a.N, raw[i]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         x[i][e] = raw[i][e];
         s[0] += x[i][e];
       }
+    }
     if (r + kRows < end) fetch(m + kRows);
     row_sums<T>(s, room[0]);
     Moments mo;
@@ -229,6 +231,8 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
     for (int i = 0; i < V; ++i) {
       xr[i] = xn[i];
       dr[i] = dn[i];
+      settle8<XBF, T == 1>((t + i * T) * 8, a.N, xr[i]);
+      settle8<YBF, T == 1>((t + i * T) * 8, a.N, dr[i]);
     }
     if (kAhead && r + kRows < end) fetch(m + kRows);
 #pragma unroll
@@ -244,7 +248,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
       __builtin_amdgcn_sched_barrier(0);  // (a vector at a time: fewer registers)
     }
     row_sums<T>(s, room[odd]);
-    const A c1 = s[0] / a.N, c2 = s[1] / a.N;
+    const A c1 = s[0] / a.N * rstd, c2 = s[1] / a.N * rstd;
     if (m < end) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -256,7 +260,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const A x = ((A)xr[i][e] - mean) * rstd, dy = (A)dr[i][e] * w[i][e];
-          d[e] = (float)(rstd * (dy - c1 - x * c2));
+          d[e] = (float)(dy * rstd - c1 - x * c2);
         }
         store8<XBF>(a.dX, g * a.sd + m * a.ldd, n, a.N, d);
         __builtin_amdgcn_sched_barrier(0);

@@ -44,9 +44,10 @@ struct Raw8 {
   }
 };
 
-// The columns n .. n + 7 of the row of N values that starts at element `row`; zeros past the
-// last. The vector that the row ends in is the row's last eight, moved: one load whatever N, where
-// a row has eight values (SMALL: it may have fewer).
+// The columns n .. n + 7 of the row of N values that starts at element `row`, zeros past the
+// last: fetch8, and settle8 once they are needed. The vector that the row ends in is the row's last
+// eight, which settle8 moves: one load whatever N, where a row has eight values (SMALL: it may
+// have fewer), and none that waits for another.
 template <bool BF, bool SMALL = false>
 __device__ __forceinline__ void fetch8(const void* X, long long row, int n, int N, Raw8<BF>& v) {
 #pragma unroll
@@ -65,7 +66,7 @@ __device__ __forceinline__ void fetch8(const void* X, long long row, int n, int 
     }
   }
   if (n >= N) return;
-  const int first = min(n, N - 8), k = n - first;
+  const int first = min(n, N - 8);
   if constexpr (BF) {
     const row_u32x4 a = *(const row_u32x4_any*)((const bf16_t*)X + row + first);
 #pragma unroll
@@ -76,16 +77,21 @@ __device__ __forceinline__ void fetch8(const void* X, long long row, int n, int 
 #pragma unroll
     for (int i = 0; i < 8; ++i) v.w[i] = i < 4 ? a[i] : b[i - 4];
   }
-  if (k) {
-    if (k & 4) v.template drop<4>();
-    if (k & 2) v.template drop<2>();
-    if (k & 1) v.template drop<1>();
-  }
+}
+template <bool BF, bool SMALL = false>
+__device__ __forceinline__ void settle8(int n, int N, Raw8<BF>& v) {
+  const int left = N - n;
+  if (left >= 8 || left <= 0 || (SMALL && N < 8)) return;
+  const int k = 8 - left;
+  if (k & 4) v.template drop<4>();
+  if (k & 2) v.template drop<2>();
+  if (k & 1) v.template drop<1>();
 }
 template <bool BF, bool SMALL = false>
 __device__ __forceinline__ void load8(const void* X, long long row, int n, int N, float (&v)[8]) {
   Raw8<BF> r;
   fetch8<BF, SMALL>(X, row, n, N, r);
+  settle8<BF, SMALL>(n, N, r);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = r[i];
 }

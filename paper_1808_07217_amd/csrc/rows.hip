@@ -130,10 +130,14 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_rows(RowQuantAr
 #pragma unroll
     for (int i = 0; i < V; ++i) fetch8<BF, kSmall>(a.X, x, (t + i * T) * 8, in ? a.N : 0, v[i]);
 #pragma unroll
-    for (int i = 0; i < V; ++i) top = max(top, most8<BF, false>(v[i], none));
+    for (int i = 0; i < V; ++i) {
+      settle8<BF, kSmall>((t + i * T) * 8, a.N, v[i]);
+      top = max(top, most8<BF, false>(v[i], none));
+    }
   } else {
     for (int k = t; k < vecs; k += T) {
       fetch8<BF>(a.X, x, k * 8, a.N, v[0]);
+      settle8<BF>(k * 8, a.N, v[0]);
       top = max(top, most8<BF, false>(v[0], none));
     }
   }
@@ -155,53 +159,65 @@ __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_rows(RowQuantAr
   } else {
     for (int k = t; k < vecs; k += T) {
       fetch8<BF>(a.X, x, k * 8, a.N, v[0]);
+      settle8<BF>(k * 8, a.N, v[0]);
       q[k] = pack8<BF>(v[0], s, r);
     }
   }
   if (t == 0) a.S[row] = s;
 }
 
-// Both ways, in two launches: the largest magnitudes of strips of rows by 512 columns, and from
-// those and a second read of X the scales and the integers of 128 x 128 tiles, from the last
-// tile to the first: what the first launch read last is in the last-level cache still.
-constexpr int kMostThreads = 1024, kMostWaves = kMostThreads / 64, kMostCols = 512;
-constexpr int kMostRows = 8;  // of a wavefront in flight
+// Both ways, in two launches: the largest magnitudes of strips of rows by 512 columns (of up to 128
+// columns: by all of them), and from those and a second read of X the scales and the integers of 128 x
+// 128 tiles, from the last tile to the first: what the first launch read last is in the last-level
+// cache still.
+constexpr int kMostThreads = 1024, kMostWaves = kMostThreads / 64;
+constexpr int kMostRows = 8;  // of a lane in flight
+constexpr int most_lanes(int N) { return N <= 128 ? 16 : 64; }  // a row
 
-// Wavefront w of a strip takes its rows w, w + 16, ..., a lane eight columns.
-template <bool BF, bool SMALL>
+// L lanes a row, each eight columns; a wavefront's rows lie side by side, the wavefronts' after each
+// other.
+template <bool BF, bool SMALL, int L>
 __global__ __launch_bounds__(kMostThreads) void k_rows_most(RowQuantArgs a, int tm, int tn,
                                                             int total) {
-  typedef Most8<BF> L;
-  __shared__ uint32_t most[kMostWaves][kMostCols];
+  typedef Most8<BF> Most;
+  constexpr int kCols = 8 * L, kEach = 64 / L;  // rows of a wavefront at one time
+  __shared__ uint32_t most[kMostWaves][kCols];
   const unsigned id = workgroup_id();
   if (id >= (unsigned)total) return;
   const int g = id / (tm * tn), mt = id % (tm * tn) / tn, nt = id % tn;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n = nt * kMostCols + lane * 8, m0 = mt * a.strip, end = min(a.M, m0 + a.strip);
+  const int lane = threadIdx.x % L, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = nt * kCols + lane * 8, m0 = mt * a.strip, end = min(a.M, m0 + a.strip);
   uint32_t cm[Raw8<BF>::kDwords] = {};
-  for (int m = m0 + wave; m < end; m += kMostWaves * kMostRows) {
+  for (int r = m0 + wave * kEach; r < end; r += kMostWaves * kEach * kMostRows) {
+    const int m = L == 64 ? r : r + (threadIdx.x & 63) / L;
     Raw8<BF> v[kMostRows];
 #pragma unroll
     for (int k = 0; k < kMostRows; ++k) {
-      const int mk = m + k * kMostWaves;
+      const int mk = m + k * kMostWaves * kEach;
       fetch8<BF, SMALL>(a.X, g * a.sX + mk * a.ldx, n, mk < end ? a.N : 0, v[k]);
     }
 #pragma unroll
     for (int k = 0; k < kMostRows; ++k) {
-      const int mk = m + k * kMostWaves;
-      const uint32_t rm = lanes_max<64>(most8<BF, true>(v[k], cm));
+      const int mk = m + k * kMostWaves * kEach;
+      settle8<BF, SMALL>(n, a.N, v[k]);
+      const uint32_t rm = lanes_max<L>(most8<BF, true>(v[k], cm));
       if (lane == 0 && mk < end) a.rowmost[((long long)g * tn + nt) * a.M + mk] = rm;
     }
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) most[wave][lane * 8 + i] = L::bits(cm[BF ? i / 2 : i], i % 2);
+  for (int i = 0; i < 8; ++i) {
+    uint32_t c = Most::bits(cm[BF ? i / 2 : i], i % 2);
+    if constexpr (L == 16)
+      c = over_rows(c, [](uint32_t a, uint32_t b) __attribute__((always_inline)) { return max(a, b); });
+    if ((threadIdx.x & 63) < L) most[wave][lane * 8 + i] = c;
+  }
   __syncthreads();
   const int c = threadIdx.x;
-  if (c < kMostCols && nt * kMostCols + c < a.N) {
+  if (c < kCols && nt * kCols + c < a.N) {
     uint32_t top = 0;
 #pragma unroll
     for (int w = 0; w < kMostWaves; ++w) top = max(top, most[w][c]);
-    a.colmost[((long long)g * tm + mt) * a.N + nt * kMostCols + c] = top;
+    a.colmost[((long long)g * tm + mt) * a.N + nt * kCols + c] = top;
   }
 }
 
@@ -253,6 +269,8 @@ __global__ __launch_bounds__(kThreads) void k_rows_both(RowQuantArgs a, int tm, 
 #pragma unroll
   for (int p = 0; p < 8; ++p)
     fetch8<BF, SMALL>(a.X, g * a.sX + (r0 + p) * a.ldx, n, r0 + p < a.M ? a.N : 0, v[p]);
+#pragma unroll
+  for (int p = 0; p < 8; ++p) settle8<BF, SMALL>(n, a.N, v[p]);
   if constexpr (ONE) {
     __shared__ uint32_t rows[128], cols[4][128];
     uint32_t cm[Raw8<BF>::kDwords] = {};
@@ -313,10 +331,10 @@ __global__ __launch_bounds__(kThreads) void k_rows_both(RowQuantArgs a, int tm, 
 // maxima to read again, and a workgroup a compute unit is enough where all start at once.
 // (16384 x 8192 in bf16, in 256, 512, 1024 strips: both launches 139, 163, 203 us.)
 int strip_rows(int G, int M, int N) {
-  constexpr int kSet = kMostWaves * kMostRows;
-  const long long across = ((long long)N + kMostCols - 1) / kMostCols * G;
+  const int L = most_lanes(N), set = kMostWaves * kMostRows * (64 / L);
+  const long long across = ((long long)N + 8 * L - 1) / (8 * L) * G;
   const long long strips = (across <= 64 ? 256 + across - 1 : 1024 + across - 1) / across;
-  const long long rows = ((M + strips - 1) / strips + kSet - 1) / kSet * kSet;
+  const long long rows = ((M + strips - 1) / strips + set - 1) / set * set;
   return (int)rows;
 }
 
@@ -326,7 +344,8 @@ template <bool BF, bool SMALL, bool STREAM>
 hipError_t quantise_both(RowQuantArgs a, void* ws, hipStream_t s) {
   a.strip = strip_rows(a.G, a.M, a.N);
   const long long tm = ((long long)a.M + a.strip - 1) / a.strip;
-  const long long tn = (a.N + kMostCols - 1LL) / kMostCols;
+  const int L = most_lanes(a.N);
+  const long long tn = (a.N + 8LL * L - 1) / (8 * L);
   const long long bm = (a.M + 127LL) / 128, bn = (a.N + 127LL) / 128;
   if (one_tile(a.M, a.N)) {
     if constexpr (!STREAM)
@@ -337,8 +356,13 @@ hipError_t quantise_both(RowQuantArgs a, void* ws, hipStream_t s) {
   if (bm * bn > 0x7fffffffLL / a.G) return hipErrorInvalidValue;
   a.rowmost = (uint32_t*)ws;
   a.colmost = a.rowmost + a.G * tn * a.M;
-  hipLaunchKernelGGL((k_rows_most<BF, SMALL>), grid_of(tm * tn * a.G), dim3(kMostThreads), 0, s, a,
-                     (int)tm, (int)tn, (int)(tm * tn * a.G));
+  if (L == 16) {
+    hipLaunchKernelGGL((k_rows_most<BF, SMALL, 16>), grid_of(tm * tn * a.G), dim3(kMostThreads), 0, s,
+                       a, (int)tm, (int)tn, (int)(tm * tn * a.G));
+  } else if constexpr (!SMALL) {
+    hipLaunchKernelGGL((k_rows_most<BF, false, 64>), grid_of(tm * tn * a.G), dim3(kMostThreads), 0, s,
+                       a, (int)tm, (int)tn, (int)(tm * tn * a.G));
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((k_rows_both<BF, SMALL, STREAM, false>), grid_of(bm * bn * a.G), dim3(kThreads), 0, s,
@@ -641,7 +665,7 @@ hipError_t gemm_tiles(const RowGemmArgs& a, const RowCut& c, hipStream_t s) {
 size_t rows_quantise_workspace_bytes(int G, int M, int N) {
   if (one_tile(M, N)) return 0;
   const size_t strip = strip_rows(G, M, N), tm = ((size_t)M + strip - 1) / strip;
-  const size_t tn = ((size_t)N + kMostCols - 1) / kMostCols;
+  const size_t L = most_lanes(N), tn = (N + 8 * L - 1) / (8 * L);
   return ((size_t)G * tn * M + (size_t)G * tm * N) * sizeof(uint32_t);
 }
 
