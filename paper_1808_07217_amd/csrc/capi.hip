@@ -2096,14 +2096,14 @@ lsgd_status lsgd_quantise_rows(int32_t dtype, int32_t G, int32_t M, int32_t N, c
 lsgd_status lsgd_grouped_gemm_rows_workspace_bytes(int32_t out_dtype, int32_t G, int32_t M,
                                                    int32_t N, int32_t Kd, size_t* bytes) {
   if (!float_type(out_dtype) || !bytes || !block_sizes(G, M, N, Kd)) return LSGD_E_INVALID;
-  *bytes = lsgd::gemm_rows_workspace_bytes(out_dtype == LSGD_BF16, G, M, N, Kd);
+  *bytes = lsgd::gemm_rows_workspace_bytes(G, M, N, Kd);
   return LSGD_OK;
 }
 
 lsgd_status lsgd_grouped_gemm_rows_cut(int32_t out_dtype, int32_t G, int32_t M, int32_t N,
                                        int32_t Kd, int32_t cut[3]) {
   if (!float_type(out_dtype) || !cut || !block_sizes(G, M, N, Kd)) return LSGD_E_INVALID;
-  lsgd::gemm_rows_cut(out_dtype == LSGD_BF16, G, M, N, Kd, cut);
+  lsgd::gemm_rows_cut(G, M, N, Kd, cut);
   return LSGD_OK;
 }
 
@@ -2120,7 +2120,7 @@ lsgd_status lsgd_grouped_gemm_rows(int32_t out_dtype, int32_t G, int32_t M, int3
       (uintptr_t)d_B % 16 || (uintptr_t)d_SA % 4 || (uintptr_t)d_SB % 4 ||
       !read_vectors(d_bias, sbias))
     return LSGD_E_INVALID;
-  const size_t need = lsgd::gemm_rows_workspace_bytes(out_dtype == LSGD_BF16, G, M, N, Kd);
+  const size_t need = lsgd::gemm_rows_workspace_bytes(G, M, N, Kd);
   if (need && (!d_ws || (uintptr_t)d_ws % 16)) return LSGD_E_INVALID;
   if (ws_bytes < need) return LSGD_E_WORKSPACE;
   lsgd::RowGemmArgs a{};

@@ -199,8 +199,8 @@ struct RowGemmArgs {
   // set by launch_gemm_rows: ranges of `chunk` steps of 128
   int splits, chunk;
 };
-size_t gemm_rows_workspace_bytes(int bf16, int G, int M, int N, int Kd);
-void gemm_rows_cut(int bf16, int G, int M, int N, int Kd, int cut[3]);  // tile, stages, ranges
+size_t gemm_rows_workspace_bytes(int G, int M, int N, int Kd);
+void gemm_rows_cut(int G, int M, int N, int Kd, int cut[3]);  // tile, stages, ranges
 hipError_t launch_gemm_rows(RowGemmArgs a, hipStream_t s);
 
 // ---------------------------------------------------------------- layer norm

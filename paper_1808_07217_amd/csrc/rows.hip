@@ -601,34 +601,50 @@ long long tiles_of(int G, int M, int N, long long b) {
   return (N + b - 1) / b * ((M + b - 1) / b) * G;
 }
 
-// Ranges of the inner dimension: as many as leave the least estimated time where 64 x 64
-// tiles leave compute units idle (see blocks.hip's), and as many as its length needs.
+// The tile, its stages, and the ranges of the inner dimension, by estimated time in us: a workgroup
+// alone on its unit takes 0.18 a step, all of them together cannot beat 5 TB/s, and a
+// second launch joins the ranges' sums (4, and their bytes); 64 x 64 tiles are split where they leave
+// units idle. Whole products by the rounds of the 256 compute units and a tile's relative time, from
+// (us, to bf16, tiles of 64, 128 with four stages and with two, 256) 4096^3 99 / 80 / 68 / 58,
+// 2048 x 2048 x 8192 50 / 36 / 48 / 82, 8192 x 1024 x 1024 23 / 18 / 16 / 22, 16 x 128 x 512 x 512
+// 10.8 / 11.0 / 10.8 / 14.1. Where the inner dimension is so long that 64 x 64 tiles, two a unit, take
+// 0.45 a step, tiles of 128 in ranges, which take 0.7, can be faster: 1024 x 1024 x 65536 141 -> 93.
 struct RowCut {
   int tile, stages, splits, chunk;
 };
-RowCut row_cut(bool bf16, int G, int M, int N, int Kd) {
+RowCut row_cut(int G, int M, int N, int Kd) {
   const int nb = (Kd + 127) / 128;
   RowCut c{0, 0, 1, nb};
-  const long long tiles = tiles_of(G, M, N, 64);
+  const long long tiles = tiles_of(G, M, N, 64), large = tiles_of(G, M, N, 128);
   const double bytes = (double)G * ((double)M + N) * nb * 128 / 5e6;
   const double sums = 2.0 * G * M * N * sizeof(int) / 4e6;
+  auto joined = [&](int s) { return s > 1 ? 4 + sums * s : 0.0; };
   double least = std::max(0.18 * nb, bytes);
   for (int s = 2; s <= 64 && tiles * s <= 2 * kCus && nb >= 4 * s; s *= 2) {
-    const double t = std::max(0.18 * nb / s, bytes) + 4 + sums * s;
+    const double t = std::max(0.18 * nb / s, bytes) + joined(s);
     if (t < least) {
       c.splits = s;
       least = t;
     }
   }
+  int wide = 0;  // ranges of tiles of 128
+  least = 0.9 * (nb * (tiles * c.splits > kCus ? 0.45 : 0.25) / c.splits + joined(c.splits));
+  for (int s = 2; s <= 64 && large * s <= kCus && nb >= 64 * s && tiles * c.splits <= 2 * kCus; s *= 2) {
+    const double t = 0.7 * nb / s + joined(s);
+    if (t < least) {
+      wide = s;
+      least = t;
+    }
+  }
   const bool few = c.splits > 1;
-  c.splits = std::max(c.splits, (nb + kMostSteps - 1) / kMostSteps);
+  c.splits = std::max(wide ? wide : c.splits, (nb + kMostSteps - 1) / kMostSteps);
   c.chunk = (nb + c.splits - 1) / c.splits;
   c.splits = (nb + c.chunk - 1) / c.chunk;
   const RowCut cuts[4] = {{64, 4}, {128, 4}, {128, 2}, {256, 2}};
   const int per_cu[4] = {2, 1, 2, 1};
   const double each[4] = {1.6, 4.5, 3.8, 12.6};
-  int at = 0;
-  for (int i = 0; i < (few ? 1 : 4); ++i) {
+  int at = wide ? 1 : 0;
+  for (int i = 0; i < (few || wide ? 0 : 4); ++i) {
     const double rounds = std::ceil((double)tiles_of(G, M, N, cuts[i].tile) * c.splits /
                                     (kCus * per_cu[i]));
     const double t = rounds * per_cu[i] * each[i];
@@ -673,20 +689,20 @@ hipError_t launch_quantise_rows(int bf16, const RowQuantArgs& a, void* ws, hipSt
   return bf16 ? quantise<true>(a, ws, s) : quantise<false>(a, ws, s);
 }
 
-size_t gemm_rows_workspace_bytes(int bf16, int G, int M, int N, int Kd) {
-  const RowCut c = row_cut(bf16, G, M, N, Kd);
+size_t gemm_rows_workspace_bytes(int G, int M, int N, int Kd) {
+  const RowCut c = row_cut(G, M, N, Kd);
   return c.splits == 1 ? 0 : (size_t)c.splits * G * M * N * sizeof(int);
 }
 
-void gemm_rows_cut(int bf16, int G, int M, int N, int Kd, int cut[3]) {
-  const RowCut c = row_cut(bf16, G, M, N, Kd);
+void gemm_rows_cut(int G, int M, int N, int Kd, int cut[3]) {
+  const RowCut c = row_cut(G, M, N, Kd);
   cut[0] = c.tile;
   cut[1] = c.stages;
   cut[2] = c.splits;
 }
 
 hipError_t launch_gemm_rows(RowGemmArgs a, hipStream_t s) {
-  const RowCut c = row_cut(a.out_bf16, a.G, a.M, a.N, a.Kd);
+  const RowCut c = row_cut(a.G, a.M, a.N, a.Kd);
   a.splits = c.splits;
   a.chunk = c.chunk;
   if (a.splits == 1)

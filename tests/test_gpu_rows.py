@@ -246,15 +246,19 @@ def test_product_cuts(shape, out):
         assert bool((room == 7.0).all())
 
 
-@pytest.mark.parametrize("M,N,K", [(1300, 1250, 131200), (2500, 4200, 131200)])
+# (M, N, K): the cut: past 32-bit sums in each tile of 128 and 256, and a long one in ranges
+RANGES = {(1300, 1250, 131200): (128, 4, 2), (2500, 4200, 131200): (128, 2, 2),
+          (4000, 4090, 131200): (256, 2, 2), (1024, 1000, 65536): (128, 4, 4)}
+
+
+@pytest.mark.parametrize("M,N,K", RANGES)
 def test_large_products_in_ranges(M, N, K):
-    """An inner dimension past 32-bit sums in tiles of 128 and 256: sums by way of the workspace,
-    checked at some rows and columns."""
+    """Sums by way of the workspace, checked at some rows and columns."""
     L = _lsgd()
     print(f"rows product ranges {M} {N} {K}", flush=True)
     cut = (ctypes.c_int32 * 3)()
     assert L._lib.lsgd_grouped_gemm_rows_cut(0, 1, M, N, K, cut) == 0
-    assert cut[2] > 1 and cut[0] > 64
+    assert tuple(cut) == RANGES[M, N, K]
     gen = torch.Generator(device=device()).manual_seed(M)
     a = L.quantise_rows(torch.randn(1, M, K, generator=gen, device=device(), dtype=torch.bfloat16))
     b = L.quantise_rows(torch.randn(1, N, K, generator=gen, device=device(), dtype=torch.bfloat16))
