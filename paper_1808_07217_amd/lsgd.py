@@ -1105,17 +1105,14 @@ def _geometry(shape, stride, dtype) -> Tuple[int, bytes]:
 def _clip_call(tensors, call, *bound) -> torch.Tensor:
     if isinstance(tensors, torch.Tensor) or not len(tensors):
         raise ValueError("tensors must be a non-empty sequence of tensors")
-    index, fields, K = tensors[0].get_device(), [], None
-    for t in tensors:
-        k, geometry = _geometry(t.shape, t.stride(), t.dtype)
-        if t.get_device() != index or index < 0:
-            raise ValueError("tensors must be on one CUDA (HIP) device")
-        if k != K:
-            if K is not None:
-                raise ValueError("tensors must have one number of replicas")
-            K = k
-        fields += (t.data_ptr().to_bytes(8, sys.byteorder), geometry)
-    n, h, nb = len(tensors), b"".join(fields), _c.c_size_t()
+    fields = [_geometry(t.shape, t.stride(), t.dtype) for t in tensors]
+    K, devices = fields[0][0], {t.get_device() for t in tensors}
+    if len(devices) > 1 or -1 in devices:
+        raise ValueError("tensors must be on one CUDA (HIP) device")
+    if any([f[0] != K for f in fields]):
+        raise ValueError("tensors must have one number of replicas")
+    h = b"".join([t.data_ptr().to_bytes(8, sys.byteorder) + f[1] for t, f in zip(tensors, fields)])
+    n, nb = len(tensors), _c.c_size_t()
     _check(_lib.lsgd_gradient_norm_workspace_bytes(K, n, h, _c.byref(nb)))
     t = tensors[0]
     ws = t.new_empty(nb.value, dtype=torch.uint8) if nb.value else None
