@@ -386,6 +386,8 @@ bool clip_tensors(int32_t K, int32_t count, const lsgd_tensor* h, bool written,
     const lsgd_tensor& t = h[i];
     if (!float_type(t.dtype) || t.reserved || !t.d_data || (uintptr_t)t.d_data % float_size(t.dtype))
       return false;
+    // (a row of a pitch is taken by 32-bit column numbers)
+    if (t.M > 1 && t.ld != t.N && t.N > kMaxBlockRows) return false;
     if (t.M < 1 || t.N < 1 || t.M > kMost / t.N || t.ld < t.N || t.ld > kMost / t.M || t.s < 0 || t.s > kMost)
       return false;
     // replicas that do not overlap, one after the other or side by side in rows

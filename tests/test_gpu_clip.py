@@ -140,6 +140,21 @@ def test_flat_rows_and_views():
             assert torch.equal(t, c)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("N", [1, 3, 8, 37, 1001])
+def test_rows_with_a_pitch_over_many_chunks(N, dtype):
+    """Rows shorter and longer than a vector, whose chunks end inside a row: every value once, and
+    nothing between the rows."""
+    print(f"clip pitch {N} {dtype}", flush=True)
+    rng = np.random.default_rng(N)
+    room = to_dev(rng.standard_normal((2, 60000 // N + 7, N + 5)).astype(np.float32)).to(dtype)
+    t, kept = room[:, 3:, 2:N + 2], room.clone()
+    _check([t], 10.0)
+    t.zero_()
+    kept[:, 3:, 2:N + 2].zero_()
+    assert torch.equal(room, kept)
+
+
 def test_norms_of_shared_and_repeated_tensors():
     """The norm reads: replicas of one matrix (expand), a tensor twice."""
     L = _lsgd()

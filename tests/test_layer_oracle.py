@@ -205,10 +205,12 @@ def test_clip_refusals():
         assert size(*bad, ctypes.byref(nb)) == 1, bad
         assert norm(*bad, f, f, 1 << 20, None) == 1, bad
         assert clip(*bad, d(1.0), f, f, 1 << 20, None) == 1, bad
+    # (the last: a column past 32-bit numbers, in rows of a pitch)
     for k, v in ((0, 0), (0, 8194), (1, 0), (1, 2**44), (2, 0), (2, -5), (3, 4), (3, 2**50), (4, -1),
-                 (4, 2**50), (5, 2), (5, 1 << 32)):
+                 (4, 2**50), (5, 2), (5, 1 << 32), ((2, 2**30 + 1), (3, 2**30 + 2))):
         row = list(good)
-        row[k] = v
+        for k, v in ((k, v),) if isinstance(k, int) else (k, v):
+            row[k] = v
         for t in (_table(row), _table(good, row)):
             n = len(t) // 6
             assert size(2, n, t, ctypes.byref(nb)) == 1, (k, v)
