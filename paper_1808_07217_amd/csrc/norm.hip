@@ -285,10 +285,10 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
         }
       __syncthreads();
       for (int n = threadIdx.x; n < a.N; n += kBlock) {
-        float sum = slots[n];
+        double sum = slots[n];
 #pragma unroll
         for (int k = 1; k < kSlots; ++k) sum += slots[k * kCols + n];
-        to[n] = sum;
+        to[n] = (float)sum;
       }
     }
   }
