@@ -247,7 +247,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
       }
     }
     row_sums<T>(s, room[odd]);
-    const A c1 = s[0] / a.N * rstd, c2 = s[1] / a.N * rstd;
+    const A c1 = s[0] / a.N, c2 = s[1] / a.N;
     if (m < end) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const A x = ((A)xr[i][e] - mean) * rstd, dy = (A)dr[i][e] * w[i][e];
-          d[e] = (float)(dy * rstd - c1 - x * c2);
+          d[e] = (float)(rstd * (dy - c1 - x * c2));  // (zero where dy is c1: of one column)
         }
         store8<XBF>(a.dX, g * a.sd + m * a.ldd, n, a.N, d);
       }

@@ -145,6 +145,24 @@ def test_rows_far_from_zero_and_large_ones():
         assert torch.equal(got[0][0, 4:], b.expand(2, N))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_one_column_and_equal_gradients(dtype):
+    """A row of one value, and rows whose dy w is one number throughout (a power of two, whose sums
+    are exact): no gradient at all, not even a rounding of one."""
+    L = _lsgd()
+    print(f"layer norm one column {dtype}", flush=True)
+    dt = _dt(dtype)
+    X, dY, w, _ = _inputs((3, 200, 1), dt, dt)
+    y, mean, rstd = L.layer_norm(X, w)
+    dx, dw, db = L.layer_norm_backward(dY, X, mean, rstd, w)
+    assert not dx.any() and not dw.any() and not y.any()
+    for N in (4, 32, 64, 1024, 8192):
+        X = to_dev(np.tile([1.5, -1.5], (1, 5, N // 2)).astype(np.float32)).to(dt)
+        _, mean, rstd = L.layer_norm(X)
+        dx, dw, db = L.layer_norm_backward(torch.full_like(X, 0.25), X, mean, rstd)
+        assert not dx.any() and torch.equal(db, torch.full_like(db, 1.25)), N
+
+
 def test_rows_that_are_not_finite():
     """A NaN or an infinity makes its own row NaN and reaches the gradients of its columns;
     other rows keep their bits."""
