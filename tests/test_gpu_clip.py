@@ -55,6 +55,7 @@ LISTS = {
     "mixed": (5, [("b", 33, 7), ("f", 129), ("b", 1), ("f", 3, 5, 2, 11), ("b", 4097), ("f", 1, 1)]),
     "one replica": (1, [("f", 300, 500), ("b", 7, 9)]),
     "many": (3, [("f" if i % 3 else "b", i % 7 + 1, 13 * (i % 5) + 1) for i in range(150)]),
+    "hundreds": (2, [("b" if i % 2 else "f", i % 5 + 1, 40) for i in range(700)]),
     "large": (2, [("f", 2000, 3001), ("b", 1500, 2003), ("f", 5)]),
     "many replicas": (700, [("f", 5, 9), ("b", 31)]),
 }
@@ -220,6 +221,66 @@ def test_past_32_bit_offsets():
     assert t[0, 0, 0] == 1.0 and t[0, -1, -1] == 4.0 and t[0, -1, 2 ** 15 - 1] == 4.0
     assert L.clip_gradients([t], 1.0).item() == np.float32(33.0 ** 0.5)
     assert abs(t[0, -1, -1].item() - 4 / 33.0 ** 0.5) <= 2.0 ** -8
+
+
+def test_steps_on_four_streams_at_once():
+    """Every operator's calls side by side on streams of their own: the bits of one after the other."""
+    L = _lsgd()
+    print("layer steps on streams", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(5)
+    rand = lambda *s: torch.randn(*s, generator=gen, device=device())  # noqa: E731
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    inputs = [(rand(4, 500, 700), rand(4, 700), rand(4, 700, 300)) for _ in streams]
+
+    def step(x, gamma, w):
+        h, mean, rstd = L.layer_norm(x, gamma)
+        (hq, ht), (wq, wt) = L.quantise_rows(h, both=True), L.quantise_rows(w, both=True)
+        y = L.grouped_gemm_rows(hq, wt)
+        dq, dt = L.quantise_rows(y, both=True)
+        dw = L.grouped_gemm_rows(ht, dt)
+        grads = L.layer_norm_backward(L.grouped_gemm_rows(dq, wq), x, mean, rstd, gamma)
+        return (L.clip_gradients([dw, *grads], 1.0), y, dw, *grads)
+
+    want = [step(*i) for i in inputs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = []
+        for s, i in zip(streams, inputs):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got.append(step(*i))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+
+
+def test_the_most_groups():
+    """65535 groups, of one value and of a few."""
+    L = _lsgd()
+    print("most groups", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(6)
+    for M, N in ((1, 1), (2, 9), (1, 200)):
+        X = torch.randn(65535, M, N, generator=gen, device=device())
+        x = X.double()
+        q, t = L.quantise_rows(X, both=True)
+        for r, v in ((q, x), (t, x.transpose(1, 2))):
+            s = r.scale.double()[..., None]
+            assert bool(((r.q[..., :r.n].double() * s - v).abs() <= s * 0.500001).all())
+        C = L.grouped_gemm_rows(q, q)
+        s, v = q.scale.double(), q.q.double()
+        for g in (0, 40000, 65534):
+            want = (v[g] @ v[g].t()) * s[g][:, None] * s[g]
+            assert bool(((C[g].double() - want).abs() <= 3.1 * U32 * want.abs()).all())
+        y, mean, rstd = L.layer_norm(X)
+        some = slice(65500, 65535)
+        want, m, r = O.layer_norm(_np(X[some]), np.ones((35, N)), np.zeros((35, N)), 1e-5)
+        assert np.abs(_np(y[some]) - want).max() <= 16 * U32 * (1 + np.abs(want).max())
+        dx, dw, db = L.layer_norm_backward(X, X, mean, rstd)
+        rx, rw, rb = O.layer_norm_backward(_np(X[some]), _np(X[some]), _np(mean[some]),
+                                           _np(rstd[some]), np.ones((35, N)))
+        size = _np(rstd[some]).max() * np.abs(_np(X[some])).max() * np.abs(want).max()
+        assert np.abs(_np(dx[some]) - rx).max() <= gamma(60) * (1 + size)
+        assert np.all(np.abs(_np(db[some]) - rb) <= gamma(3) * np.abs(_np(X[some])).sum(1))
+        _check([X, y], 0.5)
 
 
 def test_a_layer_s_local_step():

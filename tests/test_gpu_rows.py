@@ -211,6 +211,26 @@ def test_product_of_the_largest_integers(K):
     _check_product(L.grouped_gemm_rows(x, x, out_dtype=torch.bfloat16), x, x)
 
 
+def test_product_of_the_longest_inner_dimension():
+    """2^22 products a sum, in 33 ranges."""
+    L = _lsgd()
+    print("rows product longest", flush=True)
+    K = 2 ** 22
+    gen = torch.Generator(device=device()).manual_seed(3)
+    a, b = (L.Rows(torch.randint(-127, 128, (1, n, K), generator=gen, device=device(),
+                                 dtype=torch.int8), torch.rand(1, n, generator=gen, device=device()), K)
+            for n in (3, 5))
+    C = L.grouped_gemm_rows(a, b)
+    # (exact in float64: below 2^36)
+    exact = (a.q[0].double() @ b.q[0].double().t().contiguous()
+             * a.scale[0].double()[:, None] * b.scale[0].double())
+    assert bool(((C[0].double() - exact).abs() <= 3.1 * U32 * exact.abs()).all())
+    bad = L.Rows(torch.zeros(1, 1, K + 128, dtype=torch.int8, device=device()),
+                 torch.ones(1, 1, device=device()), K + 1)
+    with pytest.raises(L.LsgdError):
+        L.grouped_gemm_rows(bad, bad)
+
+
 # (G, M, N): the cut that a product of theirs takes: the tile's side, and its stages of loads
 CUTS = {(3, 150, 331): (64, 4), (1, 1501, 1487): (128, 4), (1, 2503, 2291): (128, 2),
         (10, 378, 2492): (256, 2)}
