@@ -121,7 +121,7 @@ template <bool BF, int T, int V>
 __global__ __launch_bounds__(T < kThreads ? kThreads : T) void k_rows(RowQuantArgs a,
                                                                       long long rows) {
   constexpr int kBlock = T < kThreads ? kThreads : T, kRows = kBlock / T, kWaves = kBlock / 64;
-  constexpr bool kSmall = T == 16;
+  constexpr bool kSmall = T == 16 && V == 1;
   __shared__ uint32_t most[T > 64 ? kWaves : 1];
   const int t = threadIdx.x % T;
   const long long row = (long long)workgroup_id() * kRows + threadIdx.x / T;
@@ -392,8 +392,10 @@ hipError_t quantise(const RowQuantArgs& a, void* ws, hipStream_t s) {
     hipLaunchKernelGGL(kernel, grid_of(n), dim3(threads), 0, s, a, rows);
     return hipGetLastError();
   };
+  // (us in bf16 by 16 threads a row and by 64: 250000 x 256 34 and 61, 131072 x 512 34 and 40)
   if (a.N <= 128) return launch(k_rows<BF, 16, 1>, 16, 256);
-  if (a.N <= 512) return launch(k_rows<BF, 64, 1>, 4, 256);
+  if (a.N <= 256) return launch(k_rows<BF, 16, 2>, 16, 256);
+  if (a.N <= 512) return launch(k_rows<BF, 16, 4>, 16, 256);
   if (a.N <= 1024) return launch(k_rows<BF, 64, 2>, 4, 256);
   if (a.N <= 2048) return launch(k_rows<BF, 64, 4>, 4, 256);
   if (a.N <= 4096) return launch(k_rows<BF, 256, 2>, 1, 256);
