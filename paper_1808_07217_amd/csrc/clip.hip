@@ -109,10 +109,11 @@ struct Chunk {
       long long m = first / across;
       int j = (int)(first - m * across);
       for (int e = tid * 8; e < values;) {
-        long long row[U];
-        int n[U];
+        constexpr int W = 2;  // (in flight: four take the registers of every fourth workgroup)
+        long long row[W];
+        int n[W];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < W; ++u) {
           row[u] = x + m * t.ld;
           n[u] = e < values ? j * 8 : N;
           fetch8<BF, true>(t.p, row[u], n[u], N, v[u]);
@@ -125,7 +126,7 @@ struct Chunk {
           }
         }
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+        for (int u = 0; u < W; ++u) {
           settle8<BF, true>(n[u], N, v[u]);
           if (n[u] < N) eight<WRITE>(u, row[u], n[u], N, f);
         }
