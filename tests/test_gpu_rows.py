@@ -88,6 +88,64 @@ def test_quantise_extremes():
         assert torch.isnan(got.scale[0, 8:11]).all() and torch.isnan(t.scale).all()
 
 
+@pytest.mark.parametrize("N", [5, 100, 128])
+def test_quantise_specials_in_one_tile(N):
+    """Matrices of a single tile, some of them with zeros, subnormals, the largest value, infinities
+    and NaN; a column's special leaves the other columns as they are."""
+    L = _lsgd()
+    print(f"quantise rows one tile {N}", flush=True)
+    rng = np.random.default_rng(N)
+    X = rng.standard_normal((4, 90, N)).astype(np.float32)
+    X[0, 3], X[0, 4], X[0, 5, N - 1] = 0, 1e-42, np.finfo(np.float32).max
+    X[1, 89, 0], X[1, 7, N - 1] = np.nan, -np.inf
+    X[2] = 0
+    for dt in (torch.float32, torch.bfloat16):
+        Xd = to_dev(X).to(dt)
+        q, t = L.quantise_rows(Xd, both=True)
+        _check_rows(q, _np(Xd))
+        _check_rows(t, _np(Xd).transpose(0, 2, 1))
+
+
+@pytest.mark.parametrize("shape", [(2, 300, 700), (1, 5000, 90), (1, 129, 3)])
+def test_quantise_whatever_the_workspace_holds(shape):
+    """The caller's own workspace of exactly the size asked for: the same bits, nothing behind its end
+    or the results' written."""
+    L = _lsgd()
+    print(f"quantise rows workspace {shape}", flush=True)
+    G, M, N = shape
+    X = to_dev(np.random.default_rng(1).standard_normal(shape).astype(np.float32))
+    q, t = L.quantise_rows(X, both=True)
+    nb = L._rows_workspace(G, M, N)
+    assert nb > 0
+    for fill in (0, 255):
+        room = [torch.full((n + 64,), 77, device=device(), dtype=torch.uint8)
+                for n in (q.q.numel(), 4 * q.scale.numel(), t.q.numel(), 4 * t.scale.numel(), nb)]
+        room[4][:nb] = fill
+        assert L._lib.lsgd_quantise_rows(
+            0, G, M, N, X.data_ptr(), N, M * N, *[r.data_ptr() for r in room], nb,
+            torch.cuda.current_stream().cuda_stream) == 0
+        for r, want in zip(room, (q.q, q.scale, t.q, t.scale)):
+            assert torch.equal(r[:-64], want.flatten().view(torch.uint8)) and (r[-64:] == 77).all()
+        assert (room[4][nb:] == 77).all()
+
+
+@pytest.mark.parametrize("M,N,dtype", [(7000, 8300, "fp32"), (2 ** 24 + 5, 7, "bf16"),
+                                       (700001, 123, "fp32")])
+def test_quantise_tensors_past_the_caches(M, N, dtype):
+    """Hundreds of MB, whose integers are streamed past the caches: rows and columns as on their own."""
+    L = _lsgd()
+    print(f"quantise rows streamed {M} {N} {dtype}", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(3)
+    X = torch.randn(1, M, N, generator=gen, device=device()).to(_dt(dtype))
+    q, t = L.quantise_rows(X, both=True)
+    alone = L.quantise_rows(X)
+    assert torch.equal(alone.q, q.q) and torch.equal(alone.scale, q.scale)
+    _check_rows(L.Rows(q.q[:, -40:].contiguous(), q.scale[:, -40:].contiguous(), N), _np(X[:, -40:]))
+    for n in (0, N // 2, N - 1):
+        column = L.quantise_rows(X[:, :, n].unsqueeze(1).contiguous())
+        assert torch.equal(column.q[0, 0], t.q[0, n]) and torch.equal(column.scale[0], t.scale[0, n:n + 1])
+
+
 def test_quantise_every_quotient():
     """All 2^16 bfloat16 values against scales whose quotients fall near ties, and fp32
     neighbours of every tie of odd scales."""
@@ -123,6 +181,9 @@ def test_quantise_strided_and_shared_inputs():
         _check_rows(t, _np(X).transpose(0, 2, 1))
         E = X[:1].expand(4, 33, 131)
         _check_rows(L.quantise_rows(E), _np(E))
+        q, t = L.quantise_rows(E, both=True)
+        _check_rows(q, _np(E))
+        _check_rows(t, _np(E).transpose(0, 2, 1))
         rows = X[0, :1].unsqueeze(0).expand(2, 7, 131)  # one row again and again
         with pytest.raises(L.LsgdError):  # (rows that overlap: a pitch below the columns)
             L.quantise_rows(rows)
