@@ -400,8 +400,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_params(NormBackArgs a, int ti
 // Threads and vectors a row of N values takes, and threads of a workgroup; T == 0: any length. Few
 // threads, two to four vectors each: the sums over lanes and the statistics cost a row's threads as
 // much as some ten values each. (us in bf16, so and by one vector a thread: 500000 x 64 26 and 51,
-// 250000 x 256 48 and 103, 131072 x 512 53 and 66, 32768 x 2048 51 and 62; four against two: 16384 x
-// 8192 107 and 115, but 16384 x 4096 54 and 51.)
+// 250000 x 256 48 and 103, 131072 x 512 53 and 66, 32768 x 2048 51 and 62. Threads without values
+// wait all the same: of three vectors and, as for the next longer rows, two or four 18678 x 2063 48
+// and 58, 6000 x 9000 53 and 77, 100000 x 384 31 and 36. Four vectors against two: 16384 x 8192 107
+// and 115, 4096 x 16384 70 and 72, but 16384 x 4096 54 and 51.)
 template <int T_, int V_, int B_>
 struct Shape {
   static constexpr int T = T_, V = V_, B = B_;
@@ -414,19 +416,25 @@ auto with_shape(int N, F f) {
   if (N <= 64) return f(Shape<4, 2, 256>{});
   if (N <= 128) return f(Shape<4, 4, 256>{});
   if (N <= 256) return f(Shape<16, 2, 256>{});
+  if (N <= 16 * 3 * 8) return f(Shape<16, 3, 256>{});
   if (N <= 512) return f(Shape<16, 4, 256>{});
   if (N <= 1024) return f(Shape<64, 2, 256>{});
+  if (N <= 64 * 3 * 8) return f(Shape<64, 3, 256>{});
   if (N <= 2048) return f(Shape<64, 4, 256>{});
+  if (N <= 128 * 3 * 8) return f(Shape<128, 3, 256>{});
   if (N <= 4096) return f(Shape<256, 2, 256>{});
+  if (N <= 256 * 3 * 8) return f(Shape<256, 3, 256>{});
   if (N <= 8192) return f(Shape<256, 4, 256>{});
-  if (N <= 16384) return f(Shape<1024, 2, 1024>{});
+  if (N <= 512 * 3 * 8) return f(Shape<512, 3, 512>{});
+  if (N <= 16384) return f(Shape<512, 4, 512>{});
   return f(Shape<0, 0, 0>{});
 }
 // Backward, where sums of the columns stay in registers too, and few strips leave few of them to
 // add: large workgroups, one or two a compute unit. (16 x 128 x 512 in workgroups of 256 and two launches
 // 19.4 us, of 1024 and one 13.7; in bf16 by two vectors a thread and by one 500000 x 64 44 and 50, 250000 x 256
-// 81 and 92, 4 x 9777 x 1134 73 and 83; 4096 x 16384 by 1024 threads, which spill, 278, by 512 without a
-// row ahead 98.)
+// 81 and 92, 4 x 9777 x 1134 73 and 83; by three and by two or four 4 x 9777 x 1134 61 and 73, 18678 x
+// 2063 60 and 80, 6000 x 9000 76 and 85; 4096 x 16384 by 1024 threads, which spill, 278, by 512 without
+// a row ahead 98.)
 template <class F>
 auto with_back_shape(int N, F f) {
   if (N <= 8) return f(Shape<1, 1, 256>{});
@@ -436,9 +444,13 @@ auto with_back_shape(int N, F f) {
   if (N <= 256) return f(Shape<16, 2, 512>{});
   if (N <= 512) return f(Shape<64, 1, 1024>{});
   if (N <= 1024) return f(Shape<64, 2, 512>{});
+  if (N <= 64 * 3 * 8) return f(Shape<64, 3, 512>{});
   if (N <= 2048) return f(Shape<128, 2, 512>{});
+  if (N <= 128 * 3 * 8) return f(Shape<128, 3, 512>{});
   if (N <= 4096) return f(Shape<256, 2, 512>{});
+  if (N <= 256 * 3 * 8) return f(Shape<256, 3, 512>{});
   if (N <= 8192) return f(Shape<512, 2, 512>{});
+  if (N <= 512 * 3 * 8) return f(Shape<512, 3, 512>{});
   if (N <= 16384) return f(Shape<512, 4, 512>{});
   return f(Shape<0, 0, 0>{});
 }

@@ -88,7 +88,8 @@ SHAPES = [(1, 1, 1), (2, 5, 1), (3, 7, 2), (2, 300, 3), (1, 33, 8), (2, 5, 9), (
           (1, 65, 512), (2, 9, 513), (1, 6, 1024), (1, 5, 1027), (2, 3, 2049), (1, 3, 4096), (1, 3, 4099),
           (1, 2, 8192), (1, 3, 8195), (1, 2, 16384), (1, 5, 16385), (2, 2, 40003), (1, 5000, 33),
           (3, 1537, 771), (300, 1, 130), (40, 70, 20), (2, 50, 13), (1, 77, 63), (2, 400, 64), (2, 40, 300),
-          (1, 30, 256), (3, 999, 16), (2, 260, 32)]
+          (1, 30, 256), (3, 999, 16), (2, 260, 32), (2, 37, 1530), (1, 41, 1537), (3, 45, 2303), (2, 29, 5555),
+          (2, 11, 12001), (1, 7, 12289), (1, 9, 383), (1, 9001, 1100), (1, 5001, 2063), (1, 1100, 8200)]
 
 
 @pytest.mark.parametrize("types", ["fp32 fp32", "bf16 bf16", "fp32 bf16", "bf16 fp32"])
