@@ -392,14 +392,19 @@ hipError_t quantise(const RowQuantArgs& a, void* ws, hipStream_t s) {
     hipLaunchKernelGGL(kernel, grid_of(n), dim3(threads), 0, s, a, rows);
     return hipGetLastError();
   };
-  // (us in bf16 by 16 threads a row and by 64: 250000 x 256 34 and 61, 131072 x 512 34 and 40)
+  // (us in bf16 by 16 threads a row and by 64: 250000 x 256 34 and 61, 131072 x 512 34 and 40; by three or six
+  // vectors a thread and by twice the threads or by four: 18678 x 2063 21 and 26, 6000 x 9000 27 and 37)
   if (a.N <= 128) return launch(k_rows<BF, 16, 1>, 16, 256);
   if (a.N <= 256) return launch(k_rows<BF, 16, 2>, 16, 256);
   if (a.N <= 512) return launch(k_rows<BF, 16, 4>, 16, 256);
   if (a.N <= 1024) return launch(k_rows<BF, 64, 2>, 4, 256);
+  if (a.N <= 64 * 3 * 8) return launch(k_rows<BF, 64, 3>, 4, 256);
   if (a.N <= 2048) return launch(k_rows<BF, 64, 4>, 4, 256);
+  if (a.N <= 64 * 6 * 8) return launch(k_rows<BF, 64, 6>, 4, 256);
   if (a.N <= 4096) return launch(k_rows<BF, 256, 2>, 1, 256);
+  if (a.N <= 256 * 3 * 8) return launch(k_rows<BF, 256, 3>, 1, 256);
   if (a.N <= 8192) return launch(k_rows<BF, 256, 4>, 1, 256);
+  if (a.N <= 512 * 3 * 8) return launch(k_rows<BF, 512, 3>, 1, 512);
   if (a.N <= 16384) return launch(k_rows<BF, 1024, 2>, 1, 1024);
   return launch(k_rows<BF, 1024, 0>, 1, 1024);
 }

@@ -37,7 +37,8 @@ def _check_rows(got, X):
 # each number of threads and vectors a row takes, and sizes on both sides of a tile's edge
 SHAPES = [(1, 1, 1), (2, 1, 7), (3, 5, 1), (2, 16, 128), (1, 64, 512), (2, 129, 127), (3, 130, 257),
           (1, 17, 1025), (1, 700, 9), (2, 127, 641), (2, 3, 2049), (1, 5, 4097), (1, 3, 8191), (1, 2, 16384),
-          (1, 3, 16385), (1, 2, 40001), (1, 1030, 3), (2, 513, 513), (300, 1, 130)]
+          (1, 3, 16385), (1, 2, 40001), (1, 1030, 3), (2, 513, 513), (300, 1, 130), (2, 9, 1530), (3, 9, 1537),
+          (3, 13, 2303), (2, 7, 5555), (1, 5, 12001), (1, 5, 12289)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
