@@ -7,7 +7,7 @@
 // chunks by bound / norm in fp64, one rounding a value.
 //
 // Bound by HBM: two reads and a write (2 x 402M values in fp32 1810 us, 5.3 TB/s; the fp64 products
-// cost 1%). What the caches hold is read once (16 x 530K values, 34 MB: 7.6 and 10.4 us).
+// cost 1%). What the caches hold is read once (16 x 530K values, 34 MB: 8.0 and 11.1 us).
 #include <algorithm>
 #include <cmath>
 
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kThreads) void k_clip_scale(ClipArgs a, long long t
 
 // The cut: values a chunk, for about kChunks chunks in all and at least kLeast values; and a
 // replica's chunks. (2 x 402M values in 2048, 8192, 16384 chunks 1945, 1837, 1810 us; 16 x 530K in chunks of
-// 4096, 6144, 8192 values 20.5, 18.2, 19.3.) From kWide of them on their sums are added by a launch of
+// 4096, 6144, 8192 values 19.8, 18.6, 19.5.) From kWide of them on their sums are added by a launch of
 // its own (4.8 us for 8200), not by every workgroup.
 constexpr long long kChunks = 16384, kLeast = 6144, kStep = 2048;
 constexpr int kWide = 512;
