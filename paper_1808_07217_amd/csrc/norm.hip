@@ -460,8 +460,14 @@ int strip_rows(long long strips, int each, int G, int M) {
   const long long rows = (M + strips - 1) / strips;
   return (int)((rows + each - 1) / each * each);
 }
-// (of workgroups of 256 threads 1024, 2048, 4096 strips: 4 x 9777 x 333 in fp32 23.9, 22.8, 25.9 us)
-constexpr long long kStrips = 1024, kSmallStrips = 2048;  // of workgroups of 1024 threads, of 256
+// Four sets of rows a strip, for which w and b are read once; but five workgroups a compute unit, and
+// no more than 4096. (us, of sets a strip: 16384 x 8192 in bf16 4 106, 8 109, 16 114; 32768 x 2048 2 52, 4 50,
+// 8 51.5; 131072 x 512 1 58, 2 51, 4 49, 8 52; 4000 x 12000 in fp32 1 102, 2 86, 4 79, 8 80; 3000 x 3500 2 17.3,
+// 3 16.5.) Of 512 threads 1024 strips (16384 x 16384 in 1024, 2048, 4096 strips 236, 243, 256).
+int norm_strip_rows(int each, bool large, int G, int M) {
+  const long long sets = ((long long)M + each - 1) / each * G;
+  return strip_rows(large ? 1024 : std::min(4096LL, std::max(1280LL, sets / 4)), each, G, M);
+}
 
 template <bool XBF, bool YBF>
 hipError_t norm(NormArgs a, hipStream_t s) {
@@ -472,7 +478,7 @@ hipError_t norm(NormArgs a, hipStream_t s) {
       if (total > 0x7fffffffLL) return hipErrorInvalidValue;
       hipLaunchKernelGGL((k_norm_long<XBF, YBF>), grid_of(total), dim3(kLong), 0, s, a, total);
     } else {
-      a.strip = strip_rows(B == 256 ? kSmallStrips : kStrips, B / T, a.G, a.M);
+      a.strip = norm_strip_rows(B / T, B > 256, a.G, a.M);
       const int strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
       const long long total = (long long)strips * a.G;
       hipLaunchKernelGGL((k_norm<XBF, YBF, T, V, B>), grid_of(total), dim3(B), 0, s, a, strips, total);
