@@ -183,6 +183,16 @@ __global__ __launch_bounds__(kLong) void k_norm_long(NormArgs a, long long total
 }
 
 // ---------------------------------------------------------------- backward
+// (x - mean) rstd of a row. `far`: it may leave fp32's range in columns past the last, which hold zeros.
+constexpr float kFar = 2048.f;
+template <class A>
+struct Row {
+  A mean, rstd;
+  bool far;
+  __device__ __forceinline__ Row(float m, float r) : mean(m), rstd(r), far(!(fabsf(m) * r < kFar)) {}
+  __device__ __forceinline__ A operator()(float x) const { return ((A)x - mean) * rstd; }
+};
+
 // A strip of rows a workgroup; a thread keeps the sums of its columns over them. A: the
 // arithmetic of a row. Of rows of few columns little is left beside the two directions that are
 // taken out (of two columns eps / variance of e): those of up to eight, a thread's each, in fp64.
@@ -226,7 +236,8 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
     const int m = r + slot;
     A s[2] = {0, 0};
     if (!kAhead) fetch(m);
-    const A mean = mean_next, rstd = rstd_next;
+    const float mean = mean_next, rstd = rstd_next;
+    const Row<A> row(mean, rstd);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       xr[i] = xn[i];
@@ -235,16 +246,46 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
       settle8<YBF, T == 1>((t + i * T) * 8, a.N, dr[i]);
     }
     if (kAhead && r + kRows < end) fetch(m + kRows);
+    if (V <= 2 || !row.far) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
+      for (int i = 0; i < V; ++i) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const A x = ((A)xr[i][e] - mean) * rstd, dy = (A)dr[i][e] * w[i][e];
-        dw[i][e] += dr[i][e] * (float)x;
-        db[i][e] += dr[i][e];
-        s[0] += dy;
-        s[1] += dy * x;
+        for (int e = 0; e < 8; ++e) {
+          const A x = row(xr[i][e]), dy = (A)dr[i][e] * w[i][e];
+          s[0] += dy;
+          s[1] += dy * x;
+        }
       }
+    }
+    if (row.far) {
+      double f[2] = {0.0, 0.0};
+      const auto add = [&](bool in, float x, float dy, float w) __attribute__((always_inline)) {
+        const A n = in ? row(x) : (A)0, e = (A)dy * w;
+        f[0] += e;
+        f[1] += (double)e * n;
+      };
+      if constexpr (V <= 2) {
+        int left = a.N - t * 8;
+        asm volatile("" : "+v"(left));  // (or the comparisons are kept over the rows, two registers each)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) add(i * T * 8 + e < left, xr[i][e], dr[i][e], w[i][e]);
+        }
+      } else {  // (read again: kept in registers up to here it takes them from every row)
+#pragma unroll 1
+        for (int i = 0; i < V; ++i) {
+          const int n = (t + i * T) * 8;
+          float xs[8], ds[8], ws[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+          load8<XBF>(a.X, g * a.sX + m * a.ldx, n, a.N, xs);
+          load8<YBF>(a.dY, g * a.sg + m * a.ldg, n, a.N, ds);
+          if (a.w) load8<false>(a.w, g * a.sw, n, a.N, ws);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) add(n + e < a.N, xs[e], ds[e], ws[e]);
+        }
+      }
+      s[0] = (A)f[0];
+      s[1] = (A)f[1];
     }
     row_sums<T>(s, room[odd]);
     const A c1 = s[0] / a.N, c2 = s[1] / a.N;
@@ -255,8 +296,10 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
         float d[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const A x = ((A)xr[i][e] - mean) * rstd, dy = (A)dr[i][e] * w[i][e];
+          const A x = row(xr[i][e]), dy = (A)dr[i][e] * w[i][e];
           d[e] = (float)(rstd * (dy - c1 - x * c2));  // (zero where dy is c1: of one column)
+          dw[i][e] += dr[i][e] * (float)x;
+          db[i][e] += dr[i][e];
         }
         store8<XBF>(a.dX, g * a.sd + m * a.ldd, n, a.N, d);
       }
@@ -331,6 +374,7 @@ __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long l
   const int g = id / a.M, m = id - g * a.M;
   const long long x0 = g * a.sX + m * a.ldx, d0 = g * a.sg + m * a.ldg;
   const float mean = a.mean[id], rstd = a.rstd[id];
+  const Row<float> row(mean, rstd);
   float s[2] = {0.f, 0.f}, x[8], dy[8];
   auto take = [&](int n) __attribute__((always_inline)) {
     float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
@@ -339,12 +383,18 @@ __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long l
     if (a.w) load8<false>(a.w, g * a.sw, n, a.N, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      x[e] = (x[e] - mean) * rstd;
+      x[e] = row(x[e]);
       dy[e] *= w[e];
     }
   };
   for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
     take(n);
+    if (row.far) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (n + e >= a.N) x[e] = 0.f;  // (it may have left fp32's range)
+      }
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       s[0] += dy[e];
@@ -371,13 +421,14 @@ __global__ __launch_bounds__(kThreads) void k_norm_params(NormBackArgs a, int ti
   const int n0 = (id - gs * tiles) * 512, n = n0 + lane * 8;
   float dw[8] = {}, db[8] = {};
   for (int m = m0 + wave; m < end; m += 4) {
-    const float mean = a.mean[(long long)g * a.M + m], rstd = a.rstd[(long long)g * a.M + m];
+    const long long at = (long long)g * a.M + m;
+    const Row<float> row(a.mean[at], a.rstd[at]);
     float x[8], dy[8];
     load8<XBF>(a.X, g * a.sX + m * a.ldx, n, a.N, x);
     load8<YBF>(a.dY, g * a.sg + m * a.ldg, n, a.N, dy);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      dw[e] += dy[e] * ((x[e] - mean) * rstd);
+      dw[e] += dy[e] * row(x[e]);
       db[e] += dy[e];
     }
   }

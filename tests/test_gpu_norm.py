@@ -340,3 +340,24 @@ def test_past_32_bit_offsets(N):
         sums += dY[0, m:m + 8192].sum(0, dtype=torch.float64)
         size += dY[0, m:m + 8192].abs().sum(0, dtype=torch.float32)
     assert bool(((db[0] - sums).abs() <= gamma(M // 256 + 60) * size).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("N", [5, 40, 64, 700, 1100, 5000, 8192, 9000, 16384, 20001])
+def test_constant_rows_far_out(N, dtype):
+    """One value throughout, so far from zero that it leaves fp32's range in deviations of
+    eps: no deviations, and the gradient that is left."""
+    L = _lsgd()
+    print(f"layer norm constant rows {N} {dtype}", flush=True)
+    dt = _dt(dtype)
+    rng = np.random.default_rng(N)
+    X = np.repeat(np.array([2e36, -3e37, 1.0, 3e38])[None, :, None], N, 2)
+    X = to_dev(X.astype(np.float32)).to(dt)
+    dY, w, b = (to_dev(rng.standard_normal(s).astype(np.float32)) for s in ((1, 4, N), (1, N), (1, N)))
+    dY = (dY * 1e-3).to(dt)
+    for eps in (1e-5, 1e-12):
+        y, mean, rstd = L.layer_norm(X, w, b, eps=eps)
+        assert torch.equal(y[0], b.to(dt).expand(4, N)) and torch.equal(mean[0], X[0, :, 0].float())
+        got = L.layer_norm_backward(dY, X, mean, rstd, w)
+        assert not got[1].any()
+        _check_backward(got, _np(dY), _np(X), _np(mean), _np(rstd), _np(w))
