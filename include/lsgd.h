@@ -663,9 +663,11 @@ lsgd_status lsgd_layer_norm(int32_t dtype, int32_t out_dtype, int32_t G,
  *   dX = rstd (e - sum e / N - n sum (e n) / N) (dtype),
  *   dw = sum over the group's rows of dy n, db = sum of dy (fp32 [G][N], group strides sdw,
  *   sdb >= N; both NULL: not wanted).
+ * The fp32 mean is off the row's own by up to 2^-24 |mean|, and n by that times rstd: of rows
+ * of |mean| rstd >= 2048 the row's own mean is found again from X and d_mean and used instead.
  * The sums over rows are added in an order that the sizes alone decide. Workspace
  * (not without dw and db): lsgd_layer_norm_backward_workspace_bytes, 16-byte aligned (LSGD_E_WORKSPACE
- * if smaller; 0 for few rows; then NULL is allowed), one call's at a time. Limits as
+ * if smaller; may be 0; then NULL is allowed), one call's at a time. Limits as
  * above. Results must not overlap each other or anything that is read.
  */
 lsgd_status lsgd_layer_norm_backward_workspace_bytes(int32_t G, int32_t M,

@@ -234,9 +234,9 @@ struct NormBackArgs {
   float *dw, *db;
   long long sdw, sdb;
   // set by launch_norm_back: rows a workgroup takes, their number in a group, and its sums
-  // [G][strips][2][N]
+  // [G][strips][2][N]; of long rows [G][M]: what is to be taken off (x - mean) rstd
   int strip, strips;
-  float* part;
+  float *part, *shift;
 };
 size_t norm_back_workspace_bytes(int G, int M, int N);
 hipError_t launch_norm_back(int x_bf16, int y_bf16, const NormBackArgs& a, void* ws, hipStream_t s);

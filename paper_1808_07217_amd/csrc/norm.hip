@@ -4,7 +4,8 @@
 // Both sums are held in fp64, and the mean in two floats: rows far from zero and
 // values whose squares leave fp32's range come out as exactly as others.
 // Backward, from the mean and rstd that the forward pass wrote: n = (x - mean) rstd, e = dy w,
-// dx = rstd (e - sum e / N - n sum (e n) / N), dw = sum over rows of dy n, db of dy.
+// dx = rstd (e - sum e / N - n sum (e n) / N), dw = sum over rows of dy n, db of dy. The mean is a
+// float there: of rows far from zero it is found again from x.
 //
 // Bound by HBM (each tensor is read or written once: 16384 x 8192 in bf16 5.1 TB/s forward, 4.9
 // backward; a copy of 4 GB 4.8), small ones by a launch and a load's latency (3 x 1537 x 771 in fp32
@@ -183,7 +184,10 @@ __global__ __launch_bounds__(kLong) void k_norm_long(NormArgs a, long long total
 }
 
 // ---------------------------------------------------------------- backward
-// (x - mean) rstd of a row. `far`: it may leave fp32's range in columns past the last, which hold zeros.
+// (x - mean) rstd of a row, from the mean as it was written. `far`: its rounding to fp32 moves that by
+// up to 2^-13 and more. What is left is then the mean of the results, and taken off; and in columns past
+// the last, which hold zeros, it may leave fp32's range. (Below, the mean is what the caller gave: of two
+// columns, whose dx is 10^-5 of dy, the difference shows.)
 constexpr float kFar = 2048.f;
 template <class A>
 struct Row {
@@ -199,7 +203,7 @@ struct Row {
 template <bool XBF, bool YBF, int T, int V, int B, class A>
 __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total) {
   constexpr int kBlock = B, kRows = kBlock / T, kCols = T * V * 8;
-  __shared__ A room[2][kBlock / 64][2];
+  __shared__ A room[2][kBlock / 64][2], off[2][kBlock / 64];
   // the columns' sums of several rows at work at one time: a wavefront's, or its rows' each
   constexpr int kSlots = T < 64 ? kBlock / 64 : kRows;
   __shared__ float slots[kSlots > 1 ? kSlots * kCols : 1];
@@ -257,12 +261,14 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
         }
       }
     }
+    A shift = 0;
     if (row.far) {
-      double f[2] = {0.0, 0.0};
+      double f[3] = {0.0, 0.0, 0.0};
       const auto add = [&](bool in, float x, float dy, float w) __attribute__((always_inline)) {
         const A n = in ? row(x) : (A)0, e = (A)dy * w;
         f[0] += e;
         f[1] += (double)e * n;
+        f[2] += n;
       };
       if constexpr (V <= 2) {
         int left = a.N - t * 8;
@@ -286,8 +292,22 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
       }
       s[0] = (A)f[0];
       s[1] = (A)f[1];
+      shift = lanes_sum<(T < 64 ? T : 64)>((A)f[2]);
+      if constexpr (T > 64) {
+        if ((threadIdx.x & 63) == 0) off[odd][threadIdx.x >> 6] = shift;
+      }
     }
     row_sums<T>(s, room[odd]);
+    if (row.far) {
+      if constexpr (T > 64) {
+        const int first = (threadIdx.x >> 6) / (T / 64) * (T / 64);
+        shift = off[odd][first];
+#pragma unroll
+        for (int k = 1; k < T / 64; ++k) shift += off[odd][first + k];
+      }
+      shift /= a.N;
+      s[1] -= shift * s[0];
+    }
     const A c1 = s[0] / a.N, c2 = s[1] / a.N;
     if (m < end) {
 #pragma unroll
@@ -296,7 +316,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
         float d[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const A x = row(xr[i][e]), dy = (A)dr[i][e] * w[i][e];
+          const A x = row(xr[i][e]) - shift, dy = (A)dr[i][e] * w[i][e];
           d[e] = (float)(rstd * (dy - c1 - x * c2));  // (zero where dy is c1: of one column)
           dw[i][e] += dr[i][e] * (float)x;
           db[i][e] += dr[i][e];
@@ -368,14 +388,14 @@ __global__ __launch_bounds__(kJoin) void k_norm_join(NormBackArgs a, int tiles, 
 // in bf16 217 us, 2.3 TB/s of what has to move).
 template <bool XBF, bool YBF>
 __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long long total) {
-  __shared__ float room[kLong / 64][2];
+  __shared__ float room[kLong / 64][3];
   const unsigned id = workgroup_id();
   if (id >= total) return;
   const int g = id / a.M, m = id - g * a.M;
   const long long x0 = g * a.sX + m * a.ldx, d0 = g * a.sg + m * a.ldg;
   const float mean = a.mean[id], rstd = a.rstd[id];
   const Row<float> row(mean, rstd);
-  float s[2] = {0.f, 0.f}, x[8], dy[8];
+  float s[3] = {0.f, 0.f, 0.f}, x[8], dy[8];
   auto take = [&](int n) __attribute__((always_inline)) {
     float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
     load8<XBF>(a.X, x0, n, a.N, x);
@@ -393,6 +413,7 @@ __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long l
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (n + e >= a.N) x[e] = 0.f;  // (it may have left fp32's range)
+        s[2] += x[e];
       }
     }
 #pragma unroll
@@ -402,11 +423,13 @@ __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long l
     }
   }
   row_sums<kLong>(s, room);
-  const float c1 = s[0] / a.N, c2 = s[1] / a.N;
+  const float shift = s[2] / a.N;  // (none but of far rows)
+  const float c1 = s[0] / a.N, c2 = (s[1] - shift * s[0]) / a.N;
+  if (a.dw && threadIdx.x == 0) a.shift[id] = shift;
   for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
     take(n);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = rstd * (dy[e] - c1 - x[e] * c2);
+    for (int e = 0; e < 8; ++e) x[e] = rstd * (dy[e] - c1 - (x[e] - shift) * c2);
     store8<XBF>(a.dX, g * a.sd + m * a.ldd, n, a.N, x);
   }
 }
@@ -423,12 +446,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_params(NormBackArgs a, int ti
   for (int m = m0 + wave; m < end; m += 4) {
     const long long at = (long long)g * a.M + m;
     const Row<float> row(a.mean[at], a.rstd[at]);
+    const float shift = a.shift[at];
     float x[8], dy[8];
     load8<XBF>(a.X, g * a.sX + m * a.ldx, n, a.N, x);
     load8<YBF>(a.dY, g * a.sg + m * a.ldg, n, a.N, dy);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      dw[e] += dy[e] * row(x[e]);
+      dw[e] += dy[e] * (row(x[e]) - shift);
       db[e] += dy[e];
     }
   }
@@ -486,6 +510,7 @@ auto with_shape(int N, F f) {
 // 81 and 92, 4 x 9777 x 1134 73 and 83; by three and by two or four 4 x 9777 x 1134 61 and 73, 18678 x
 // 2063 60 and 80, 6000 x 9000 76 and 85; 4096 x 16384 by 1024 threads, which spill, 278, by 512 without
 // a row ahead 98.)
+constexpr int kHeld = 16384;  // columns of the longest
 template <class F>
 auto with_back_shape(int N, F f) {
   if (N <= 8) return f(Shape<1, 1, 256>{});
@@ -502,7 +527,7 @@ auto with_back_shape(int N, F f) {
   if (N <= 256 * 3 * 8) return f(Shape<256, 3, 512>{});
   if (N <= 8192) return f(Shape<512, 2, 512>{});
   if (N <= 512 * 3 * 8) return f(Shape<512, 3, 512>{});
-  if (N <= 16384) return f(Shape<512, 4, 512>{});
+  if (N <= kHeld) return f(Shape<512, 4, 512>{});
   return f(Shape<0, 0, 0>{});
 }
 // Rows of a strip: about `strips` strips in all, of whole sets of `each` rows at work at one time.
@@ -556,6 +581,7 @@ hipError_t norm_back(NormBackArgs a, void* ws, hipStream_t s) {
   a.strip = back_strip_rows(a.G, a.M, a.N);
   a.strips = (int)((a.M + (long long)a.strip - 1) / a.strip);
   a.part = (float*)ws;
+  a.shift = (float*)ws + (a.strips == 1 ? 0 : (size_t)a.G * a.strips * 2 * a.N);
   const long long strips = (long long)a.strips * a.G;
   hipError_t e = with_back_shape(a.N, [&](auto z) {
     constexpr int T = decltype(z)::T, V = decltype(z)::V, B = decltype(z)::B;
@@ -590,7 +616,9 @@ hipError_t launch_norm(int x_bf16, int y_bf16, const NormArgs& a, hipStream_t s)
 
 size_t norm_back_workspace_bytes(int G, int M, int N) {
   const long long strip = back_strip_rows(G, M, N), strips = (M + strip - 1) / strip;
-  return strips == 1 ? 0 : (size_t)G * strips * 2 * N * sizeof(float);
+  const size_t sums = strips == 1 ? 0 : (size_t)G * strips * 2 * N;
+  // (of rows past what registers hold: how far each is off its mean as it was written)
+  return (sums + (N > kHeld ? (size_t)G * M : 0)) * sizeof(float);
 }
 
 hipError_t launch_norm_back(int x_bf16, int y_bf16, const NormBackArgs& a, void* ws, hipStream_t s) {

@@ -361,3 +361,44 @@ def test_constant_rows_far_out(N, dtype):
         got = L.layer_norm_backward(dY, X, mean, rstd, w)
         assert not got[1].any()
         _check_backward(got, _np(dY), _np(X), _np(mean), _np(rstd), _np(w))
+
+
+@pytest.mark.parametrize("types", ["fp32 fp32", "fp32 bf16"])
+@pytest.mark.parametrize("N", [2, 5, 9, 40, 130, 700, 1100, 1500, 2500, 5000, 9000, 16000, 20001])
+def test_gradients_of_rows_far_from_zero(N, types):
+    """Means of 10^4 and 10^6 deviations: the gradients of the values' own mean, which the fp32 one
+    that is handed over misses by up to 6% of a deviation. x - mean as it was written is rounded to u,
+    times rstd once more; what is taken off is the mean of those, rounded, as is the difference."""
+    L = _lsgd()
+    print(f"layer norm far rows {N} {types}", flush=True)
+    xt, yt = map(_dt, types.split())
+    rng = np.random.default_rng(N)
+    M = 21
+    X = rng.standard_normal((1, M, N))
+    X[0, 0:5] += 1e4
+    X[0, 5:10] -= 1e6
+    X[0, 10:13] = 1e4 + 1e-2 * X[0, 10:13]
+    X[0, 13:15] = 1e9 + 1e4 * X[0, 13:15]
+    X[0, 15:16] = 1e34 + 1e29 * X[0, 15:16]
+    X = to_dev(X.astype(np.float32)).to(xt)
+    dY, w = (to_dev(rng.standard_normal(s).astype(np.float32)) for s in ((1, M, N), (1, N)))
+    dY = dY.to(yt)
+    _, mean, rstd = L.layer_norm(X, w)
+    dx, dw, db = L.layer_norm_backward(dY, X, mean, rstd, w)
+    x, d, r = _np(X), _np(dY), _np(rstd)[..., None]
+    own = x.mean(2)
+    far = np.abs(own) * r[..., 0] >= 2100
+    assert far[0, :13].sum() >= 10 and not far[0, 16:].any()
+    own = np.where(far, own, _np(mean))
+    rx, rw, rb = O.layer_norm_backward(d, x, own, _np(rstd), _np(w))
+    a = lambda t: np.abs(t)  # noqa: E731
+    av = lambda t: t.mean(2, keepdims=True)  # noqa: E731
+    n, e, off = (x - own[..., None]) * r, d * _np(w)[:, None], 2.0 ** -24 * a(own[..., None]) * r
+    en = U32 * (4 * (a(n) + off) + np.where(far[..., None], 4 * (av(a(n)) + off), 0))
+    D = 46 + N // 1024
+    bound = r * (a(av(e * n)) * en + (a(n) + en) * (av(a(e) * en) + gamma(D) * av(a(e) * (a(n) + off)))
+                 + gamma(D) * av(a(e)) + 6 * U32 * (a(e) + a(av(e)) + a(n * av(e * n)))) + 1.01 * U32 * a(rx)
+    err, bound = a(_np(dx) - rx), _rounded(bound, rx, dx.dtype)
+    assert np.all(err <= bound), np.max(err / bound)
+    assert np.all(a(_np(dw) - rw) <= (a(d) * en).sum(1) + gamma(M + 3) * a(d * n).sum(1))
+    assert np.all(a(_np(db) - rb) <= gamma(M + 3) * a(d).sum(1))
