@@ -200,9 +200,13 @@ struct Row {
 // A strip of rows a workgroup; a thread keeps the sums of its columns over them. A: the
 // arithmetic of a row. Of rows of few columns little is left beside the two directions that are
 // taken out (of two columns eps / variance of e): those of up to eight, a thread's each, in fp64.
+// A column's sum is fp32 over kChain rows of a thread, and fp64 over those; of three vectors and more,
+// which leave no registers for that, fp32 over the strip, of kFewSums rows a thread at most.
+constexpr int kChain = 4;
 template <bool XBF, bool YBF, int T, int V, int B, class A>
 __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total) {
   constexpr int kBlock = B, kRows = kBlock / T, kCols = T * V * 8;
+  constexpr bool kWide = V <= 2;
   __shared__ A room[2][kBlock / 64][2], off[2][kBlock / 64];
   // the columns' sums of several rows at work at one time: a wavefront's, or its rows' each
   constexpr int kSlots = T < 64 ? kBlock / 64 : kRows;
@@ -228,6 +232,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
   };
   if (kAhead) fetch(m0 + slot);
   float w[V][8], dw[V][8], db[V][8];
+  double wide_w[kWide ? V : 1][8] = {}, wide_b[kWide ? V : 1][8] = {};
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int n = (t + i * T) * 8;
@@ -235,7 +240,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
     for (int e = 0; e < 8; ++e) w[i][e] = 1.f, dw[i][e] = db[i][e] = 0.f;
     if (a.w) load8<false, T == 1>(a.w, g * a.sw, n, a.N, w[i]);
   }
-  int odd = 0;
+  int odd = 0, chain = 0;
   for (int r = m0; r < end; r += kRows, odd ^= 1) {
     const int m = r + slot;
     A s[2] = {0, 0};
@@ -250,7 +255,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
       settle8<YBF, T == 1>((t + i * T) * 8, a.N, dr[i]);
     }
     if (kAhead && r + kRows < end) fetch(m + kRows);
-    if (V <= 2 || !row.far) {
+    if (kWide || !row.far) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
 #pragma unroll
@@ -270,7 +275,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
         f[1] += (double)e * n;
         f[2] += n;
       };
-      if constexpr (V <= 2) {
+      if constexpr (kWide) {
         int left = a.N - t * 8;
         asm volatile("" : "+v"(left));  // (or the comparisons are kept over the rows, two registers each)
 #pragma unroll
@@ -324,8 +329,26 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
         store8<XBF>(a.dX, g * a.sd + m * a.ldd, n, a.N, d);
       }
     }
+    if constexpr (kWide) {
+      if (++chain == kChain && r + kRows < end) {
+        chain = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            wide_w[i][e] += dw[i][e];
+            wide_b[i][e] += db[i][e];
+            dw[i][e] = db[i][e] = 0.f;
+          }
+      }
+    }
   }
   if (!a.dw) return;
+  const auto column = [&](int h, int i, int e) __attribute__((always_inline)) {
+    double v = h ? db[i][e] : dw[i][e];
+    if constexpr (kWide) v += h ? wide_b[i][e] : wide_w[i][e];
+    return v;
+  };
   // joined in order; one strip is the result itself
   float* to_w = a.strips == 1 ? a.dw + g * a.sdw : a.part + (long long)id * 2 * a.N;
   float* to_b = a.strips == 1 ? a.db + g * a.sdb : a.part + ((long long)id * 2 + 1) * a.N;
@@ -334,8 +357,12 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
     float* to = h ? to_b : to_w;
     if constexpr (kSlots == 1) {
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        store8<false>(to, 0, (t + i * T) * 8, a.N, h ? db[i] : dw[i]);
+      for (int i = 0; i < V; ++i) {
+        float sum[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = (float)column(h, i, e);
+        store8<false>(to, 0, (t + i * T) * 8, a.N, sum);
+      }
     } else {
       const int mine = T < 64 ? threadIdx.x >> 6 : slot;
       __syncthreads();
@@ -343,7 +370,7 @@ __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total
       for (int i = 0; i < V; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float v = strided_sum<(T < 64 ? T : 64)>(h ? db[i][e] : dw[i][e]);
+          const float v = (float)strided_sum<(T < 64 ? T : 64)>(column(h, i, e));
           if (T >= 64 || (threadIdx.x & 63) < T) slots[mine * kCols + (t + i * T) * 8 + e] = v;
         }
       __syncthreads();
@@ -388,14 +415,15 @@ __global__ __launch_bounds__(kJoin) void k_norm_join(NormBackArgs a, int tiles, 
 // in bf16 217 us, 2.3 TB/s of what has to move).
 template <bool XBF, bool YBF>
 __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long long total) {
-  __shared__ float room[kLong / 64][3];
+  __shared__ double room[kLong / 64][3];
   const unsigned id = workgroup_id();
   if (id >= total) return;
   const int g = id / a.M, m = id - g * a.M;
   const long long x0 = g * a.sX + m * a.ldx, d0 = g * a.sg + m * a.ldg;
   const float mean = a.mean[id], rstd = a.rstd[id];
   const Row<float> row(mean, rstd);
-  float s[3] = {0.f, 0.f, 0.f}, x[8], dy[8];
+  double s[3] = {0.0, 0.0, 0.0};
+  float x[8], dy[8];
   auto take = [&](int n) __attribute__((always_inline)) {
     float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
     load8<XBF>(a.X, x0, n, a.N, x);
@@ -416,15 +444,18 @@ __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long l
         s[2] += x[e];
       }
     }
+    float f[2] = {0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      s[0] += dy[e];
-      s[1] += dy[e] * x[e];
+      f[0] += dy[e];
+      f[1] += dy[e] * x[e];
     }
+    s[0] += f[0];
+    s[1] += f[1];
   }
   row_sums<kLong>(s, room);
-  const float shift = s[2] / a.N;  // (none but of far rows)
-  const float c1 = s[0] / a.N, c2 = (s[1] - shift * s[0]) / a.N;
+  const double off = s[2] / a.N;  // (none but of far rows)
+  const float c1 = (float)(s[0] / a.N), shift = (float)off, c2 = (float)((s[1] - off * s[0]) / a.N);
   if (a.dw && threadIdx.x == 0) a.shift[id] = shift;
   for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
     take(n);
@@ -442,7 +473,18 @@ __global__ __launch_bounds__(kThreads) void k_norm_params(NormBackArgs a, int ti
   const int gs = id / tiles, g = gs / a.strips, m0 = (gs - g * a.strips) * a.strip;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, end = min(a.M, m0 + a.strip);
   const int n0 = (id - gs * tiles) * 512, n = n0 + lane * 8;
-  float dw[8] = {}, db[8] = {};
+  double dw[8] = {}, db[8] = {};
+  float w8[8] = {}, b8[8] = {};
+  int chain = 0;
+  const auto flush = [&]() __attribute__((always_inline)) {
+    chain = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      dw[e] += w8[e];
+      db[e] += b8[e];
+      w8[e] = b8[e] = 0.f;
+    }
+  };
   for (int m = m0 + wave; m < end; m += 4) {
     const long long at = (long long)g * a.M + m;
     const Row<float> row(a.mean[at], a.rstd[at]);
@@ -452,14 +494,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_params(NormBackArgs a, int ti
     load8<YBF>(a.dY, g * a.sg + m * a.ldg, n, a.N, dy);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      dw[e] += dy[e] * (row(x[e]) - shift);
-      db[e] += dy[e];
+      w8[e] += dy[e] * (row(x[e]) - shift);
+      b8[e] += dy[e];
     }
+    if (++chain == kChain) flush();
   }
+  flush();
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    room[0][wave][lane * 8 + e] = dw[e];
-    room[1][wave][lane * 8 + e] = db[e];
+    room[0][wave][lane * 8 + e] = (float)dw[e];
+    room[1][wave][lane * 8 + e] = (float)db[e];
   }
   __syncthreads();
 #pragma unroll
@@ -467,7 +511,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_params(NormBackArgs a, int ti
     float* to = a.strips == 1 ? (h ? a.db + g * a.sdb : a.dw + g * a.sdw)
                               : a.part + ((long long)gs * 2 + h) * a.N;
     for (int c = threadIdx.x; c < 512 && n0 + c < a.N; c += kThreads)
-      to[n0 + c] = (room[h][0][c] + room[h][1][c]) + (room[h][2][c] + room[h][3][c]);
+      to[n0 + c] = (float)(((double)room[h][0][c] + room[h][1][c]) +
+                           ((double)room[h][2][c] + room[h][3][c]));
   }
 }
 
@@ -565,14 +610,15 @@ hipError_t norm(NormArgs a, hipStream_t s) {
 
 // One strip, and no second launch, where each of a workgroup's places for rows gets few; else 256
 // (16384 x 8192 in bf16 in 256, 512, 1024 strips 186, 194, 206 us, when the sums still went by LDS).
-constexpr int kFewRows = 8;
+constexpr int kFewRows = 8, kFewSums = 32;
 constexpr long long kBackStrips = 256, kNarrowStrips = 1024;
 int back_strip_rows(int G, int M, int N) {
   return with_back_shape(N, [&](auto z) {
     constexpr int T = decltype(z)::T, B = decltype(z)::B;
     constexpr int each = T == 0 ? 4 : B / (T == 0 ? 1 : T);
     if (M <= kFewRows * each) return (M + each - 1) / each * each;
-    return strip_rows(T == 1 ? kNarrowStrips : kBackStrips, each, G, M);
+    const int rows = strip_rows(T == 1 ? kNarrowStrips : kBackStrips, each, G, M);
+    return decltype(z)::V <= 2 ? rows : std::min(rows, kFewSums * each);
   });
 }
 

@@ -402,3 +402,53 @@ def test_gradients_of_rows_far_from_zero(N, types):
     assert np.all(err <= bound), np.max(err / bound)
     assert np.all(a(_np(dw) - rw) <= (a(d) * en).sum(1) + gamma(M + 3) * a(d * n).sum(1))
     assert np.all(a(_np(db) - rb) <= gamma(M + 3) * a(d).sum(1))
+
+
+# of each the roundings of a column's sum one after the other: kept over four rows and joined in
+# fp64 (a thread's three, its workgroup's slot, its strip and the result), or over 32 rows
+@pytest.mark.parametrize("shape, D", [((129, 80000, 500), 6), ((129, 4000, 8000), 6), ((1, 60000, 8000), 6),
+                                      ((129, 200000, 40), 6), ((300, 100000, 6), 6), ((129, 4000, 17000), 6),
+                                      ((129, 40000, 1100), 34), ((200, 8000, 4200), 34), ((129, 6000, 9000), 34)])
+def test_sums_over_any_number_of_rows(shape, D):
+    """Columns of one sign, whose sums every rounding moves, in groups that share them: no more of
+    them for more rows or groups."""
+    L = _lsgd()
+    print(f"layer norm sums {shape}", flush=True)
+    G, M, N = shape
+    gen = torch.Generator(device=device()).manual_seed(sum(shape))
+    sign = torch.where(torch.arange(N, device=device()) % 2 == 0, 1.0, -1.0)
+    X = (torch.randn((1, M, N), generator=gen, device=device()) * 0.1 + sign).bfloat16()
+    dY = torch.rand((1, M, N), generator=gen, device=device()) * 0.1 + 0.05
+    _, mean, rstd = L.layer_norm(X)
+    mean, rstd = (t.repeat(G, 1) for t in (mean, rstd))
+    dx, dw, db = L.layer_norm_backward(dY.expand(shape), X.expand(shape), mean, rstd)
+    del dx
+    want, size, sums = (torch.zeros(N, device=device(), dtype=torch.float64) for _ in range(3))
+    for m in range(0, M, 5000):
+        at = slice(m, m + 5000)
+        d = dY[0, at].double()
+        dn = d * ((X[0, at].double() - mean[0, at, None].double()) * rstd[0, at, None].double())
+        want += dn.sum(0)
+        size += dn.abs().sum(0)
+        sums += d.sum(0)
+    # (n is rounded twice, its product with dy once more)
+    assert bool(((dw.double() - want).abs() <= gamma(D + 3) * size).all())
+    assert bool(((db.double() - sums).abs() <= gamma(D) * sums).all())
+    assert torch.equal(dw, dw[:1].expand(G, N)) and torch.equal(db, db[:1].expand(G, N))
+
+
+@pytest.mark.parametrize("N", [16385, 40003, 2 ** 24 + 5])
+def test_statistics_of_long_rows(N):
+    """One gradient throughout: its mean is itself, whatever the length, to the roundings of eight terms
+    and a few more."""
+    L = _lsgd()
+    print(f"layer norm long rows {N}", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(N)
+    X = torch.randn(1, 2, N, generator=gen, device=device())
+    dY = torch.full_like(X, 0.1)
+    _, mean, rstd = L.layer_norm(X)
+    dx, _, _ = L.layer_norm_backward(dY, X, mean, rstd)
+    n = (X - mean[..., None]) * rstd[..., None]
+    # (sum n is that of the mean's rounding and of n's own, u |x| and 2 u |n| a term)
+    size = 0.1 * (1 + n.abs() * n.abs().mean(2, keepdim=True))
+    assert bool((dx.abs() <= gamma(16) * rstd[..., None] * size).all())
