@@ -645,7 +645,8 @@ lsgd_status lsgd_grouped_gemm_rows(int32_t out_dtype, int32_t G, int32_t M,
  * of its own (fp32 [G][N], group strides sw, sb >= 0; NULL: ones, zeros):
  *   mean = sum x / N, rstd = (sum (x - mean)^2 / N + eps)^-1/2,
  *   Y = (x - mean) rstd w + b (out_dtype, rounded once), d_mean, d_rstd fp32 [G][M].
- * The sums are held in fp64. A NaN or an infinity in a row makes the row NaN. X's pitch
+ * The sums are held in fp64. A NaN or an infinity in a row makes the row NaN, finite values of
+ * any size do not (a d_rstd below 2^-126 holds fewer bits). X's pitch
  * ldx >= N and stride sX >= 0 in elements; Y's groups must not overlap (as C of
  * lsgd_grouped_gemm_blocks). eps finite and > 0. G <= 65535, M, N <= 2^30, else
  * LSGD_E_INVALID. Results must not overlap anything that is read.

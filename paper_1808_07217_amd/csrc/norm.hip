@@ -2,7 +2,7 @@
 //
 // Forward: mean = sum x / N, d = x - mean, rstd = (sum d^2 / N + eps)^-1/2, y = d rstd w + b.
 // Both sums are held in fp64, and the mean in two floats: rows far from zero and
-// values whose squares leave fp32's range come out as exactly as others.
+// finite values of any size come out as exactly as others.
 // Backward, from the mean and rstd that the forward pass wrote: n = (x - mean) rstd, e = dy w,
 // dx = rstd (e - sum e / N - n sum (e n) / N), dw = sum over rows of dy n, db of dy. The mean is a
 // float there: of rows far from zero it is found again from x.
@@ -50,16 +50,38 @@ __device__ __forceinline__ int slot_of() {
   return T < 64 ? threadIdx.x / T : __builtin_amdgcn_readfirstlane(threadIdx.x / T);
 }
 
-struct Moments {
-  float hi, lo, rstd;
+// Where |mean| is below it, no distance of an x from it leaves fp32's range.
+constexpr float kLarge = 0x1p100f;
+// The mean in two floats. A large one is taken by a sixteenth, as is x then.
+struct Mean {
+  float hi, by, at, lo;
+  __device__ __forceinline__ explicit Mean(double mean) {
+    hi = (float)mean;
+    by = fabsf(hi) >= kLarge ? 0x1p-4f : 1.f;
+    at = -hi * by;
+    lo = (float)(mean - hi) * by;
+  }
+  // (x - mean) by
+  __device__ __forceinline__ float operator()(float x) const {
+    return __builtin_fmaf(x, by, at) - lo;
+  }
+  // 1 / deviation, from the sum of those distances' squares. A distance becomes its deviations
+  // through first and factor, the second no subnormal number (of which bits are lost).
+  __device__ __forceinline__ float inverse_root(double squares, int N, float eps, float& factor,
+                                                float& first) const {
+    const bool large = by != 1.f;
+    if (large) squares *= 0x1p8;
+    const double rstd = 1.0 / sqrt(squares / N + eps);
+    factor = (float)rstd;
+    first = 1.f;
+    if (large || factor < 0x1p-120f) {
+      const double f = large ? rstd * 0x1p4 : rstd;
+      if (f < 0x1p-120) first = 0x1p-8f;
+      factor = (float)(f / first);
+    }
+    return (float)rstd;
+  }
 };
-__device__ __forceinline__ void split_mean(double mean, Moments& s) {
-  s.hi = (float)mean;
-  s.lo = (float)(mean - s.hi);
-}
-__device__ __forceinline__ float inverse_root(double mean_square, float eps) {
-  return (float)(1.0 / sqrt(mean_square + eps));
-}
 
 // A strip of rows a workgroup, T threads a row, V vectors of eight values each, in registers;
 // the next row is on its way while one is summed. w and b stay in registers over the strip: from
@@ -105,32 +127,37 @@ __global__ __launch_bounds__(B) void k_norm(NormArgs a, int strips, long long to
     }
     if (r + kRows < end) fetch(m + kRows);
     row_sums<T>(s, room[0]);
-    Moments mo;
-    const double mean = s[0] / a.N;
-    split_mean(mean, mo);
+    const Mean mean(s[0] / a.N);
     s[0] = 0.0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int n = (t + i * T) * 8;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        x[i][e] = n + e < a.N ? (x[i][e] - mo.hi) - mo.lo : 0.f;
+        x[i][e] = n + e < a.N ? mean(x[i][e]) : 0.f;
         s[0] += (double)x[i][e] * x[i][e];
       }
     }
     row_sums<T>(s, room[1]);
-    mo.rstd = inverse_root(s[0] / a.N, a.eps);
+    float factor, first;
+    const float rstd = mean.inverse_root(s[0], a.N, a.eps, factor, first);
+    if (first != 1.f) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] *= first;
+    }
     if (m < end) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int n = (t + i * T) * 8;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = __builtin_fmaf(x[i][e] * mo.rstd, w[i][e], b[i][e]);
+        for (int e = 0; e < 8; ++e) x[i][e] = __builtin_fmaf(x[i][e] * factor, w[i][e], b[i][e]);
         store8<YBF>(a.Y, g * a.sY + m * a.ldy, n, a.N, x[i]);
       }
       if (t == 0) {
-        a.mean[(long long)g * a.M + m] = mo.hi;
-        a.rstd[(long long)g * a.M + m] = mo.rstd;
+        a.mean[(long long)g * a.M + m] = mean.hi;
+        a.rstd[(long long)g * a.M + m] = rstd;
       }
     }
   }
@@ -154,19 +181,19 @@ __global__ __launch_bounds__(kLong) void k_norm_long(NormArgs a, long long total
     for (int e = 0; e < 8; ++e) s[0] += x[e];
   }
   row_sums<kLong>(s, room[0]);
-  Moments mo;
-  split_mean(s[0] / a.N, mo);
+  const Mean mean(s[0] / a.N);
   s[0] = 0.0;
   for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
     load8<XBF>(a.X, x0, n, a.N, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float d = n + e < a.N ? (x[e] - mo.hi) - mo.lo : 0.f;
+      const float d = n + e < a.N ? mean(x[e]) : 0.f;
       s[0] += (double)d * d;
     }
   }
   row_sums<kLong>(s, room[1]);
-  mo.rstd = inverse_root(s[0] / a.N, a.eps);
+  float factor, first;
+  const float rstd = mean.inverse_root(s[0], a.N, a.eps, factor, first);
   for (int n = threadIdx.x * 8; n < a.N; n += kLong * 8) {
     float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f}, b[8] = {};
     load8<XBF>(a.X, x0, n, a.N, x);
@@ -174,12 +201,12 @@ __global__ __launch_bounds__(kLong) void k_norm_long(NormArgs a, long long total
     if (a.b) load8<false>(a.b, g * a.sb, n, a.N, b);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      x[e] = __builtin_fmaf(((x[e] - mo.hi) - mo.lo) * mo.rstd, w[e], b[e]);
+      x[e] = __builtin_fmaf(mean(x[e]) * first * factor, w[e], b[e]);
     store8<YBF>(a.Y, g * a.sY + m * a.ldy, n, a.N, x);
   }
   if (threadIdx.x == 0) {
-    a.mean[(long long)g * a.M + m] = mo.hi;
-    a.rstd[(long long)g * a.M + m] = mo.rstd;
+    a.mean[(long long)g * a.M + m] = mean.hi;
+    a.rstd[(long long)g * a.M + m] = rstd;
   }
 }
 
@@ -191,10 +218,22 @@ __global__ __launch_bounds__(kLong) void k_norm_long(NormArgs a, long long total
 constexpr float kFar = 2048.f;
 template <class A>
 struct Row {
-  A mean, rstd;
+  A by, at, rstd;
   bool far;
-  __device__ __forceinline__ Row(float m, float r) : mean(m), rstd(r), far(!(fabsf(m) * r < kFar)) {}
-  __device__ __forceinline__ A operator()(float x) const { return ((A)x - mean) * rstd; }
+  __device__ __forceinline__ Row(float mean, float rs) {
+    const bool large = fabsf(mean) >= kLarge;
+    by = large ? 0x1p-4f : 1.f;
+    at = -(A)mean * by;
+    rstd = (A)rs * (large ? 0x1p4f : 1.f);
+    far = !(fabsf(mean) * rs < kFar);
+  }
+  // (a large mean by a sixteenth, as above)
+  __device__ __forceinline__ A operator()(float x) const {
+    if constexpr (sizeof(A) == 8)
+      return __builtin_fma((double)x, by, at) * rstd;
+    else
+      return __builtin_fmaf(x, by, at) * rstd;
+  }
 };
 
 // A strip of rows a workgroup; a thread keeps the sums of its columns over them. A: the

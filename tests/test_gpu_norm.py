@@ -452,3 +452,37 @@ def test_statistics_of_long_rows(N):
     # (sum n is that of the mean's rounding and of n's own, u |x| and 2 u |n| a term)
     size = 0.1 * (1 + n.abs() * n.abs().mean(2, keepdim=True))
     assert bool((dx.abs() <= gamma(16) * rstd[..., None] * size).all())
+
+
+@pytest.mark.parametrize("N", [4, 40, 64, 700, 1100, 5000, 9000, 20001])
+def test_rows_as_wide_as_fp32(N):
+    """Finite rows whose values lie further from their mean than fp32 reaches, or whose
+    deviation's inverse is subnormal: results as exact as others', but for rstd's own lost bits."""
+    L = _lsgd()
+    print(f"layer norm wide rows {N}", flush=True)
+    big = float(np.finfo(np.float32).max)
+    rng = np.random.default_rng(N)
+    X = np.empty((1, 8, N))
+    X[0, 0] = -3e38
+    X[0, 0, ::4] = 3e38
+    X[0, 1] = big
+    X[0, 1, N // 3] = -big
+    X[0, 2] = np.where(np.arange(N) % 2, big, -big)
+    X[0, 3] = rng.uniform(-big, big, N)
+    X[0, 4] = big
+    X[0, 5] = 1e-40
+    X[0, 5, 1] = -3e38
+    X[0, 6] = 1e38 + 1e37 * rng.standard_normal(N)
+    X[0, 7] = rng.standard_normal(N)
+    X = to_dev(X.astype(np.float32))
+    dY, w, b = (to_dev(rng.standard_normal(s).astype(np.float32)) for s in ((1, 8, N), (1, N), (1, N)))
+    y, mean, rstd = L.layer_norm(X, w, b)
+    x, wd = _np(X), _np(w)
+    ry, rm, rr = O.layer_norm(x, wd, _np(b), EPS)
+    assert np.all(np.abs(_np(mean) - rm) <= 1.01 * U32 * np.abs(rm) + 2.0 ** -50 * np.abs(x).mean(2))
+    assert np.all(np.abs(_np(rstd) - rr) <= 4 * U32 * rr + 1.01 * 2.0 ** -150)
+    n = np.abs((x - rm[..., None]) * rr[..., None])
+    rest = (2.0 ** -46 * np.abs(rm) + 2.0 ** -50 * np.abs(x).mean(2)) * rr
+    bound = (8 * U32 * n + rest[..., None]) * np.abs(wd)[:, None] + 1.01 * U32 * np.abs(ry)
+    assert np.all(np.abs(_np(y) - ry) <= bound), np.max(np.abs(_np(y) - ry) / bound)
+    _check_backward(L.layer_norm_backward(dY, X, mean, rstd, w), _np(dY), x, _np(mean), _np(rstd), wd)
