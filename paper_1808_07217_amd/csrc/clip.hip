@@ -50,9 +50,19 @@ __host__ __device__ inline long long eights_values(const ClipTensor& t) {
   return flat(t) ? t.M * t.N : t.M * ((t.N + 7) / 8) * 8;
 }
 
+// The bits of a value of bfloat16 or fp32 nearest to p. (By way of a float p would be rounded to
+// bfloat16 twice; the compiler makes one of it, but need not.)
+template <bool BF>
+__device__ __forceinline__ uint32_t nearest(double p) {
+  if constexpr (BF)
+    return __builtin_bit_cast(bf16_t, (__bf16)p);
+  else
+    return __float_as_uint((float)p);
+}
+
 // The values of a chunk of one replica's tensor as T threads take them, `tid` of them this
 // one: eights, U of a thread in flight. run(f): f(value) for every one, from a set that start() has on
-// its way (of values side by side); WRITE: the value becomes f's.
+// its way (of values side by side); WRITE: the value becomes f's (a double), rounded once.
 constexpr int kFlight = 4;
 template <bool BF, int T>
 struct Chunk {
@@ -77,10 +87,20 @@ struct Chunk {
   }
   template <bool WRITE, class F>
   __device__ __forceinline__ void eight(int u, long long row, int n, int N, F f) {
-    float w[8];
+    if constexpr (WRITE) {
+      Raw8<BF> w;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = f(v[u][i]);
-    if constexpr (WRITE) store8<BF>(t.p, row, n, N, w);
+      for (int i = 0; i < Raw8<BF>::kDwords; ++i) {
+        if constexpr (BF)
+          w.w[i] = nearest<BF>(f(v[u][2 * i])) | nearest<BF>(f(v[u][2 * i + 1])) << 16;
+        else
+          w.w[i] = nearest<BF>(f(v[u][i]));
+      }
+      store8<BF>(t.p, row, n, N, w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f(v[u][i]);
+    }
   }
   template <bool WRITE, class F>
   __device__ __forceinline__ void run(F f) {
@@ -94,13 +114,13 @@ struct Chunk {
       }
       if (tid < values - whole) {
         const long long at = x + e0 + whole + tid;
-        const float w = f(BF ? bf16_to_f32(((const bf16_t*)t.p)[at]) : ((const float*)t.p)[at]);
-        if constexpr (WRITE) {
-          if constexpr (BF)
-            ((bf16_t*)t.p)[at] = f32_to_bf16(w);
-          else
-            ((float*)t.p)[at] = w;
-        }
+        const float x = BF ? bf16_to_f32(((const bf16_t*)t.p)[at]) : ((const float*)t.p)[at];
+        if constexpr (!WRITE)
+          f(x);
+        else if constexpr (BF)
+          ((bf16_t*)t.p)[at] = (bf16_t)nearest<BF>(f(x));
+        else
+          ((uint32_t*)t.p)[at] = nearest<BF>(f(x));
       }
     } else {
       // (zeros past a row's last value add nothing to a sum)
@@ -155,16 +175,15 @@ __device__ __forceinline__ void with_chunk(const ClipArgs& a, int k, int c, int 
 }
 struct Squares {
   double sum = 0.0;
-  __device__ __forceinline__ float operator()(float v) {
+  __device__ __forceinline__ void operator()(float v) {
     sum = __builtin_fma((double)v, (double)v, sum);
-    return v;
   }
 };
 template <class C>
 __device__ __forceinline__ double squares_of(C& chunk) {
   Squares q;
   chunk.start();
-  chunk.template run<false>([&](float v) __attribute__((always_inline)) { return q(v); });
+  chunk.template run<false>([&](float v) __attribute__((always_inline)) { q(v); });
   return q.sum;
 }
 
@@ -197,7 +216,7 @@ __global__ __launch_bounds__(kOneThreads) void k_clip_one(ClipArgs a, int scale)
   for (int c = wave; c < a.chunks; c += kOneThreads / 64)
     with_chunk<64>(a, k, c, lane, [&](auto& chunk) {
       chunk.start();
-      chunk.template run<true>([&](float v) { return (float)(v * f); });
+      chunk.template run<true>([&](float v) { return v * f; });
     });
 }
 
@@ -236,7 +255,7 @@ __global__ __launch_bounds__(kThreads) void k_clip_scale(ClipArgs a, long long t
     // (a norm that is infinite or no number leaves the values as they are)
     if (!(norm > a.most) || norm == __builtin_inf()) return;
     const double f = a.most / norm;
-    chunk.template run<true>([&](float v) { return (float)(v * f); });
+    chunk.template run<true>([&](float v) { return v * f; });
   });
 }
 

@@ -342,3 +342,54 @@ def test_a_layer_s_local_step():
     new[:, :used.shape[1]] -= float(np.float32(lr)) * clipped
     np.testing.assert_allclose(_np(params), np.repeat(new.mean(0, keepdims=True), K, 0), rtol=0,
                                atol=6 * U32 * np.abs(new).max())
+
+
+def _to_bf16(v):
+    """float64 to the nearest bf16, ties to even, as a float64."""
+    m, e = np.frexp(v)  # |m| in [1/2, 1): eight bits of it, fewer below 2^-126
+    unit = np.ldexp(1.0, np.maximum(e - 8, -133))
+    return np.rint(v / unit) * unit
+
+
+@pytest.mark.parametrize("root", [32, 128, 1024])
+def test_bf16_is_rounded_once(root):
+    """Factors that lie next to the middle of two bf16 values, closer than a float tells: the
+    norm is a power of two, so that the factor is the bound's own digits."""
+    L = _lsgd()
+    print(f"clip bf16 rounding {root}", flush=True)
+    x = np.ones(root * root)
+    x[::3] = -1
+    x[100:164], x[164:180], x[180:500] = 1.5, 0.25, 0.0
+    x[500:540] = 2.0 ** -133 * np.arange(1, 41)  # subnormal, and nothing beside the others' squares
+    left, more = root * root - ((x[:500] ** 2).sum() + (x[540:] ** 2).sum()), []
+    while left > 0:
+        more.append(2.0 ** np.floor(np.log2(left) / 2))
+        left -= more[-1] ** 2
+    assert left == 0
+    x = np.concatenate([x, more])[None]
+    src = to_dev(x.astype(np.float32)).to(torch.bfloat16)
+    assert np.array_equal(_np(src), x)
+    moved = 0
+    for j in range(128):
+        for step in (2.0 ** -30, -2.0 ** -30, 2.0 ** -50, 0.0):
+            f = (1 + (2 * j + 1) / 256) / 2 * (1 + step)
+            t = src.clone()
+            assert L.clip_gradients([t], root * f).item() == root
+            want = _to_bf16(x * f)
+            assert np.array_equal(_np(t), want), (j, step)
+            moved += not np.array_equal(_to_bf16((x * f).astype(np.float32).astype(np.float64)), want)
+    assert moved > 100  # (by way of a float)
+
+
+@pytest.mark.parametrize("shape", [(2, 3000001), (2, 3000, 1001)])
+def test_bf16_matches_bit_for_bit(shape):
+    L = _lsgd()
+    print(f"clip bf16 bits {shape}", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(8)
+    room = torch.randn(*shape[:-1], shape[-1] + 3, generator=gen, device=device()).to(torch.bfloat16)
+    t = room[..., :shape[-1]]
+    v = _np(t)
+    norm, (want,) = O.clip([v], 7.0)
+    L.clip_gradients([t], 7.0)
+    # (a factor off by 2^-52 turns none of these products' roundings)
+    assert np.array_equal(_np(t), _to_bf16(want))
