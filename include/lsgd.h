@@ -704,7 +704,8 @@ typedef struct lsgd_tensor {
  * whose norm is above max_norm (finite, > 0) by max_norm / norm, the factor and the product in
  * fp64, rounded once; the others' stay as they are, as do those of a replica whose norm is not finite.
  * d_norm holds the norms before clipping. K <= 65535, count <= LSGD_MAX_TENSORS, M and N at
- * least 1, M N, M ld, s <= 2^44, N <= 2^30 where M > 1 and ld > N, else LSGD_E_INVALID. Clipped tensors' replicas must not overlap
+ * least 1, M N, M ld, s <= 2^44, N <= 2^30 where M > 1 and ld > N, no more than 2^57 values in all (a
+ * shared one for each replica), else LSGD_E_INVALID. Clipped tensors' replicas must not overlap
  * (s >= (M - 1) ld + N, or rows of all K side by side), nor two tensors (lsgd_tensors_apart says
  * whether they do, or where that would take over 2^24 runs of values, may), else LSGD_E_INVALID;
  * nor d_norm or the workspace a tensor. Workspace of

@@ -381,6 +381,7 @@ bool clip_tensors(int32_t K, int32_t count, const lsgd_tensor* h, bool written,
                   std::vector<lsgd::ClipTensor>& to) {
   if (K < 1 || K > 65535 || count < 1 || count > LSGD_MAX_TENSORS || !h) return false;
   constexpr int64_t kMost = 1LL << 44;
+  double all = 0;  // values of a replica, rows of a pitch in whole eights
   to.resize(count);
   for (int i = 0; i < count; ++i) {
     const lsgd_tensor& t = h[i];
@@ -395,8 +396,9 @@ bool clip_tensors(int32_t K, int32_t count, const lsgd_tensor* h, bool written,
         (t.s < t.N || !((t.s - t.N) / t.ld >= t.M - 1 || (t.ld - t.N) / t.s >= K - 1)))
       return false;
     to[i] = lsgd::ClipTensor{t.d_data, t.M, t.N, t.ld, t.s, t.dtype == LSGD_BF16, 0};
+    all += (double)t.M * (t.M == 1 || t.ld == t.N ? t.N : (t.N + 7) / 8 * 8);
   }
-  return true;
+  return all * K <= (double)lsgd::kMostClipped;
 }
 
 // Whether no two of the tensors share a byte (each one's own replicas being apart); false

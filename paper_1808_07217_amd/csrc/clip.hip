@@ -299,9 +299,10 @@ hipError_t launch_clip(int K, int count, const ClipTensor* t, bool scale, double
   a.most = most;
   a.part = (double*)ws;
   a.norm = norm;
+  // (below 2^30 chunks of kMostClipped's values, and one more for each of a launch's kBatch tensors of
+  // 2^16 replicas: a launch's chunks, and a replica's, number below 2^31; all replicas' need not)
   long long all = 0;
   for (int i = 0; i < count; ++i) all += chunks_of(t[i], a.each);
-  if (all > 0x7fffffffLL / K) return hipErrorInvalidValue;
   a.all = (int)all;
   if (in_one(count, t)) {
     a.count = count;

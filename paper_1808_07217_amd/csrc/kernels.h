@@ -249,6 +249,8 @@ struct ClipTensor {
   int bf16;
   int first;  // set by launch_clip: its first chunk of a replica's
 };
+// Values of all replicas together, rows of a pitch in whole eights: 2^30 chunks of 2^30.
+constexpr long long kMostClipped = 1LL << 60;
 size_t clip_workspace_bytes(int K, int count, const ClipTensor* t);
 // norm[k]: the root of the sum of squares over all the tensors of replica k; scale: where it is
 // finite and above `most`, they are multiplied by most / norm.

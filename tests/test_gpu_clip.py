@@ -393,3 +393,22 @@ def test_bf16_matches_bit_for_bit(shape):
     L.clip_gradients([t], 7.0)
     # (a factor off by 2^-52 turns none of these products' roundings)
     assert np.array_equal(_np(t), _to_bf16(want))
+
+
+def test_more_chunks_than_32_bits_number():
+    """65535 replicas of 32800 values, each a tensor of its own: 2^31 chunks and more of all replicas
+    together."""
+    L = _lsgd()
+    print("clip chunks", flush=True)
+    K, n = 65535, 32800
+    flat = torch.zeros(K, n, device=device())
+    flat[0], flat[1, 5], flat[-1, -1], flat[-1, 0], flat[40000, 17000] = 2.0, 3.0, 6.0, 8.0, -1.0
+    norm = L.clip_gradients([flat[:, i] for i in range(n)], 2.0)
+    want = torch.zeros(K, device=device())
+    want[0], want[1], want[-1], want[40000] = 2.0 * n ** 0.5, 3.0, 10.0, 1.0
+    assert torch.allclose(norm, want, rtol=2 * U32, atol=0)
+    two = torch.tensor(2.0, dtype=torch.float64) * (2.0 / (4.0 * n) ** 0.5)
+    assert torch.allclose(flat[0], two.float().to(device()), rtol=2 * U32, atol=0)
+    assert [flat[1, 5].item(), flat[40000, 17000].item()] == [2.0, -1.0]
+    np.testing.assert_allclose([flat[-1, -1].item(), flat[-1, 0].item()], [1.2, 1.6], rtol=2 * U32)
+    assert int((flat != 0).sum()) == n + 4

@@ -298,3 +298,27 @@ def test_overlapping_tensors_are_found_exactly():
     assert lib.lsgd_tensors_apart(0, 3, _table(*row), ctypes.byref(one)) == 1
     assert lib.lsgd_tensors_apart(5, 3, None, ctypes.byref(one)) == 1
     assert lib.lsgd_tensors_apart(5, 1, _table((4096, 4, 6, 6, 20, 0)), ctypes.byref(one)) == 1
+
+
+def test_the_most_values_to_clip():
+    """The workspace's query, the norm and the clip have one limit, of all values together."""
+    lib, f, nb, d = _lib(), P(1 << 40), ctypes.c_size_t(), ctypes.c_double
+    huge = (1 << 40, 2**20, 2**24, 2**24, 0, 0)  # 2^44 values, one tensor for every replica
+    for K, n, want in ((2**13 + 1, 2, 0), (2**15 + 1, 2, 1), (2**13, 8, 0), (2**13 + 1, 8, 1)):
+        t = _table(*[huge] * n)
+        assert lib.lsgd_gradient_norm_workspace_bytes(K, n, t, ctypes.byref(nb)) == want, (K, n)
+        # (with no workspace at all: refused as such, or before)
+        assert lib.lsgd_gradient_norm(K, n, t, f, None, 0, None) == 1
+        assert lib.lsgd_gradient_norm(K, n, t, f, f, 0, None) == (1 if want else 2)
+    # rows of a pitch count in eights
+    narrow = (1 << 40, 2**41, 1, 2, 0, 0)
+    for K, want in ((2**16 - 1, 0), (2**15, 0)):
+        assert lib.lsgd_gradient_norm_workspace_bytes(K, 1, _table(narrow), ctypes.byref(nb)) == want
+    for n, want in ((1, 0), (2, 1)):
+        t = _table(*[narrow] * n)
+        assert lib.lsgd_gradient_norm_workspace_bytes(2**16 - 1, n, t, ctypes.byref(nb)) == want
+    # every list of small tensors for every replica
+    many = _table(*[(4096 + 4 * i, 1, 1, 1, 65536, 0) for i in range(65536)])
+    assert lib.lsgd_gradient_norm_workspace_bytes(65535, 65536, many, ctypes.byref(nb)) == 0
+    assert nb.value == (65536 + 1) * 65535 * 8
+    assert lib.lsgd_clip_gradients(65535, 65536, many, d(1.0), f, f, nb.value - 1, None) == 2
