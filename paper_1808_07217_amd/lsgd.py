@@ -448,6 +448,13 @@ def post_local_schedule(H: int, rounds: int, lr: float, warm_rounds: int = 0,
 
 
 # -- building blocks ------------------------------------------------------
+def _int32(*sizes: int) -> None:
+    """Refuses sizes past the ABI's 32-bit integers, of which ctypes would pass the last 32 bits."""
+    for n in sizes:
+        if n >> 31:
+            raise ValueError(f"{n} groups, replicas, rows or columns: at most 2^31 - 1")
+
+
 def grouped_gemm(A: torch.Tensor, B: torch.Tensor, trans_a=False, trans_b=False,
                  out: Optional[torch.Tensor] = None, splits: int = 1) -> torch.Tensor:
     """C[g] = op(A[g]) @ op(B[g]) on the matrix cores (fp32 or bf16 inputs,
@@ -463,6 +470,7 @@ def grouped_gemm(A: torch.Tensor, B: torch.Tensor, trans_a=False, trans_b=False,
     Kb, N = (B.shape[2], B.shape[1]) if trans_b else (B.shape[1], B.shape[2])
     if Kb != Kd:
         raise ValueError("inner dimensions differ")
+    _int32(G, M, N, Kd)
     out = out if out is not None else torch.empty((G, M, N), device=A.device)
     dt = BF16 if A.dtype == torch.bfloat16 else FP32
     part = (torch.empty((splits, G, M, N), device=A.device) if splits > 1
@@ -479,6 +487,7 @@ def replica_average(W: torch.Tensor) -> None:
     """In-place K-way average of a contiguous float32 [K][P] tensor."""
     if W.dtype != torch.float32 or W.dim() != 2 or not W.is_contiguous():
         raise ValueError("W must be contiguous float32 [K][P]")
+    _int32(W.shape[0])
     _check(_lib.lsgd_replica_average(
         _ptr(W), W.shape[0], W.shape[1],
         _stream_handle(torch.cuda.current_stream(W.device))))
@@ -489,6 +498,7 @@ def replica_average_blocks(W: torch.Tensor, Kb: int) -> None:
     contiguous float32 [K][P] tensor."""
     if W.dtype != torch.float32 or W.dim() != 2 or not W.is_contiguous():
         raise ValueError("W must be contiguous float32 [K][P]")
+    _int32(W.shape[0])
     _check(_lib.lsgd_replica_average_blocks(
         _ptr(W), W.shape[0], int(Kb), W.shape[1],
         _stream_handle(torch.cuda.current_stream(W.device))))
@@ -504,6 +514,7 @@ def replica_average_global_momentum(W: torch.Tensor, w_sync: torch.Tensor,
             raise ValueError("tensors must be contiguous float32")
     if W.dim() != 2 or w_sync.numel() != W.shape[1] or u_global.numel() != W.shape[1]:
         raise ValueError("W must be [K][P], w_sync and u_global [P]")
+    _int32(W.shape[0])
     _check(_lib.lsgd_replica_average_global_momentum(
         _ptr(W), W.shape[0], W.shape[1], _ptr(w_sync), _ptr(u_global),
         float(m_global), float(lr),
@@ -523,6 +534,7 @@ def replica_sign_sync(W: torch.Tensor, w_sync: torch.Tensor,
             E is not None and E.shape != W.shape):
         raise ValueError("W, E must be [K][P] and w_sync [P]")
     K, P = W.shape
+    _int32(K)
     nb = _c.c_size_t()
     _check(_lib.lsgd_sign_sync_scratch_bytes(K, P, _c.byref(nb)))
     scratch = torch.empty(max(1, nb.value), dtype=torch.uint8, device=W.device)
@@ -543,6 +555,7 @@ def replica_sign_sync_static(W: torch.Tensor, w_sync: torch.Tensor,
             E is not None and E.shape != W.shape):
         raise ValueError("W, E must be [K][P] and w_sync [P]")
     K, P = W.shape
+    _int32(K)
     _check(_lib.lsgd_replica_sign_sync_static(
         _ptr(W), K, P, _ptr(w_sync), _ptr(E),
         _stream_handle(torch.cuda.current_stream(W.device))))
@@ -609,6 +622,8 @@ def _matrices(name: str, X: torch.Tensor, dtypes) -> Tuple[int, int]:
     G, M, N = X.shape
     if not (G and M and N):
         raise ValueError(f"{name} is empty")
+    if (G | M | N) >> 31:
+        _int32(G, M, N)
     sG, sM, sN = X.stride()
     if N > 1 and sN != 1:
         raise ValueError(f"{name}'s columns must be contiguous")
@@ -689,6 +704,8 @@ def _block_operand(name: str, X: Blocks) -> Tuple[int, int, int, int, int]:
     lds = _up((n + 127) // 128, 4)
     if n < 1 or L != _up(n, 128) or s.shape != (G, M, lds) or not (G and M):
         raise ValueError(f"{name}: shapes do not match the block layout of {n} columns")
+    if (G | M | n) >> 31:
+        _int32(G, M, n)
     if not (q.is_cuda and s.is_cuda):
         raise ValueError(f"{name} must be on a CUDA (HIP) device")
     if q.is_contiguous() and s.is_contiguous():
@@ -893,6 +910,8 @@ def _row_operand(name: str, X: Rows) -> Tuple[int, int, int, int]:
     G, M, L = shape
     if n < 1 or L != _up(n, 128) or s.shape != (G, M) or not (G and M):
         raise ValueError(f"{name}: shapes do not match the row layout of {n} columns")
+    if (G | M | n) >> 31:
+        _int32(G, M, n)
     if not (q.is_cuda and s.is_cuda):
         raise ValueError(f"{name} must be on a CUDA (HIP) device")
     if q.is_contiguous() and s.is_contiguous():
@@ -1097,6 +1116,7 @@ def _geometry(shape, stride, dtype) -> Tuple[int, bytes]:
         ld = N
     if not K * M * N:
         raise ValueError("tensors must not be empty")
+    _int32(K)
     if one != 1 or ld < N:
         raise ValueError("a replica's values must be contiguous, or [M][N] of contiguous rows")
     return K, struct.pack("=5q", M, N, ld, stride[0] if K > 1 else 0, code)

@@ -486,3 +486,20 @@ def test_rows_as_wide_as_fp32(N):
     bound = (8 * U32 * n + rest[..., None]) * np.abs(wd)[:, None] + 1.01 * U32 * np.abs(ry)
     assert np.all(np.abs(_np(y) - ry) <= bound), np.max(np.abs(_np(y) - ry) / bound)
     _check_backward(L.layer_norm_backward(dY, X, mean, rstd, w), _np(dY), x, _np(mean), _np(rstd), wd)
+
+
+def test_sizes_past_32_bits_are_refused():
+    """Groups, rows or columns past the ABI's integers, in views of a few values: refused before
+    anything is made."""
+    L = _lsgd()
+    print("layer norm refused sizes", flush=True)
+    x = torch.ones(1, 1, 1, device=device())
+    n = 2 ** 32 + 1
+    for X in (x.expand(n, 1, 1), x.expand(1, n, 1)):
+        for call in (L.layer_norm, L.quantise_rows, L.quantise_blocks, L.orthogonalise,
+                     lambda X: L.layer_norm_backward(X, X, X[..., 0], X[..., 0])):
+            with pytest.raises(ValueError, match="2\\^31"):
+                call(X)
+    for call in (L.gradient_norm, lambda t: L.clip_gradients(t, 1.0)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call([x.expand(n, 1, 1)])

@@ -322,3 +322,25 @@ def test_the_most_values_to_clip():
     assert lib.lsgd_gradient_norm_workspace_bytes(65535, 65536, many, ctypes.byref(nb)) == 0
     assert nb.value == (65536 + 1) * 65535 * 8
     assert lib.lsgd_clip_gradients(65535, 65536, many, d(1.0), f, f, nb.value - 1, None) == 2
+
+
+def test_binding_refuses_sizes_past_32_bits():
+    """Not the call of their last 32 bits. (Expanded tensors: nothing of that size is held.)"""
+    from paper_1808_07217_amd import lsgd as L
+    n = 2**32 + 1
+    for call in (lambda: L._int32(3, n), lambda: L._int32(2**31),
+                 lambda: L._geometry((n, 3), (0, 1), torch.float32),
+                 lambda: L.replica_average(torch.empty(n, 0)),
+                 lambda: L.replica_average_blocks(torch.empty(n, 0), 1),
+                 lambda: L.grouped_gemm(torch.empty(n, 0, 1), torch.empty(n, 1, 0))):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
+    L._int32(2**31 - 1, 1)
+    q, s = torch.zeros(1, 1, 128, dtype=torch.int8), torch.zeros(1, 1)
+    wide = L.Rows(q.expand(n, 1, 128), s.expand(n, 1), 5)
+    with pytest.raises(ValueError, match="2\\^31"):
+        L.grouped_gemm_rows(wide, wide)
+    b = L.Blocks(q.to(torch.float8_e4m3fn).expand(n, 1, 128),
+                 torch.zeros(1, 1, 4).to(torch.float8_e8m0fnu).expand(n, 1, 4), 5)
+    with pytest.raises(ValueError, match="2\\^31"):
+        L.grouped_gemm_blocks(b, b)
