@@ -644,7 +644,7 @@ lsgd_status lsgd_grouped_gemm_rows(int32_t out_dtype, int32_t G, int32_t M,
  * Layer norm of the rows of G matrices X_g [M][N] (dtype), each with a weight and a bias
  * of its own (fp32 [G][N], group strides sw, sb >= 0; NULL: ones, zeros):
  *   mean = sum x / N, rstd = (sum (x - mean)^2 / N + eps)^-1/2,
- *   Y = (x - mean) rstd w + b (out_dtype, rounded once), d_mean, d_rstd fp32 [G][M].
+ *   Y = (x - mean) rstd w + b (in fp32, then rounded to out_dtype), d_mean, d_rstd fp32 [G][M].
  * The sums are held in fp64. A NaN or an infinity in a row makes the row NaN, finite values of
  * any size do not (a d_rstd below 2^-126 holds fewer bits). X's pitch
  * ldx >= N and stride sX >= 0 in elements; Y's groups must not overlap (as C of
@@ -666,6 +666,8 @@ lsgd_status lsgd_layer_norm(int32_t dtype, int32_t out_dtype, int32_t G,
  *   sdb >= N; both NULL: not wanted).
  * The fp32 mean is off the row's own by up to 2^-24 |mean|, and n by that times rstd: of rows
  * of |mean| rstd >= 2048 the row's own mean is found again from X and d_mean and used instead.
+ * A row's sums of e and e n are held in fp32 (in fp64 from 16385 columns on and up to 8), whose range
+ * they must not leave. A column's sum takes fp32 steps over at most 32 rows, fp64 ones over those.
  * The sums over rows are added in an order that the sizes alone decide. Workspace
  * (not without dw and db): lsgd_layer_norm_backward_workspace_bytes, 16-byte aligned (LSGD_E_WORKSPACE
  * if smaller; may be 0; then NULL is allowed), one call's at a time. Limits as
@@ -702,8 +704,9 @@ typedef struct lsgd_tensor {
  * replica k's tensors, squares and sum in fp64, in an order that the sizes alone decide (a tensor
  * listed twice counts twice). lsgd_clip_gradients also multiplies the values of each replica
  * whose norm is above max_norm (finite, > 0) by max_norm / norm, the factor and the product in
- * fp64, rounded once; the others' stay as they are, as do those of a replica whose norm is not finite.
- * d_norm holds the norms before clipping. K <= 65535, count <= LSGD_MAX_TENSORS, M and N at
+ * fp64, rounded once; the others' stay as they are, as do those of a replica that holds an infinity or a
+ * NaN. d_norm holds the norms before clipping (past fp32's range an infinity, but clipped by the
+ * fp64 norm all the same). K <= 65535, count <= LSGD_MAX_TENSORS, M and N at
  * least 1, M N, M ld, s <= 2^44, N <= 2^30 where M > 1 and ld > N, no more than 2^57 values in all (a
  * shared one for each replica), else LSGD_E_INVALID. Clipped tensors' replicas must not overlap
  * (s >= (M - 1) ld + N, or rows of all K side by side), nor two tensors (lsgd_tensors_apart says

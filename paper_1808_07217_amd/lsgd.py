@@ -1039,7 +1039,8 @@ def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor,
                         dbias: Optional[torch.Tensor] = None
                         ) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
     """(dX, dweight, dbias) of ``layer_norm`` from the gradient dY of its result, its X,
-    mean, rstd and weight (lsgd_layer_norm_backward). dX has X's type, the others are float32
+    mean, rstd and weight (lsgd_layer_norm_backward; rows more than 2048 deviations from zero by
+    their own mean, which float32 does not hold). dX has X's type, the others are float32
     [G][N], or None without ``parameters``. ``out``, ``dweight`` and ``dbias`` take the
     results (the last two, views into flat rows of gradients for instance, with any group
     stride) and must not overlap each other or what is read."""
@@ -1157,7 +1158,8 @@ def gradient_norm(tensors: Sequence[torch.Tensor]) -> torch.Tensor:
 
 def clip_gradients(tensors: Sequence[torch.Tensor], max_norm: float) -> torch.Tensor:
     """In place: the ``tensors`` of each replica whose ``gradient_norm`` is above ``max_norm``
-    (finite, > 0), times max_norm / norm; the others, and those of a replica whose norm
-    is not finite, stay as they are. Returns the norms before clipping
-    (lsgd_clip_gradients). The tensors must not overlap."""
+    (finite, > 0), times max_norm / norm; the others, and those of a replica that holds an
+    infinity or a NaN, stay as they are. Returns the norms before clipping, an infinity
+    for one past float32's range, which is clipped all the same (lsgd_clip_gradients). The
+    tensors must not overlap."""
     return _clip_call(tensors, _lib.lsgd_clip_gradients, float(max_norm))

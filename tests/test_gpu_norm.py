@@ -343,7 +343,7 @@ def test_past_32_bit_offsets(N):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("N", [5, 40, 64, 700, 1100, 5000, 8192, 9000, 16384, 20001])
+@pytest.mark.parametrize("N", [5, 40, 64, 100, 700, 1100, 2000, 4000, 5000, 7000, 8192, 9000, 16384, 20001])
 def test_constant_rows_far_out(N, dtype):
     """One value throughout, so far from zero that it leaves fp32's range in deviations of
     eps: no deviations, and the gradient that is left."""
@@ -364,7 +364,8 @@ def test_constant_rows_far_out(N, dtype):
 
 
 @pytest.mark.parametrize("types", ["fp32 fp32", "fp32 bf16"])
-@pytest.mark.parametrize("N", [2, 5, 9, 40, 130, 700, 1100, 1500, 2500, 5000, 9000, 16000, 20001])
+@pytest.mark.parametrize("N", [2, 5, 9, 40, 100, 130, 400, 700, 1100, 1500, 2000, 2500, 4000, 5000, 8000, 9000,
+                               16000, 20001])
 def test_gradients_of_rows_far_from_zero(N, types):
     """Means of 10^4 and 10^6 deviations: the gradients of the values' own mean, which the fp32 one
     that is handed over misses by up to 6% of a deviation. x - mean as it was written is rounded to u,
@@ -454,7 +455,7 @@ def test_statistics_of_long_rows(N):
     assert bool((dx.abs() <= gamma(16) * rstd[..., None] * size).all())
 
 
-@pytest.mark.parametrize("N", [4, 40, 64, 700, 1100, 5000, 9000, 20001])
+@pytest.mark.parametrize("N", [4, 40, 64, 100, 400, 700, 1100, 2000, 4000, 5000, 8000, 9000, 16000, 20001])
 def test_rows_as_wide_as_fp32(N):
     """Finite rows whose values lie further from their mean than fp32 reaches, or whose
     deviation's inverse is subnormal: results as exact as others', but for rstd's own lost bits."""
@@ -503,3 +504,26 @@ def test_sizes_past_32_bits_are_refused():
     for call in (L.gradient_norm, lambda t: L.clip_gradients(t, 1.0)):
         with pytest.raises(ValueError, match="2\\^31"):
             call([x.expand(n, 1, 1)])
+
+
+@pytest.mark.parametrize("N", [7, 40, 700, 1100, 2500, 8000, 9000, 20001])
+def test_far_rows_in_strided_views(N):
+    """Rows far from zero among others, with pitches, without weights and without parameters' gradients:
+    the bits of contiguous ones."""
+    L = _lsgd()
+    print(f"layer norm far strided {N}", flush=True)
+    gen = torch.Generator(device=device()).manual_seed(N)
+    G, M = 3, 37
+    room = torch.randn(G, M + 2, N + 5, generator=gen, device=device())
+    room[:, ::3] += 3e4
+    room[:, 1::7] -= 1e32
+    more = torch.randn(M, G, N + 3, generator=gen, device=device()).bfloat16()
+    X, dY = room[:, 1:M + 1, 3:N + 3], more[:, :, 1:N + 1].transpose(0, 1)
+    w = torch.randn(1, N, generator=gen, device=device()).expand(G, N)
+    for weight in (None, w):
+        _, mean, rstd = L.layer_norm(X, weight)
+        want = L.layer_norm_backward(dY.contiguous(), X.contiguous(), mean, rstd, weight)
+        got = L.layer_norm_backward(dY, X, mean, rstd, weight)
+        assert all(torch.equal(a, b) and bool(torch.isfinite(a).all()) for a, b in zip(got, want))
+        alone = L.layer_norm_backward(dY, X, mean, rstd, weight, parameters=False)
+        assert torch.equal(alone[0], want[0])
