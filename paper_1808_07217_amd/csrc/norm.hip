@@ -7,8 +7,8 @@
 // dx = rstd (e - sum e / N - n sum (e n) / N), dw = sum over rows of dy n, db of dy. The mean is a
 // float there: of rows far from zero it is found again from x.
 //
-// Bound by HBM (each tensor is read or written once: 16384 x 8192 in bf16 5.1 TB/s forward, 4.9
-// backward; a copy of 4 GB 4.8), small ones by a launch and a load's latency (3 x 1537 x 771 in fp32
+// Bound by HBM (each tensor is read or written once: 16384 x 8192 in bf16 107 us, 5.0 TB/s, forward, 168 us,
+// 4.8, backward; a copy of 4 GB 4.8), small ones by a launch and a load's latency (3 x 1537 x 771 in fp32
 // 10 us). A row lies in the registers of as few threads as hold it, sums go over lanes by rotations
 // (by way of LDS 127 -> 119 us, 185 -> 167 backward), and the next row is on its way meanwhile.
 #include <algorithm>
@@ -240,7 +240,9 @@ struct Row {
 // arithmetic of a row. Of rows of few columns little is left beside the two directions that are
 // taken out (of two columns eps / variance of e): those of up to eight, a thread's each, in fp64.
 // A column's sum is fp32 over kChain rows of a thread, and fp64 over those; of three vectors and more,
-// which leave no registers for that, fp32 over the strip, of kFewSums rows a thread at most.
+// which leave no registers for that, fp32 over the strip, of kFewSums rows a thread at most. (us, of 16 x
+// 128 x 512: fp64 at every row 15.5, over four 14.6, fp32 alone 14.7. Of 20000 x 10000 in bf16: strips of
+// 32 rows 275, of 79 253.)
 constexpr int kChain = 4;
 template <bool XBF, bool YBF, int T, int V, int B, class A>
 __global__ __launch_bounds__(B) void k_norm_back(NormBackArgs a, long long total) {
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(kJoin) void k_norm_join(NormBackArgs a, int tiles, 
 }
 
 // Rows of any length: dx in two passes over a row, dw and db from a third, by columns (2048 x 40000
-// in bf16 217 us, 2.3 TB/s of what has to move).
+// in bf16 229 us, 2.1 TB/s of what has to move).
 template <bool XBF, bool YBF>
 __global__ __launch_bounds__(kLong) void k_norm_back_long(NormBackArgs a, long long total) {
   __shared__ double room[kLong / 64][3];
@@ -589,8 +591,8 @@ auto with_shape(int N, F f) {
   return f(Shape<0, 0, 0>{});
 }
 // Backward, where sums of the columns stay in registers too, and few strips leave few of them to
-// add: large workgroups, one or two a compute unit. (16 x 128 x 512 in workgroups of 256 and two launches
-// 19.4 us, of 1024 and one 13.7; in bf16 by two vectors a thread and by one 500000 x 64 44 and 50, 250000 x 256
+// add: large workgroups, one or two a compute unit. (With column sums in fp32 throughout: 16 x 128 x 512 in
+// workgroups of 256 and two launches 19.4 us, of 1024 and one 13.7; in bf16 by two vectors a thread and by one 500000 x 64 44 and 50, 250000 x 256
 // 81 and 92, 4 x 9777 x 1134 73 and 83; by three and by two or four 4 x 9777 x 1134 61 and 73, 18678 x
 // 2063 60 and 80, 6000 x 9000 76 and 85; 4096 x 16384 by 1024 threads, which spill, 278, by 512 without
 // a row ahead 98.)

@@ -9,8 +9,9 @@
 // Rows alone take one read of X, a row in registers meanwhile (16384 x 8192 in bf16 73 us, 5.5
 // TB/s). A column's scale needs all rows first: both ways take two reads, the second in part from
 // the last-level cache (137 us: the maxima 53, at 5.1 TB/s, the integers 86). The product is bound by the
-// matrix cores at the power limit where it is large (8192^3 to bf16 430 us, 2.56 POPS; of zeros 339), by the
-// weights' bytes for a token (1 x 8192 x 8192 14.0 us, 4.8 TB/s).
+// matrix cores where it is large (8192^3 to bf16 431 us, 2.55 POPS: busy in 60% of the cycles, at a clock
+// of 1.95 of 2.4 GHz; operands of zeros, which leave the clock up, 339), by the weights' bytes
+// for a token (1 x 8192 x 8192 14.0 us, 4.8 TB/s).
 #include <algorithm>
 #include <cmath>
 
