@@ -707,8 +707,8 @@ typedef struct lsgd_tensor {
  * fp64, rounded once; the others' stay as they are, as do those of a replica that holds an infinity or a
  * NaN. d_norm holds the norms before clipping (past fp32's range an infinity, but clipped by the
  * fp64 norm all the same). K <= 65535, count <= LSGD_MAX_TENSORS, M and N at
- * least 1, M N, M ld, s <= 2^44, N <= 2^30 where M > 1 and ld > N, no more than 2^57 values in all (a
- * shared one for each replica), else LSGD_E_INVALID. Clipped tensors' replicas must not overlap
+ * least 1, M N, M ld, s <= 2^44, N <= 2^30 where M > 1 and ld > N, no more than 2^60 values in all (a
+ * shared one for each replica, rows of a pitch rounded up to eights), else LSGD_E_INVALID. Clipped tensors' replicas must not overlap
  * (s >= (M - 1) ld + N, or rows of all K side by side), nor two tensors (lsgd_tensors_apart says
  * whether they do, or where that would take over 2^24 runs of values, may), else LSGD_E_INVALID;
  * nor d_norm or the workspace a tensor. Workspace of
